@@ -1,0 +1,81 @@
+/*
+ * fc_lm.h -- C ABI of the operators at the ends of a language model and of its
+ * matrix update, for MI355X (gfx950): what produces the gradients that fc.h
+ * aggregates, and what else may consume their sum.
+ *   fc_embed : scaled rows of a table for a list of tokens, and the table's
+ *              gradient, summed token by token in sorted order
+ *   fc_xent  : softmax cross entropy over a vocabulary, computed in pieces of
+ *              the vocabulary without keeping the logits, with both gradients
+ *   fc_muon  : momentum updates made orthogonal by Newton-Schulz products,
+ *              for every matrix of a flat parameter vector at once
+ *
+ * Conventions for every entry point, as in fc.h:
+ *   - Buffers are device pointers owned by the caller.  A plan owns its tables
+ *     and workspaces (hipMalloc on the device current when it is created) and
+ *     nothing of a call is kept for the next.
+ *   - Pointers are aligned to their element type (FC_EALIGN otherwise); the
+ *     flat vectors of fc_muon to 16 bytes, as in fc.h.  A row stride `ld` is in
+ *     elements and at least the row's length; 16-byte aligned rows are the
+ *     fast case.
+ *   - Calls are asynchronous on `stream` and validate before they enqueue.
+ *     Calls on one plan take effect in the order they are made, whatever their
+ *     streams (a call on another stream than the previous one makes its stream
+ *     wait, on the device).  They must not run concurrently from several host
+ *     threads.
+ *   - Every call enqueues kernel launches only (no copies, memsets or
+ *     allocations), so it may be captured in a HIP graph; a captured call
+ *     neither waits for the plan's previous call nor becomes it.
+ *   - A written buffer may not overlap any other buffer of the call
+ *     (FC_EALIAS).
+ *   - Results do not depend on timing: sums are taken in a fixed order, so the
+ *     same inputs give the same bits.
+ *   - Token and target lists hold int32 or int64 (`token_bytes` 4 or 8).  An
+ *     entry outside [0, rows) -- below zero is the usual padding -- names no
+ *     row: its looked-up row is zeros, it has loss 0 and no gradient, whatever
+ *     its inputs hold (infinities and NaN included).
+ *   - Return value: FC_OK or a negative code of fc.h (fc_strerror names it).
+ */
+#ifndef FC_LM_H
+#define FC_LM_H
+
+#include <stdint.h>
+
+#include "fc.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* Storage types are fc.h's fc_dtype values and this one. */
+#define FC_BF16 2
+
+/* ---- embedding ---------------------------------------------------------- */
+
+typedef struct fc_embed fc_embed;
+
+/* A plan for tables of `rows` rows of `dim` elements and up to `max_tokens`
+ * tokens a gradient (1 <= rows < 2^31, 1 <= dim <= 2^20, 0 <= max_tokens < 2^31).
+ * Its workspace holds the sorted tokens and partial sums: 16 + dim / 4 bytes per
+ * token (dim for the first 4096). */
+int fc_embed_create(fc_embed** plan, int64_t rows, int64_t dim, int64_t max_tokens);
+void fc_embed_destroy(fc_embed* plan);
+
+/* out[t, :] = scale * table[tokens[t], :] for t < n, computed in fp32 and
+ * rounded once to the output's type.  n < 2^31. */
+int fc_embed_lookup(fc_embed* plan, const void* table, int table_dtype, int64_t ld_table, const void* tokens,
+                    int token_bytes, int64_t n, float scale, void* out, int out_dtype, int64_t ld_out, void* stream);
+
+/* dtable[r, :] = (accumulate ? dtable[r, :] : 0) + scale * sum of dy[t, :] over
+ * the t with tokens[t] == r, for every row of the table.  The tokens are sorted
+ * (stable), the sum of a row is taken in fp32 in ascending t, in runs of a
+ * fixed length that are then added in order, and rounded once to the output's
+ * type.  n <= max_tokens (FC_EINVAL). */
+int fc_embed_grad(fc_embed* plan, const void* dy, int dy_dtype, int64_t ld_dy, const void* tokens, int token_bytes,
+                  int64_t n, float scale, void* dtable, int dtable_dtype, int64_t ld_dtable, int accumulate,
+                  void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* FC_LM_H */

@@ -20,7 +20,8 @@ from ._fc import (FC_F16, FC_F32, FC_NOALLOC_MAX_ELEMS, FC_ORDER_LINEAR, FC_ORDE
 __all__ = ["Plan", "FcError", "fc_plan_create", "fc_plan_destroy", "fc_plan_query", "fc_plan_set_timing",
            "fc_plan_read_timing", "fc_plan_balance", "fc_tree_reduce", "fc_sgd_step", "fc_broadcast", "fc_step",
            "fc_step_noalloc", "fc_strerror",
-           "fc_lr_at", "fc_train", "lr_policy", "lr_at", "fc_read_probe", "fc_read_probe_blocks", "read_probe"]
+           "fc_lr_at", "fc_train", "lr_policy", "lr_at", "fc_read_probe", "fc_read_probe_blocks", "read_probe",
+           "Embedding"]
 
 
 def lr_at(iter, batch, **policy):
@@ -312,3 +313,6 @@ class Plan:
         rc = _lib_step_noalloc(self.handle, g, wp, vp, lr, mu, wd, int(batch), op, bp, _stream(stream))
         if rc:
             raise FcError("fc_step_noalloc", rc)
+
+
+from .lm import Embedding  # noqa: E402,F401

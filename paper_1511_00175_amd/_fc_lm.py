@@ -1,0 +1,27 @@
+"""ctypes binding of libfc_lm.so (include/fc_lm.h), argument marshalling only,
+as _fc.py is for libfc.so.  If the library is missing the import fails: there
+is no other implementation to fall back to."""
+import ctypes
+import os
+
+from ._fc import PKG
+
+LIB_PATH = os.path.join(PKG, "libfc_lm.so")
+FC_BF16 = 2
+
+if not os.path.exists(LIB_PATH):
+    raise ImportError(f"{LIB_PATH} is not built; run __graft_entry__.build() or "
+                      "python paper_1511_00175_amd/build.py")
+
+lib = ctypes.CDLL(LIB_PATH)
+
+_vp, _i, _l, _f = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_float
+_pp = ctypes.POINTER(ctypes.c_void_p)
+
+lib.fc_embed_create.argtypes = [_pp, _l, _l, _l]
+lib.fc_embed_destroy.argtypes = [_vp]
+lib.fc_embed_destroy.restype = None
+lib.fc_embed_lookup.argtypes = [_vp, _vp, _i, _l, _vp, _i, _l, _f, _vp, _i, _l, _vp]
+lib.fc_embed_grad.argtypes = [_vp, _vp, _i, _l, _vp, _i, _l, _f, _vp, _i, _l, _i, _vp]
+for _n in ("fc_embed_create", "fc_embed_lookup", "fc_embed_grad"):
+    getattr(lib, _n).restype = _i

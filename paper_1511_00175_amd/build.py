@@ -1,4 +1,5 @@
-"""Build libfc.so (HIP kernels + C ABI) for gfx950, in place, with hipcc.
+"""Build libfc.so (aggregation and update) and libfc_lm.so (the operators of
+fc_lm.h), HIP kernels + C ABI each, for gfx950, in place, with hipcc.
 
 Flags that matter for results:
   -ffp-contract=off   no fused multiply-add: every operation is rounded once
@@ -16,7 +17,9 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libfc.so")
+LIB_LM = os.path.join(PKG, "libfc_lm.so")
 SOURCES = ["fc_reduce_f32.hip", "fc_reduce_f16.hip", "fc_update.hip", "fc_api.cpp"]
+SOURCES_LM = ["fc_embed.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", "-ffp-contract=off",
@@ -59,24 +62,27 @@ def _compile(src, obj, extra):
 
 
 def build(out=LIB, extra=()):
-    """Compile every source and link the shared library; returns its path."""
+    """Compile every source and link the shared libraries; returns the first's
+    path."""
     objdir = os.path.join(PKG, "_build")
     os.makedirs(objdir, exist_ok=True)
-    objs = [os.path.join(objdir, s + ".o") for s in SOURCES]
-    with ThreadPoolExecutor(len(SOURCES)) as ex:
+    sources = SOURCES + SOURCES_LM
+    objs = [os.path.join(objdir, s + ".o") for s in sources]
+    with ThreadPoolExecutor(len(sources)) as ex:
         usage = {}
-        for u in ex.map(lambda a: _compile(*a, list(extra)), zip(SOURCES, objs)):
+        for u in ex.map(lambda a: _compile(*a, list(extra)), zip(sources, objs)):
             usage.update(u)
-    # every kernel keeps its reduction stack in registers: no scratch memory
+    # every kernel keeps its sums and tiles in registers and LDS: no scratch memory
     with open(RESOURCES, "w") as f:
         for name in sorted(usage):
             f.write(name + " " + " ".join(f"{k}={v}" for k, v in sorted(usage[name].items())) + "\n")
     spill = [n for n, u in usage.items() if u.get("ScratchSize", 0)]
     if spill:
         raise RuntimeError("kernels using scratch memory: " + ", ".join(spill))
-    tmp = out + ".tmp"
-    subprocess.run([HIPCC, "-shared", "-fPIC", f"--offload-arch={ARCH}", *objs, "-o", tmp], check=True)
-    os.replace(tmp, out)
+    for lib, part in ((out, objs[:len(SOURCES)]), (LIB_LM, objs[len(SOURCES):])):
+        tmp = lib + ".tmp"
+        subprocess.run([HIPCC, "-shared", "-fPIC", f"--offload-arch={ARCH}", *part, "-o", tmp], check=True)
+        os.replace(tmp, lib)
     return out
 
 

@@ -1,0 +1,210 @@
+"""Embedding rows and their gradient on the GPU against the definition in 64
+bits.
+
+Bounds, from the operations: a looked-up element is one fp32 product rounded to
+the output's type, so |err| <= (u32 + u_out) |y| (+ the type's smallest step).
+A gradient element is an fp32 sum of c terms, one product with the scale and,
+with accumulate, one more sum: |err| <= (c + 3) u32 * (sum of |terms|) + u_out
+|y|, u = 2^-24, 2^-11, 2^-8 for the three types, all doubled for the terms of
+second order."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+U = {"f32": 2.0 ** -24, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}
+TINY = {"f32": 1e-37, "f16": 2.0 ** -24, "bf16": 1e-37}
+
+
+@pytest.fixture(scope="module")
+def fc(device):
+    import paper_1511_00175_amd as m
+    return m
+
+
+def tokens_of(kind, n, rows, gen, dev):
+    if kind == "same":
+        return torch.full((n,), rows - 1, device=dev)
+    if kind == "pad":
+        return torch.full((n,), -1, device=dev)
+    if kind == "ends":  # first and last row, and everything outside
+        v = torch.tensor([0, rows - 1, rows, -1, 2 ** 31 - 1, -2 ** 31, 2 ** 40, -2 ** 40], device=dev)
+        return v[torch.randint(0, len(v), (n,), generator=gen, device=dev)]
+    if kind == "few":  # a few rows hold most of the tokens
+        u = torch.rand(n, generator=gen, device=dev)
+        t = (float(rows) ** u - 1).long().clamp(0, rows - 1)
+        return torch.where(torch.rand(n, generator=gen, device=dev) < 0.1, -1, t)
+    return torch.randint(0, rows, (n,), generator=gen, device=dev)
+
+
+def strided(rows, cols, dtype, dev, pad=0, shift=0):
+    """A (rows, cols) tensor whose rows are cols + pad apart, `shift` elements into its memory."""
+    base = torch.zeros(shift + max(rows, 1) * (cols + pad), dtype=dtype, device=dev)
+    return base[shift:].view(-1)[:rows * (cols + pad)].view(rows, cols + pad)[:, :cols]
+
+
+def run_case(fc, device, rows, dim, n, ti="f32", to="f32", kind="uniform", wide=True, pad=0, shift=0, accumulate=False,
+             scale=1.75):
+    g = torch.Generator(device=device)
+    g.manual_seed(rows * 7 + dim * 3 + n)
+    tok = tokens_of(kind, n, rows, g, device)
+    plan = fc.Embedding(rows, dim, n)
+    passed = tok if wide else tok.clamp(-2 ** 31, 2 ** 31 - 1).to(torch.int32)
+    live = (tok >= 0) & (tok < rows)
+    at = tok.clamp(0, rows - 1)
+
+    table = strided(rows, dim, DT[ti], device, pad, shift)
+    table.copy_(torch.randn(rows, dim, generator=g, device=device))
+    out = strided(n, dim, DT[to], device, pad, shift)
+    out.fill_(float("nan"))
+    plan.lookup(table, passed, out, scale=scale)
+    want = torch.where(live[:, None], table.double()[at] * scale, 0.0)
+    err = (out.double() - want).abs()
+    assert bool((err <= 2 * (U["f32"] + U[to]) * want.abs() + TINY[to]).all())
+
+    dy = strided(n, dim, DT[ti], device, pad, shift)
+    dy.copy_(torch.randn(n, dim, generator=g, device=device))
+    dy[~live] = float("nan")  # what padding holds does not matter
+    grad = strided(rows, dim, DT[to], device, pad, shift)
+    old = torch.randn(rows, dim, generator=g, device=device).to(DT[to])
+    grad.copy_(old if accumulate else torch.full_like(old, float("nan")))
+    plan.grad(dy, passed, grad, scale=scale, accumulate=accumulate)
+    first = grad.clone()
+    terms = dy[live].double() * scale
+    want = torch.zeros(rows, dim, dtype=torch.float64, device=device).index_add_(0, at[live], terms)
+    size = torch.zeros_like(want).index_add_(0, at[live], terms.abs())
+    count = torch.bincount(at[live], minlength=rows).double()[:, None]
+    if accumulate:
+        want += old.double()
+        size += old.double().abs()
+    err = (first.double() - want).abs()
+    assert bool((err <= 2 * ((count + 3) * U["f32"] * size + U[to] * want.abs()) + TINY[to]).all())
+
+    grad.copy_(old if accumulate else torch.full_like(old, float("nan")))
+    plan.grad(dy, passed, grad, scale=scale, accumulate=accumulate)
+    assert torch.equal(grad, first)  # the same bits again
+    if pad:  # between the rows nothing is written
+        whole = torch.as_strided(grad, (rows, dim + pad), (dim + pad, 1))
+        assert float(whole[:-1, dim:].abs().max() if rows > 1 else 0) == 0
+
+
+@pytest.mark.parametrize("rows,dim,n", [(1, 1, 1), (5, 3, 0), (7, 64, 1), (1000, 1001, 33), (50, 8, 4096), (511, 24, 4097),
+                                        (513, 130, 9000), (300000, 16, 20000), (40, 2048, 12289)])
+@pytest.mark.parametrize("kind", ["uniform", "few"])
+def test_sizes(fc, device, rows, dim, n, kind):
+    run_case(fc, device, rows, dim, n, kind=kind)
+
+
+@pytest.mark.parametrize("kind", ["same", "pad", "ends"])
+@pytest.mark.parametrize("n", [1, 9, 700, 20000])
+@pytest.mark.parametrize("wide", [True, False])
+def test_token_lists(fc, device, kind, n, wide):
+    run_case(fc, device, 97, 72, n, kind=kind, wide=wide)
+
+
+@pytest.mark.parametrize("ti", list(DT))
+@pytest.mark.parametrize("to", list(DT))
+@pytest.mark.parametrize("dim,pad,shift", [(256, 0, 0), (256, 8, 0), (100, 0, 0), (102, 2, 2), (33, 4, 1)])
+def test_types_strides_alignment(fc, device, ti, to, dim, pad, shift):
+    run_case(fc, device, 301, dim, 900, ti, to, "few", pad=pad, shift=shift)
+
+
+@pytest.mark.parametrize("to", list(DT))
+@pytest.mark.parametrize("n", [0, 300, 9000])
+def test_accumulate(fc, device, to, n):
+    run_case(fc, device, 211, 96, n, "f16", to, "few", accumulate=True)
+
+
+def test_gradient_is_that_of_the_lookup(fc, device):
+    """<lookup(table + d) - lookup(table), dy> == <d, grad(dy)>: the lookup is
+    linear, so differences are exact but for the roundings (fp32, 1e-4 of the
+    terms' size)."""
+    rows, dim, n = 61, 40, 500
+    g = torch.Generator(device=device)
+    g.manual_seed(3)
+    tok = torch.randint(-3, rows, (n,), generator=g, device=device)
+    table, d = (torch.randn(rows, dim, generator=g, device=device) for _ in range(2))
+    dy = torch.randn(n, dim, generator=g, device=device)
+    plan = fc.Embedding(rows, dim, n)
+    a, b, grad = torch.empty_like(dy), torch.empty_like(dy), torch.empty_like(table)
+    plan.lookup(table + d, tok, a, scale=3.0)
+    plan.lookup(table, tok, b, scale=3.0)
+    plan.grad(dy, tok, grad, scale=3.0)
+    left, right = ((a - b).double() * dy.double()).sum(), (d.double() * grad.double()).sum()
+    size = ((a - b).double() * dy.double()).abs().sum()
+    assert abs(float(left - right)) <= 1e-4 * float(size)
+
+
+def test_streams_are_ordered(fc, device):
+    """One plan on two streams in turn: the second call waits for the first,
+    which uses the same workspace."""
+    rows, dim, n = 5000, 256, 20000
+    g = torch.Generator(device=device)
+    g.manual_seed(4)
+    plan = fc.Embedding(rows, dim, n)
+    sets = [(torch.randint(0, rows, (n,), generator=g, device=device), torch.randn(n, dim, generator=g, device=device))
+            for _ in range(4)]
+    want = []
+    for tok, dy in sets:
+        out = torch.empty(rows, dim, device=device)
+        plan.grad(dy, tok, out)
+        want.append(out)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [torch.empty(rows, dim, device=device) for _ in sets]
+    for _ in range(3):
+        for i, (tok, dy) in enumerate(sets):
+            plan.grad(dy, tok, got[i], stream=streams[i % 2])
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+
+
+def test_graph(fc, device):
+    rows, dim, n = 700, 128, 6000
+    g = torch.Generator(device=device)
+    g.manual_seed(5)
+    plan = fc.Embedding(rows, dim, n)
+    tok = torch.randint(-1, rows, (n,), generator=g, device=device)
+    table = torch.randn(rows, dim, generator=g, device=device)
+    y, grad = torch.empty(n, dim, device=device), torch.empty(rows, dim, device=device)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        plan.lookup(table, tok, y, scale=2.0)
+        plan.grad(y, tok, grad)
+    for k in range(4):
+        tok.copy_(torch.randint(-1, rows, (n,), generator=g, device=device))
+        y.fill_(7.0)
+        grad.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        a, b = y.clone(), grad.clone()
+        other = fc.Embedding(rows, dim, n)
+        other.lookup(table, tok, y, scale=2.0)
+        other.grad(y, tok, grad)
+        assert torch.equal(a, y) and torch.equal(b, grad), k
+
+
+def test_refusals(fc, device):
+    plan = fc.Embedding(100, 64, 32)
+    tok = torch.zeros(16, dtype=torch.int64, device=device)
+    table = torch.zeros(100, 64, device=device)
+    out = torch.zeros(16, 64, device=device)
+    for bad in (lambda: plan.lookup(table[:99], tok, out), lambda: plan.lookup(table.double(), tok, out),
+                lambda: plan.lookup(table, tok.float(), out), lambda: plan.lookup(table, tok[::2], out[:8]),
+                lambda: plan.lookup(table, tok, out[:15]), lambda: plan.lookup(table.cpu(), tok, out),
+                lambda: plan.lookup(table.t().contiguous().t(), tok, out), lambda: plan.lookup(table, tok.tolist(), out),
+                lambda: plan.grad(out.repeat(3, 1), tok.repeat(3), table),     # more tokens than the plan's
+                lambda: plan.lookup(table, tok, out[:1].expand(16, 64))):      # rows over each other
+        with pytest.raises(ValueError):
+            bad()
+    for bad in (lambda: plan.lookup(table, tok, table[:16]), lambda: plan.grad(table[:16], tok, table)):
+        with pytest.raises(fc.FcError) as e:
+            bad()
+        assert e.value.code == -3  # FC_EALIAS
+    for args in ((0, 64, 1), (100, 0, 1), (100, 64, -1), (1 << 31, 1, 1), (10, (1 << 20) + 1, 1)):
+        with pytest.raises(fc.FcError) as e:
+            fc.Embedding(*args)
+        assert e.value.code == -1  # FC_EINVAL
