@@ -74,6 +74,38 @@ int fc_embed_grad(fc_embed* plan, const void* dy, int dy_dtype, int64_t ld_dy, c
                   int64_t n, float scale, void* dtable, int dtable_dtype, int64_t ld_dtable, int accumulate,
                   void* stream);
 
+/* ---- cross entropy ------------------------------------------------------ */
+
+typedef struct fc_xent fc_xent;
+
+/* A plan for a vocabulary of `rows` rows of `dim` elements and up to
+ * `max_tokens` tokens a call; x and w are of `dtype`, FC_F16 or FC_BF16.
+ * 1 <= rows, dim <= 2^21, 0 <= max_tokens < 2^31.  The workspace holds, for
+ * `chunk_tokens` tokens at a time (0: as many as fit in 4 GiB, at least 256),
+ * 16 bits per token and row, and for plans of more tokens than that 4 bytes per
+ * element of dw. */
+int fc_xent_create(fc_xent** plan, int64_t rows, int64_t dim, int64_t max_tokens, int dtype, int64_t chunk_tokens);
+void fc_xent_destroy(fc_xent* plan);
+
+/* loss[t] = log sum over r of exp(l[t, r]) - l[t, targets[t]], l[t, r] = the sum
+ * over d of x[t, d] w[r, d], for t < n <= max_tokens.  Products, logits,
+ * maxima, sums and the loss are fp32.  Unless dim is not a multiple of 8 (x and
+ * w are then copied), ld_x and ld_w are multiples of 8 and x and w 16-byte
+ * aligned (FC_EALIGN); both strides are at most 2^21. */
+int fc_xent_loss(fc_xent* plan, const void* x, int64_t ld_x, const void* w, int64_t ld_w, const void* targets,
+                 int token_bytes, int64_t n, float* loss, void* stream);
+
+/* The same, with the gradients of scale * the sum of the losses:
+ *   dx[t, :] = scale * sum over r of d[t, r] w[r, :]
+ *   dw[r, :] = scale * sum over t of d[t, r] x[t, :]
+ *   d[t, r] = exp(l[t, r] - lse[t]) - (r == targets[t])
+ * d is rounded to x's type for the products (its numerator once before), their
+ * sums are fp32 and rounded once to the output's type.  Either output may be
+ * null.  Without tokens dw is zeros. */
+int fc_xent_loss_grad(fc_xent* plan, const void* x, int64_t ld_x, const void* w, int64_t ld_w, const void* targets,
+                      int token_bytes, int64_t n, float scale, float* loss, void* dx, int dx_dtype, int64_t ld_dx,
+                      void* dw, int dw_dtype, int64_t ld_dw, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -23,5 +23,10 @@ lib.fc_embed_destroy.argtypes = [_vp]
 lib.fc_embed_destroy.restype = None
 lib.fc_embed_lookup.argtypes = [_vp, _vp, _i, _l, _vp, _i, _l, _f, _vp, _i, _l, _vp]
 lib.fc_embed_grad.argtypes = [_vp, _vp, _i, _l, _vp, _i, _l, _f, _vp, _i, _l, _i, _vp]
-for _n in ("fc_embed_create", "fc_embed_lookup", "fc_embed_grad"):
+lib.fc_xent_create.argtypes = [_pp, _l, _l, _l, _i, _l]
+lib.fc_xent_destroy.argtypes = [_vp]
+lib.fc_xent_destroy.restype = None
+lib.fc_xent_loss.argtypes = [_vp, _vp, _l, _vp, _l, _vp, _i, _l, _vp, _vp]
+lib.fc_xent_loss_grad.argtypes = [_vp, _vp, _l, _vp, _l, _vp, _i, _l, _f, _vp, _vp, _i, _l, _vp, _i, _l, _vp]
+for _n in ("fc_embed_create", "fc_embed_lookup", "fc_embed_grad", "fc_xent_create", "fc_xent_loss", "fc_xent_loss_grad"):
     getattr(lib, _n).restype = _i

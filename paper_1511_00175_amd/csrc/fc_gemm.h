@@ -58,12 +58,15 @@ template <> struct Half<__bf16> {
 // A matrix operand: element (row, k) at p + row * ld + k (contiguous) or
 // p + k * ld + row (slow), in elements.  p is 16-byte aligned and ld a multiple
 // of 8; a contiguous operand's k extent is a multiple of 8 and a slow one's rows
-// are readable up to the next multiple of 8.  `lo` is where the second half of a
-// value kept as a sum of two 16-bit numbers lies, from p (products of 3 parts).
+// are readable up to the next multiple of 8.  `ks` is its k extent: beyond it the
+// operand is zero.  256 ld < 2^30: offsets within a tile are 32 bits.  `lo` is
+// where the second half of a value kept as a sum of two 16-bit numbers lies,
+// from p (products of 3 parts).
 struct Operand {
     const void* p;
     int64_t ld;
     int rows;
+    int ks;
     int64_t lo;
 };
 
@@ -96,12 +99,14 @@ template <int R, bool SLOW, int WAVES> struct TileLoads {
     uint64_t base;   // of the operand's tile row, k = 0
     uint64_t ldb;
     int64_t lob;
+    int ks;
     uint32_t span;   // bytes from a k's base to the end of the tile's last valid row, k extent apart
     uint32_t tail;   // slow: bytes of a row from the tile's first column to the operand's last
 
     __device__ __forceinline__ void init(const Operand& o, int row0, int wave, int lane) {
         ldb = 2 * (uint64_t)o.ld;
         lob = 2 * o.lo;
+        ks = o.ks;
         const int left = o.rows - row0;
         if constexpr (!SLOW) {
             const int chunk = (lane & 7) ^ (lane >> 3);
@@ -131,16 +136,16 @@ template <int R, bool SLOW, int WAVES> struct TileLoads {
             }
         }
     }
-    // Loads of the tile at k0 of K in all, into LDS at `lds`; part 1 = the second halves.
-    __device__ __forceinline__ void issue(uint32_t lds, int k0, int K, bool part, int wave) const {
+    // Loads of the tile at k0 (below ks) into LDS at `lds`; `part`: of the second halves.
+    __device__ __forceinline__ void issue(uint32_t lds, int k0, bool part, int wave) const {
         uint64_t b = base + (part ? (uint64_t)lob : 0);
         uint32_t records;
         if constexpr (!SLOW) {
             b += 2 * (uint64_t)k0;
-            records = span + 2u * (K - k0);
+            records = span + 2u * (ks - k0);
         } else {
             b += (uint64_t)k0 * ldb;
-            const int left = K - k0;
+            const int left = ks - k0;
             records = (uint32_t)((uint64_t)((left < GEMM_BK ? left : GEMM_BK) - 1) * ldb) + tail;
         }
         u32x4 d;
@@ -149,7 +154,7 @@ template <int R, bool SLOW, int WAVES> struct TileLoads {
         d.z = __builtin_amdgcn_readfirstlane(records);
         d.w = 0x00020000u;
         const uint32_t to = __builtin_amdgcn_readfirstlane(lds + wave * COUNT * 1024);
-        const bool past = !SLOW && k0 + (int)kpart >= K;
+        const bool past = !SLOW && k0 + (int)kpart >= ks;
 #pragma unroll
         for (int i = 0; i < COUNT; ++i) load_to_lds(d, to + i * 1024, past ? GEMM_OUTSIDE : off[i]);
     }
@@ -202,9 +207,9 @@ template <typename T_, int BM_, int BN_, int WM_, int WN_, bool AS, bool BS, int
 
     // Parts: 1, or 3 for operands kept as sums of two 16-bit numbers (high by
     // high, high by low, low by high; low by low is below the result's last bit).
-    // k runs over [kb, ke) of K in all.
-    __device__ __forceinline__ void run(char* lds, const Operand& A, const Operand& B, int m0, int n0, int K, int kb, int ke,
-                                        int parts) {
+    // k runs over [kb, ke), kb below both operands' extents, and ke - kb a multiple
+    // of 64 unless one of them ends there.
+    __device__ __forceinline__ void run(char* lds, const Operand& A, const Operand& B, int m0, int n0, int kb, int ke, int parts) {
         const int lane = threadIdx.x & 63;
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const uint32_t la = lds_address(lds), lb = la + BM * GEMM_BK * 2;
@@ -225,8 +230,8 @@ template <typename T_, int BM_, int BN_, int WM_, int WN_, bool AS, bool BS, int
         int part = 0, k = kb, issued = 0;
         auto issue = [&]() {
             const uint32_t s = (issued % STAGES) * STAGE;
-            ta.issue(la + s, k, ke, part == 2, wave);
-            tb.issue(lb + s, k, ke, part == 1, wave);
+            ta.issue(la + s, k, part == 2, wave);
+            tb.issue(lb + s, k, part == 1, wave);
             k += GEMM_BK;
             if (k >= ke) {
                 k = kb;

@@ -1,0 +1,632 @@
+// Softmax cross entropy over a vocabulary, with its gradients (fc_lm.h).
+//
+//   l = x w^T, lse[t] = log sum exp l[t, :], loss[t] = lse[t] - l[t, y[t]]
+//   d = softmax(l) - onehot(y), dx = scale d w, dw = scale d^T x
+//
+// The products are 2 tokens rows dim operations each and bound everything but
+// short lists, where reading w does.  The logits are never stored.  A wave of the
+// first product holds a piece of the vocabulary for its tokens in fp32: it takes
+// the piece's maximum m and sum of exponentials, keeps both (8 bytes), the
+// target's logit, and, when gradients are wanted, the numerators exp(l - m) in 16
+// bits.  One small kernel joins a token's pieces into lse and the loss; one pass
+// over the numerators then turns them into d (numerator * exp(m - lse), minus one
+// at the target), and two products make the gradients of it.  The alternative
+// that keeps nothing computes the first product twice: 8 instead of 6 units of
+// work, against one read and one write of 16 bits per token and row.
+//
+// Tokens go through in chunks so that the numerators take at most 4 GiB; with
+// more than one chunk, dw is summed in fp32 over them and rounded after the last.
+#include <algorithm>
+
+#include "fc_gemm.h"
+#include "fc_lm_host.h"
+
+using fc::Operand;
+using fc::f32x2;
+using fc::f32x4;
+using fc::Half;
+
+namespace {
+
+typedef _Float16 f16;
+typedef __bf16 bf16;
+
+extern __shared__ __align__(1024) char lds[];
+
+constexpr float LOG2E = 1.44269504088896341f;
+
+// d is stored times this: fp16 then keeps probabilities down to 2^-29 with all
+// their bits, and its largest, 1, is still in range.  bf16 needs no scale.
+template <typename T> constexpr float D_SCALE = 1.f;
+template <> constexpr float D_SCALE<f16> = 32768.f;
+
+__device__ __forceinline__ float exp_(float x) { return __builtin_amdgcn_exp2f(x * LOG2E); }
+
+__device__ __forceinline__ int64_t target_of(const void* p, int bytes, int64_t t) {
+    return bytes == 8 ? static_cast<const int64_t*>(p)[t] : static_cast<const int32_t*>(p)[t];
+}
+
+// ---- the first product ----------------------------------------------------
+
+struct LogitArgs {
+    Operand x, w;            // both along k = dim
+    int n, rows, dim;
+    const void* targets;
+    int target_bytes;
+    f32x2* stats;            // [piece][token]: maximum, sum
+    float* target_logit;
+    void* numer;             // [token][ld], or null
+    int64_t ld;
+    int tm, tn;
+};
+
+template <typename P> __global__ __launch_bounds__(P::THREADS, P::THREADS / 256) void logit_kernel(LogitArgs a) {
+    typedef typename P::T T;
+    int ti, tj;
+    fc::tile_place(fc::xcd_order(blockIdx.x, a.tm * a.tn), a.tm, a.tn, 4, ti, tj);
+    P p;
+    p.run(lds, a.x, a.w, ti * P::BM, tj * P::BN, 0, a.dim, 1);
+    const int n0 = tj * P::BN + P::col(0);
+    const int piece = (tj * P::BN) / P::WN + (threadIdx.x >> 6) % (P::BN / P::WN);
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < P::FM; ++i) {
+        const int m = ti * P::BM + P::row(i);
+        const bool live = m < a.n;
+        const int64_t y = live ? target_of(a.targets, a.target_bytes, m) : -1;
+        const int at = y >= 0 && y < a.rows ? (int)y - n0 : -1;  // the target among the lane's columns
+        float top = -__builtin_inff();
+#pragma unroll
+        for (int j = 0; j < P::FN; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (n0 + 16 * j + e >= a.rows) p.acc[i][j][e] = -__builtin_inff();
+                top = fmaxf(top, p.acc[i][j][e]);
+                if (at == 16 * j + e) a.target_logit[m] = p.acc[i][j][e];
+            }
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float ref = top == -__builtin_inff() ? 0.f : top;
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < P::FN; ++j) {
+            typename Half<T>::v4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float q = exp_(p.acc[i][j][e] - ref);
+                sum += q;
+                v[e] = (T)q;
+            }
+            const int n = n0 + 16 * j;
+            if (a.numer && live && n < a.ld)
+                *reinterpret_cast<typename Half<T>::v4*>(static_cast<T*>(a.numer) + (int64_t)m * a.ld + n) = v;
+        }
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        if (live && lane < 16 && piece * P::WN < a.rows) a.stats[(int64_t)piece * a.n + m] = f32x2{top, sum};
+    }
+}
+
+// ---- a token's pieces joined ------------------------------------------------
+
+struct JoinArgs {
+    const f32x2* stats;
+    const float* target_logit;
+    const void* targets;
+    int target_bytes;
+    int n, rows, pieces;
+    float* lse;
+    int* row;                // the token's target, or -1
+    float* loss;
+};
+
+// 16 tokens per block, 16 threads each.
+__global__ __launch_bounds__(256) void join_kernel(JoinArgs a) {
+    __shared__ f32x2 part[16][17];
+    const int i = threadIdx.x & 15, q = threadIdx.x >> 4;
+    const int64_t t = (int64_t)blockIdx.x * 16 + i;
+    float top = -__builtin_inff(), sum = 0.f;
+    if (t < a.n)
+        for (int k = q; k < a.pieces; k += 16) {
+            const f32x2 s = a.stats[(int64_t)k * a.n + t];
+            const float m = fmaxf(top, s.x);
+            if (m > -__builtin_inff()) sum = sum * exp_(top - m) + s.y * exp_(s.x - m);
+            else sum += s.y;
+            top = m;
+        }
+    part[i][q] = f32x2{top, sum};
+    __syncthreads();
+    if (q || t >= a.n) return;
+    for (int k = 1; k < 16; ++k) {
+        const f32x2 s = part[i][k];
+        const float m = fmaxf(top, s.x);
+        if (m > -__builtin_inff()) sum = sum * exp_(top - m) + s.y * exp_(s.x - m);
+        else sum += s.y;
+        top = m;
+    }
+    const int64_t y = target_of(a.targets, a.target_bytes, t);
+    const bool real = y >= 0 && y < a.rows;
+    const float lse = top + logf(sum);
+    if (a.lse) {
+        a.lse[t] = lse;
+        a.row[t] = real ? (int)y : -1;
+    }
+    a.loss[t] = real ? lse - a.target_logit[t] : 0.f;
+}
+
+// ---- numerators to d --------------------------------------------------------
+
+struct DiffArgs {
+    void* numer;
+    int64_t ld;
+    int n;
+    int width;               // of a piece
+    int pieces;
+    const f32x2* stats;
+    const float* lse;
+    const int* row;
+};
+
+constexpr int DIFF_ROWS = 8;
+
+// A block's 256 threads hold 8 columns each, of DIFF_ROWS tokens one after the
+// other, whose stats are neighbours in memory.
+template <typename T> __global__ __launch_bounds__(256) void diff_kernel(DiffArgs a) {
+    typedef typename Half<T>::v8 v8;
+    const int64_t col = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+    if (col >= a.ld) return;
+    const int piece = min((int)(col / a.width), a.pieces - 1);
+    const int t0 = blockIdx.y * DIFF_ROWS;
+    v8 x[DIFF_ROWS];
+    float f[DIFF_ROWS];
+    int row[DIFF_ROWS];
+#pragma unroll
+    for (int i = 0; i < DIFF_ROWS; ++i) {
+        const int t = min(t0 + i, a.n - 1);
+        x[i] = *reinterpret_cast<const v8*>(static_cast<const T*>(a.numer) + t * a.ld + col);
+        row[i] = a.row[t];
+        f[i] = exp_(a.stats[(int64_t)piece * a.n + t].x - a.lse[t]) * D_SCALE<T>;
+    }
+#pragma unroll
+    for (int i = 0; i < DIFF_ROWS; ++i) {
+        if (t0 + i >= a.n) break;
+        v8 y;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float v = (float)x[i][e] * f[i];
+            if (col + e == row[i]) v -= D_SCALE<T>;
+            y[e] = (T)(row[i] >= 0 ? v : 0.f);
+        }
+        *reinterpret_cast<v8*>(static_cast<T*>(a.numer) + (t0 + i) * a.ld + col) = y;
+    }
+}
+
+// ---- the gradients' products ------------------------------------------------
+
+__device__ __forceinline__ void store_one(void* p, int dt, int64_t at, float v) {
+    if (dt == FC_F32) static_cast<float*>(p)[at] = v;
+    else if (dt == FC_F16) static_cast<f16*>(p)[at] = (f16)v;
+    else static_cast<bf16*>(p)[at] = (bf16)v;
+}
+
+// Up to 4 neighbouring elements; `wide`: the row starts allow whole vectors.
+__device__ __forceinline__ void store_four(void* p, int dt, int64_t at, f32x4 v, int left, bool wide) {
+    if (wide && left >= 4) {
+        if (dt == FC_F32) {
+            *reinterpret_cast<f32x4*>(static_cast<float*>(p) + at) = v;
+        } else if (dt == FC_F16) {
+            fc::f16x4 o;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = (f16)v[e];
+            *reinterpret_cast<fc::f16x4*>(static_cast<f16*>(p) + at) = o;
+        } else {
+            fc::b16x4 o;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = (bf16)v[e];
+            *reinterpret_cast<fc::b16x4*>(static_cast<bf16*>(p) + at) = o;
+        }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (e < left) store_one(p, dt, at + e, v[e]);
+}
+
+struct GradArgs {
+    Operand a, b;
+    int m, n, k;             // of the product
+    int kper;                // of one split, a multiple of 64
+    float scale;
+    const int* row;          // per m: below 0, the result is zero; or null
+    void* out;
+    int dt;
+    int64_t ld;
+    bool wide;
+    float* sum;              // fp32 sums over calls or splits, [split][m][n], or null
+    bool first, last;        // of the calls that add to `sum`
+    int tm, tn;
+};
+
+template <typename P> __global__ __launch_bounds__(P::THREADS, P::THREADS / 256) void grad_kernel(GradArgs a) {
+    int ti, tj;
+    fc::tile_place(fc::xcd_order(blockIdx.x, a.tm * a.tn), a.tm, a.tn, 8, ti, tj);
+    const int kb = blockIdx.y * a.kper, ke = min(a.k, kb + a.kper);
+    P p;
+    p.run(lds, a.a, a.b, ti * P::BM, tj * P::BN, kb, ke, 1);
+    float* const sum = a.sum ? a.sum + (int64_t)blockIdx.y * a.m * a.n : nullptr;
+#pragma unroll
+    for (int i = 0; i < P::FM; ++i) {
+        const int m = ti * P::BM + P::row(i);
+        if (m >= a.m) continue;
+        const bool zero = a.row && a.row[m] < 0;
+#pragma unroll
+        for (int j = 0; j < P::FN; ++j) {
+            const int n = tj * P::BN + P::col(j), left = a.n - n;
+            if (left <= 0) continue;
+            f32x4 v = p.acc[i][j];
+            if (sum) {
+                float* s = sum + (int64_t)m * a.n + n;
+                if (!a.first) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (e < left) v[e] += s[e];
+                }
+                if (!a.last) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (e < left) s[e] = v[e];
+                    continue;
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = zero ? 0.f : v[e] * a.scale;
+            store_four(a.out, a.dt, (int64_t)m * a.ld + n, v, left, a.wide);
+        }
+    }
+}
+
+struct SplitArgs {
+    const float* sum;
+    int splits, m, n;
+    float scale;
+    const int* row;
+    void* out;
+    int dt;
+    int64_t ld;
+};
+
+// The splits of a product added in order.
+__global__ __launch_bounds__(256) void split_kernel(SplitArgs a) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, total = (int64_t)a.m * a.n;
+    if (i >= total) return;
+    const int m = (int)(i / a.n), n = (int)(i % a.n);
+    float v = 0.f;
+    for (int s = 0; s < a.splits; ++s) v += a.sum[s * total + i];
+    store_one(a.out, a.dt, (int64_t)m * a.ld + n, a.row && a.row[m] < 0 ? 0.f : v * a.scale);
+}
+
+struct PackArgs {
+    const void* in;
+    int64_t ld_in;
+    void* out;
+    int64_t ld_out;          // a multiple of 8; the elements past the row's length are zeros
+    int64_t rows;
+    int len;
+    const void* targets;     // or null: rows without a target become zeros
+    int target_bytes;
+    int targets_below;
+};
+
+__global__ __launch_bounds__(256) void pack_kernel(PackArgs a) {
+    typedef unsigned short u16;
+    const int per_row = (int)(a.ld_out / 8);
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t r = i / per_row;
+    const int c = (int)(i % per_row) * 8;
+    if (r >= a.rows) return;
+    bool keep = true;
+    if (a.targets) {
+        const int64_t y = target_of(a.targets, a.target_bytes, r);
+        keep = y >= 0 && y < a.targets_below;
+    }
+    const u16* in = static_cast<const u16*>(a.in) + r * a.ld_in + c;
+    struct alignas(16) V {
+        u16 x[8];
+    } v;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v.x[e] = keep && c + e < a.len ? in[e] : (u16)0;
+    *reinterpret_cast<V*>(static_cast<u16*>(a.out) + r * a.ld_out + c) = v;
+}
+
+// Tiles: large ones for products that fill the chip with them, smaller ones
+// for the others, and few rows for short token lists, which are bound by reading w.
+template <typename T, bool AS, bool BS> using Large = fc::Product<T, 256, 256, 128, 64, AS, BS>;
+template <typename T, bool AS, bool BS> using Middle = fc::Product<T, 128, 128, 64, 64, AS, BS>;
+template <typename T, bool AS, bool BS> using Short = fc::Product<T, 64, 128, 64, 32, AS, BS, 3>;
+
+enum TileKind { LARGE, MIDDLE, SHORT };
+
+constexpr int CUS = 256;
+
+TileKind tile_for(int64_t m, int64_t n) {
+    if (m <= 64) return SHORT;
+    return m > 128 && n > 128 && fc::ceil_div(m, 256) * fc::ceil_div(n, 256) >= CUS ? LARGE : MIDDLE;
+}
+
+template <typename P> hipError_t prepare(const void* kernel) {
+    return P::LDS > 64 * 1024 ? hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, P::LDS) : hipSuccess;
+}
+
+template <typename P> void launch_logit(LogitArgs a, hipStream_t s) {
+    a.tm = (int)fc::ceil_div(a.n, P::BM);
+    a.tn = (int)fc::ceil_div(a.rows, P::BN);
+    logit_kernel<P><<<a.tm * a.tn, P::THREADS, P::LDS, s>>>(a);
+}
+
+template <typename P> void launch_grad(GradArgs a, hipStream_t s) {
+    a.tm = (int)fc::ceil_div(a.m, P::BM);
+    a.tn = (int)fc::ceil_div(a.n, P::BN);
+    grad_kernel<P><<<dim3(a.tm * a.tn, (unsigned)fc::ceil_div(a.k, a.kper)), P::THREADS, P::LDS, s>>>(a);
+}
+
+template <typename T> hipError_t prepare_all() {
+    hipError_t e[9] = {
+        prepare<Large<T, false, false>>((const void*)logit_kernel<Large<T, false, false>>),
+        prepare<Middle<T, false, false>>((const void*)logit_kernel<Middle<T, false, false>>),
+        prepare<Short<T, false, false>>((const void*)logit_kernel<Short<T, false, false>>),
+        prepare<Large<T, false, true>>((const void*)grad_kernel<Large<T, false, true>>),
+        prepare<Middle<T, false, true>>((const void*)grad_kernel<Middle<T, false, true>>),
+        prepare<Short<T, false, true>>((const void*)grad_kernel<Short<T, false, true>>),
+        prepare<Large<T, true, true>>((const void*)grad_kernel<Large<T, true, true>>),
+        prepare<Middle<T, true, true>>((const void*)grad_kernel<Middle<T, true, true>>),
+        hipSuccess,
+    };
+    for (hipError_t x : e)
+        if (x != hipSuccess) return x;
+    return hipSuccess;
+}
+
+int piece_width(TileKind k) { return k == LARGE ? Large<f16, false, false>::WN : k == MIDDLE ? Middle<f16, false, false>::WN : Short<f16, false, false>::WN; }
+
+// Splits of dx's product over the vocabulary: until the tiles fill the chip,
+// with at least 16 steps of k each.
+int splits_for(int64_t m, int64_t n, int64_t k) {
+    const TileKind t = tile_for(m, n);
+    const int64_t tiles = t == LARGE ? fc::ceil_div(m, 256) * fc::ceil_div(n, 256)
+                                     : fc::ceil_div(m, t == MIDDLE ? 128 : 64) * fc::ceil_div(n, 128);
+    if (tiles >= CUS) return 1;
+    return (int)std::max<int64_t>(1, std::min<int64_t>(2 * CUS / tiles, k / (16 * fc::GEMM_BK)));
+}
+
+constexpr int64_t ROWS_LIMIT = 1 << 21, LD_LIMIT = 1 << 21, TOKENS_LIMIT = (int64_t)1 << 31;
+constexpr int64_t NUMER_BYTES = (int64_t)4 << 30;
+
+}  // namespace
+
+struct fc_xent {
+    fc::CallOrder order;
+    fc::DeviceBlock block;
+    int64_t rows = 0, dim = 0, max_tokens = 0;
+    int dtype = FC_F16;
+    int64_t chunk = 0;       // tokens that go through together
+    int64_t ld = 0;          // of the numerators
+    int64_t ldp = 0;         // of packed x and w
+    bool pack = false;       // dim is not a multiple of 8: x and w go through packed copies
+    char* numer = nullptr;
+    f32x2* stats = nullptr;
+    float* target_logit = nullptr;
+    float* lse = nullptr;
+    int* row = nullptr;
+    char* x = nullptr;
+    char* w = nullptr;
+    float* sum = nullptr;    // splits of dx
+    float* dw = nullptr;     // dw over chunks
+};
+
+namespace {
+
+template <typename T>
+int run(fc_xent* p, const void* x, int64_t ldx, const void* w, int64_t ldw, const void* targets, int target_bytes, int64_t n,
+        float scale, float* loss, void* dx, int xdt, int64_t lddx, void* dw, int wdt, int64_t lddw, hipStream_t s) {
+    const bool grads = dx || dw;
+    auto pack = [&](const void* in, int64_t ld, void* out, int64_t rows, const void* mask) {
+        PackArgs a{in, ld, out, p->ldp, rows, (int)p->dim, mask, target_bytes, (int)p->rows};
+        pack_kernel<<<(unsigned)fc::ceil_div(rows * (p->ldp / 8), 256), 256, 0, s>>>(a);
+    };
+    if (p->pack) {
+        pack(w, ldw, p->w, p->rows, nullptr);
+        w = p->w;
+        ldw = p->ldp;
+    }
+    const int dimk = (int)(p->pack ? p->ldp : p->dim);
+    for (int64_t t0 = 0; t0 < n; t0 += p->chunk) {
+        const int m = (int)std::min(p->chunk, n - t0);
+        const void* xt = static_cast<const char*>(x) + t0 * ldx * 2;
+        const void* yt = static_cast<const char*>(targets) + t0 * target_bytes;
+        // dw's product must not meet what padding's rows hold (0 * NaN)
+        if (p->pack || dw) pack(xt, ldx, p->x, m, yt);
+        const Operand ox{p->pack || dw ? p->x : xt, p->pack || dw ? p->ldp : ldx, m, dimk, 0};
+        const Operand ow{w, ldw, (int)p->rows, dimk, 0};
+        const TileKind kind = tile_for(m, p->rows);
+        LogitArgs l{ox, ow, m, (int)p->rows, dimk, yt, target_bytes, p->stats, p->target_logit, grads ? p->numer : nullptr, p->ld, 0, 0};
+        if (kind == LARGE) launch_logit<Large<T, false, false>>(l, s);
+        else if (kind == MIDDLE) launch_logit<Middle<T, false, false>>(l, s);
+        else launch_logit<Short<T, false, false>>(l, s);
+        const int width = piece_width(kind), pieces = (int)fc::ceil_div(p->rows, width);
+        JoinArgs j{p->stats, p->target_logit, yt, target_bytes, m, (int)p->rows, pieces, p->lse, p->row, loss + t0};
+        join_kernel<<<(unsigned)fc::ceil_div(m, 16), 256, 0, s>>>(j);
+        if (!grads) continue;
+        DiffArgs d{p->numer, p->ld, m, width, pieces, p->stats, p->lse, p->row};
+        diff_kernel<T><<<dim3((unsigned)fc::ceil_div(p->ld, 2048), (unsigned)fc::ceil_div(m, DIFF_ROWS)), 256, 0, s>>>(d);
+        const float back = scale / D_SCALE<T>;
+        if (dx) {
+            GradArgs g{};
+            g.a = Operand{p->numer, p->ld, m, (int)p->ld, 0};
+            g.b = Operand{w, ldw, (int)p->dim, (int)p->rows, 0};
+            g.m = m;
+            g.n = (int)p->dim;
+            g.k = (int)p->rows;
+            const int splits = splits_for(m, p->dim, p->rows);
+            g.kper = (int)fc::ceil_div(fc::ceil_div(g.k, splits), fc::GEMM_BK) * fc::GEMM_BK;
+            g.scale = back;
+            g.row = p->row;
+            g.dt = xdt;
+            g.out = static_cast<char*>(dx) + t0 * lddx * fc::dtype_bytes(xdt);
+            g.ld = lddx;
+            g.wide = fc::vector_width({{dx, n, 4, lddx, fc::dtype_bytes(xdt), true}}, 4) == 4;
+            g.sum = splits > 1 ? p->sum : nullptr;
+            g.first = true;
+            g.last = splits == 1;
+            const TileKind k = tile_for(m, p->dim);
+            if (k == LARGE) launch_grad<Large<T, false, true>>(g, s);
+            else if (k == MIDDLE) launch_grad<Middle<T, false, true>>(g, s);
+            else launch_grad<Short<T, false, true>>(g, s);
+            if (splits > 1) {
+                SplitArgs q{p->sum, (int)fc::ceil_div(g.k, g.kper), m, g.n, back, p->row, g.out, xdt, lddx};
+                split_kernel<<<(unsigned)fc::ceil_div((int64_t)m * g.n, 256), 256, 0, s>>>(q);
+            }
+        }
+        if (dw) {
+            GradArgs g{};
+            g.a = Operand{p->numer, p->ld, (int)p->rows, m, 0};
+            g.b = Operand{p->x, p->ldp, (int)p->dim, m, 0};
+            g.m = (int)p->rows;
+            g.n = (int)p->dim;
+            g.k = m;
+            g.kper = (int)fc::ceil_div(m, fc::GEMM_BK) * fc::GEMM_BK;
+            g.scale = back;
+            g.out = dw;
+            g.dt = wdt;
+            g.ld = lddw;
+            g.wide = fc::vector_width({{dw, p->rows, 4, lddw, fc::dtype_bytes(wdt), true}}, 4) == 4;
+            g.sum = n > p->chunk ? p->dw : nullptr;
+            g.first = t0 == 0;
+            g.last = t0 + p->chunk >= n;
+            if (tile_for(g.m, g.n) == LARGE) launch_grad<Large<T, true, true>>(g, s);
+            else launch_grad<Middle<T, true, true>>(g, s);
+        }
+    }
+    return fc::hip_code(hipGetLastError());
+}
+
+// Zeros for a gradient without tokens.
+__global__ __launch_bounds__(256) void zero_kernel(void* p, int dt, int64_t rows, int64_t len, int64_t ld) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i < rows * len) store_one(p, dt, i / len * ld + i % len, 0.f);
+}
+
+int call(fc_xent* p, const void* x, int64_t ldx, const void* w, int64_t ldw, const void* targets, int target_bytes, int64_t n,
+         float scale, float* loss, void* dx, int xdt, int64_t lddx, void* dw, int wdt, int64_t lddw, hipStream_t s) {
+    if (!p || n < 0 || n > p->max_tokens || (target_bytes != 4 && target_bytes != 8)) return FC_EINVAL;
+    if (ldx > LD_LIMIT || ldw > LD_LIMIT) return FC_EINVAL;
+    const fc::Span none{nullptr, 0, 0, 0, 1, false};
+    int rc = fc::check_spans({{x, n, p->dim, ldx, 2, false},
+                              {w, p->rows, p->dim, ldw, 2, false},
+                              {targets, 1, n, n, target_bytes, false},
+                              {loss, 1, n, n, 4, true},
+                              dx ? fc::Span{dx, n, p->dim, lddx, fc::dtype_bytes(xdt), true} : none,
+                              dw ? fc::Span{dw, p->rows, p->dim, lddw, fc::dtype_bytes(wdt), true} : none});
+    if (rc) return rc;
+    // rows of whole 16-byte vectors, unless they are copied anyway
+    if (!p->pack && (ldx % 8 || ldw % 8 || reinterpret_cast<uintptr_t>(x) % 16 || reinterpret_cast<uintptr_t>(w) % 16)) return FC_EALIGN;
+    bool note;
+    rc = p->order.begin(s, note);
+    if (rc) return rc;
+    if (n == 0) {
+        if (dw) zero_kernel<<<(unsigned)fc::ceil_div(p->rows * p->dim, 256), 256, 0, s>>>(dw, wdt, p->rows, p->dim, lddw);
+        rc = fc::hip_code(hipGetLastError());
+    } else if (p->dtype == FC_F16) {
+        rc = run<f16>(p, x, ldx, w, ldw, targets, target_bytes, n, scale, loss, dx, xdt, lddx, dw, wdt, lddw, s);
+    } else {
+        rc = run<bf16>(p, x, ldx, w, ldw, targets, target_bytes, n, scale, loss, dx, xdt, lddx, dw, wdt, lddw, s);
+    }
+    p->order.done(s, note);
+    return rc;
+}
+
+}  // namespace
+
+extern "C" {
+
+int fc_xent_create(fc_xent** plan, int64_t rows, int64_t dim, int64_t max_tokens, int dtype, int64_t chunk_tokens) {
+    if (!plan) return FC_EINVAL;
+    *plan = nullptr;
+    if (rows < 1 || dim < 1 || max_tokens < 0 || rows > ROWS_LIMIT || dim > LD_LIMIT || max_tokens >= TOKENS_LIMIT ||
+        chunk_tokens < 0 || (dtype != FC_F16 && dtype != FC_BF16))
+        return FC_EINVAL;
+    return fc::no_throw([&] {
+        fc_xent* p = new fc_xent;
+        p->rows = rows;
+        p->dim = dim;
+        p->max_tokens = max_tokens;
+        p->dtype = dtype;
+        p->ld = fc::ceil_div(rows, 64) * 64;
+        p->ldp = fc::ceil_div(dim, 8) * 8;
+        p->pack = dim % 8 != 0;
+        int64_t most = NUMER_BYTES / (2 * p->ld);
+        most = std::max<int64_t>(256, most / 256 * 256);
+        if (chunk_tokens) most = std::min(most, chunk_tokens);
+        p->chunk = std::max<int64_t>(1, std::min(most, max_tokens));
+        const int64_t c = p->chunk;
+        // the most pieces and splits of any chunk length up to c
+        int64_t stats = 0, sums = 0;
+        for (int64_t m : {std::min<int64_t>(c, 64), c}) {
+            stats = std::max(stats, m * fc::ceil_div(rows, m <= 64 ? 32 : 64));
+        }
+        for (int64_t m = 1; m <= c; m = m < c && m + 64 > c ? c : m + 64) {
+            const int64_t up = std::min(c, m + 63);
+            const int sp = std::max(splits_for(m, dim, rows), splits_for(up, dim, rows));
+            if (sp > 1) sums = std::max(sums, sp * up * dim);
+        }
+        fc::Layout at;
+        const uint64_t o_numer = at.take(c * p->ld * 2), o_stats = at.take(stats * 8), o_logit = at.take(c * 4),
+                       o_lse = at.take(c * 4), o_row = at.take(c * 4), o_x = at.take(c * p->ldp * 2),
+                       o_w = at.take(p->pack ? rows * p->ldp * 2 : 0), o_sum = at.take(sums * 4),
+                       o_dw = at.take(max_tokens > c ? rows * dim * 4 : 0);
+        int rc = p->order.create();
+        if (!rc) rc = fc::hip_code(dtype == FC_F16 ? prepare_all<f16>() : prepare_all<bf16>());
+        if (!rc) rc = p->block.create(at.size);
+        if (rc) {
+            fc_xent_destroy(p);
+            return rc;
+        }
+        char* b = p->block.p;
+        p->numer = b + o_numer;
+        p->stats = reinterpret_cast<f32x2*>(b + o_stats);
+        p->target_logit = reinterpret_cast<float*>(b + o_logit);
+        p->lse = reinterpret_cast<float*>(b + o_lse);
+        p->row = reinterpret_cast<int*>(b + o_row);
+        p->x = b + o_x;
+        p->w = b + o_w;
+        p->sum = reinterpret_cast<float*>(b + o_sum);
+        p->dw = reinterpret_cast<float*>(b + o_dw);
+        *plan = p;
+        return FC_OK;
+    });
+}
+
+void fc_xent_destroy(fc_xent* p) {
+    if (!p) return;
+    p->block.destroy();
+    p->order.destroy();
+    delete p;
+}
+
+int fc_xent_loss(fc_xent* p, const void* x, int64_t ld_x, const void* w, int64_t ld_w, const void* targets, int token_bytes,
+                 int64_t n, float* loss, void* stream) {
+    return fc::no_throw([&] {
+        return call(p, x, ld_x, w, ld_w, targets, token_bytes, n, 1.f, loss, nullptr, 0, 0, nullptr, 0, 0,
+                    static_cast<hipStream_t>(stream));
+    });
+}
+
+int fc_xent_loss_grad(fc_xent* p, const void* x, int64_t ld_x, const void* w, int64_t ld_w, const void* targets,
+                      int token_bytes, int64_t n, float scale, float* loss, void* dx, int dx_dtype, int64_t ld_dx, void* dw,
+                      int dw_dtype, int64_t ld_dw, void* stream) {
+    return fc::no_throw([&] {
+        return call(p, x, ld_x, w, ld_w, targets, token_bytes, n, scale, loss, dx, dx_dtype, ld_dx, dw, dw_dtype, ld_dw,
+                    static_cast<hipStream_t>(stream));
+    });
+}
+
+}  // extern "C"

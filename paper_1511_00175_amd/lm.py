@@ -55,6 +55,21 @@ def _list(t, name, device):
     return t.data_ptr(), t.element_size(), t.shape[0]
 
 
+def _vector(t, name, n, device, code):
+    """`t` must be a contiguous vector of n elements of type `code` on the
+    device; returns its pointer."""
+    import torch
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{name} must be a torch tensor")
+    if _code(t) != code:
+        raise ValueError(f"{name} must not be {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the plan on {device}")
+    if t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous vector of {n} elements")
+    return t.data_ptr()
+
+
 def _stream(stream):
     from . import _stream as current
     return current(stream)
@@ -128,3 +143,44 @@ class Embedding(_Handle):
         yp, yc, yl = _matrix(dy, "dy", n, self.dim, self.device)
         gp, gc, gl = _matrix(dtable, "dtable", self.rows, self.dim, self.device)
         self._call("fc_embed_grad", yp, yc, yl, tok, size, n, scale, gp, gc, gl, bool(accumulate), _stream(stream))
+
+
+class CrossEntropy(_Handle):
+    """Softmax cross entropy over a vocabulary of `rows` rows of `dim` elements
+    (fc_xent), from the last layer's outputs x (tokens, dim) and the rows w, both
+    of `dtype` ("f16" or "bf16"), for up to `max_tokens` tokens.  The logits are
+    not kept; `chunk` tokens (0: as many as fit) go through together.
+
+    Targets outside [0, rows) are padding: loss 0, and no gradient."""
+
+    _destroy = "fc_xent_destroy"
+
+    def __init__(self, rows, dim, max_tokens, dtype="f16", chunk=0):
+        if dtype not in ("f16", "bf16"):
+            raise ValueError(f"dtype must be f16 or bf16, not {dtype}")
+        self.code = DTYPES[dtype]
+        self._create("fc_xent_create", rows, dim, max_tokens, self.code, chunk)
+        self.rows, self.dim, self.max_tokens = rows, dim, max_tokens
+
+    def _inputs(self, x, w, targets, loss):
+        yp, size, n = _list(targets, "targets", self.device)
+        if n > self.max_tokens:
+            raise ValueError(f"{n} tokens for a plan of {self.max_tokens}")
+        xp, _, xl = _matrix(x, "x", n, self.dim, self.device, self.code)
+        wp, _, wl = _matrix(w, "w", self.rows, self.dim, self.device, self.code)
+        lp = _vector(loss, "loss", n, self.device, FC_F32)
+        return xp, xl, wp, wl, yp, size, n, lp
+
+    def loss(self, x, w, targets, loss, stream=None):
+        """loss[t] = logsumexp(x[t] w^T) - x[t] . w[targets[t]], in fp32."""
+        xp, xl, wp, wl, yp, size, n, lp = self._inputs(x, w, targets, loss)
+        self._call("fc_xent_loss", xp, xl, wp, wl, yp, size, n, lp, _stream(stream))
+
+    def loss_grad(self, x, w, targets, loss, dx, dw, scale=1.0, stream=None):
+        """The losses, and the gradients of scale times their sum by x and w,
+        each of its tensor's type; dx or dw may be None."""
+        xp, xl, wp, wl, yp, size, n, lp = self._inputs(x, w, targets, loss)
+        dxp, dxc, dxl = (None, 0, 0) if dx is None else _matrix(dx, "dx", n, self.dim, self.device)
+        dwp, dwc, dwl = (None, 0, 0) if dw is None else _matrix(dw, "dw", self.rows, self.dim, self.device)
+        self._call("fc_xent_loss_grad", xp, xl, wp, wl, yp, size, n, scale, lp, dxp, dxc, dxl, dwp, dwc, dwl,
+                   _stream(stream))

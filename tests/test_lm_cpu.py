@@ -71,3 +71,21 @@ def test_embedding_checks_its_buffers():
         with pytest.raises(ValueError):
             bad()
     assert len(reached) == 3 and m.Embedding is fc.Embedding
+
+
+def test_cross_entropy_checks_its_buffers():
+    torch = pytest.importorskip("torch")
+    import paper_1511_00175_amd as fc
+    plan = object.__new__(fc.CrossEntropy)
+    plan.device, plan.rows, plan.dim, plan.max_tokens, plan.code = torch.device("cpu"), 10, 8, 4, 1
+    reached = []
+    plan._call = lambda name, *args: reached.append(name)
+    x, w, y, loss = torch.zeros(3, 8).half(), torch.zeros(10, 8).half(), torch.zeros(3, dtype=torch.int64), torch.zeros(3)
+    plan.loss(x, w, y, loss, stream=0)
+    plan.loss_grad(x, w, y, loss, x.float(), None, stream=0)
+    assert reached == ["fc_xent_loss", "fc_xent_loss_grad"]
+    for bad in (lambda: plan.loss(x.bfloat16(), w, y, loss, stream=0), lambda: plan.loss(x, w, y, loss.double(), stream=0),
+                lambda: plan.loss_grad(x, w, y, loss, x[:2], None, stream=0), lambda: plan.loss(x, w.t(), y, loss, stream=0)):
+        with pytest.raises(ValueError):
+            bad()
+    assert len(reached) == 2
