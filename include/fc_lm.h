@@ -106,6 +106,51 @@ int fc_xent_loss_grad(fc_xent* plan, const void* x, int64_t ld_x, const void* w,
                       int token_bytes, int64_t n, float scale, float* loss, void* dx, int dx_dtype, int64_t ld_dx,
                       void* dw, int dw_dtype, int64_t ld_dw, void* stream);
 
+/* ---- orthogonal updates ------------------------------------------------- */
+
+/* A matrix within the flat vectors of fc.h: element (r, c) is at
+ * offset + r * cols + c.  Offsets are multiples of 4 (FC_EALIGN); matrices are
+ * sorted by offset and do not overlap.  The multipliers scale lr and wd, as
+ * fc_segment's do. */
+typedef struct {
+    uint64_t offset;
+    uint64_t rows, cols; /* 1 to 2^20 each */
+    float lr_mult;
+    float decay_mult;
+} fc_matrix;
+
+typedef struct fc_muon fc_muon;
+
+/* A plan for n matrices (n may be 0) and `steps` (1 to 64) Newton-Schulz steps
+ *   X = D / |D|_F;  X <- a X + (b A + c A A) X, A = X X^T, `steps` times
+ * (a matrix of more rows than columns is transposed before and after; a matrix
+ * of zeros stays zeros; |D|_F is taken in 64 bits).
+ *   coefficients : a, b, c, or null for 3.4445, -4.7750, 2.0315, which bring
+ *                  every singular value above about 0.001 near 1 in 5 steps.
+ *                  Others must keep singular values in [0, 2] (FC_EINVAL).
+ *   dtype        : of the result.  FC_BF16: products of 11-bit numbers (fp16,
+ *                  scaled), sums in fp32, and X's own term at 22 bits; the error is
+ *                  below bf16's rounding.  FC_F16, FC_F32: every product from 22-bit
+ *                  operands, for 3 times the work; fp32's accuracy.
+ *   nesterov     : for fc_muon_step.
+ * The workspace holds 8 bytes per element and 4 (FC_BF16) or 8 per element of
+ * the shorter side's square. */
+int fc_muon_create(fc_muon** plan, const fc_matrix* matrices, int n, int dtype, int steps, const double* coefficients,
+                   int nesterov);
+void fc_muon_destroy(fc_muon* plan);
+
+/* out = the steps above of g, matrix by matrix; elements of no matrix are not
+ * written.  g is of any type, out of the plan's. */
+int fc_muon_orthogonalize(fc_muon* plan, const void* g, int g_dtype, void* out, void* stream);
+
+/* One momentum step from a raw sum g (as fc_sgd_step takes it), for the plan's
+ * matrices:
+ *   ga = g * (1 / batch),  v' = mu * v + ga
+ *   D  = nesterov ? ga + mu * v' : v',  O = the steps above of D
+ *   w' = w - lr_j * (sqrt(max(1, rows / cols)) * O + wd_j * w)
+ * O at the plan's accuracy (the plan's dtype), all else fp32. */
+int fc_muon_step(fc_muon* plan, float* w, float* v, const float* g, float lr, float mu, float wd, int batch, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -21,7 +21,7 @@ __all__ = ["Plan", "FcError", "fc_plan_create", "fc_plan_destroy", "fc_plan_quer
            "fc_plan_read_timing", "fc_plan_balance", "fc_tree_reduce", "fc_sgd_step", "fc_broadcast", "fc_step",
            "fc_step_noalloc", "fc_strerror",
            "fc_lr_at", "fc_train", "lr_policy", "lr_at", "fc_read_probe", "fc_read_probe_blocks", "read_probe",
-           "Embedding", "CrossEntropy"]
+           "Embedding", "CrossEntropy", "Muon"]
 
 
 def lr_at(iter, batch, **policy):
@@ -315,4 +315,4 @@ class Plan:
             raise FcError("fc_step_noalloc", rc)
 
 
-from .lm import CrossEntropy, Embedding  # noqa: E402,F401
+from .lm import CrossEntropy, Embedding, Muon  # noqa: E402,F401

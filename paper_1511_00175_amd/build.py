@@ -19,7 +19,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libfc.so")
 LIB_LM = os.path.join(PKG, "libfc_lm.so")
 SOURCES = ["fc_reduce_f32.hip", "fc_reduce_f16.hip", "fc_update.hip", "fc_api.cpp"]
-SOURCES_LM = ["fc_embed.hip", "fc_xent.hip"]
+SOURCES_LM = ["fc_embed.hip", "fc_xent.hip", "fc_muon.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", "-ffp-contract=off",

@@ -192,8 +192,10 @@ template <typename T, int R, bool SLOW, int F> struct Fragments {
     }
 };
 
-// The product of one block's BM x BN tile, WM x WN per wave.
-template <typename T_, int BM_, int BN_, int WM_, int WN_, bool AS, bool BS, int STAGES = 2> struct Product {
+// The product of one block's BM x BN tile, WM x WN per wave.  RUN > 0: sums are
+// taken over runs of RUN tiles of k and then added, so that a long sum's rounding
+// error grows with the root of RUN + tiles / RUN instead of that of tiles.
+template <typename T_, int BM_, int BN_, int WM_, int WN_, bool AS, bool BS, int STAGES = 2, int RUN = 0> struct Product {
     typedef T_ T;
     typedef typename Half<T>::v8 v8;
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
@@ -205,8 +207,9 @@ template <typename T_, int BM_, int BN_, int WM_, int WN_, bool AS, bool BS, int
 
     f32x4 acc[FM][FN];
 
-    // Parts: 1, or 3 for operands kept as sums of two 16-bit numbers (high by
-    // high, high by low, low by high; low by low is below the result's last bit).
+    // Parts: 1, or 3 for operands kept as sums of two 16-bit numbers: high by low,
+    // low by high, then high by high (the small terms first, while the sums are
+    // small; low by low is below the result's last bit).
     // k runs over [kb, ke), kb below both operands' extents, and ke - kb a multiple
     // of 64 unless one of them ends there.
     __device__ __forceinline__ void run(char* lds, const Operand& A, const Operand& B, int m0, int n0, int kb, int ke, int parts) {
@@ -226,12 +229,20 @@ template <typename T_, int BM_, int BN_, int WM_, int WN_, bool AS, bool BS, int
 #pragma unroll
             for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
+        f32x4 total_of[RUN ? FM : 1][RUN ? FN : 1];
+        if constexpr (RUN > 0) {
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int j = 0; j < FN; ++j) total_of[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+
         const int per = (ke - kb + GEMM_BK - 1) / GEMM_BK, total = per * parts;
         int part = 0, k = kb, issued = 0;
         auto issue = [&]() {
             const uint32_t s = (issued % STAGES) * STAGE;
-            ta.issue(la + s, k, part == 2, wave);
-            tb.issue(lb + s, k, part == 1, wave);
+            ta.issue(la + s, k, parts == 3 && part == 1, wave);
+            tb.issue(lb + s, k, parts == 3 && part == 0, wave);
             k += GEMM_BK;
             if (k >= ke) {
                 k = kb;
@@ -262,6 +273,18 @@ template <typename T_, int BM_, int BN_, int WM_, int WN_, bool AS, bool BS, int
                 for (int i = 0; i < FM; ++i)
 #pragma unroll
                     for (int j = 0; j < FN; ++j) acc[i][j] = Half<T>::mma(b[j], a[i], acc[i][j]);
+            }
+            if constexpr (RUN > 0) {
+                if (t % RUN == RUN - 1 || t == total - 1) {
+                    const bool last = t == total - 1;
+#pragma unroll
+                    for (int i = 0; i < FM; ++i)
+#pragma unroll
+                        for (int j = 0; j < FN; ++j) {
+                            total_of[i][j] += acc[i][j];
+                            acc[i][j] = last ? total_of[i][j] : f32x4{0.f, 0.f, 0.f, 0.f};
+                        }
+                }
             }
             asm volatile("" ::: "memory");
         }

@@ -1,0 +1,611 @@
+// Momentum updates made orthogonal by Newton-Schulz products (fc_lm.h).
+//
+//   X = D / |D|_F (rows <= columns; a taller matrix is transposed)
+//   repeat: A = X X^T, B = b A + c A A, X <- a X + B X
+//
+// for every matrix of a flat vector at once: each of a step's three products is
+// one launch over the tiles of all matrices.  A step is s^2 l + s^3 + 2 s^2 l
+// operations for s x l (A and B are symmetric: only tiles on and above the
+// diagonal are computed, the others are their mirror image); the bytes are
+// small beside them, so the products are bound by the matrix cores where the
+// matrices fill the chip and by their longest k loop where they do not.
+//
+// Numbers.  Everything is fp16 times a power of two that puts the largest
+// possible value (known from the polynomial) below 2^15, so that small entries
+// keep all their bits; sums are fp32.  X is kept as a sum of two fp16 numbers,
+// high and low (22 bits).  With `parts` 1 the products read the high halves
+// alone: the relative error of a step is that of one rounding to 11 bits, but
+// only along directions X already has -- a X, which carries X's weak directions
+// (a rounding there would be noise of full rank, grown by 3.4 a step), is formed
+// from both halves.  With 3 parts every operand is such a sum and a product is
+// high * high + high * low + low * high: fp32's accuracy for 3 times the work;
+// the sums are then taken in runs of 512 of k.  A matrix of at most 64 rows or
+// columns always has 3 parts: roundings average out over few terms only (its
+// error against a bf16 result's own was 1.0 with one part, at 16 x 20, and 0.4 at
+// 512 x 512), and its launches are too short for the work to matter.
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <vector>
+
+#include "fc_gemm.h"
+#include "fc_lm_host.h"
+
+using fc::f16x4;
+using fc::f32x4;
+using fc::Operand;
+
+namespace {
+
+typedef _Float16 f16;
+typedef __bf16 bf16;
+
+extern __shared__ __align__(1024) char lds[];
+
+struct Matrix {
+    uint64_t offset;         // in the flat vectors
+    int rows, cols;
+    int s, l;                // of X: the shorter and the longer side
+    int sp, lp;              // row strides: s, l up to multiples of 64
+    int turned;              // X is the matrix transposed
+    int parts;
+    float lr_mult, decay_mult, scale;
+    f16* x[2];               // [s][lp], low halves x_lo behind
+    f16* a;                  // [s][sp], low halves a_lo behind
+    f16* b;
+    int64_t x_lo, a_lo;
+    int piece0, pieces;      // of the sum of squares
+    int64_t piece_len;
+};
+
+struct Tile {
+    int mat, i, j;
+};
+
+// Where results go: to out, or into the weights w.
+struct Output {
+    void* out;
+    int dt;
+    float* w;
+    float lr, wd;
+};
+
+// u = element (i, j) of X's orthogonal form.
+__device__ __forceinline__ void store_out(const Output& a, const Matrix& m, int i, int j, float u) {
+    const uint64_t at = m.offset + (m.turned ? (uint64_t)j * m.cols + i : (uint64_t)i * m.cols + j);
+    if (!a.out) {
+        const float w = a.w[at];
+        a.w[at] = w - a.lr * m.lr_mult * (m.scale * u + a.wd * m.decay_mult * w);
+    } else if (a.dt == FC_F32) {
+        static_cast<float*>(a.out)[at] = u;
+    } else if (a.dt == FC_F16) {
+        static_cast<f16*>(a.out)[at] = (f16)u;
+    } else {
+        static_cast<bf16*>(a.out)[at] = (bf16)u;
+    }
+}
+
+// The direction made orthogonal: g itself, or a momentum update of it.
+struct Source {
+    const void* g;
+    float* v;                // momentum, or null: g itself
+    float c, mu;             // 1 / batch
+    int nesterov;
+};
+
+// Element i of the direction; `update`: the momentum is updated and stored first.
+template <typename T, bool STEP> __device__ __forceinline__ float direction(const Source& a, uint64_t i, bool update) {
+    float g = (float)static_cast<const T*>(a.g)[i];
+    if constexpr (STEP) {
+        g *= a.c;
+        float v = a.v[i];
+        if (update) {
+            v = a.mu * v + g;
+            a.v[i] = v;
+        }
+        return a.nesterov ? g + a.mu * v : v;
+    }
+    return g;
+}
+
+// Sums of squares of one piece of a matrix, in 64 bits: neither tiny nor huge
+// gradients leave its range.
+struct NormArgs {
+    const Matrix* mats;
+    const int2* pieces;      // (matrix, piece)
+    double* partial;
+    Source d;
+};
+
+template <typename T, bool STEP> __global__ __launch_bounds__(256) void norm_kernel(NormArgs a) {
+    __shared__ double part[4];
+    const int2 pc = a.pieces[blockIdx.x];
+    const Matrix& m = a.mats[pc.x];
+    const int64_t total = (int64_t)m.rows * m.cols, lo = pc.y * m.piece_len, hi = min(lo + m.piece_len, total);
+    double sum = 0;
+    for (int64_t i = lo + threadIdx.x; i < hi; i += 256) {
+        const double x = direction<T, STEP>(a.d, m.offset + i, true);
+        sum += x * x;
+    }
+#pragma unroll
+    for (int k = 32; k > 0; k /= 2) sum += __shfl_xor(sum, k);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) a.partial[m.piece0 + pc.y] = (part[0] + part[1]) + (part[2] + part[3]);
+}
+
+__device__ __forceinline__ void split(float v, f16& hi, f16& lo) {
+    hi = (f16)v;
+    lo = (f16)(v - (float)hi);
+}
+
+struct ScaleArgs {
+    const Matrix* mats;
+    const Tile* tiles;       // 64 x 64 of X
+    const double* partial;
+    double top;              // the scale of X
+    double alone;            // what the steps make of a singular value of 1
+    Source d;
+    Output to;
+};
+
+// X of one tile: the direction over its norm.  A matrix of one row or column has
+// the one singular value 1 and is finished here.
+template <typename T, bool STEP> __global__ __launch_bounds__(256) void scale_kernel(ScaleArgs a) {
+    __shared__ float tile[64][65];
+    __shared__ double part[4];
+    const Tile t = a.tiles[blockIdx.x];
+    const Matrix& m = a.mats[t.mat];
+    double sum = threadIdx.x < m.pieces ? a.partial[m.piece0 + threadIdx.x] : 0;
+#pragma unroll
+    for (int k = 32; k > 0; k /= 2) sum += __shfl_xor(sum, k);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    sum = (part[0] + part[1]) + (part[2] + part[3]);
+    const double f = sum == 0 ? 0 : (m.s == 1 ? a.alone : a.top) / sqrt(sum);
+    const int r0 = 64 * (m.turned ? t.j : t.i), c0 = 64 * (m.turned ? t.i : t.j);
+    const int c = threadIdx.x & 63;
+#pragma unroll 4
+    for (int q = 0; q < 16; ++q) {
+        const int r = (threadIdx.x >> 6) + 4 * q;
+        const bool in = r0 + r < m.rows && c0 + c < m.cols;
+        tile[r][c] = in ? (float)(direction<T, STEP>(a.d, m.offset + (uint64_t)(r0 + r) * m.cols + c0 + c, false) * f) : 0.f;
+    }
+    __syncthreads();
+#pragma unroll 4
+    for (int q = 0; q < 16; ++q) {
+        const int r = (threadIdx.x >> 6) + 4 * q;
+        if (64 * t.i + r >= m.s) break;
+        const float x = m.turned ? tile[c][r] : tile[r][c];
+        if (m.s == 1) {
+            if (64 * t.j + c < m.l) store_out(a.to, m, 0, 64 * t.j + c, x);
+            continue;
+        }
+        f16 hi, lo;
+        split(x, hi, lo);
+        f16* p = m.x[0] + (int64_t)(64 * t.i + r) * m.lp + 64 * t.j + c;
+        p[0] = hi;
+        p[m.x_lo] = lo;
+    }
+}
+
+enum Stage { GRAM, POLY, NEXT, LAST };
+
+struct ProductArgs {
+    const Matrix* mats;
+    const Tile* tiles;
+    int count;
+    int from;                // which x holds X
+    // GRAM: A = f0 acc; POLY: B = f0 acc + f1 A; NEXT: X = f0 acc + f1 X.  Each the
+    // sum of two floats: a coefficient's rounding is an error of every entry's alike.
+    float f0, f1, f0_low, f1_low;
+    float unscale;           // LAST: 1 / the scale of X
+    Output to;
+};
+
+__device__ __forceinline__ f32x4 load_four(const f16* p, int64_t lo, bool both) {
+    const f16x4 h = *reinterpret_cast<const f16x4*>(p);
+    f32x4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = (float)h[e];
+    if (both) {
+        const f16x4 l = *reinterpret_cast<const f16x4*>(p + lo);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += (float)l[e];
+    }
+    return v;
+}
+
+template <typename P, int STAGE> __global__ __launch_bounds__(P::THREADS, P::THREADS / 256) void product_kernel(ProductArgs a) {
+    const Tile t = a.tiles[fc::xcd_order(blockIdx.x, a.count)];
+    const Matrix& m = a.mats[t.mat];
+    const f16* x = m.x[a.from];
+    Operand A, B;
+    int k;
+    if constexpr (STAGE == GRAM) {
+        A = B = Operand{x, m.lp, m.s, m.lp, m.x_lo};
+        k = m.lp;
+    } else if constexpr (STAGE == POLY) {
+        A = B = Operand{m.a, m.sp, m.s, m.sp, m.a_lo};
+        k = m.sp;
+    } else {
+        A = Operand{m.b, m.sp, m.s, m.sp, m.a_lo};
+        B = Operand{x, m.lp, m.l, m.s, m.x_lo};
+        k = m.s;
+    }
+    P p;
+    p.run(lds, A, B, t.i * P::BM, t.j * P::BN, 0, k, m.parts);
+    const bool both = m.parts == 3;
+    f16* const to = STAGE == GRAM ? m.a : STAGE == POLY ? m.b : m.x[1 - a.from];
+    const int ld = STAGE <= POLY ? m.sp : m.lp;
+    const int64_t lo = STAGE <= POLY ? m.a_lo : m.x_lo;
+#pragma unroll
+    for (int i = 0; i < P::FM; ++i) {
+        const int r = t.i * P::BM + P::row(i);
+        if (r >= m.s) continue;
+#pragma unroll
+        for (int j = 0; j < P::FN; ++j) {
+            const int c = t.j * P::BN + P::col(j);
+            if (c >= ld) continue;
+            f32x4 v = a.f0 * p.acc[i][j];
+            if constexpr (STAGE != GRAM) {
+                const f32x4 q = STAGE == POLY ? load_four(m.a + (int64_t)r * ld + c, lo, both) : load_four(x + (int64_t)r * ld + c, lo, true);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float z = p.acc[i][j][e];
+                    v[e] = fmaf(z, a.f0, fmaf(q[e], a.f1, fmaf(z, a.f0_low, q[e] * a.f1_low)));
+                }
+            }
+            if constexpr (STAGE == LAST) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (c + e < m.l) store_out(a.to, m, r, c + e, v[e] * a.unscale);
+            } else {
+                f16x4 hi, low;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    f16 h, l;
+                    split(v[e], h, l);
+                    hi[e] = h;
+                    low[e] = l;
+                }
+                const bool halves = STAGE == NEXT || both;
+                f16* q = to + (int64_t)r * ld + c;
+                *reinterpret_cast<f16x4*>(q) = hi;
+                if (halves) *reinterpret_cast<f16x4*>(q + lo) = low;
+                if (STAGE <= POLY && t.i != t.j) {  // the mirror image
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (c + e < m.s) {
+                            f16* z = to + (int64_t)(c + e) * ld + r;
+                            z[0] = hi[e];
+                            if (halves) z[lo] = low[e];
+                        }
+                }
+            }
+        }
+    }
+}
+
+template <bool BS> using Large = fc::Product<f16, 256, 256, 128, 64, false, BS>;
+template <bool BS> using Middle = fc::Product<f16, 128, 128, 64, 64, false, BS>;
+template <bool BS> using Small = fc::Product<f16, 64, 64, 32, 32, false, BS, 2, 8>;
+template <bool BS> using Exact = fc::Product<f16, 128, 128, 64, 64, false, BS, 2, 8>;
+
+// EXACT has the registers for sums in runs, which LARGE has not.
+enum TileKind { LARGE, MIDDLE, SMALL, EXACT };
+constexpr int TILE[4] = {256, 128, 64, 128};
+constexpr int CUS = 256;
+
+template <typename P, int STAGE> hipError_t prepare_one() {
+    return hipFuncSetAttribute((const void*)product_kernel<P, STAGE>, hipFuncAttributeMaxDynamicSharedMemorySize, P::LDS);
+}
+
+template <template <bool> class P> hipError_t prepare() {
+    for (hipError_t e : {prepare_one<P<false>, GRAM>(), prepare_one<P<false>, POLY>(), prepare_one<P<true>, NEXT>(), prepare_one<P<true>, LAST>()})
+        if (e != hipSuccess) return e;
+    return hipSuccess;
+}
+
+template <typename P, int STAGE> void launch(const ProductArgs& a, hipStream_t s) {
+    product_kernel<P, STAGE><<<a.count, P::THREADS, P::LDS, s>>>(a);
+}
+
+template <int STAGE> void launch_kind(int kind, const ProductArgs& a, hipStream_t s) {
+    constexpr bool BS = STAGE >= NEXT;
+    if (kind == LARGE) launch<Large<BS>, STAGE>(a, s);
+    else if (kind == MIDDLE) launch<Middle<BS>, STAGE>(a, s);
+    else if (kind == EXACT) launch<Exact<BS>, STAGE>(a, s);
+    else launch<Small<BS>, STAGE>(a, s);
+}
+
+constexpr int64_t SIDE_LIMIT = 1 << 20;
+constexpr int64_t COUNT_LIMIT = 1 << 20;
+constexpr int MOST_STEPS = 64;
+
+double most(double a, double b, double c, double top) {  // of |a x + b x^3 + c x^5| on [0, top]
+    double m = 0;
+    for (int i = 0; i <= 4096; ++i) {
+        const double x = top * i / 4096, y = x * x;
+        m = std::max(m, std::fabs(x * (a + y * (b + y * c))));
+    }
+    return std::isfinite(a) && std::isfinite(b) && std::isfinite(c) ? m : HUGE_VAL;
+}
+
+double pow2_below(double x) { return std::exp2(std::floor(std::log2(x))); }
+
+}  // namespace
+
+struct fc_muon {
+    fc::CallOrder order;
+    fc::DeviceBlock block;
+    std::vector<fc_matrix> host;
+    uint64_t extent = 0;
+    int dtype = FC_BF16;
+    int steps = 5, nesterov = 1;
+    double a = 0, b = 0, c = 0;
+    double sx = 1, sa = 1, sb = 1;   // scales of X, A, B
+    double alone = 1;                // what the steps make of a singular value of 1
+    const Matrix* mats = nullptr;
+    const int2* pieces = nullptr;
+    int n_pieces = 0;
+    double* partial = nullptr;
+    const Tile* scale_tiles = nullptr;
+    int n_scale = 0;
+    const Tile* tiles[2] = {nullptr, nullptr};  // of the symmetric products, of X's
+    int n_tiles[2] = {0, 0};
+    int kind[2] = {SMALL, SMALL};
+};
+
+namespace {
+
+// Everything of the plan in device memory, built on the host.
+int build(fc_muon* p) {
+    const int n = (int)p->host.size();
+    std::vector<Matrix> mats(n);
+    fc::Layout at;
+    const uint64_t o_mats = at.take(n * sizeof(Matrix));
+    std::vector<int2> pieces;
+    std::vector<Tile> scale, tiles[2];
+    int64_t counts[2][3] = {};
+    std::vector<int> by_work(n);
+    for (int i = 0; i < n; ++i) {
+        const fc_matrix& h = p->host[i];
+        Matrix& m = mats[i];
+        std::memset(&m, 0, sizeof m);
+        m.offset = h.offset;
+        m.rows = (int)h.rows;
+        m.cols = (int)h.cols;
+        m.turned = h.rows > h.cols;
+        m.s = std::min(m.rows, m.cols);
+        m.l = std::max(m.rows, m.cols);
+        m.sp = (m.s + 63) / 64 * 64;
+        m.lp = (m.l + 63) / 64 * 64;
+        m.parts = p->dtype == FC_BF16 && m.s > 64 ? 1 : 3;
+        m.lr_mult = h.lr_mult;
+        m.decay_mult = h.decay_mult;
+        m.scale = (float)std::sqrt(std::max(1.0, (double)h.rows / h.cols));
+        const int64_t total = (int64_t)m.rows * m.cols;
+        m.pieces = (int)std::min<int64_t>(256, fc::ceil_div(total, 4096));
+        m.piece_len = fc::ceil_div(total, m.pieces);
+        m.piece0 = (int)pieces.size();
+        for (int k = 0; k < m.pieces; ++k) pieces.push_back({i, k});
+        for (int r = 0; r < (m.s + 63) / 64; ++r)
+            for (int c = 0; c < m.lp / 64; ++c) scale.push_back({i, r, c});
+        for (int k = 0; k < 3 && m.s > 1; ++k) {
+            const int64_t s = fc::ceil_div(m.s, TILE[k]), l = fc::ceil_div(m.l, TILE[k]);
+            counts[0][k] += s * (s + 1) / 2;
+            counts[1][k] += s * l;
+        }
+        by_work[i] = i;
+    }
+    // the longest k loops first
+    std::stable_sort(by_work.begin(), by_work.end(), [&](int i, int j) { return mats[i].l > mats[j].l; });
+    for (int q = 0; q < 2; ++q) {
+        if (p->dtype != FC_BF16) p->kind[q] = counts[q][LARGE] >= CUS * 3 / 4 ? LARGE : counts[q][MIDDLE] >= CUS ? EXACT : SMALL;
+        else p->kind[q] = counts[q][LARGE] >= CUS * 3 / 4 ? LARGE : counts[q][MIDDLE] >= CUS ? MIDDLE : SMALL;
+        const int size = TILE[p->kind[q]];
+        for (int i : by_work) {
+            if (mats[i].s == 1) continue;
+            const int s = (int)fc::ceil_div(mats[i].s, size), l = (int)fc::ceil_div(mats[i].l, size);
+            for (int g = 0; g < s; g += 8)  // groups of 8 tile rows, down the rows first
+                for (int c = 0; c < (q ? l : s); ++c)
+                    for (int r = g; r < std::min(g + 8, s); ++r)
+                        if (q || r <= c) tiles[q].push_back({i, r, c});
+        }
+    }
+    const uint64_t o_pieces = at.take(pieces.size() * sizeof(int2)), o_partial = at.take(pieces.size() * sizeof(double)),
+                   o_scale = at.take(scale.size() * sizeof(Tile)), o_sym = at.take(tiles[0].size() * sizeof(Tile)),
+                   o_x = at.take(tiles[1].size() * sizeof(Tile));
+    const uint64_t tables = at.size;
+    std::vector<uint64_t> places(n * 4);
+    for (int i = 0; i < n; ++i) {
+        Matrix& m = mats[i];
+        m.x_lo = (int64_t)m.s * m.lp;
+        m.a_lo = (int64_t)m.s * m.sp;
+        for (int k = 0; k < 2; ++k) places[4 * i + k] = at.take(2 * m.x_lo * sizeof(f16));
+        for (int k = 2; k < 4; ++k) places[4 * i + k] = at.take((m.parts == 3 ? 2 : 1) * m.a_lo * sizeof(f16));
+    }
+    int rc = p->block.create(at.size);
+    if (rc) return rc;
+    char* b = p->block.p;
+    for (int i = 0; i < n; ++i) {
+        mats[i].x[0] = reinterpret_cast<f16*>(b + places[4 * i]);
+        mats[i].x[1] = reinterpret_cast<f16*>(b + places[4 * i + 1]);
+        mats[i].a = reinterpret_cast<f16*>(b + places[4 * i + 2]);
+        mats[i].b = reinterpret_cast<f16*>(b + places[4 * i + 3]);
+    }
+    std::vector<char> image(tables);
+    auto put = [&](uint64_t to, const void* from, size_t bytes) {
+        if (bytes) std::memcpy(image.data() + to, from, bytes);
+    };
+    put(o_mats, mats.data(), n * sizeof(Matrix));
+    put(o_pieces, pieces.data(), pieces.size() * sizeof(int2));
+    put(o_scale, scale.data(), scale.size() * sizeof(Tile));
+    put(o_sym, tiles[0].data(), tiles[0].size() * sizeof(Tile));
+    put(o_x, tiles[1].data(), tiles[1].size() * sizeof(Tile));
+    if (tables && hipMemcpy(b, image.data(), tables, hipMemcpyHostToDevice) != hipSuccess) return FC_EHIP;
+    p->mats = reinterpret_cast<const Matrix*>(b + o_mats);
+    p->pieces = reinterpret_cast<const int2*>(b + o_pieces);
+    p->n_pieces = (int)pieces.size();
+    p->partial = reinterpret_cast<double*>(b + o_partial);
+    p->scale_tiles = reinterpret_cast<const Tile*>(b + o_scale);
+    p->n_scale = (int)scale.size();
+    p->tiles[0] = reinterpret_cast<const Tile*>(b + o_sym);
+    p->tiles[1] = reinterpret_cast<const Tile*>(b + o_x);
+    for (int q = 0; q < 2; ++q) p->n_tiles[q] = (int)tiles[q].size();
+    return FC_OK;
+}
+
+template <typename T, bool STEP> void start(fc_muon* p, const Source& d, const Output& to, hipStream_t s) {
+    NormArgs n{p->mats, p->pieces, p->partial, d};
+    norm_kernel<T, STEP><<<p->n_pieces, 256, 0, s>>>(n);
+    ScaleArgs a{p->mats, p->scale_tiles, p->partial, p->sx, p->alone, d, to};
+    scale_kernel<T, STEP><<<p->n_scale, 256, 0, s>>>(a);
+}
+
+// The products; the last one writes the output.
+int products(fc_muon* p, const Output& to, hipStream_t s) {
+    int from = 0;
+    auto set = [](ProductArgs& a, double f0, double f1) {
+        a.f0 = (float)f0;
+        a.f1 = (float)f1;
+        a.f0_low = (float)(f0 - a.f0);
+        a.f1_low = (float)(f1 - a.f1);
+    };
+    for (int k = 0; k < p->steps && p->n_tiles[0] > 0; ++k) {
+        ProductArgs a{};
+        a.to = to;
+        a.mats = p->mats;
+        a.from = from;
+        a.tiles = p->tiles[0];
+        a.count = p->n_tiles[0];
+        set(a, p->sa / (p->sx * p->sx), 0);
+        launch_kind<GRAM>(p->kind[0], a, s);
+        set(a, p->c * p->sb / (p->sa * p->sa), p->b * p->sb / p->sa);
+        launch_kind<POLY>(p->kind[0], a, s);
+        a.tiles = p->tiles[1];
+        a.count = p->n_tiles[1];
+        set(a, 1 / p->sb, p->a);
+        a.unscale = (float)(1 / p->sx);
+        if (k + 1 < p->steps) launch_kind<NEXT>(p->kind[1], a, s);
+        else launch_kind<LAST>(p->kind[1], a, s);
+        from ^= 1;
+    }
+    return fc::hip_code(hipGetLastError());
+}
+
+int orthogonalize_body(fc_muon* p, const void* g, int gdt, void* out, hipStream_t s) {
+    if (!p) return FC_EINVAL;
+    const int64_t n = (int64_t)p->extent;
+    int rc = fc::check_spans({{g, 1, n, n, fc::dtype_bytes(gdt), false}, {out, 1, n, n, fc::dtype_bytes(p->dtype), true}});
+    if (rc || n == 0) return rc;
+    if (reinterpret_cast<uintptr_t>(g) % 16 || reinterpret_cast<uintptr_t>(out) % 16) return FC_EALIGN;
+    bool note;
+    rc = p->order.begin(s, note);
+    if (rc) return rc;
+    const Source d{g, nullptr, 1.f, 0.f, 0};
+    const Output to{out, p->dtype, nullptr, 0.f, 0.f};
+    if (gdt == FC_F32) start<float, false>(p, d, to, s);
+    else if (gdt == FC_F16) start<f16, false>(p, d, to, s);
+    else start<bf16, false>(p, d, to, s);
+    rc = products(p, to, s);
+    p->order.done(s, note);
+    return rc;
+}
+
+int step_body(fc_muon* p, float* w, float* v, const float* g, float lr, float mu, float wd, int batch, hipStream_t s) {
+    if (!p || batch < 1) return FC_EINVAL;
+    const int64_t n = (int64_t)p->extent;
+    int rc = fc::check_spans({{w, 1, n, n, 4, true}, {v, 1, n, n, 4, true}, {g, 1, n, n, 4, false}});
+    if (rc || n == 0) return rc;
+    for (const void* q : {(const void*)w, (const void*)v, (const void*)g})
+        if (reinterpret_cast<uintptr_t>(q) % 16) return FC_EALIGN;
+    bool note;
+    rc = p->order.begin(s, note);
+    if (rc) return rc;
+    const Source d{g, v, 1.0f / (float)batch, mu, p->nesterov};
+    const Output to{nullptr, FC_F32, w, lr, wd};
+    start<float, true>(p, d, to, s);
+    rc = products(p, to, s);
+    p->order.done(s, note);
+    return rc;
+}
+
+}  // namespace
+
+extern "C" {
+
+int fc_muon_create(fc_muon** plan, const fc_matrix* mats, int n, int dtype, int steps, const double* coefficients, int nesterov) {
+    if (!plan) return FC_EINVAL;
+    *plan = nullptr;
+    if (n < 0 || n > COUNT_LIMIT || (n > 0 && !mats) || !fc::dtype_bytes(dtype) || steps < 1 || steps > MOST_STEPS) return FC_EINVAL;
+    const double usual[3] = {3.4445, -4.7750, 2.0315};
+    const double* q = coefficients ? coefficients : usual;
+    uint64_t end = 0;
+    for (int i = 0; i < n; ++i) {
+        const fc_matrix& m = mats[i];
+        if (m.rows < 1 || m.cols < 1 || m.rows > SIDE_LIMIT || m.cols > SIDE_LIMIT || m.offset < end || m.offset >= (uint64_t)1 << 48) return FC_EINVAL;
+        if (m.offset % 4) return FC_EALIGN;
+        end = m.offset + m.rows * m.cols;
+    }
+    // singular values start in [0, 1]; the scales hold for what the polynomial makes of them
+    double top = 1;
+    for (int k = 0; k < steps; ++k) {
+        top = std::max(top, most(q[0], q[1], q[2], top));
+        if (!(top <= 2)) return FC_EINVAL;
+    }
+    double by = 0;
+    for (int i = 0; i <= 4096; ++i) {
+        const double y = top * top * i / 4096;
+        by = std::max(by, std::fabs(y * (q[1] + y * q[2])));
+    }
+    if (!(by <= 1024)) return FC_EINVAL;
+    return fc::no_throw([&] {
+        fc_muon* p = new fc_muon;
+        p->host.assign(mats, mats + n);
+        p->extent = end;
+        p->dtype = dtype;
+        p->steps = steps;
+        p->nesterov = nesterov != 0;
+        p->a = q[0];
+        p->b = q[1];
+        p->c = q[2];
+        for (int k = 0; k < steps; ++k) {
+            const double y = p->alone * p->alone;
+            p->alone *= q[0] + y * (q[1] + y * q[2]);
+        }
+        p->sx = pow2_below(32768 / top);
+        p->sa = pow2_below(32768 / (top * top));
+        p->sb = by > 0 ? pow2_below(32768 / by) : 1;
+        int rc = p->order.create();
+        if (!rc) rc = fc::hip_code(prepare<Large>());
+        if (!rc) rc = fc::hip_code(prepare<Middle>());
+        if (!rc) rc = fc::hip_code(prepare<Small>());
+        if (!rc) rc = fc::hip_code(prepare<Exact>());
+        if (!rc) rc = build(p);
+        if (rc) {
+            fc_muon_destroy(p);
+            return rc;
+        }
+        *plan = p;
+        return FC_OK;
+    });
+}
+
+void fc_muon_destroy(fc_muon* p) {
+    if (!p) return;
+    p->block.destroy();
+    p->order.destroy();
+    delete p;
+}
+
+int fc_muon_orthogonalize(fc_muon* p, const void* g, int g_dtype, void* out, void* stream) {
+    return fc::no_throw([&] { return orthogonalize_body(p, g, g_dtype, out, static_cast<hipStream_t>(stream)); });
+}
+
+int fc_muon_step(fc_muon* p, float* w, float* v, const float* g, float lr, float mu, float wd, int batch, void* stream) {
+    return fc::no_throw([&] { return step_body(p, w, v, g, lr, mu, wd, batch, static_cast<hipStream_t>(stream)); });
+}
+
+}  // extern "C"

@@ -6,7 +6,7 @@ stream or torch's current one."""
 import ctypes
 
 from ._fc import FC_F16, FC_F32, FcError
-from ._fc_lm import FC_BF16, lib
+from ._fc_lm import FC_BF16, fc_matrix, lib
 
 DTYPES = {"f32": FC_F32, "f16": FC_F16, "bf16": FC_BF16}
 _CODES = None  # torch dtype -> fc_dtype value, made at the first call
@@ -184,3 +184,59 @@ class CrossEntropy(_Handle):
         dwp, dwc, dwl = (None, 0, 0) if dw is None else _matrix(dw, "dw", self.rows, self.dim, self.device)
         self._call("fc_xent_loss_grad", xp, xl, wp, wl, yp, size, n, scale, lp, dxp, dxc, dxl, dwp, dwc, dwl,
                    _stream(stream))
+
+
+class Muon(_Handle):
+    """Momentum updates made orthogonal by Newton-Schulz products (fc_muon), for
+    the matrices of a flat vector.
+
+    matrices: rows (offset, rows, cols[, lr_mult, decay_mult]) in elements of
+              the vector, sorted, as Plan's segments are.
+    dtype   : of orthogonalize's output, and the accuracy of the products: "bf16"
+              (16-bit products) or "f16", "f32" (fp32's accuracy, 3 times the work).
+    coefficients: (a, b, c) of X <- a X + (b A + c A A) X, A = X X^T."""
+
+    _destroy = "fc_muon_destroy"
+
+    def __init__(self, matrices, dtype="bf16", steps=5, coefficients=None, nesterov=True):
+        if dtype not in DTYPES:
+            raise ValueError(f"dtype must be f32, f16 or bf16, not {dtype}")
+        matrices = [tuple(m) for m in matrices]
+        table = (fc_matrix * max(1, len(matrices)))()
+        self.extent = 0
+        for i, m in enumerate(matrices):
+            if not 3 <= len(m) <= 5 or min(m[:3]) < 0:
+                raise ValueError(f"matrix {i} is {m}, not (offset, rows, cols[, lr_mult, decay_mult])")
+            table[i] = fc_matrix(*m[:3], *(m[3:] + (1.0, 1.0)[len(m) - 3:]))
+            self.extent = max(self.extent, m[0] + m[1] * m[2])
+        abc = None if coefficients is None else (ctypes.c_double * 3)(*coefficients)
+        self.code = DTYPES[dtype]
+        self._create("fc_muon_create", table, len(matrices), self.code, steps, abc, bool(nesterov))
+
+    def _flat(self, t, name, code=None):
+        import torch
+        if not isinstance(t, torch.Tensor):
+            raise ValueError(f"{name} must be a torch tensor")
+        got = _code(t)
+        if got is None or (code is not None and got != code):
+            raise ValueError(f"{name} must not be {t.dtype}")
+        if t.device != self.device:
+            raise ValueError(f"{name} is on {t.device}, the plan on {self.device}")
+        if not t.is_contiguous() or t.numel() < self.extent:
+            raise ValueError(f"{name} must be contiguous and hold the plan's {self.extent} elements")
+        return t.data_ptr(), got
+
+    def orthogonalize(self, g, out, stream=None):
+        """out = the Newton-Schulz steps of g, matrix by matrix."""
+        gp, gc = self._flat(g, "g")
+        op, _ = self._flat(out, "out", self.code)
+        self._call("fc_muon_orthogonalize", gp, gc, op, _stream(stream))
+
+    def step(self, w, v, g, lr, mu, wd, batch, stream=None):
+        """v' = mu v + g / batch, O = the steps of g / batch + mu v' (of v'
+        without nesterov), w' = w - lr (sqrt(max(1, rows / cols)) O + wd w) for
+        the plan's matrices; g is a raw sum, as Plan.sgd_step takes it."""
+        wp, _ = self._flat(w, "w", FC_F32)
+        vp, _ = self._flat(v, "v", FC_F32)
+        gp, _ = self._flat(g, "g", FC_F32)
+        self._call("fc_muon_step", wp, vp, gp, lr, mu, wd, int(batch), _stream(stream))

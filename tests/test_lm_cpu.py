@@ -89,3 +89,25 @@ def test_cross_entropy_checks_its_buffers():
         with pytest.raises(ValueError):
             bad()
     assert len(reached) == 2
+
+
+def test_muon_checks_its_buffers():
+    torch = pytest.importorskip("torch")
+    import paper_1511_00175_amd as fc
+    plan = object.__new__(fc.Muon)
+    plan.device, plan.extent, plan.code = torch.device("cpu"), 64, 2
+    reached = []
+    plan._call = lambda name, *args: reached.append(name)
+    g, out = torch.zeros(64), torch.zeros(80, dtype=torch.bfloat16)
+    plan.orthogonalize(g.half(), out, stream=0)
+    plan.step(g, g.clone(), g.clone(), 0.1, 0.9, 0.0, 8, stream=0)
+    assert reached == ["fc_muon_orthogonalize", "fc_muon_step"]
+    for bad in (lambda: plan.orthogonalize(g, g, stream=0), lambda: plan.orthogonalize(g[:63], out, stream=0),
+                lambda: plan.orthogonalize(torch.zeros(128)[::2], out, stream=0),
+                lambda: plan.step(g, g.half(), g, 0.1, 0.9, 0.0, 8, stream=0)):
+        with pytest.raises(ValueError):
+            bad()
+    for bad in ([(0, 8)], [(0, 8, 8, 1.0, 1.0, 1.0)], [(-4, 8, 8)]):
+        with pytest.raises(ValueError):
+            fc.Muon(bad)
+    assert len(reached) == 2
