@@ -136,9 +136,16 @@ template <int R, bool SLOW, int WAVES> struct TileLoads {
             }
         }
     }
-    // Loads of the tile at k0 (below ks) into LDS at `lds`; `part`: of the second halves.
-    __device__ __forceinline__ void issue(uint32_t lds, int k0, bool part, int wave) const {
-        uint64_t b = base + (part ? (uint64_t)lob : 0);
+    // The loads of one tile: where from, where to.
+    struct Tile {
+        u32x4 desc;
+        uint32_t to;
+        bool past;  // contiguous: the lane's k is past the operand's
+    };
+    // The tile at k0 (below ks) into LDS at `lds`; `low`: of the second halves;
+    // not `live`: zeros, from nowhere.
+    __device__ __forceinline__ Tile tile(uint32_t lds, int k0, bool low, bool live, int wave) const {
+        uint64_t b = base + (low ? (uint64_t)lob : 0);
         uint32_t records;
         if constexpr (!SLOW) {
             b += 2 * (uint64_t)k0;
@@ -148,15 +155,17 @@ template <int R, bool SLOW, int WAVES> struct TileLoads {
             const int left = ks - k0;
             records = (uint32_t)((uint64_t)((left < GEMM_BK ? left : GEMM_BK) - 1) * ldb) + tail;
         }
-        u32x4 d;
-        d.x = __builtin_amdgcn_readfirstlane((uint32_t)b);
-        d.y = __builtin_amdgcn_readfirstlane((uint32_t)(b >> 32));
-        d.z = __builtin_amdgcn_readfirstlane(records);
-        d.w = 0x00020000u;
-        const uint32_t to = __builtin_amdgcn_readfirstlane(lds + wave * COUNT * 1024);
-        const bool past = !SLOW && k0 + (int)kpart >= ks;
-#pragma unroll
-        for (int i = 0; i < COUNT; ++i) load_to_lds(d, to + i * 1024, past ? GEMM_OUTSIDE : off[i]);
+        Tile t;
+        t.desc.x = __builtin_amdgcn_readfirstlane((uint32_t)b);
+        t.desc.y = __builtin_amdgcn_readfirstlane((uint32_t)(b >> 32));
+        t.desc.z = __builtin_amdgcn_readfirstlane(live ? records : 0u);
+        t.desc.w = 0x00020000u;
+        t.to = __builtin_amdgcn_readfirstlane(lds + wave * COUNT * 1024);
+        t.past = !SLOW && k0 + (int)kpart >= ks;
+        return t;
+    }
+    __device__ __forceinline__ void load(const Tile& t, int i) const {
+        load_to_lds(t.desc, t.to + i * 1024, t.past ? GEMM_OUTSIDE : off[i]);
     }
 };
 
@@ -238,11 +247,14 @@ template <typename T_, int BM_, int BN_, int WM_, int WN_, bool AS, bool BS, int
         }
 
         const int per = (ke - kb + GEMM_BK - 1) / GEMM_BK, total = per * parts;
-        int part = 0, k = kb, issued = 0;
-        auto issue = [&]() {
-            const uint32_t s = (issued % STAGES) * STAGE;
-            ta.issue(la + s, k, parts == 3 && part == 1, wave);
-            tb.issue(lb + s, k, parts == 3 && part == 0, wave);
+        int part = 0, k = kb, issued = 0, into = 0;
+        typename TileLoads<BM, AS, WAVES>::Tile ia;
+        typename TileLoads<BN, BS, WAVES>::Tile ib;
+        auto prepare = [&]() {
+            const bool live = issued < total;
+            ia = ta.tile(la + into, k, parts == 3 && part == 1, live, wave);
+            ib = tb.tile(lb + into, k, parts == 3 && part == 0, live, wave);
+            into = into == (STAGES - 1) * STAGE ? 0 : into + STAGE;
             k += GEMM_BK;
             if (k >= ke) {
                 k = kb;
@@ -250,30 +262,77 @@ template <typename T_, int BM_, int BN_, int WM_, int WN_, bool AS, bool BS, int
             }
             ++issued;
         };
-#pragma unroll
-        for (int s = 0; s < STAGES - 1; ++s)
-            if (issued < total) issue();
-        for (int t = 0; t < total; ++t) {
-            if (STAGES == 2 || issued - t < STAGES - 1)
-                wait_loads<0>();
+        auto load = [&](int l) {
+            if (l < ta.COUNT)
+                ta.load(ia, l);
             else
-                wait_loads<(STAGES - 2) * LOADS>();
+                tb.load(ib, l - ta.COUNT);
+        };
+        // The multiplications of one half tile of k run while the fragments of the
+        // next are read: a row's A fragment is replaced as soon as its row is done.
+        // Between the two halves of a tile the block meets: its last reads of the
+        // tile are done, so the loads of the tile STAGES later may overwrite it, and
+        // the next tile has arrived.  Those loads are spread over the second half's
+        // rows.  Past the last tile they store zeros that nobody reads, so that the
+        // count of loads in flight is always the same.
+        for (int s = 0; s < STAGES; ++s) {
+            prepare();
+#pragma unroll
+            for (int l = 0; l < LOADS; ++l) load(l);
+        }
+        wait_loads<(STAGES - 1) * LOADS>();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        v8 a[FM], b[FN], next[FN];
+#pragma unroll
+        for (int j = 0; j < FN; ++j) b[j] = fb.get(lb, j, 0);
+#pragma unroll
+        for (int i = 0; i < FM; ++i) a[i] = fa.get(la, i, 0);
+        constexpr int FIRST = FM >= 4 ? 2 : 1;  // rows that cover the wait for the last reads
+        constexpr int REST = FM - FIRST;
+        constexpr int EACH = (FN + REST - 1) / REST, LEACH = (LOADS + REST - 1) / REST;  // B fragments and loads per row
+        auto row_of = [&](int i) {
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int j = 0; j < FN; ++j) acc[i][j] = Half<T>::mma(b[j], a[i], acc[i][j]);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        uint32_t at = 0;
+        for (int t = 0; t < total; ++t) {
+            const uint32_t then = at == (STAGES - 1) * STAGE ? 0 : at + STAGE;
+            prepare();
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+                row_of(i);
+#pragma unroll
+                for (int j = 0; j < FN; ++j)
+                    if (j / EACH == i) next[j] = fb.get(lb + at, j, 1);
+                a[i] = fa.get(la + at, i, 1);
+            }
+#pragma unroll
+            for (int j = 0; j < FN; ++j) b[j] = next[j];
+#pragma unroll
+            for (int i = 0; i < FIRST; ++i) row_of(i);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            wait_loads<(STAGES - 2) * LOADS>();
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
-            if (issued < total) issue();
-            const uint32_t s = (t % STAGES) * STAGE;
 #pragma unroll
-            for (int kk = 0; kk < 2; ++kk) {
-                v8 b[FN], a[FM];
+            for (int i = 0; i < FIRST; ++i) a[i] = fa.get(la + then, i, 0);
 #pragma unroll
-                for (int j = 0; j < FN; ++j) b[j] = fb.get(lb + s, j, kk);
+            for (int i = FIRST; i < FM; ++i) {
 #pragma unroll
-                for (int i = 0; i < FM; ++i) a[i] = fa.get(la + s, i, kk);
+                for (int j = 0; j < FN; ++j)
+                    if (j / EACH == i - FIRST) next[j] = fb.get(lb + then, j, 0);
+                row_of(i);
+                a[i] = fa.get(la + then, i, 0);
 #pragma unroll
-                for (int i = 0; i < FM; ++i)
-#pragma unroll
-                    for (int j = 0; j < FN; ++j) acc[i][j] = Half<T>::mma(b[j], a[i], acc[i][j]);
+                for (int l = 0; l < LOADS; ++l)
+                    if (l / LEACH == i - FIRST) load(l);
             }
+#pragma unroll
+            for (int j = 0; j < FN; ++j) b[j] = next[j];
+            at = then;
             if constexpr (RUN > 0) {
                 if (t % RUN == RUN - 1 || t == total - 1) {
                     const bool last = t == total - 1;
@@ -286,8 +345,8 @@ template <typename T_, int BM_, int BN_, int WM_, int WN_, bool AS, bool BS, int
                         }
                 }
             }
-            asm volatile("" ::: "memory");
         }
+        wait_loads<0>();  // no store to LDS is left behind
     }
     // m and n of acc[i][j][0] within the block's tile.
     static __device__ __forceinline__ int row(int i) {

@@ -26,6 +26,8 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <functional>
+#include <queue>
 #include <vector>
 
 #include "fc_gemm.h"
@@ -41,6 +43,8 @@ typedef _Float16 f16;
 typedef __bf16 bf16;
 
 extern __shared__ __align__(1024) char lds[];
+
+constexpr int PIECES = 1024;  // of a matrix's sum of squares, at most
 
 struct Matrix {
     uint64_t offset;         // in the flat vectors
@@ -108,6 +112,26 @@ template <typename T, bool STEP> __device__ __forceinline__ float direction(cons
     return g;
 }
 
+// Four elements from i on, a multiple of 4; the momentum is updated and stored.
+template <typename T, bool STEP> __device__ __forceinline__ void direction4(const Source& a, uint64_t i, float* x) {
+    struct alignas(4 * sizeof(T)) G {
+        T x[4];
+    };
+    const G g = *reinterpret_cast<const G*>(static_cast<const T*>(a.g) + i);
+    f32x4 v;
+    if constexpr (STEP) v = *reinterpret_cast<const f32x4*>(a.v + i);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        x[e] = (float)g.x[e];
+        if constexpr (STEP) {
+            x[e] *= a.c;
+            v[e] = a.mu * v[e] + x[e];
+            x[e] = a.nesterov ? x[e] + a.mu * v[e] : v[e];
+        }
+    }
+    if constexpr (STEP) *reinterpret_cast<f32x4*>(a.v + i) = v;
+}
+
 // Sums of squares of one piece of a matrix, in 64 bits: neither tiny nor huge
 // gradients leave its range.
 struct NormArgs {
@@ -117,21 +141,34 @@ struct NormArgs {
     Source d;
 };
 
+__device__ __forceinline__ double block_sum(double sum, double* part) {
+#pragma unroll
+    for (int k = 32; k > 0; k /= 2) sum += __shfl_xor(sum, k);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    return (part[0] + part[1]) + (part[2] + part[3]);
+}
+
 template <typename T, bool STEP> __global__ __launch_bounds__(256) void norm_kernel(NormArgs a) {
     __shared__ double part[4];
     const int2 pc = a.pieces[blockIdx.x];
     const Matrix& m = a.mats[pc.x];
     const int64_t total = (int64_t)m.rows * m.cols, lo = pc.y * m.piece_len, hi = min(lo + m.piece_len, total);
     double sum = 0;
-    for (int64_t i = lo + threadIdx.x; i < hi; i += 256) {
-        const double x = direction<T, STEP>(a.d, m.offset + i, true);
+    const int64_t whole = lo + (hi - lo) / 4 * 4;  // lo is a multiple of 4, as the offset is
+#pragma unroll 4
+    for (int64_t i = lo + 4 * threadIdx.x; i < whole; i += 1024) {
+        float x[4];
+        direction4<T, STEP>(a.d, m.offset + i, x);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum += (double)x[e] * x[e];
+    }
+    if (whole + threadIdx.x < hi) {
+        const double x = direction<T, STEP>(a.d, m.offset + whole + threadIdx.x, true);
         sum += x * x;
     }
-#pragma unroll
-    for (int k = 32; k > 0; k /= 2) sum += __shfl_xor(sum, k);
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
-    __syncthreads();
-    if (threadIdx.x == 0) a.partial[m.piece0 + pc.y] = (part[0] + part[1]) + (part[2] + part[3]);
+    sum = block_sum(sum, part);
+    if (threadIdx.x == 0) a.partial[m.piece0 + pc.y] = sum;
 }
 
 __device__ __forceinline__ void split(float v, f16& hi, f16& lo) {
@@ -156,12 +193,11 @@ template <typename T, bool STEP> __global__ __launch_bounds__(256) void scale_ke
     __shared__ double part[4];
     const Tile t = a.tiles[blockIdx.x];
     const Matrix& m = a.mats[t.mat];
-    double sum = threadIdx.x < m.pieces ? a.partial[m.piece0 + threadIdx.x] : 0;
+    double sum = 0;
 #pragma unroll
-    for (int k = 32; k > 0; k /= 2) sum += __shfl_xor(sum, k);
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
-    __syncthreads();
-    sum = (part[0] + part[1]) + (part[2] + part[3]);
+    for (int k = 0; k < PIECES / 256; ++k)
+        if (k * 256 + threadIdx.x < m.pieces) sum += a.partial[m.piece0 + k * 256 + threadIdx.x];
+    sum = block_sum(sum, part);
     const double f = sum == 0 ? 0 : (m.s == 1 ? a.alone : a.top) / sqrt(sum);
     const int r0 = 64 * (m.turned ? t.j : t.i), c0 = 64 * (m.turned ? t.i : t.j);
     const int c = threadIdx.x & 63;
@@ -319,6 +355,31 @@ template <int STAGE> void launch_kind(int kind, const ProductArgs& a, hipStream_
     else launch<Small<BS>, STAGE>(a, s);
 }
 
+// What a tile costs, in us: per step of 64 of k with the compute unit full of such
+// tiles, per step alone, and besides (start, epilogue).  Measured at 4096 x 4096 x
+// 4096 with fp16 operands (114, 137 and 200 us for the three sizes) and on
+// single tiles.
+struct Cost {
+    double full, alone, once;
+};
+constexpr Cost COST[4] = {{1.75, 1.3, 8.0}, {0.54, 0.55, 4.0}, {0.2, 0.35, 3.0}, {0.54, 0.55, 4.0}};
+
+// Estimated time of tiles of the given numbers of steps, largest first: each goes
+// to the compute unit that is free first.
+double estimate(const std::vector<int>& steps, int kind) {
+    const Cost& c = COST[kind];
+    std::priority_queue<double, std::vector<double>, std::greater<double>> free;
+    for (int i = 0; i < CUS; ++i) free.push(0);
+    double end = 0;
+    for (int n : steps) {
+        const double t = free.top() + n * c.full + c.once * c.full / (c.full + c.alone);
+        free.pop();
+        free.push(t);
+        end = std::max({end, t, n * c.alone + c.once});
+    }
+    return end;
+}
+
 constexpr int64_t SIDE_LIMIT = 1 << 20;
 constexpr int64_t COUNT_LIMIT = 1 << 20;
 constexpr int MOST_STEPS = 64;
@@ -367,7 +428,6 @@ int build(fc_muon* p) {
     const uint64_t o_mats = at.take(n * sizeof(Matrix));
     std::vector<int2> pieces;
     std::vector<Tile> scale, tiles[2];
-    int64_t counts[2][3] = {};
     std::vector<int> by_work(n);
     for (int i = 0; i < n; ++i) {
         const fc_matrix& h = p->host[i];
@@ -386,24 +446,33 @@ int build(fc_muon* p) {
         m.decay_mult = h.decay_mult;
         m.scale = (float)std::sqrt(std::max(1.0, (double)h.rows / h.cols));
         const int64_t total = (int64_t)m.rows * m.cols;
-        m.pieces = (int)std::min<int64_t>(256, fc::ceil_div(total, 4096));
-        m.piece_len = fc::ceil_div(total, m.pieces);
+        m.piece_len = fc::ceil_div(fc::ceil_div(total, std::min<int64_t>(PIECES, fc::ceil_div(total, 4096))), 4) * 4;
+        m.pieces = (int)fc::ceil_div(total, m.piece_len);
         m.piece0 = (int)pieces.size();
         for (int k = 0; k < m.pieces; ++k) pieces.push_back({i, k});
         for (int r = 0; r < (m.s + 63) / 64; ++r)
             for (int c = 0; c < m.lp / 64; ++c) scale.push_back({i, r, c});
-        for (int k = 0; k < 3 && m.s > 1; ++k) {
-            const int64_t s = fc::ceil_div(m.s, TILE[k]), l = fc::ceil_div(m.l, TILE[k]);
-            counts[0][k] += s * (s + 1) / 2;
-            counts[1][k] += s * l;
-        }
         by_work[i] = i;
     }
     // the longest k loops first
     std::stable_sort(by_work.begin(), by_work.end(), [&](int i, int j) { return mats[i].l > mats[j].l; });
     for (int q = 0; q < 2; ++q) {
-        if (p->dtype != FC_BF16) p->kind[q] = counts[q][LARGE] >= CUS * 3 / 4 ? LARGE : counts[q][MIDDLE] >= CUS ? EXACT : SMALL;
-        else p->kind[q] = counts[q][LARGE] >= CUS * 3 / 4 ? LARGE : counts[q][MIDDLE] >= CUS ? MIDDLE : SMALL;
+        double least = HUGE_VAL;
+        for (int k : {LARGE, p->dtype == FC_BF16 ? MIDDLE : EXACT, SMALL}) {
+            std::vector<int> steps;
+            for (int i : by_work) {
+                const Matrix& m = mats[i];
+                if (m.s == 1) continue;
+                const int64_t s = fc::ceil_div(m.s, TILE[k]), l = fc::ceil_div(m.l, TILE[k]);
+                steps.insert(steps.end(), q ? s * l : s * (s + 1) / 2, m.parts * (q ? m.sp : m.lp) / 64);
+            }
+            if (steps.size() > 1 << 16) steps.resize(1 << 16);  // enough to tell
+            const double t = estimate(steps, k);
+            if (t < least) {
+                least = t;
+                p->kind[q] = k;
+            }
+        }
         const int size = TILE[p->kind[q]];
         for (int i : by_work) {
             if (mats[i].s == 1) continue;

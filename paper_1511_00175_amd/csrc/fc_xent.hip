@@ -4,7 +4,7 @@
 //   d = softmax(l) - onehot(y), dx = scale d w, dw = scale d^T x
 //
 // The products are 2 tokens rows dim operations each and bound everything but
-// short lists, where reading w does.  The logits are never stored.  A wave of the
+// short lists, where reading w does.  The logits are never stored.  A block of the
 // first product holds a piece of the vocabulary for its tokens in fp32: it takes
 // the piece's maximum m and sum of exponentials, keeps both (8 bytes), the
 // target's logit, and, when gradients are wanted, the numerators exp(l - m) in 16
@@ -67,26 +67,57 @@ template <typename P> __global__ __launch_bounds__(P::THREADS, P::THREADS / 256)
     P p;
     p.run(lds, a.x, a.w, ti * P::BM, tj * P::BN, 0, a.dim, 1);
     const int n0 = tj * P::BN + P::col(0);
-    const int piece = (tj * P::BN) / P::WN + (threadIdx.x >> 6) % (P::BN / P::WN);
-    const int lane = threadIdx.x & 63;
+    const int wn = (threadIdx.x >> 6) % (P::BN / P::WN), lane = threadIdx.x & 63;
+    constexpr int SIDE = P::BN / P::WN;                            // waves that share a token
+    float(*const part)[P::BM] = reinterpret_cast<float(*)[P::BM]>(lds);  // [SIDE][token of the tile]
+    int* const target = reinterpret_cast<int*>(lds + sizeof(float) * SIDE * P::BM);  // in the tile's columns
+    float tops[P::FM];
+    __syncthreads();  // the tiles in LDS are done with
+    if (threadIdx.x < P::BM) {
+        const int m = ti * P::BM + threadIdx.x;
+        const int64_t y = m < a.n ? target_of(a.targets, a.target_bytes, m) : -1;
+        target[threadIdx.x] = y >= 0 && y < a.rows ? (int)y - tj * P::BN : -1;
+    }
+    if ((tj + 1) * P::BN > a.rows) {  // past the vocabulary's end: no weight in maxima and sums
+#pragma unroll
+        for (int j = 0; j < P::FN; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (n0 + 16 * j + e >= a.rows) {
+#pragma unroll
+                    for (int i = 0; i < P::FM; ++i) p.acc[i][j][e] = -__builtin_inff();
+                }
+    }
+    __syncthreads();
 #pragma unroll
     for (int i = 0; i < P::FM; ++i) {
         const int m = ti * P::BM + P::row(i);
-        const bool live = m < a.n;
-        const int64_t y = live ? target_of(a.targets, a.target_bytes, m) : -1;
-        const int at = y >= 0 && y < a.rows ? (int)y - n0 : -1;  // the target among the lane's columns
+        const int at = target[P::row(i)] - P::col(0);
         float top = -__builtin_inff();
 #pragma unroll
         for (int j = 0; j < P::FN; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                if (n0 + 16 * j + e >= a.rows) p.acc[i][j][e] = -__builtin_inff();
                 top = fmaxf(top, p.acc[i][j][e]);
                 if (at == 16 * j + e) a.target_logit[m] = p.acc[i][j][e];
             }
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
-        const float ref = top == -__builtin_inff() ? 0.f : top;
+        tops[i] = top;
+        if (lane < 16) part[wn][P::row(i)] = top;
+        __builtin_amdgcn_sched_barrier(0);  // row by row: the registers hold no more
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < P::FM; ++i)
+#pragma unroll
+        for (int q = 0; q < SIDE; ++q) tops[i] = fmaxf(tops[i], part[q][P::row(i)]);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < P::FM; ++i) {
+        const int m = ti * P::BM + P::row(i);
+        T* const to = a.numer && m < a.n ? static_cast<T*>(a.numer) + (int64_t)m * a.ld + n0 : nullptr;
+        const float ref = tops[i] == -__builtin_inff() ? 0.f : tops[i];
         float sum = 0.f;
 #pragma unroll
         for (int j = 0; j < P::FN; ++j) {
@@ -97,13 +128,22 @@ template <typename P> __global__ __launch_bounds__(P::THREADS, P::THREADS / 256)
                 sum += q;
                 v[e] = (T)q;
             }
-            const int n = n0 + 16 * j;
-            if (a.numer && live && n < a.ld)
-                *reinterpret_cast<typename Half<T>::v4*>(static_cast<T*>(a.numer) + (int64_t)m * a.ld + n) = v;
+            if (to && n0 + 16 * j < a.ld) *reinterpret_cast<typename Half<T>::v4*>(to + 16 * j) = v;
         }
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
-        if (live && lane < 16 && piece * P::WN < a.rows) a.stats[(int64_t)piece * a.n + m] = f32x2{top, sum};
+        if (lane < 16) part[wn][P::row(i)] = sum;
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < P::FM; ++i) {
+        const int m = ti * P::BM + P::row(i);
+        if (wn || lane >= 16 || m >= a.n) continue;
+        float sum = 0.f;
+#pragma unroll
+        for (int q = 0; q < SIDE; ++q) sum += part[q][P::row(i)];
+        a.stats[(int64_t)tj * a.n + m] = f32x2{tops[i], sum};
     }
 }
 
@@ -120,33 +160,35 @@ struct JoinArgs {
     float* loss;
 };
 
-// 16 tokens per block, 16 threads each.
-__global__ __launch_bounds__(256) void join_kernel(JoinArgs a) {
-    __shared__ f32x2 part[16][17];
-    const int i = threadIdx.x & 15, q = threadIdx.x >> 4;
-    const int64_t t = (int64_t)blockIdx.x * 16 + i;
-    float top = -__builtin_inff(), sum = 0.f;
-    if (t < a.n)
-        for (int k = q; k < a.pieces; k += 16) {
-            const f32x2 s = a.stats[(int64_t)k * a.n + t];
-            const float m = fmaxf(top, s.x);
-            if (m > -__builtin_inff()) sum = sum * exp_(top - m) + s.y * exp_(s.x - m);
-            else sum += s.y;
-            top = m;
-        }
-    part[i][q] = f32x2{top, sum};
-    __syncthreads();
-    if (q || t >= a.n) return;
-    for (int k = 1; k < 16; ++k) {
-        const f32x2 s = part[i][k];
-        const float m = fmaxf(top, s.x);
-        if (m > -__builtin_inff()) sum = sum * exp_(top - m) + s.y * exp_(s.x - m);
-        else sum += s.y;
-        top = m;
+// The sums of exponentials s and q, of what lies below their maxima, as one.
+__device__ __forceinline__ f32x2 join(f32x2 s, f32x2 q) {
+    const float m = fmaxf(s.x, q.x);
+    if (!(m > -__builtin_inff())) return f32x2{m, s.y + q.y};
+    return f32x2{m, s.y * exp_(s.x - m) + q.y * exp_(q.x - m)};
+}
+
+// T tokens per block of 256 threads, 256 / T threads each: 16 where there are
+// enough tokens (a piece's stats of 16 tokens are neighbours), else 1.
+template <int T> __global__ __launch_bounds__(256) void join_kernel(JoinArgs a) {
+    constexpr int Q = 256 / T;
+    __shared__ f32x2 part[T][Q + 1];
+    const int i = threadIdx.x % T, q = threadIdx.x / T;
+    const int64_t t = (int64_t)blockIdx.x * T + i;
+    f32x2 sum{-__builtin_inff(), 0.f};
+    if (t < a.n) {
+#pragma unroll 8
+        for (int k = q; k < a.pieces; k += Q) sum = join(sum, a.stats[(int64_t)k * a.n + t]);
     }
+    part[i][q] = sum;
+#pragma unroll
+    for (int half = Q / 2; half > 0; half /= 2) {
+        __syncthreads();
+        if (q < half) part[i][q] = sum = join(sum, part[i][q + half]);
+    }
+    if (q || t >= a.n) return;
     const int64_t y = target_of(a.targets, a.target_bytes, t);
     const bool real = y >= 0 && y < a.rows;
-    const float lse = top + logf(sum);
+    const float lse = sum.x + logf(sum.y);
     if (a.lse) {
         a.lse[t] = lse;
         a.row[t] = real ? (int)y : -1;
@@ -386,7 +428,8 @@ template <typename T> hipError_t prepare_all() {
     return hipSuccess;
 }
 
-int piece_width(TileKind k) { return k == LARGE ? Large<f16, false, false>::WN : k == MIDDLE ? Middle<f16, false, false>::WN : Short<f16, false, false>::WN; }
+// Columns of the first product's tiles, a piece of the vocabulary.
+int piece_width(TileKind k) { return k == LARGE ? 256 : 128; }
 
 // Splits of dx's product over the vocabulary: until the tiles fill the chip,
 // with at least 16 steps of k each.
@@ -454,7 +497,8 @@ int run(fc_xent* p, const void* x, int64_t ldx, const void* w, int64_t ldw, cons
         else launch_logit<Short<T, false, false>>(l, s);
         const int width = piece_width(kind), pieces = (int)fc::ceil_div(p->rows, width);
         JoinArgs j{p->stats, p->target_logit, yt, target_bytes, m, (int)p->rows, pieces, p->lse, p->row, loss + t0};
-        join_kernel<<<(unsigned)fc::ceil_div(m, 16), 256, 0, s>>>(j);
+        if (m >= 16 * CUS) join_kernel<16><<<(unsigned)fc::ceil_div(m, 16), 256, 0, s>>>(j);
+        else join_kernel<1><<<(unsigned)m, 256, 0, s>>>(j);
         if (!grads) continue;
         DiffArgs d{p->numer, p->ld, m, width, pieces, p->stats, p->lse, p->row};
         diff_kernel<T><<<dim3((unsigned)fc::ceil_div(p->ld, 2048), (unsigned)fc::ceil_div(m, DIFF_ROWS)), 256, 0, s>>>(d);
@@ -568,11 +612,8 @@ int fc_xent_create(fc_xent** plan, int64_t rows, int64_t dim, int64_t max_tokens
         if (chunk_tokens) most = std::min(most, chunk_tokens);
         p->chunk = std::max<int64_t>(1, std::min(most, max_tokens));
         const int64_t c = p->chunk;
-        // the most pieces and splits of any chunk length up to c
-        int64_t stats = 0, sums = 0;
-        for (int64_t m : {std::min<int64_t>(c, 64), c}) {
-            stats = std::max(stats, m * fc::ceil_div(rows, m <= 64 ? 32 : 64));
-        }
+        const int64_t stats = c * fc::ceil_div(rows, 128);
+        int64_t sums = 0;  // the most splits of any chunk length up to c
         for (int64_t m = 1; m <= c; m = m < c && m + 64 > c ? c : m + 64) {
             const int64_t up = std::min(c, m + 63);
             const int sp = std::max(splits_for(m, dim, rows), splits_for(up, dim, rows));
