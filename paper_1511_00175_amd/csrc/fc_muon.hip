@@ -26,16 +26,16 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
-#include <functional>
-#include <queue>
 #include <vector>
 
 #include "fc_gemm.h"
 #include "fc_lm_host.h"
+#include "fc_tiles.h"
 
 using fc::f16x4;
 using fc::f32x4;
 using fc::Operand;
+using Tile = fc::TileAt;
 
 namespace {
 
@@ -62,10 +62,6 @@ struct Matrix {
     int64_t piece_len;
 };
 
-struct Tile {
-    int mat, i, j;
-};
-
 // Where results go: to out, or into the weights w.
 struct Output {
     void* out;
@@ -74,9 +70,7 @@ struct Output {
     float lr, wd;
 };
 
-// u = element (i, j) of X's orthogonal form.
-__device__ __forceinline__ void store_out(const Output& a, const Matrix& m, int i, int j, float u) {
-    const uint64_t at = m.offset + (m.turned ? (uint64_t)j * m.cols + i : (uint64_t)i * m.cols + j);
+__device__ __forceinline__ void store_one(const Output& a, const Matrix& m, uint64_t at, float u) {
     if (!a.out) {
         const float w = a.w[at];
         a.w[at] = w - a.lr * m.lr_mult * (m.scale * u + a.wd * m.decay_mult * w);
@@ -86,6 +80,53 @@ __device__ __forceinline__ void store_out(const Output& a, const Matrix& m, int 
         static_cast<f16*>(a.out)[at] = (f16)u;
     } else {
         static_cast<bf16*>(a.out)[at] = (bf16)u;
+    }
+}
+
+// Four neighbours of a row of the result, of which those in the matrix are
+// stored, as one vector where rows start on one (offsets are multiples of 4).
+__device__ __forceinline__ void store_out(const Output& a, const Matrix& m, int row, int col, f32x4 u) {
+    if (col >= m.cols) return;
+    const uint64_t at = m.offset + (uint64_t)row * m.cols + col;
+    if (m.cols % 4) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (col + e < m.cols) store_one(a, m, at + e, u[e]);
+    } else if (!a.out) {
+        f32x4* p = reinterpret_cast<f32x4*>(a.w + at);
+        const f32x4 w = *p;
+        const float k = a.lr * m.lr_mult, d = a.wd * m.decay_mult;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) u[e] = w[e] - k * (m.scale * u[e] + d * w[e]);
+        *p = u;
+    } else if (a.dt == FC_F32) {
+        *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + at) = u;
+    } else if (a.dt == FC_F16) {
+        *reinterpret_cast<f16x4*>(static_cast<f16*>(a.out) + at) = __builtin_convertvector(u, f16x4);
+    } else {
+        *reinterpret_cast<fc::b16x4*>(static_cast<bf16*>(a.out) + at) = __builtin_convertvector(u, fc::b16x4);
+    }
+}
+
+// The 4 x 4 numbers of 4 neighbouring lanes transposed: lane q's number e becomes
+// lane e's number q.
+__device__ __forceinline__ float other(float x, bool two) {  // of the lane 1 or 2 away
+    const int v = __float_as_int(x);
+    return __int_as_float(two ? __builtin_amdgcn_update_dpp(0, v, 0x4e, 0xf, 0xf, true) : __builtin_amdgcn_update_dpp(0, v, 0xb1, 0xf, 0xf, true));
+}
+__device__ __forceinline__ void turn(f32x4& v, int quad) {
+    const bool high = quad & 2, odd = quad & 1;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const float y = other(high ? v[k] : v[k + 2], true);
+        v[k] = high ? y : v[k];
+        v[k + 2] = high ? v[k + 2] : y;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; k += 2) {
+        const float y = other(odd ? v[k] : v[k + 1], false);
+        v[k] = odd ? y : v[k];
+        v[k + 1] = odd ? v[k + 1] : y;
     }
 }
 
@@ -214,7 +255,7 @@ template <typename T, bool STEP> __global__ __launch_bounds__(256) void scale_ke
         if (64 * t.i + r >= m.s) break;
         const float x = m.turned ? tile[c][r] : tile[r][c];
         if (m.s == 1) {
-            if (64 * t.j + c < m.l) store_out(a.to, m, 0, 64 * t.j + c, x);
+            if (64 * t.j + c < m.l) store_one(a.to, m, m.offset + 64 * t.j + c, x);
             continue;
         }
         f16 hi, lo;
@@ -230,7 +271,6 @@ enum Stage { GRAM, POLY, NEXT, LAST };
 struct ProductArgs {
     const Matrix* mats;
     const Tile* tiles;
-    int count;
     int from;                // which x holds X
     // GRAM: A = f0 acc; POLY: B = f0 acc + f1 A; NEXT: X = f0 acc + f1 X.  Each the
     // sum of two floats: a coefficient's rounding is an error of every entry's alike.
@@ -253,7 +293,8 @@ __device__ __forceinline__ f32x4 load_four(const f16* p, int64_t lo, bool both) 
 }
 
 template <typename P, int STAGE> __global__ __launch_bounds__(P::THREADS, P::THREADS / 256) void product_kernel(ProductArgs a) {
-    const Tile t = a.tiles[fc::xcd_order(blockIdx.x, a.count)];
+    const Tile t = a.tiles[blockIdx.x];
+    if (t.mat < 0) return;
     const Matrix& m = a.mats[t.mat];
     const f16* x = m.x[a.from];
     Operand A, B;
@@ -275,17 +316,37 @@ template <typename P, int STAGE> __global__ __launch_bounds__(P::THREADS, P::THR
     f16* const to = STAGE == GRAM ? m.a : STAGE == POLY ? m.b : m.x[1 - a.from];
     const int ld = STAGE <= POLY ? m.sp : m.lp;
     const int64_t lo = STAGE <= POLY ? m.a_lo : m.x_lo;
+    const bool halves = STAGE == NEXT || both;
+    auto store = [&](int r, int c, const f32x4& v) {  // 4 neighbours of row r
+        f16x4 hi, low;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            f16 h, l;
+            split(v[e], h, l);
+            hi[e] = h;
+            low[e] = l;
+        }
+        f16* q = to + (int64_t)r * ld + c;
+        *reinterpret_cast<f16x4*>(q) = hi;
+        if (halves) *reinterpret_cast<f16x4*>(q + lo) = low;
+    };
+    const int quad = threadIdx.x & 3;
+    // LAST: a wave's 16 rows of results on their way to the output's order
+    float(*const part)[P::WN + 4] = reinterpret_cast<float(*)[P::WN + 4]>(lds + (threadIdx.x >> 6) * 16 * (P::WN + 4) * sizeof(float));
+    static_assert(P::WAVES * 16 * (P::WN + 4) * sizeof(float) <= P::LDS, "the rows of all waves fit");
+    if constexpr (STAGE == LAST) __syncthreads();  // the tiles in LDS are done with
 #pragma unroll
     for (int i = 0; i < P::FM; ++i) {
         const int r = t.i * P::BM + P::row(i);
-        if (r >= m.s) continue;
+        const bool in = r < m.s;
 #pragma unroll
         for (int j = 0; j < P::FN; ++j) {
             const int c = t.j * P::BN + P::col(j);
-            if (c >= ld) continue;
             f32x4 v = a.f0 * p.acc[i][j];
             if constexpr (STAGE != GRAM) {
-                const f32x4 q = STAGE == POLY ? load_four(m.a + (int64_t)r * ld + c, lo, both) : load_four(x + (int64_t)r * ld + c, lo, true);
+                f32x4 q{0.f, 0.f, 0.f, 0.f};
+                if (in && c < ld)
+                    q = STAGE == POLY ? load_four(m.a + (int64_t)r * ld + c, lo, both) : load_four(x + (int64_t)r * ld + c, lo, true);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float z = p.acc[i][j][e];
@@ -293,91 +354,72 @@ template <typename P, int STAGE> __global__ __launch_bounds__(P::THREADS, P::THR
                 }
             }
             if constexpr (STAGE == LAST) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (c + e < m.l) store_out(a.to, m, r, c + e, v[e] * a.unscale);
+                *reinterpret_cast<f32x4*>(part[threadIdx.x & 15] + 16 * j + 4 * ((threadIdx.x & 63) >> 4)) = a.unscale * v;
             } else {
-                f16x4 hi, low;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    f16 h, l;
-                    split(v[e], h, l);
-                    hi[e] = h;
-                    low[e] = l;
-                }
-                const bool halves = STAGE == NEXT || both;
-                f16* q = to + (int64_t)r * ld + c;
-                *reinterpret_cast<f16x4*>(q) = hi;
-                if (halves) *reinterpret_cast<f16x4*>(q + lo) = low;
+                if (in && c < ld) store(r, c, v);
                 if (STAGE <= POLY && t.i != t.j) {  // the mirror image
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (c + e < m.s) {
-                            f16* z = to + (int64_t)(c + e) * ld + r;
-                            z[0] = hi[e];
-                            if (halves) z[lo] = low[e];
-                        }
+                    turn(v, quad);
+                    if (c + quad < m.s && r - quad < ld) store(c + quad, r - quad, v);
                 }
             }
         }
+        if constexpr (STAGE == LAST) {
+            // the wave's 16 rows of WN columns from LDS, in the order of the result
+            const int lane = threadIdx.x & 63, r0 = r - (lane & 15), c0 = t.j * P::BN + P::col(0) - 4 * (lane >> 4);
+            constexpr int QUADS = P::WN / 4;  // of a row
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+            for (int k = lane; k < 16 * QUADS; k += 64) {
+                f32x4 u;
+                if (!m.turned) {
+                    const int y = k / QUADS, z = k % QUADS * 4;
+                    u = *reinterpret_cast<const f32x4*>(part[y] + z);
+                    if (r0 + y < m.s) store_out(a.to, m, r0 + y, c0 + z, u);
+                } else {
+                    const int y = k % 4 * 4, z = k / 4;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) u[e] = part[y + e][z];
+                    if (c0 + z < m.l) store_out(a.to, m, c0 + z, r0 + y, u);
+                }
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
+        __builtin_amdgcn_sched_barrier(0);  // row by row: the registers hold no more
     }
 }
 
+// By fc::TileKind.  LARGE has no registers left for sums in runs, so symmetric
+// products of fp32's accuracy do without it.  BROAD's 192 is no power of two,
+// which slow operands need: it serves the symmetric products alone.
 template <bool BS> using Large = fc::Product<f16, 256, 256, 128, 64, false, BS>;
-template <bool BS> using Middle = fc::Product<f16, 128, 128, 64, 64, false, BS>;
-template <bool BS> using Small = fc::Product<f16, 64, 64, 32, 32, false, BS, 2, 8>;
-template <bool BS> using Exact = fc::Product<f16, 128, 128, 64, 64, false, BS, 2, 8>;
-
-// EXACT has the registers for sums in runs, which LARGE has not.
-enum TileKind { LARGE, MIDDLE, SMALL, EXACT };
-constexpr int TILE[4] = {256, 128, 64, 128};
-constexpr int CUS = 256;
+template <bool BS> using Broad = fc::Product<f16, 192, 192, 96, 48, false, BS, 2, 8>;
+template <bool BS> using Middle = fc::Product<f16, 128, 128, 64, 64, false, BS, 2, 8>;
+template <bool BS> using Small = fc::Product<f16, 64, 64, 32, 32, false, BS, 4, 8>;
 
 template <typename P, int STAGE> hipError_t prepare_one() {
     return hipFuncSetAttribute((const void*)product_kernel<P, STAGE>, hipFuncAttributeMaxDynamicSharedMemorySize, P::LDS);
 }
 
-template <template <bool> class P> hipError_t prepare() {
-    for (hipError_t e : {prepare_one<P<false>, GRAM>(), prepare_one<P<false>, POLY>(), prepare_one<P<true>, NEXT>(), prepare_one<P<true>, LAST>()})
+hipError_t prepare() {
+    for (hipError_t e : {prepare_one<Large<false>, GRAM>(), prepare_one<Large<false>, POLY>(), prepare_one<Large<true>, NEXT>(),
+                         prepare_one<Large<true>, LAST>(), prepare_one<Broad<false>, GRAM>(), prepare_one<Broad<false>, POLY>(),
+                         prepare_one<Middle<false>, GRAM>(), prepare_one<Middle<false>, POLY>(), prepare_one<Middle<true>, NEXT>(),
+                         prepare_one<Middle<true>, LAST>(), prepare_one<Small<false>, GRAM>(), prepare_one<Small<false>, POLY>(),
+                         prepare_one<Small<true>, NEXT>(), prepare_one<Small<true>, LAST>()})
         if (e != hipSuccess) return e;
     return hipSuccess;
 }
 
-template <typename P, int STAGE> void launch(const ProductArgs& a, hipStream_t s) {
-    product_kernel<P, STAGE><<<a.count, P::THREADS, P::LDS, s>>>(a);
+template <typename P, int STAGE> void launch(const ProductArgs& a, int count, hipStream_t s) {
+    product_kernel<P, STAGE><<<count, P::THREADS, P::LDS, s>>>(a);
 }
 
-template <int STAGE> void launch_kind(int kind, const ProductArgs& a, hipStream_t s) {
+template <int STAGE> void launch_kind(int kind, const ProductArgs& a, int count, hipStream_t s) {
     constexpr bool BS = STAGE >= NEXT;
-    if (kind == LARGE) launch<Large<BS>, STAGE>(a, s);
-    else if (kind == MIDDLE) launch<Middle<BS>, STAGE>(a, s);
-    else if (kind == EXACT) launch<Exact<BS>, STAGE>(a, s);
-    else launch<Small<BS>, STAGE>(a, s);
-}
-
-// What a tile costs, in us: per step of 64 of k with the compute unit full of such
-// tiles, per step alone, and besides (start, epilogue).  Measured at 4096 x 4096 x
-// 4096 with fp16 operands (114, 137 and 200 us for the three sizes) and on
-// single tiles.
-struct Cost {
-    double full, alone, once;
-};
-constexpr Cost COST[4] = {{1.75, 1.3, 8.0}, {0.54, 0.55, 4.0}, {0.2, 0.35, 3.0}, {0.54, 0.55, 4.0}};
-
-// Estimated time of tiles of the given numbers of steps, largest first: each goes
-// to the compute unit that is free first.
-double estimate(const std::vector<int>& steps, int kind) {
-    const Cost& c = COST[kind];
-    std::priority_queue<double, std::vector<double>, std::greater<double>> free;
-    for (int i = 0; i < CUS; ++i) free.push(0);
-    double end = 0;
-    for (int n : steps) {
-        const double t = free.top() + n * c.full + c.once * c.full / (c.full + c.alone);
-        free.pop();
-        free.push(t);
-        end = std::max({end, t, n * c.alone + c.once});
-    }
-    return end;
+    if (kind == fc::TILE_LARGE) return launch<Large<BS>, STAGE>(a, count, s);
+    if (kind == fc::TILE_MIDDLE) return launch<Middle<BS>, STAGE>(a, count, s);
+    if (kind == fc::TILE_SMALL) return launch<Small<BS>, STAGE>(a, count, s);
+    if constexpr (!BS) launch<Broad<BS>, STAGE>(a, count, s);
 }
 
 constexpr int64_t SIDE_LIMIT = 1 << 20;
@@ -413,9 +455,11 @@ struct fc_muon {
     double* partial = nullptr;
     const Tile* scale_tiles = nullptr;
     int n_scale = 0;
-    const Tile* tiles[2] = {nullptr, nullptr};  // of the symmetric products, of X's
-    int n_tiles[2] = {0, 0};
-    int kind[2] = {SMALL, SMALL};
+    struct Launch {
+        int kind, count;
+        const Tile* tiles;
+    };
+    std::vector<Launch> launches[3];  // of the products GRAM, POLY, NEXT
 };
 
 namespace {
@@ -427,8 +471,8 @@ int build(fc_muon* p) {
     fc::Layout at;
     const uint64_t o_mats = at.take(n * sizeof(Matrix));
     std::vector<int2> pieces;
-    std::vector<Tile> scale, tiles[2];
-    std::vector<int> by_work(n);
+    std::vector<Tile> scale;
+    std::vector<fc::TileShape> shapes[3];
     for (int i = 0; i < n; ++i) {
         const fc_matrix& h = p->host[i];
         Matrix& m = mats[i];
@@ -452,40 +496,21 @@ int build(fc_muon* p) {
         for (int k = 0; k < m.pieces; ++k) pieces.push_back({i, k});
         for (int r = 0; r < (m.s + 63) / 64; ++r)
             for (int c = 0; c < m.lp / 64; ++c) scale.push_back({i, r, c});
-        by_work[i] = i;
+        const bool alone = m.s == 1;  // needs no products
+        shapes[GRAM].push_back({alone ? 0 : m.s, m.s, m.parts * m.lp / 64});
+        shapes[POLY].push_back({alone ? 0 : m.s, m.s, m.parts * m.sp / 64});
+        shapes[NEXT].push_back({alone ? 0 : m.s, m.l, m.parts * m.sp / 64});
     }
-    // the longest k loops first
-    std::stable_sort(by_work.begin(), by_work.end(), [&](int i, int j) { return mats[i].l > mats[j].l; });
-    for (int q = 0; q < 2; ++q) {
-        double least = HUGE_VAL;
-        for (int k : {LARGE, p->dtype == FC_BF16 ? MIDDLE : EXACT, SMALL}) {
-            std::vector<int> steps;
-            for (int i : by_work) {
-                const Matrix& m = mats[i];
-                if (m.s == 1) continue;
-                const int64_t s = fc::ceil_div(m.s, TILE[k]), l = fc::ceil_div(m.l, TILE[k]);
-                steps.insert(steps.end(), q ? s * l : s * (s + 1) / 2, m.parts * (q ? m.sp : m.lp) / 64);
-            }
-            if (steps.size() > 1 << 16) steps.resize(1 << 16);  // enough to tell
-            const double t = estimate(steps, k);
-            if (t < least) {
-                least = t;
-                p->kind[q] = k;
-            }
-        }
-        const int size = TILE[p->kind[q]];
-        for (int i : by_work) {
-            if (mats[i].s == 1) continue;
-            const int s = (int)fc::ceil_div(mats[i].s, size), l = (int)fc::ceil_div(mats[i].l, size);
-            for (int g = 0; g < s; g += 8)  // groups of 8 tile rows, down the rows first
-                for (int c = 0; c < (q ? l : s); ++c)
-                    for (int r = g; r < std::min(g + 8, s); ++r)
-                        if (q || r <= c) tiles[q].push_back({i, r, c});
-        }
-    }
+    const bool fine = p->dtype != FC_BF16;
+    std::vector<int> symmetric{fc::TILE_LARGE, fc::TILE_BROAD, fc::TILE_MIDDLE, fc::TILE_SMALL};
+    if (fine) symmetric.erase(symmetric.begin());
+    std::vector<fc::TileLaunch> plans[3] = {fc::plan_tiles(shapes[GRAM], true, symmetric), fc::plan_tiles(shapes[POLY], true, symmetric),
+                                            fc::plan_tiles(shapes[NEXT], false, {fc::TILE_LARGE, fc::TILE_MIDDLE, fc::TILE_SMALL})};
     const uint64_t o_pieces = at.take(pieces.size() * sizeof(int2)), o_partial = at.take(pieces.size() * sizeof(double)),
-                   o_scale = at.take(scale.size() * sizeof(Tile)), o_sym = at.take(tiles[0].size() * sizeof(Tile)),
-                   o_x = at.take(tiles[1].size() * sizeof(Tile));
+                   o_scale = at.take(scale.size() * sizeof(Tile));
+    std::vector<uint64_t> o_tiles;
+    for (const auto& v : plans)
+        for (const fc::TileLaunch& l : v) o_tiles.push_back(at.take(l.tiles.size() * sizeof(Tile)));
     const uint64_t tables = at.size;
     std::vector<uint64_t> places(n * 4);
     for (int i = 0; i < n; ++i) {
@@ -511,8 +536,13 @@ int build(fc_muon* p) {
     put(o_mats, mats.data(), n * sizeof(Matrix));
     put(o_pieces, pieces.data(), pieces.size() * sizeof(int2));
     put(o_scale, scale.data(), scale.size() * sizeof(Tile));
-    put(o_sym, tiles[0].data(), tiles[0].size() * sizeof(Tile));
-    put(o_x, tiles[1].data(), tiles[1].size() * sizeof(Tile));
+    size_t next = 0;
+    for (int q = 0; q < 3; ++q)
+        for (const fc::TileLaunch& l : plans[q]) {
+            put(o_tiles[next], l.tiles.data(), l.tiles.size() * sizeof(Tile));
+            p->launches[q].push_back({l.kind, (int)l.tiles.size(), reinterpret_cast<const Tile*>(b + o_tiles[next])});
+            ++next;
+        }
     if (tables && hipMemcpy(b, image.data(), tables, hipMemcpyHostToDevice) != hipSuccess) return FC_EHIP;
     p->mats = reinterpret_cast<const Matrix*>(b + o_mats);
     p->pieces = reinterpret_cast<const int2*>(b + o_pieces);
@@ -520,9 +550,6 @@ int build(fc_muon* p) {
     p->partial = reinterpret_cast<double*>(b + o_partial);
     p->scale_tiles = reinterpret_cast<const Tile*>(b + o_scale);
     p->n_scale = (int)scale.size();
-    p->tiles[0] = reinterpret_cast<const Tile*>(b + o_sym);
-    p->tiles[1] = reinterpret_cast<const Tile*>(b + o_x);
-    for (int q = 0; q < 2; ++q) p->n_tiles[q] = (int)tiles[q].size();
     return FC_OK;
 }
 
@@ -542,23 +569,28 @@ int products(fc_muon* p, const Output& to, hipStream_t s) {
         a.f0_low = (float)(f0 - a.f0);
         a.f1_low = (float)(f1 - a.f1);
     };
-    for (int k = 0; k < p->steps && p->n_tiles[0] > 0; ++k) {
+    for (int k = 0; k < p->steps; ++k) {
         ProductArgs a{};
         a.to = to;
         a.mats = p->mats;
         a.from = from;
-        a.tiles = p->tiles[0];
-        a.count = p->n_tiles[0];
         set(a, p->sa / (p->sx * p->sx), 0);
-        launch_kind<GRAM>(p->kind[0], a, s);
+        for (const auto& l : p->launches[GRAM]) {
+            a.tiles = l.tiles;
+            launch_kind<GRAM>(l.kind, a, l.count, s);
+        }
         set(a, p->c * p->sb / (p->sa * p->sa), p->b * p->sb / p->sa);
-        launch_kind<POLY>(p->kind[0], a, s);
-        a.tiles = p->tiles[1];
-        a.count = p->n_tiles[1];
+        for (const auto& l : p->launches[POLY]) {
+            a.tiles = l.tiles;
+            launch_kind<POLY>(l.kind, a, l.count, s);
+        }
         set(a, 1 / p->sb, p->a);
         a.unscale = (float)(1 / p->sx);
-        if (k + 1 < p->steps) launch_kind<NEXT>(p->kind[1], a, s);
-        else launch_kind<LAST>(p->kind[1], a, s);
+        for (const auto& l : p->launches[NEXT]) {
+            a.tiles = l.tiles;
+            if (k + 1 < p->steps) launch_kind<NEXT>(l.kind, a, l.count, s);
+            else launch_kind<LAST>(l.kind, a, l.count, s);
+        }
         from ^= 1;
     }
     return fc::hip_code(hipGetLastError());
@@ -648,10 +680,7 @@ int fc_muon_create(fc_muon** plan, const fc_matrix* mats, int n, int dtype, int 
         p->sa = pow2_below(32768 / (top * top));
         p->sb = by > 0 ? pow2_below(32768 / by) : 1;
         int rc = p->order.create();
-        if (!rc) rc = fc::hip_code(prepare<Large>());
-        if (!rc) rc = fc::hip_code(prepare<Middle>());
-        if (!rc) rc = fc::hip_code(prepare<Small>());
-        if (!rc) rc = fc::hip_code(prepare<Exact>());
+        if (!rc) rc = fc::hip_code(prepare());
         if (!rc) rc = build(p);
         if (rc) {
             fc_muon_destroy(p);

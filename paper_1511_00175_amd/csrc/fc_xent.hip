@@ -33,7 +33,7 @@ typedef __bf16 bf16;
 
 extern __shared__ __align__(1024) char lds[];
 
-constexpr float LOG2E = 1.44269504088896341f;
+constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
 
 // d is stored times this: fp16 then keeps probabilities down to 2^-29 with all
 // their bits, and its largest, 1, is still in range.  bf16 needs no scale.
