@@ -108,28 +108,6 @@ __device__ __forceinline__ void store_out(const Output& a, const Matrix& m, int 
     }
 }
 
-// The 4 x 4 numbers of 4 neighbouring lanes transposed: lane q's number e becomes
-// lane e's number q.
-__device__ __forceinline__ float other(float x, bool two) {  // of the lane 1 or 2 away
-    const int v = __float_as_int(x);
-    return __int_as_float(two ? __builtin_amdgcn_update_dpp(0, v, 0x4e, 0xf, 0xf, true) : __builtin_amdgcn_update_dpp(0, v, 0xb1, 0xf, 0xf, true));
-}
-__device__ __forceinline__ void turn(f32x4& v, int quad) {
-    const bool high = quad & 2, odd = quad & 1;
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const float y = other(high ? v[k] : v[k + 2], true);
-        v[k] = high ? y : v[k];
-        v[k + 2] = high ? v[k + 2] : y;
-    }
-#pragma unroll
-    for (int k = 0; k < 4; k += 2) {
-        const float y = other(odd ? v[k] : v[k + 1], false);
-        v[k] = odd ? y : v[k];
-        v[k + 1] = odd ? v[k + 1] : y;
-    }
-}
-
 // The direction made orthogonal: g itself, or a momentum update of it.
 struct Source {
     const void* g;
@@ -279,20 +257,7 @@ struct ProductArgs {
     Output to;
 };
 
-__device__ __forceinline__ f32x4 load_four(const f16* p, int64_t lo, bool both) {
-    const f16x4 h = *reinterpret_cast<const f16x4*>(p);
-    f32x4 v;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = (float)h[e];
-    if (both) {
-        const f16x4 l = *reinterpret_cast<const f16x4*>(p + lo);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] += (float)l[e];
-    }
-    return v;
-}
-
-template <typename P, int STAGE> __global__ __launch_bounds__(P::THREADS, P::THREADS / 256) void product_kernel(ProductArgs a) {
+template <typename P, int STAGE> __global__ __launch_bounds__(P::THREADS, 2) void product_kernel(ProductArgs a) {
     const Tile t = a.tiles[blockIdx.x];
     if (t.mat < 0) return;
     const Matrix& m = a.mats[t.mat];
@@ -330,61 +295,78 @@ template <typename P, int STAGE> __global__ __launch_bounds__(P::THREADS, P::THR
         *reinterpret_cast<f16x4*>(q) = hi;
         if (halves) *reinterpret_cast<f16x4*>(q + lo) = low;
     };
-    const int quad = threadIdx.x & 3;
-    // LAST: a wave's 16 rows of results on their way to the output's order
+    // Strip by strip of 16 rows, each wave takes its results through LDS, so that a
+    // row's neighbours are in neighbouring lanes where A or X are read and results
+    // stored; the next strip's reads are on their way meanwhile.
     float(*const part)[P::WN + 4] = reinterpret_cast<float(*)[P::WN + 4]>(lds + (threadIdx.x >> 6) * 16 * (P::WN + 4) * sizeof(float));
-    static_assert(P::WAVES * 16 * (P::WN + 4) * sizeof(float) <= P::LDS, "the rows of all waves fit");
-    if constexpr (STAGE == LAST) __syncthreads();  // the tiles in LDS are done with
+    static_assert(P::WAVES * 16 * (P::WN + 4) * sizeof(float) <= P::LDS, "the strips of all waves fit");
+    constexpr int QUADS = P::WN / 4, PER = 16 * QUADS / 64;  // 4 neighbours each, of a row, of a lane
+    const int lane = threadIdx.x & 63;
+    const int r0 = t.i * P::BM + P::row(0) - (lane & 15), c0 = t.j * P::BN + P::col(0) - 4 * (lane >> 4);
+    const f16* const from = STAGE == POLY ? m.a : x;
+    const bool second = STAGE != POLY || both;
+    const bool mirror = STAGE <= POLY && t.i != t.j;
+    f16x4 high[PER], low[PER];
+    auto fetch = [&](int i) {
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            const int r = r0 + 16 * i + (lane + 64 * k) / QUADS, c = c0 + (lane + 64 * k) % QUADS * 4;
+            const f16* q = from + (int64_t)r * ld + c;
+            const bool in = r < m.s && c < ld;
+            high[k] = in ? *reinterpret_cast<const f16x4*>(q) : f16x4{};
+            low[k] = in && second ? *reinterpret_cast<const f16x4*>(q + lo) : f16x4{};
+        }
+    };
+    if constexpr (STAGE != GRAM) fetch(0);
+    __syncthreads();  // the tiles in LDS are done with
 #pragma unroll
     for (int i = 0; i < P::FM; ++i) {
-        const int r = t.i * P::BM + P::row(i);
-        const bool in = r < m.s;
 #pragma unroll
-        for (int j = 0; j < P::FN; ++j) {
-            const int c = t.j * P::BN + P::col(j);
-            f32x4 v = a.f0 * p.acc[i][j];
-            if constexpr (STAGE != GRAM) {
-                f32x4 q{0.f, 0.f, 0.f, 0.f};
-                if (in && c < ld)
-                    q = STAGE == POLY ? load_four(m.a + (int64_t)r * ld + c, lo, both) : load_four(x + (int64_t)r * ld + c, lo, true);
+        for (int j = 0; j < P::FN; ++j) *reinterpret_cast<f32x4*>(part[lane & 15] + 16 * j + 4 * (lane >> 4)) = p.acc[i][j];
+        f32x4 q[PER];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float z = p.acc[i][j][e];
-                    v[e] = fmaf(z, a.f0, fmaf(q[e], a.f1, fmaf(z, a.f0_low, q[e] * a.f1_low)));
-                }
-            }
+        for (int k = 0; k < PER; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) q[k][e] = STAGE == GRAM ? 0.f : (float)high[k][e] + (float)low[k][e];
+        if (STAGE != GRAM && i + 1 < P::FM) fetch(i + 1);
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            const int y = (lane + 64 * k) / QUADS, z = (lane + 64 * k) % QUADS * 4, r = r0 + 16 * i + y, c = c0 + z;
+            f32x4 v = *reinterpret_cast<const f32x4*>(part[y] + z);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                v[e] = STAGE == GRAM ? a.f0 * v[e] : fmaf(v[e], a.f0, fmaf(q[k][e], a.f1, fmaf(v[e], a.f0_low, q[k][e] * a.f1_low)));
             if constexpr (STAGE == LAST) {
-                *reinterpret_cast<f32x4*>(part[threadIdx.x & 15] + 16 * j + 4 * ((threadIdx.x & 63) >> 4)) = a.unscale * v;
+                *reinterpret_cast<f32x4*>(part[y] + z) = a.unscale * v;
             } else {
-                if (in && c < ld) store(r, c, v);
-                if (STAGE <= POLY && t.i != t.j) {  // the mirror image
-                    turn(v, quad);
-                    if (c + quad < m.s && r - quad < ld) store(c + quad, r - quad, v);
-                }
+                if (r < m.s && c < ld) store(r, c, v);
+                if (mirror) *reinterpret_cast<f32x4*>(part[y] + z) = v;
             }
         }
         if constexpr (STAGE == LAST) {
-            // the wave's 16 rows of WN columns from LDS, in the order of the result
-            const int lane = threadIdx.x & 63, r0 = r - (lane & 15), c0 = t.j * P::BN + P::col(0) - 4 * (lane >> 4);
-            constexpr int QUADS = P::WN / 4;  // of a row
             __builtin_amdgcn_wave_barrier();
 #pragma unroll 1
             for (int k = lane; k < 16 * QUADS; k += 64) {
-                f32x4 u;
-                if (!m.turned) {
-                    const int y = k / QUADS, z = k % QUADS * 4;
-                    u = *reinterpret_cast<const f32x4*>(part[y] + z);
-                    if (r0 + y < m.s) store_out(a.to, m, r0 + y, c0 + z, u);
-                } else {
-                    const int y = k % 4 * 4, z = k / 4;
+                const int y = m.turned ? k % 4 * 4 : k / QUADS, z = m.turned ? k / 4 : k % QUADS * 4, r = r0 + 16 * i + y, c = c0 + z;
+                f32x4 v;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) u[e] = part[y + e][z];
-                    if (c0 + z < m.l) store_out(a.to, m, c0 + z, r0 + y, u);
-                }
+                for (int e = 0; e < 4; ++e) v[e] = m.turned ? part[y + e][z] : part[y][z + e];
+                if (m.turned ? c < m.l : r < m.s) store_out(a.to, m, m.turned ? c : r, m.turned ? r : c, v);
             }
+        } else if (mirror) {  // 4 neighbours down a column at a time
             __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int k = 0; k < PER; ++k) {
+                const int y = (lane + 64 * k) % 4 * 4, z = (lane + 64 * k) / 4, r = r0 + 16 * i + y, c = c0 + z;
+                f32x4 v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = part[y + e][z];
+                if (c < m.s && r < ld) store(c, r, v);
+            }
         }
-        __builtin_amdgcn_sched_barrier(0);  // row by row: the registers hold no more
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_sched_barrier(0);
     }
 }
 
