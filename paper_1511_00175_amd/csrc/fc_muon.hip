@@ -306,18 +306,22 @@ template <typename P, int STAGE> __global__ __launch_bounds__(P::THREADS, 2) voi
     const f16* const from = STAGE == POLY ? m.a : x;
     const bool second = STAGE != POLY || both;
     const bool mirror = STAGE <= POLY && t.i != t.j;
-    f16x4 high[PER], low[PER];
+    constexpr int AHEAD = P::FM < 4 ? P::FM : 4;  // strips whose reads are on their way
+    f16x4 high[AHEAD][PER], low[AHEAD][PER];
     auto fetch = [&](int i) {
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
             const int r = r0 + 16 * i + (lane + 64 * k) / QUADS, c = c0 + (lane + 64 * k) % QUADS * 4;
             const f16* q = from + (int64_t)r * ld + c;
             const bool in = r < m.s && c < ld;
-            high[k] = in ? *reinterpret_cast<const f16x4*>(q) : f16x4{};
-            low[k] = in && second ? *reinterpret_cast<const f16x4*>(q + lo) : f16x4{};
+            high[i % AHEAD][k] = in ? *reinterpret_cast<const f16x4*>(q) : f16x4{};
+            low[i % AHEAD][k] = in && second ? *reinterpret_cast<const f16x4*>(q + lo) : f16x4{};
         }
     };
-    if constexpr (STAGE != GRAM) fetch(0);
+    if constexpr (STAGE != GRAM) {
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) fetch(i);
+    }
     __syncthreads();  // the tiles in LDS are done with
 #pragma unroll
     for (int i = 0; i < P::FM; ++i) {
@@ -327,8 +331,8 @@ template <typename P, int STAGE> __global__ __launch_bounds__(P::THREADS, 2) voi
 #pragma unroll
         for (int k = 0; k < PER; ++k)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) q[k][e] = STAGE == GRAM ? 0.f : (float)high[k][e] + (float)low[k][e];
-        if (STAGE != GRAM && i + 1 < P::FM) fetch(i + 1);
+            for (int e = 0; e < 4; ++e) q[k][e] = STAGE == GRAM ? 0.f : (float)high[i % AHEAD][k][e] + (float)low[i % AHEAD][k][e];
+        if (STAGE != GRAM && i + AHEAD < P::FM) fetch(i + AHEAD);
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
