@@ -26,6 +26,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <type_traits>
 #include <vector>
 
 #include "fc_gemm.h"
@@ -131,8 +132,9 @@ template <typename T, bool STEP> __device__ __forceinline__ float direction(cons
     return g;
 }
 
-// Four elements from i on, a multiple of 4; the momentum is updated and stored.
-template <typename T, bool STEP> __device__ __forceinline__ void direction4(const Source& a, uint64_t i, float* x) {
+// Four elements from i on, a multiple of 4; UPDATE: the momentum is updated and
+// stored first.
+template <typename T, bool STEP, bool UPDATE> __device__ __forceinline__ void direction4(const Source& a, uint64_t i, float* x) {
     struct alignas(4 * sizeof(T)) G {
         T x[4];
     };
@@ -144,11 +146,11 @@ template <typename T, bool STEP> __device__ __forceinline__ void direction4(cons
         x[e] = (float)g.x[e];
         if constexpr (STEP) {
             x[e] *= a.c;
-            v[e] = a.mu * v[e] + x[e];
+            if (UPDATE) v[e] = a.mu * v[e] + x[e];
             x[e] = a.nesterov ? x[e] + a.mu * v[e] : v[e];
         }
     }
-    if constexpr (STEP) *reinterpret_cast<f32x4*>(a.v + i) = v;
+    if constexpr (STEP && UPDATE) *reinterpret_cast<f32x4*>(a.v + i) = v;
 }
 
 // Sums of squares of one piece of a matrix, in 64 bits: neither tiny nor huge
@@ -178,7 +180,7 @@ template <typename T, bool STEP> __global__ __launch_bounds__(256) void norm_ker
 #pragma unroll 4
     for (int64_t i = lo + 4 * threadIdx.x; i < whole; i += 1024) {
         float x[4];
-        direction4<T, STEP>(a.d, m.offset + i, x);
+        direction4<T, STEP, true>(a.d, m.offset + i, x);
 #pragma unroll
         for (int e = 0; e < 4; ++e) sum += (double)x[e] * x[e];
     }
@@ -205,6 +207,23 @@ struct ScaleArgs {
     Output to;
 };
 
+// Up to 4 neighbours of the direction, `left` of them in the matrix's row, as one
+// vector where rows start on one.
+template <typename T, bool STEP> __device__ __forceinline__ f32x4 direction_row(const Source& a, uint64_t i, int left, bool wide) {
+    f32x4 v{0.f, 0.f, 0.f, 0.f};
+    if (wide && left >= 4) {
+        float x[4];
+        direction4<T, STEP, false>(a, i, x);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = x[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < left) v[e] = direction<T, STEP>(a, i + e, false);
+    }
+    return v;
+}
+
 // X of one tile: the direction over its norm.  A matrix of one row or column has
 // the one singular value 1 and is finished here.
 template <typename T, bool STEP> __global__ __launch_bounds__(256) void scale_kernel(ScaleArgs a) {
@@ -212,35 +231,57 @@ template <typename T, bool STEP> __global__ __launch_bounds__(256) void scale_ke
     __shared__ double part[4];
     const Tile t = a.tiles[blockIdx.x];
     const Matrix& m = a.mats[t.mat];
+    const int r0 = 64 * (m.turned ? t.j : t.i), c0 = 64 * (m.turned ? t.i : t.j);
+    const int y = threadIdx.x / 16, z = threadIdx.x % 16 * 4;
+    const bool wide = m.cols % 4 == 0;
+    f32x4 d[4];  // rows y, y + 16, ... of the tile in the vector's order
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int r = r0 + y + 16 * q, left = r < m.rows ? m.cols - c0 - z : 0;
+        d[q] = direction_row<T, STEP>(a.d, m.offset + (uint64_t)r * m.cols + c0 + z, left, wide);
+    }
     double sum = 0;
 #pragma unroll
     for (int k = 0; k < PIECES / 256; ++k)
         if (k * 256 + threadIdx.x < m.pieces) sum += a.partial[m.piece0 + k * 256 + threadIdx.x];
     sum = block_sum(sum, part);
     const double f = sum == 0 ? 0 : (m.s == 1 ? a.alone : a.top) / sqrt(sum);
-    const int r0 = 64 * (m.turned ? t.j : t.i), c0 = 64 * (m.turned ? t.i : t.j);
-    const int c = threadIdx.x & 63;
-#pragma unroll 4
-    for (int q = 0; q < 16; ++q) {
-        const int r = (threadIdx.x >> 6) + 4 * q;
-        const bool in = r0 + r < m.rows && c0 + c < m.cols;
-        tile[r][c] = in ? (float)(direction<T, STEP>(a.d, m.offset + (uint64_t)(r0 + r) * m.cols + c0 + c, false) * f) : 0.f;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) d[q][e] = (float)(d[q][e] * f);
+    if (m.turned) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) tile[y + 16 * q][z + e] = d[q][e];
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) d[q][e] = tile[z + e][y + 16 * q];
     }
-    __syncthreads();
-#pragma unroll 4
-    for (int q = 0; q < 16; ++q) {
-        const int r = (threadIdx.x >> 6) + 4 * q;
-        if (64 * t.i + r >= m.s) break;
-        const float x = m.turned ? tile[c][r] : tile[r][c];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int r = 64 * t.i + y + 16 * q, c = 64 * t.j + z;
+        if (r >= m.s) break;
         if (m.s == 1) {
-            if (64 * t.j + c < m.l) store_one(a.to, m, m.offset + 64 * t.j + c, x);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (c + e < m.l) store_one(a.to, m, m.offset + c + e, d[q][e]);
             continue;
         }
-        f16 hi, lo;
-        split(x, hi, lo);
-        f16* p = m.x[0] + (int64_t)(64 * t.i + r) * m.lp + 64 * t.j + c;
-        p[0] = hi;
-        p[m.x_lo] = lo;
+        f16x4 hi, lo;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            f16 h, l;
+            split(d[q][e], h, l);
+            hi[e] = h;
+            lo[e] = l;
+        }
+        f16* p = m.x[0] + (int64_t)r * m.lp + c;
+        *reinterpret_cast<f16x4*>(p) = hi;
+        *reinterpret_cast<f16x4*>(p + m.x_lo) = lo;
     }
 }
 
@@ -374,6 +415,335 @@ template <typename P, int STAGE> __global__ __launch_bounds__(P::THREADS, 2) voi
     }
 }
 
+// ---- small matrices in one block ---------------------------------------------
+
+// All steps of a matrix of at most 128 rows in one block, where it fits: X in
+// registers in fp32 (in the layout of the products' results), its high halves (and
+// low ones, with 3 parts), A and B in LDS.  Products this small are bound by
+// latency: as launches of their own they took 5 us each (96 x 363: 93 us in 17
+// launches).  In one block LDS reads would bound them, so that fragments are
+// shared: X X^T and A A are computed by a wave per tile row (and per part of k
+// where rows are few), B X by a wave per 16 columns, for all rows.
+struct WholeArgs {
+    const Matrix* mats;
+    const int* which;                    // the launch's matrices
+    int dt;                              // of the gradient
+    bool step;                           // a momentum step
+    double top, alone;                   // as ScaleArgs
+    Source d;
+    Output to;
+    int steps;
+    float fa;                            // A = fa acc
+    float fb, fb_low, fb1, fb1_low;      // B = fb acc + fb1 A
+    float fx, fx1, fx1_low;              // X = fx acc + fx1 X
+    float unscale;
+};
+
+constexpr int WHOLE_WAVES = 8, WHOLE_TILES = 20, WHOLE_ROWS = 8;  // waves; tiles of X of 16 x 16 per wave; tile rows
+
+template <int ST> struct Whole {
+    static constexpr int ROWS = ST;
+    static constexpr int NJ = WHOLE_TILES / ST;                  // tile columns of a wave
+    static constexpr int S32 = (ST + 1) / 2 * 32, PA = S32 + 8;  // k of A and B, and their row pitch in LDS
+    static constexpr int KS = ST <= 2 ? 4 : ST <= 4 ? 2 : 1;     // waves that share a tile row of A
+    static constexpr int TILES = ST * ST;
+    static __host__ __device__ int pitch(int l) { return (l + 63) / 64 * 64 + 8; }
+    static __host__ __device__ int halves(int l) { return S32 * pitch(l) + 2 * S32 * PA; }
+    static int bytes(int l, int parts) {
+        const int lt = (l + 63) / 64 * 4, flat = 256 + 16 * ST * (16 * lt + 4) * 4;
+        const int b = std::max(flat, 256 + halves(l) * 2 * (parts == 3 ? 2 : 1) + (KS - 1) * TILES * 1024);
+        return lt <= NJ * WHOLE_WAVES && b <= 160 * 1024 ? b : 0;
+    }
+};
+
+typedef FC_LDS const fc::f16x8* RowAt;
+typedef FC_LDS fc::s16x4* TurnAt;
+
+template <int ST> __global__ __launch_bounds__(64 * WHOLE_WAVES) void whole_kernel(WholeArgs a) {
+    typedef Whole<ST> W;
+    typedef fc::Half<f16> H;
+    constexpr int NJ = W::NJ, S32 = W::S32, PA = W::PA, KS = W::KS;
+    const Matrix& m = a.mats[a.which[blockIdx.x]];
+    const int parts = m.parts, l64 = (m.l + 63) / 64 * 64, px = W::pitch(m.l), lt = l64 / 16;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int row = lane & 15, four = 4 * (lane >> 4);
+    double* const part = reinterpret_cast<double*>(lds);
+    f16* const xs = reinterpret_cast<f16*>(lds + 256);
+    f16* const as = xs + S32 * px;
+    f16* const bs = as + S32 * PA;
+    const int low = W::halves(m.l);      // from a high half to its low one
+    f32x4* const sums = reinterpret_cast<f32x4*>(xs + low * (parts == 3 ? 2 : 1));  // [part of k][tile][lane]
+    // The direction, read in the order of memory, goes through LDS in fp32 to the
+    // layout of results: tile (i, j) of a wave is X's tile row i, column
+    // wave + 8 j, a lane's 4 neighbours of a row.  (Short loops: code run once is
+    // read from memory, and unrolled it cost more time than the steps.)
+    float* const flat = reinterpret_cast<float*>(lds + 256);
+    const int pf = l64 + 4, count = m.rows * m.cols;
+    for (int i = threadIdx.x; i < 16 * ST * pf / 4; i += 64 * WHOLE_WAVES) reinterpret_cast<f32x4*>(flat)[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    __syncthreads();
+    double sum = 0;
+    constexpr int THREADS = 64 * WHOLE_WAVES, AHEAD = 16;  // elements of a thread whose reads are under way together
+    const int down = THREADS / m.cols, right = THREADS % m.cols;
+    // body(u, element's place in LDS) for a thread's elements k0 + THREADS u that are in the matrix
+    auto each = [&](int k0, int& r, int& c, auto&& body) {
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            if (k0 + THREADS * u < count) body(u, m.turned ? c * pf + r : r * pf + c);
+            r += down;
+            c += right;
+            if (c >= m.cols) {
+                c -= m.cols;
+                ++r;
+            }
+        }
+    };
+    auto read = [&](auto* type) {
+        typedef std::remove_pointer_t<decltype(type)> T;
+        const T* const g = static_cast<const T*>(a.d.g) + m.offset;
+        int r = threadIdx.x / m.cols, c = threadIdx.x % m.cols;
+        for (int k0 = threadIdx.x; k0 < count; k0 += THREADS * AHEAD) {
+            T q[AHEAD];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) q[u] = g[min(k0 + THREADS * u, count - 1)];
+            each(k0, r, c, [&](int u, int place) {
+                float d = (float)q[u];
+                if (a.step) {
+                    float* const p = a.d.v + m.offset + k0 + THREADS * u;
+                    d *= a.d.c;
+                    const float v = a.d.mu * *p + d;
+                    *p = v;
+                    d = a.d.nesterov ? d + a.d.mu * v : v;
+                }
+                flat[place] = d;
+                sum += (double)d * d;
+            });
+        }
+    };
+    if (a.dt == FC_F32) read(static_cast<float*>(nullptr));
+    else if (a.dt == FC_F16) read(static_cast<f16*>(nullptr));
+    else read(static_cast<bf16*>(nullptr));
+#pragma unroll
+    for (int k = 32; k > 0; k /= 2) sum += __shfl_xor(sum, k);
+    if (lane == 0) part[wave] = sum;
+    __syncthreads();
+    sum = 0;
+#pragma unroll
+    for (int k = 0; k < WHOLE_WAVES; ++k) sum += part[k];
+    const bool alone = m.s == 1;  // has the one singular value 1
+    const double f = sum == 0 ? 0 : (alone ? a.alone : a.top) / sqrt(sum);
+    const float unscale = alone ? 1.f : a.unscale;
+
+    auto four_of = [](const float* q, float k) { return f32x4{q[0] * k, q[1] * k, q[2] * k, q[3] * k}; };
+    auto put = [&](f16* p, const f32x4& v) {
+        f16x4 hi, lo;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            f16 h, l;
+            split(v[e], h, l);
+            hi[e] = h;
+            lo[e] = l;
+        }
+        *reinterpret_cast<f16x4*>(p) = hi;
+        if (parts == 3) *reinterpret_cast<f16x4*>(p + low) = lo;
+    };
+    float x[NJ][ST][4];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int i = 0; i < ST; ++i) {
+            // past X's last column: that one again, not kept
+            const f32x4 q = *reinterpret_cast<const f32x4*>(flat + (16 * i + row) * pf + 16 * min(wave + WHOLE_WAVES * j, lt - 1) + four);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[j][i][e] = (float)(q[e] * f);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    __syncthreads();
+    for (int i = threadIdx.x; i < low * (parts == 3 ? 2 : 1) / 4; i += 64 * WHOLE_WAVES) reinterpret_cast<f16x4*>(xs)[i] = f16x4{};
+    __syncthreads();
+    auto put_x = [&]() {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+#pragma unroll
+            for (int i = 0; i < ST; ++i) {
+                if (wave + WHOLE_WAVES * j < lt) put(xs + (16 * i + row) * px + 16 * (wave + WHOLE_WAVES * j) + four, four_of(x[j][i], 1.f));
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    };
+    put_x();
+    __syncthreads();
+
+    // Fragments: 16 rows by 32 of k, along k; and 16 columns by 32 of k, across it.
+    auto along = [](uint32_t at) { return *(RowAt)(uintptr_t)at; };
+    auto across = [](uint32_t at, uint32_t four_rows) {
+        union {
+            fc::s16x4 s[2];
+            fc::f16x8 v;
+        } u;
+        u.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((TurnAt)(uintptr_t)at);
+        u.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((TurnAt)(uintptr_t)(at + four_rows));
+        return u.v;
+    };
+    // products of `parts` parts: high by low, low by high, high by high
+    auto first = [&](int q) -> uint32_t { return parts == 3 && q == 1 ? 2 * low : 0; };
+    auto second = [&](int q) -> uint32_t { return parts == 3 && q == 0 ? 2 * low : 0; };
+    const uint32_t xa = fc::lds_address(xs), aa = fc::lds_address(as), ba = fc::lds_address(bs);
+    const int mine = wave % ST, share = wave / ST;  // the tile row of A, the part of k
+
+    // the tile row `mine` of P P^T, P's rows along k of k32 in all
+    auto square = [&](uint32_t base, int pitch, int k32, bool active, f32x4* acc) {
+#pragma unroll
+        for (int j = 0; j < ST; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (!active) return;
+        const uint32_t at = base + 2 * (row * pitch + 2 * four);
+        constexpr int UNROLL = ST <= 4 ? 2 : 1;
+        for (int q = 0; q < parts; ++q)
+#pragma unroll UNROLL
+            for (int k = share * 64; k < 2 * k32; k += 64 * KS) {
+                const fc::f16x8 fa = along(at + first(q) + 32 * mine * pitch + k);
+                fc::f16x8 fb[ST];
+#pragma unroll
+                for (int j = 0; j < ST; ++j)
+                    fb[j] = along(at + second(q) + 32 * j * pitch + k);
+#pragma unroll
+                for (int j = 0; j < ST; ++j)
+                    acc[j] = H::mma(fb[j], fa, acc[j]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        if constexpr (KS > 1) {
+            if (share > 0) {
+#pragma unroll
+                for (int j = 0; j < ST; ++j)
+                    sums[((share - 1) * W::TILES + mine * ST + j) * 64 + lane] = acc[j];
+            }
+        }
+    };
+    auto join = [&](f32x4* acc) {
+        if constexpr (KS > 1) {
+            __syncthreads();
+            if (share > 0) return;
+#pragma unroll
+            for (int k = 0; k < KS - 1; ++k)
+#pragma unroll
+                for (int j = 0; j < ST; ++j)
+                    acc[j] += sums[(k * W::TILES + mine * ST + j) * 64 + lane];
+        }
+    };
+
+    for (int step = 0; step < a.steps && !alone; ++step) {
+        f32x4 g[ST], b[ST];
+        asm volatile("" : "+v"(row), "+v"(four));  // addresses are made again in every step: kept, they would not fit
+        square(xa, px, l64, share < KS, g);
+        join(g);
+        if (share == 0) {
+#pragma unroll
+            for (int j = 0; j < ST; ++j) {
+                g[j] *= a.fa;
+                put(as + (16 * mine + row) * PA + 16 * j + four, g[j]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        __syncthreads();
+        square(aa, PA, S32, share < KS, b);
+        join(b);
+        if (share == 0) {
+#pragma unroll
+            for (int j = 0; j < ST; ++j) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    b[j][e] = fmaf(b[j][e], a.fb, fmaf(g[j][e], a.fb1, fmaf(b[j][e], a.fb_low, g[j][e] * a.fb1_low)));
+                put(bs + (16 * mine + row) * PA + 16 * j + four, b[j]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        __syncthreads();
+        f32x4 acc[NJ][ST];
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int i = 0; i < ST; ++i) acc[j][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int q = 0; q < parts; ++q)
+            for (int k = 0; k < S32; k += 32) {
+                fc::f16x8 fa[ST];
+#pragma unroll
+                for (int i = 0; i < ST; ++i) fa[i] = along(ba + first(q) + 2 * ((16 * i + row) * PA + k + 2 * four));
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) {
+                    const int c = wave + WHOLE_WAVES * j;
+                    if (c >= lt) break;
+                    const fc::f16x8 fb = across(xa + second(q) + 2 * ((k + 2 * four + (row >> 2)) * px + 16 * c + 4 * (row & 3)), 8 * px);
+#pragma unroll
+                    for (int i = 0; i < ST; ++i) acc[j][i] = H::mma(fb, fa[i], acc[j][i]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int i = 0; i < ST; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    x[j][i][e] = fmaf(acc[j][i][e], a.fx, fmaf(x[j][i][e], a.fx1, x[j][i][e] * a.fx1_low));
+        __builtin_amdgcn_sched_barrier(0);
+        if (step + 1 < a.steps) {
+            __syncthreads();
+            put_x();
+            __syncthreads();
+        }
+    }
+    __syncthreads();  // A, B and X in LDS are done with
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int i = 0; i < ST; ++i) {
+            const int c = 16 * (wave + WHOLE_WAVES * j) + four;
+            if (c < l64) *reinterpret_cast<f32x4*>(flat + (16 * i + row) * pf + c) = four_of(x[j][i], unscale);
+        }
+    __syncthreads();
+    auto write = [&](auto&& store) {
+        int r = threadIdx.x / m.cols, c = threadIdx.x % m.cols;
+        for (int k0 = threadIdx.x; k0 < count; k0 += THREADS * AHEAD)
+            each(k0, r, c, [&](int u, int place) { store(m.offset + k0 + THREADS * u, flat[place]); });
+    };
+    if (!a.to.out) {
+        const float k = a.to.lr * m.lr_mult, d = a.to.wd * m.decay_mult;
+        write([&](uint64_t at, float u) {
+            const float w = a.to.w[at];
+            a.to.w[at] = w - k * (m.scale * u + d * w);
+        });
+    } else if (a.to.dt == FC_F32) {
+        write([&](uint64_t at, float u) { static_cast<float*>(a.to.out)[at] = u; });
+    } else if (a.to.dt == FC_F16) {
+        write([&](uint64_t at, float u) { static_cast<f16*>(a.to.out)[at] = (f16)u; });
+    } else {
+        write([&](uint64_t at, float u) { static_cast<bf16*>(a.to.out)[at] = (bf16)u; });
+    }
+}
+
+// f(Whole<tile rows>) for a matrix's shorter side.
+template <typename F> auto with_rows(int tile_rows, F&& f) {
+    switch (tile_rows) {
+        case 1: return f(Whole<1>{});
+        case 2: return f(Whole<2>{});
+        case 3: return f(Whole<3>{});
+        case 4: return f(Whole<4>{});
+        case 5: return f(Whole<5>{});
+        case 6: return f(Whole<6>{});
+        case 7: return f(Whole<7>{});
+        default: return f(Whole<8>{});
+    }
+}
+
+// Bytes of LDS of a matrix in one block, or 0 where it is too large.
+int whole_lds(int s, int l, int parts) {
+    if (s > 16 * WHOLE_ROWS || l > 8192) return 0;
+    return with_rows((s + 15) / 16, [&](auto w) { return decltype(w)::bytes(l, parts); });
+}
+
+template <int ST> hipError_t prepare_whole() {
+    return hipFuncSetAttribute((const void*)whole_kernel<ST>, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+}
+
 // By fc::TileKind.  LARGE has no registers left for sums in runs, so symmetric
 // products of fp32's accuracy do without it.  BROAD's 192 is no power of two,
 // which slow operands need: it serves the symmetric products alone.
@@ -391,7 +761,9 @@ hipError_t prepare() {
                          prepare_one<Large<true>, LAST>(), prepare_one<Broad<false>, GRAM>(), prepare_one<Broad<false>, POLY>(),
                          prepare_one<Middle<false>, GRAM>(), prepare_one<Middle<false>, POLY>(), prepare_one<Middle<true>, NEXT>(),
                          prepare_one<Middle<true>, LAST>(), prepare_one<Small<false>, GRAM>(), prepare_one<Small<false>, POLY>(),
-                         prepare_one<Small<true>, NEXT>(), prepare_one<Small<true>, LAST>()})
+                         prepare_one<Small<true>, NEXT>(), prepare_one<Small<true>, LAST>(), prepare_whole<1>(),
+                         prepare_whole<2>(), prepare_whole<3>(), prepare_whole<4>(), prepare_whole<5>(), prepare_whole<6>(),
+                         prepare_whole<7>(), prepare_whole<8>()})
         if (e != hipSuccess) return e;
     return hipSuccess;
 }
@@ -446,6 +818,11 @@ struct fc_muon {
         const Tile* tiles;
     };
     std::vector<Launch> launches[3];  // of the products GRAM, POLY, NEXT
+    struct WholeLaunch {
+        int tile_rows, count, lds;
+        const int* which;
+    };
+    std::vector<WholeLaunch> whole;   // where every matrix is one block's
 };
 
 namespace {
@@ -487,13 +864,31 @@ int build(fc_muon* p) {
         shapes[POLY].push_back({alone ? 0 : m.s, m.s, m.parts * m.sp / 64});
         shapes[NEXT].push_back({alone ? 0 : m.s, m.l, m.parts * m.sp / 64});
     }
+    // Every matrix in a block of its own, where all of them fit: beside the larger
+    // ones of a mixed list they would only add a launch.
+    std::vector<int> lists[WHOLE_ROWS];
+    int bytes[WHOLE_ROWS] = {};
+    bool whole = n > 0;
+    for (int i = 0; i < n && whole; ++i) {
+        const int need = whole_lds(mats[i].s, mats[i].l, mats[i].parts), t = std::min((mats[i].s + 15) / 16, WHOLE_ROWS) - 1;
+        whole = need > 0;
+        lists[t].push_back(i);
+        bytes[t] = std::max(bytes[t], need);
+    }
+    std::vector<int> which;
+    if (whole) {
+        pieces.clear();
+        scale.clear();
+        for (auto& v : shapes) v.clear();
+        for (const auto& v : lists) which.insert(which.end(), v.begin(), v.end());
+    }
     const bool fine = p->dtype != FC_BF16;
     std::vector<int> symmetric{fc::TILE_LARGE, fc::TILE_BROAD, fc::TILE_MIDDLE, fc::TILE_SMALL};
     if (fine) symmetric.erase(symmetric.begin());
     std::vector<fc::TileLaunch> plans[3] = {fc::plan_tiles(shapes[GRAM], true, symmetric), fc::plan_tiles(shapes[POLY], true, symmetric),
                                             fc::plan_tiles(shapes[NEXT], false, {fc::TILE_LARGE, fc::TILE_MIDDLE, fc::TILE_SMALL})};
     const uint64_t o_pieces = at.take(pieces.size() * sizeof(int2)), o_partial = at.take(pieces.size() * sizeof(double)),
-                   o_scale = at.take(scale.size() * sizeof(Tile));
+                   o_scale = at.take(scale.size() * sizeof(Tile)), o_which = at.take(which.size() * sizeof(int));
     std::vector<uint64_t> o_tiles;
     for (const auto& v : plans)
         for (const fc::TileLaunch& l : v) o_tiles.push_back(at.take(l.tiles.size() * sizeof(Tile)));
@@ -503,13 +898,14 @@ int build(fc_muon* p) {
         Matrix& m = mats[i];
         m.x_lo = (int64_t)m.s * m.lp;
         m.a_lo = (int64_t)m.s * m.sp;
+        if (whole) continue;
         for (int k = 0; k < 2; ++k) places[4 * i + k] = at.take(2 * m.x_lo * sizeof(f16));
         for (int k = 2; k < 4; ++k) places[4 * i + k] = at.take((m.parts == 3 ? 2 : 1) * m.a_lo * sizeof(f16));
     }
     int rc = p->block.create(at.size);
     if (rc) return rc;
     char* b = p->block.p;
-    for (int i = 0; i < n; ++i) {
+    for (int i = 0; i < n && !whole; ++i) {
         mats[i].x[0] = reinterpret_cast<f16*>(b + places[4 * i]);
         mats[i].x[1] = reinterpret_cast<f16*>(b + places[4 * i + 1]);
         mats[i].a = reinterpret_cast<f16*>(b + places[4 * i + 2]);
@@ -522,6 +918,13 @@ int build(fc_muon* p) {
     put(o_mats, mats.data(), n * sizeof(Matrix));
     put(o_pieces, pieces.data(), pieces.size() * sizeof(int2));
     put(o_scale, scale.data(), scale.size() * sizeof(Tile));
+    put(o_which, which.data(), which.size() * sizeof(int));
+    const int* list = reinterpret_cast<const int*>(b + o_which);
+    for (int t = 0; t < WHOLE_ROWS && whole; ++t) {
+        const int count = (int)lists[t].size();
+        if (count) p->whole.push_back({t + 1, count, bytes[t], list});
+        list += count;
+    }
     size_t next = 0;
     for (int q = 0; q < 3; ++q)
         for (const fc::TileLaunch& l : plans[q]) {
@@ -539,38 +942,62 @@ int build(fc_muon* p) {
     return FC_OK;
 }
 
-template <typename T, bool STEP> void start(fc_muon* p, const Source& d, const Output& to, hipStream_t s) {
-    NormArgs n{p->mats, p->pieces, p->partial, d};
-    norm_kernel<T, STEP><<<p->n_pieces, 256, 0, s>>>(n);
-    ScaleArgs a{p->mats, p->scale_tiles, p->partial, p->sx, p->alone, d, to};
-    scale_kernel<T, STEP><<<p->n_scale, 256, 0, s>>>(a);
+// A coefficient as the sum of two floats.
+void halve(double f, float& high, float& low) {
+    high = (float)f;
+    low = (float)(f - high);
 }
 
-// The products; the last one writes the output.
-int products(fc_muon* p, const Output& to, hipStream_t s) {
+template <typename T, bool STEP> int run(fc_muon* p, const Source& d, int dt, const Output& to, hipStream_t s) {
+    const double fa = p->sa / (p->sx * p->sx), fb = p->c * p->sb / (p->sa * p->sa), fb1 = p->b * p->sb / p->sa;
+    if (!p->whole.empty()) {
+        WholeArgs a{};
+        a.mats = p->mats;
+        a.dt = dt;
+        a.step = STEP;
+        a.top = p->sx;
+        a.alone = p->alone;
+        a.d = d;
+        a.to = to;
+        a.steps = p->steps;
+        a.fa = (float)fa;
+        halve(fb, a.fb, a.fb_low);
+        halve(fb1, a.fb1, a.fb1_low);
+        a.fx = (float)(1 / p->sb);
+        halve(p->a, a.fx1, a.fx1_low);
+        a.unscale = (float)(1 / p->sx);
+        for (const auto& w : p->whole) {
+            a.which = w.which;
+            with_rows(w.tile_rows, [&](auto k) {
+                whole_kernel<decltype(k)::ROWS><<<w.count, 64 * WHOLE_WAVES, w.lds, s>>>(a);
+                return 0;
+            });
+        }
+        return fc::hip_code(hipGetLastError());
+    }
+    NormArgs norm{p->mats, p->pieces, p->partial, d};
+    norm_kernel<T, STEP><<<p->n_pieces, 256, 0, s>>>(norm);
+    ScaleArgs scale{p->mats, p->scale_tiles, p->partial, p->sx, p->alone, d, to};
+    scale_kernel<T, STEP><<<p->n_scale, 256, 0, s>>>(scale);
     int from = 0;
-    auto set = [](ProductArgs& a, double f0, double f1) {
-        a.f0 = (float)f0;
-        a.f1 = (float)f1;
-        a.f0_low = (float)(f0 - a.f0);
-        a.f1_low = (float)(f1 - a.f1);
-    };
     for (int k = 0; k < p->steps; ++k) {
         ProductArgs a{};
         a.to = to;
         a.mats = p->mats;
         a.from = from;
-        set(a, p->sa / (p->sx * p->sx), 0);
+        a.f0 = (float)fa;
         for (const auto& l : p->launches[GRAM]) {
             a.tiles = l.tiles;
             launch_kind<GRAM>(l.kind, a, l.count, s);
         }
-        set(a, p->c * p->sb / (p->sa * p->sa), p->b * p->sb / p->sa);
+        halve(fb, a.f0, a.f0_low);
+        halve(fb1, a.f1, a.f1_low);
         for (const auto& l : p->launches[POLY]) {
             a.tiles = l.tiles;
             launch_kind<POLY>(l.kind, a, l.count, s);
         }
-        set(a, 1 / p->sb, p->a);
+        halve(1 / p->sb, a.f0, a.f0_low);
+        halve(p->a, a.f1, a.f1_low);
         a.unscale = (float)(1 / p->sx);
         for (const auto& l : p->launches[NEXT]) {
             a.tiles = l.tiles;
@@ -593,10 +1020,9 @@ int orthogonalize_body(fc_muon* p, const void* g, int gdt, void* out, hipStream_
     if (rc) return rc;
     const Source d{g, nullptr, 1.f, 0.f, 0};
     const Output to{out, p->dtype, nullptr, 0.f, 0.f};
-    if (gdt == FC_F32) start<float, false>(p, d, to, s);
-    else if (gdt == FC_F16) start<f16, false>(p, d, to, s);
-    else start<bf16, false>(p, d, to, s);
-    rc = products(p, to, s);
+    if (gdt == FC_F32) rc = run<float, false>(p, d, gdt, to, s);
+    else if (gdt == FC_F16) rc = run<f16, false>(p, d, gdt, to, s);
+    else rc = run<bf16, false>(p, d, gdt, to, s);
     p->order.done(s, note);
     return rc;
 }
@@ -613,8 +1039,7 @@ int step_body(fc_muon* p, float* w, float* v, const float* g, float lr, float mu
     if (rc) return rc;
     const Source d{g, v, 1.0f / (float)batch, mu, p->nesterov};
     const Output to{nullptr, FC_F32, w, lr, wd};
-    start<float, true>(p, d, to, s);
-    rc = products(p, to, s);
+    rc = run<float, true>(p, d, FC_F32, to, s);
     p->order.done(s, note);
     return rc;
 }
