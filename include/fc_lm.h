@@ -82,7 +82,7 @@ typedef struct fc_xent fc_xent;
  * `max_tokens` tokens a call; x and w are of `dtype`, FC_F16 or FC_BF16.
  * 1 <= rows, dim <= 2^21, 0 <= max_tokens < 2^31.  The workspace holds, for
  * `chunk_tokens` tokens at a time (0: as many as fit in 4 GiB, at least 256),
- * 16 bits per token and row, and for plans of more tokens than that 4 bytes per
+ * 16 bits per token and row (64 for the first 64), and for plans of more tokens than that 4 bytes per
  * element of dw. */
 int fc_xent_create(fc_xent** plan, int64_t rows, int64_t dim, int64_t max_tokens, int dtype, int64_t chunk_tokens);
 void fc_xent_destroy(fc_xent* plan);
@@ -99,8 +99,9 @@ int fc_xent_loss(fc_xent* plan, const void* x, int64_t ld_x, const void* w, int6
  *   dx[t, :] = scale * sum over r of d[t, r] w[r, :]
  *   dw[r, :] = scale * sum over t of d[t, r] x[t, :]
  *   d[t, r] = exp(l[t, r] - lse[t]) - (r == targets[t])
- * d is rounded to x's type for the products (its numerator once before), their
- * sums are fp32 and rounded once to the output's type.  Either output may be
+ * d is rounded to x's type for the products (its numerator once before; up to 64
+ * tokens d is kept to twice that type's bits), their sums are fp32 and rounded once
+ * to the output's type.  Either output may be
  * null.  Without tokens dw is zeros. */
 int fc_xent_loss_grad(fc_xent* plan, const void* x, int64_t ld_x, const void* w, int64_t ld_w, const void* targets,
                       int token_bytes, int64_t n, float scale, float* loss, void* dx, int dx_dtype, int64_t ld_dx,

@@ -216,9 +216,9 @@ template <typename T_, int BM_, int BN_, int WM_, int WN_, bool AS, bool BS, int
 
     f32x4 acc[FM][FN];
 
-    // Parts: 1, or 3 for operands kept as sums of two 16-bit numbers: high by low,
-    // low by high, then high by high (the small terms first, while the sums are
-    // small; low by low is below the result's last bit).
+    // Parts: 1; 2 where A is kept as a sum of two 16-bit numbers: low by B, then high
+    // by B; 3 where both are: high by low, low by high, then high by high (the small
+    // terms first, while the sums are small; low by low is below the result's last bit).
     // k runs over [kb, ke), kb below both operands' extents, and ke - kb a multiple
     // of 64 unless one of them ends there.
     __device__ __forceinline__ void run(char* lds, const Operand& A, const Operand& B, int m0, int n0, int kb, int ke, int parts) {
@@ -252,7 +252,7 @@ template <typename T_, int BM_, int BN_, int WM_, int WN_, bool AS, bool BS, int
         typename TileLoads<BN, BS, WAVES>::Tile ib;
         auto prepare = [&]() {
             const bool live = issued < total;
-            ia = ta.tile(la + into, k, parts == 3 && part == 1, live, wave);
+            ia = ta.tile(la + into, k, part == parts - 2, live, wave);
             ib = tb.tile(lb + into, k, parts == 3 && part == 0, live, wave);
             into = into == (STAGES - 1) * STAGE ? 0 : into + STAGE;
             k += GEMM_BK;

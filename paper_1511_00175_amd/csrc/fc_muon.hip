@@ -19,10 +19,10 @@
 // (a rounding there would be noise of full rank, grown by 3.4 a step), is formed
 // from both halves.  With 3 parts every operand is such a sum and a product is
 // high * high + high * low + low * high: fp32's accuracy for 3 times the work;
-// the sums are then taken in runs of 512 of k.  A matrix of at most 64 rows or
-// columns always has 3 parts: roundings average out over few terms only (its
-// error against a bf16 result's own was 1.0 with one part, at 16 x 20, and 0.4 at
-// 512 x 512), and its launches are too short for the work to matter.
+// the sums are then taken in runs of 512 of k.  A matrix of at most 32 rows or
+// columns always has 3 parts: roundings average out over few terms only (with one
+// part the products' error was 1.0 times a bf16 result's own at 16 x 20, 0.7 at
+// 64 x 64, 0.4 at 512 x 512), and its launches are too short for the work to matter.
 #include <algorithm>
 #include <cmath>
 #include <cstring>
@@ -534,17 +534,22 @@ template <int ST> __global__ __launch_bounds__(64 * WHOLE_WAVES) void whole_kern
     const float unscale = alone ? 1.f : a.unscale;
 
     auto four_of = [](const float* q, float k) { return f32x4{q[0] * k, q[1] * k, q[2] * k, q[3] * k}; };
+    // Returns the values as stored: b A + c A A is formed from one A, of which the
+    // rounding then cancels where the terms do.
     auto put = [&](f16* p, const f32x4& v) {
         f16x4 hi, lo;
+        f32x4 kept;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             f16 h, l;
             split(v[e], h, l);
             hi[e] = h;
             lo[e] = l;
+            kept[e] = parts == 3 ? (float)h + (float)l : (float)h;
         }
         *reinterpret_cast<f16x4*>(p) = hi;
         if (parts == 3) *reinterpret_cast<f16x4*>(p + low) = lo;
+        return kept;
     };
     float x[NJ][ST][4];
 #pragma unroll
@@ -638,8 +643,7 @@ template <int ST> __global__ __launch_bounds__(64 * WHOLE_WAVES) void whole_kern
         if (share == 0) {
 #pragma unroll
             for (int j = 0; j < ST; ++j) {
-                g[j] *= a.fa;
-                put(as + (16 * mine + row) * PA + 16 * j + four, g[j]);
+                g[j] = put(as + (16 * mine + row) * PA + 16 * j + four, a.fa * g[j]);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
@@ -848,7 +852,7 @@ int build(fc_muon* p) {
         m.l = std::max(m.rows, m.cols);
         m.sp = (m.s + 63) / 64 * 64;
         m.lp = (m.l + 63) / 64 * 64;
-        m.parts = p->dtype == FC_BF16 && m.s > 64 ? 1 : 3;
+        m.parts = p->dtype == FC_BF16 && m.s > 32 ? 1 : 3;
         m.lr_mult = h.lr_mult;
         m.decay_mult = h.decay_mult;
         m.scale = (float)std::sqrt(std::max(1.0, (double)h.rows / h.cols));

@@ -46,6 +46,12 @@ __device__ __forceinline__ int64_t target_of(const void* p, int bytes, int64_t t
     return bytes == 8 ? static_cast<const int64_t*>(p)[t] : static_cast<const int32_t*>(p)[t];
 }
 
+// Up to so many tokens d is kept as a sum of two 16-bit numbers, of numerators in
+// fp32: the rounding of d at the target, up to 2^-9 in bf16, averages out over
+// many tokens, not over a few (5 tokens: the error of dw was 1.5 times its output's
+// own rounding), and so short a product is bound by reading w.
+constexpr int FINE = 64;
+
 // ---- the first product ----------------------------------------------------
 
 struct LogitArgs {
@@ -57,6 +63,7 @@ struct LogitArgs {
     float* target_logit;
     void* numer;             // [token][ld], or null
     int64_t ld;
+    bool fine;               // numerators in fp32
     int tm, tn;
 };
 
@@ -116,19 +123,24 @@ template <typename P> __global__ __launch_bounds__(P::THREADS, P::THREADS / 256)
 #pragma unroll
     for (int i = 0; i < P::FM; ++i) {
         const int m = ti * P::BM + P::row(i);
-        T* const to = a.numer && m < a.n ? static_cast<T*>(a.numer) + (int64_t)m * a.ld + n0 : nullptr;
+        const bool keep = a.numer && m < a.n;
+        const int64_t to = (int64_t)m * a.ld + n0;
         const float ref = tops[i] == -__builtin_inff() ? 0.f : tops[i];
         float sum = 0.f;
 #pragma unroll
         for (int j = 0; j < P::FN; ++j) {
-            typename Half<T>::v4 v;
+            f32x4 q;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float q = exp_(p.acc[i][j][e] - ref);
-                sum += q;
-                v[e] = (T)q;
+                q[e] = exp_(p.acc[i][j][e] - ref);
+                sum += q[e];
             }
-            if (to && n0 + 16 * j < a.ld) *reinterpret_cast<typename Half<T>::v4*>(to + 16 * j) = v;
+            if (keep && n0 + 16 * j < a.ld) {
+                if (P::BM <= FINE && a.fine)
+                    *reinterpret_cast<f32x4*>(static_cast<float*>(a.numer) + to + 16 * j) = q;
+                else
+                    *reinterpret_cast<typename Half<T>::v4*>(static_cast<T*>(a.numer) + to + 16 * j) = __builtin_convertvector(q, typename Half<T>::v4);
+            }
         }
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
@@ -199,7 +211,9 @@ template <int T> __global__ __launch_bounds__(256) void join_kernel(JoinArgs a) 
 // ---- numerators to d --------------------------------------------------------
 
 struct DiffArgs {
-    void* numer;
+    const void* numer;       // T, or fp32 where d has two halves
+    void* d;                 // may be numer
+    int64_t low;             // from a high half to its low one
     int64_t ld;
     int n;
     int width;               // of a piece
@@ -213,33 +227,38 @@ constexpr int DIFF_ROWS = 8;
 
 // A block's 256 threads hold 8 columns each, of DIFF_ROWS tokens one after the
 // other, whose stats are neighbours in memory.
-template <typename T> __global__ __launch_bounds__(256) void diff_kernel(DiffArgs a) {
+template <typename T, typename N> __global__ __launch_bounds__(256) void diff_kernel(DiffArgs a) {
     typedef typename Half<T>::v8 v8;
+    typedef N n8 __attribute__((ext_vector_type(8)));
     const int64_t col = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
     if (col >= a.ld) return;
     const int piece = min((int)(col / a.width), a.pieces - 1);
     const int t0 = blockIdx.y * DIFF_ROWS;
-    v8 x[DIFF_ROWS];
+    n8 x[DIFF_ROWS];
     float f[DIFF_ROWS];
     int row[DIFF_ROWS];
 #pragma unroll
     for (int i = 0; i < DIFF_ROWS; ++i) {
         const int t = min(t0 + i, a.n - 1);
-        x[i] = *reinterpret_cast<const v8*>(static_cast<const T*>(a.numer) + t * a.ld + col);
+        x[i] = *reinterpret_cast<const n8*>(static_cast<const N*>(a.numer) + t * a.ld + col);
         row[i] = a.row[t];
         f[i] = exp_(a.stats[(int64_t)piece * a.n + t].x - a.lse[t]) * D_SCALE<T>;
     }
 #pragma unroll
     for (int i = 0; i < DIFF_ROWS; ++i) {
         if (t0 + i >= a.n) break;
-        v8 y;
+        v8 y, z;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             float v = (float)x[i][e] * f[i];
             if (col + e == row[i]) v -= D_SCALE<T>;
-            y[e] = (T)(row[i] >= 0 ? v : 0.f);
+            if (row[i] < 0) v = 0.f;
+            y[e] = (T)v;
+            z[e] = (T)(v - (float)y[e]);
         }
-        *reinterpret_cast<v8*>(static_cast<T*>(a.numer) + (t0 + i) * a.ld + col) = y;
+        T* const p = static_cast<T*>(a.d) + (t0 + i) * a.ld + col;
+        *reinterpret_cast<v8*>(p) = y;
+        if constexpr (sizeof(N) == 4) *reinterpret_cast<v8*>(p + a.low) = z;
     }
 }
 
@@ -278,6 +297,7 @@ struct GradArgs {
     Operand a, b;
     int m, n, k;             // of the product
     int kper;                // of one split, a multiple of 64
+    int parts;               // 2: a has two halves
     float scale;
     const int* row;          // per m: below 0, the result is zero; or null
     void* out;
@@ -294,7 +314,7 @@ template <typename P> __global__ __launch_bounds__(P::THREADS, P::THREADS / 256)
     fc::tile_place(fc::xcd_order(blockIdx.x, a.tm * a.tn), a.tm, a.tn, 8, ti, tj);
     const int kb = blockIdx.y * a.kper, ke = min(a.k, kb + a.kper);
     P p;
-    p.run(lds, a.a, a.b, ti * P::BM, tj * P::BN, kb, ke, 1);
+    p.run(lds, a.a, a.b, ti * P::BM, tj * P::BN, kb, ke, a.parts);
     float* const sum = a.sum ? a.sum + (int64_t)blockIdx.y * a.m * a.n : nullptr;
 #pragma unroll
     for (int i = 0; i < P::FM; ++i) {
@@ -456,6 +476,7 @@ struct fc_xent {
     int64_t ldp = 0;         // of packed x and w
     bool pack = false;       // dim is not a multiple of 8: x and w go through packed copies
     char* numer = nullptr;
+    char* fine = nullptr;    // numerators in fp32, of up to FINE tokens
     f32x2* stats = nullptr;
     float* target_logit = nullptr;
     float* lse = nullptr;
@@ -491,7 +512,8 @@ int run(fc_xent* p, const void* x, int64_t ldx, const void* w, int64_t ldw, cons
         const Operand ox{p->pack || dw ? p->x : xt, p->pack || dw ? p->ldp : ldx, m, dimk, 0};
         const Operand ow{w, ldw, (int)p->rows, dimk, 0};
         const TileKind kind = tile_for(m, p->rows);
-        LogitArgs l{ox, ow, m, (int)p->rows, dimk, yt, target_bytes, p->stats, p->target_logit, grads ? p->numer : nullptr, p->ld, 0, 0};
+        const bool fine = m <= FINE;
+        LogitArgs l{ox, ow, m, (int)p->rows, dimk, yt, target_bytes, p->stats, p->target_logit, grads ? fine ? p->fine : p->numer : nullptr, p->ld, fine, 0, 0};
         if (kind == LARGE) launch_logit<Large<T, false, false>>(l, s);
         else if (kind == MIDDLE) launch_logit<Middle<T, false, false>>(l, s);
         else launch_logit<Short<T, false, false>>(l, s);
@@ -500,12 +522,16 @@ int run(fc_xent* p, const void* x, int64_t ldx, const void* w, int64_t ldw, cons
         if (m >= 16 * CUS) join_kernel<16><<<(unsigned)fc::ceil_div(m, 16), 256, 0, s>>>(j);
         else join_kernel<1><<<(unsigned)m, 256, 0, s>>>(j);
         if (!grads) continue;
-        DiffArgs d{p->numer, p->ld, m, width, pieces, p->stats, p->lse, p->row};
-        diff_kernel<T><<<dim3((unsigned)fc::ceil_div(p->ld, 2048), (unsigned)fc::ceil_div(m, DIFF_ROWS)), 256, 0, s>>>(d);
+        const int64_t low = m * p->ld;
+        DiffArgs d{fine ? p->fine : p->numer, p->numer, low, p->ld, m, width, pieces, p->stats, p->lse, p->row};
+        const dim3 grid((unsigned)fc::ceil_div(p->ld, 2048), (unsigned)fc::ceil_div(m, DIFF_ROWS));
+        if (fine) diff_kernel<T, float><<<grid, 256, 0, s>>>(d);
+        else diff_kernel<T, T><<<grid, 256, 0, s>>>(d);
         const float back = scale / D_SCALE<T>;
         if (dx) {
             GradArgs g{};
-            g.a = Operand{p->numer, p->ld, m, (int)p->ld, 0};
+            g.a = Operand{p->numer, p->ld, m, (int)p->ld, low};
+            g.parts = fine ? 2 : 1;
             g.b = Operand{w, ldw, (int)p->dim, (int)p->rows, 0};
             g.m = m;
             g.n = (int)p->dim;
@@ -532,7 +558,8 @@ int run(fc_xent* p, const void* x, int64_t ldx, const void* w, int64_t ldw, cons
         }
         if (dw) {
             GradArgs g{};
-            g.a = Operand{p->numer, p->ld, (int)p->rows, m, 0};
+            g.a = Operand{p->numer, p->ld, (int)p->rows, m, low};
+            g.parts = fine ? 2 : 1;
             g.b = Operand{p->x, p->ldp, (int)p->dim, m, 0};
             g.m = (int)p->rows;
             g.n = (int)p->dim;
@@ -620,7 +647,8 @@ int fc_xent_create(fc_xent** plan, int64_t rows, int64_t dim, int64_t max_tokens
             if (sp > 1) sums = std::max(sums, sp * up * dim);
         }
         fc::Layout at;
-        const uint64_t o_numer = at.take(c * p->ld * 2), o_stats = at.take(stats * 8), o_logit = at.take(c * 4),
+        const int64_t few = std::min<int64_t>(c, FINE);
+        const uint64_t o_numer = at.take(std::max(c, 2 * few) * p->ld * 2), o_fine = at.take(few * p->ld * 4), o_stats = at.take(stats * 8), o_logit = at.take(c * 4),
                        o_lse = at.take(c * 4), o_row = at.take(c * 4), o_x = at.take(c * p->ldp * 2),
                        o_w = at.take(p->pack ? rows * p->ldp * 2 : 0), o_sum = at.take(sums * 4),
                        o_dw = at.take(max_tokens > c ? rows * dim * 4 : 0);
@@ -633,6 +661,7 @@ int fc_xent_create(fc_xent** plan, int64_t rows, int64_t dim, int64_t max_tokens
         }
         char* b = p->block.p;
         p->numer = b + o_numer;
+        p->fine = b + o_fine;
         p->stats = reinterpret_cast<f32x2*>(b + o_stats);
         p->target_logit = reinterpret_cast<float*>(b + o_logit);
         p->lse = reinterpret_cast<float*>(b + o_lse);
