@@ -288,7 +288,7 @@ template <typename T_, int BM_, int BN_, int WM_, int WN_, bool AS, bool BS, int
         for (int j = 0; j < FN; ++j) b[j] = fb.get(lb, j, 0);
 #pragma unroll
         for (int i = 0; i < FM; ++i) a[i] = fa.get(la, i, 0);
-        constexpr int FIRST = FM >= 4 ? 2 : 1;  // rows that cover the wait for the last reads
+        constexpr int FIRST = FM >= 4 ? 2 : FM >= 2 ? 1 : 0;  // rows that cover the wait for the last reads
         constexpr int REST = FM - FIRST;
         constexpr int EACH = (FN + REST - 1) / REST, LEACH = (LOADS + REST - 1) / REST;  // B fragments and loads per row
         auto row_of = [&](int i) {

@@ -270,27 +270,24 @@ __device__ __forceinline__ void store_one(void* p, int dt, int64_t at, float v) 
     else static_cast<bf16*>(p)[at] = (bf16)v;
 }
 
-// Up to 4 neighbouring elements; `wide`: the row starts allow whole vectors.
-__device__ __forceinline__ void store_four(void* p, int dt, int64_t at, f32x4 v, int left, bool wide) {
-    if (wide && left >= 4) {
-        if (dt == FC_F32) {
-            *reinterpret_cast<f32x4*>(static_cast<float*>(p) + at) = v;
-        } else if (dt == FC_F16) {
-            fc::f16x4 o;
+// Vectors wherever elements may start: global memory takes any alignment.
+typedef f32x4 f32x4_any __attribute__((aligned(4)));
+typedef fc::f16x4 f16x4_any __attribute__((aligned(2)));
+typedef fc::b16x4 b16x4_any __attribute__((aligned(2)));
+
+// Up to four neighbouring elements of a row, of which `left` are in it.
+__device__ __forceinline__ void store_four(void* p, int dt, int64_t at, f32x4 v, int left) {
+    if (left < 4) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = (f16)v[e];
-            *reinterpret_cast<fc::f16x4*>(static_cast<f16*>(p) + at) = o;
-        } else {
-            fc::b16x4 o;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = (bf16)v[e];
-            *reinterpret_cast<fc::b16x4*>(static_cast<bf16*>(p) + at) = o;
-        }
-        return;
+        for (int e = 0; e < 3; ++e)
+            if (e < left) store_one(p, dt, at + e, v[e]);
+    } else if (dt == FC_F32) {
+        *reinterpret_cast<f32x4_any*>(static_cast<float*>(p) + at) = v;
+    } else if (dt == FC_F16) {
+        *reinterpret_cast<f16x4_any*>(static_cast<f16*>(p) + at) = __builtin_convertvector(v, fc::f16x4);
+    } else {
+        *reinterpret_cast<b16x4_any*>(static_cast<bf16*>(p) + at) = __builtin_convertvector(v, fc::b16x4);
     }
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-        if (e < left) store_one(p, dt, at + e, v[e]);
 }
 
 struct GradArgs {
@@ -303,7 +300,6 @@ struct GradArgs {
     void* out;
     int dt;
     int64_t ld;
-    bool wide;
     float* sum;              // fp32 sums over calls or splits, [split][m][n], or null
     bool first, last;        // of the calls that add to `sum`
     int tm, tn;
@@ -316,34 +312,38 @@ template <typename P> __global__ __launch_bounds__(P::THREADS, P::THREADS / 256)
     P p;
     p.run(lds, a.a, a.b, ti * P::BM, tj * P::BN, kb, ke, a.parts);
     float* const sum = a.sum ? a.sum + (int64_t)blockIdx.y * a.m * a.n : nullptr;
+    // Results go through LDS by strips of 16 rows, so that a row's neighbours are
+    // stored by neighbouring lanes, whatever its start's alignment.
+    float(*const part)[P::WN + 4] = reinterpret_cast<float(*)[P::WN + 4]>(lds + (threadIdx.x >> 6) * 16 * (P::WN + 4) * sizeof(float));
+    static_assert(P::WAVES * 16 * (P::WN + 4) * sizeof(float) <= P::LDS, "the strips of all waves fit");
+    const int lane = threadIdx.x & 63, n0 = tj * P::BN + P::col(0) - 4 * (lane >> 4);
+    __syncthreads();  // the tiles in LDS are done with
 #pragma unroll
     for (int i = 0; i < P::FM; ++i) {
-        const int m = ti * P::BM + P::row(i);
-        if (m >= a.m) continue;
-        const bool zero = a.row && a.row[m] < 0;
+        const int m0 = ti * P::BM + P::row(i) - (lane & 15);
 #pragma unroll
-        for (int j = 0; j < P::FN; ++j) {
-            const int n = tj * P::BN + P::col(j), left = a.n - n;
-            if (left <= 0) continue;
-            f32x4 v = p.acc[i][j];
+        for (int j = 0; j < P::FN; ++j) *reinterpret_cast<f32x4*>(part[lane & 15] + 16 * j + 4 * (lane >> 4)) = p.acc[i][j];
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll 2
+        for (int k = lane; k < 16 * P::WN / 4; k += 64) {
+            const int y = k / (P::WN / 4), z = k % (P::WN / 4) * 4, m = m0 + y, left = a.n - n0 - z;
+            if (m >= a.m || left <= 0) continue;
+            f32x4 v = *reinterpret_cast<const f32x4*>(part[y] + z);
             if (sum) {
-                float* s = sum + (int64_t)m * a.n + n;
+                float* const s = sum + (int64_t)m * a.n + n0 + z;
                 if (!a.first) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (e < left) v[e] += s[e];
+                    for (int e = 0; e < 4; ++e) v[e] += s[min(e, left - 1)];
                 }
                 if (!a.last) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (e < left) s[e] = v[e];
+                    store_four(s, FC_F32, 0, v, left);
                     continue;
                 }
             }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = zero ? 0.f : v[e] * a.scale;
-            store_four(a.out, a.dt, (int64_t)m * a.ld + n, v, left, a.wide);
+            store_four(a.out, a.dt, (int64_t)m * a.ld + n0 + z, a.row && a.row[m] < 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : a.scale * v, left);
         }
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_sched_barrier(0);
     }
 }
 
@@ -363,6 +363,7 @@ __global__ __launch_bounds__(256) void split_kernel(SplitArgs a) {
     if (i >= total) return;
     const int m = (int)(i / a.n), n = (int)(i % a.n);
     float v = 0.f;
+#pragma unroll 8
     for (int s = 0; s < a.splits; ++s) v += a.sum[s * total + i];
     store_one(a.out, a.dt, (int64_t)m * a.ld + n, a.row && a.row[m] < 0 ? 0.f : v * a.scale);
 }
@@ -391,28 +392,73 @@ __global__ __launch_bounds__(256) void pack_kernel(PackArgs a) {
         const int64_t y = target_of(a.targets, a.target_bytes, r);
         keep = y >= 0 && y < a.targets_below;
     }
+    typedef u16 u16x8 __attribute__((ext_vector_type(8)));
+    typedef u16x8 u16x8_any __attribute__((aligned(2)));
     const u16* in = static_cast<const u16*>(a.in) + r * a.ld_in + c;
-    struct alignas(16) V {
-        u16 x[8];
-    } v;
+    u16x8 v{};
+    if (keep && c + 8 <= a.len) {
+        v = *reinterpret_cast<const u16x8_any*>(in);
+    } else if (keep) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v.x[e] = keep && c + e < a.len ? in[e] : (u16)0;
-    *reinterpret_cast<V*>(static_cast<u16*>(a.out) + r * a.ld_out + c) = v;
+        for (int e = 0; e < 8; ++e)
+            if (c + e < a.len) v[e] = in[e];
+    }
+    *reinterpret_cast<u16x8*>(static_cast<u16*>(a.out) + r * a.ld_out + c) = v;
 }
 
-// Tiles: large ones for products that fill the chip with them, smaller ones
-// for the others, and few rows for short token lists, which are bound by reading w.
+// Tiles by size; SHORT and NARROW are for up to 64 tokens, which are bound by
+// reading w: a compute unit reads at most about 50 GB/s, so that few rows of w are
+// read faster by more blocks.
 template <typename T, bool AS, bool BS> using Large = fc::Product<T, 256, 256, 128, 64, AS, BS>;
 template <typename T, bool AS, bool BS> using Middle = fc::Product<T, 128, 128, 64, 64, AS, BS>;
 template <typename T, bool AS, bool BS> using Short = fc::Product<T, 64, 128, 64, 32, AS, BS, 3>;
+template <typename T, bool AS, bool BS> using Narrow = fc::Product<T, 64, 32, 16, 32, AS, BS, 6>;
 
-enum TileKind { LARGE, MIDDLE, SHORT };
+enum TileKind { LARGE, MIDDLE, SHORT, NARROW, KINDS };
 
 constexpr int CUS = 256;
 
-TileKind tile_for(int64_t m, int64_t n) {
-    if (m <= 64) return SHORT;
-    return m > 128 && n > 128 && fc::ceil_div(m, 256) * fc::ceil_div(n, 256) >= CUS ? LARGE : MIDDLE;
+// In us, measured with 1 to 512 tiles: a step of 64 of k with the compute unit full
+// of such tiles (`per` at a time) and alone, and a tile's start and end.
+struct KindCost {
+    int bm, bn;
+    double full, alone, once;
+    int per;
+};
+constexpr KindCost COST[KINDS] = {{256, 256, 1.7, 1.15, 9.5, 1}, {128, 128, 0.52, 0.6, 5.0, 2}, {64, 128, 0.55, 0.6, 4.0, 2}, {64, 32, 0.2, 0.3, 4.0, 2}};
+
+struct Choice {
+    TileKind kind;
+    int splits;      // parts of k, of `steps` of 64 each
+    int steps;
+};
+
+constexpr int64_t SPLIT_FLOATS = (int64_t)1 << 27;
+
+// The tiles of an m x n product over k, and the parts k is split into, by the
+// least estimated time; m and k are taken up to multiples of 64, so that the
+// choice is one for every list of as many 64s of tokens.
+Choice choose(int64_t m, int64_t n, int64_t k, bool few, bool may_split) {
+    m = fc::ceil_div(m, 64) * 64;
+    const int64_t total = fc::ceil_div(k, fc::GEMM_BK);
+    Choice best{MIDDLE, 1, (int)total};
+    double least = 1e300;
+    for (int kind = few ? SHORT : LARGE; kind <= (few ? NARROW : MIDDLE); ++kind) {
+        const KindCost& c = COST[kind];
+        const int64_t tiles = fc::ceil_div(m, c.bm) * fc::ceil_div(n, c.bn);
+        for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+            const int64_t steps = fc::ceil_div(total, s), parts = fc::ceil_div(total, steps), blocks = tiles * parts;
+            if (s > 1 && (!may_split || steps < 2 || parts * m * n > SPLIT_FLOATS)) break;
+            const double at_once = (double)std::min<int64_t>(c.per, fc::ceil_div(blocks, CUS));
+            double t = fc::ceil_div(blocks, CUS * c.per) * (steps * std::max(c.alone, c.full * at_once) + c.once);
+            if (parts > 1) t += 5.0 + 8.0 * parts * m * n / 4.5e6;  // partial sums, written and read
+            if (t < least) {
+                least = t;
+                best = {(TileKind)kind, (int)parts, (int)steps};
+            }
+        }
+    }
+    return best;
 }
 
 template <typename P> hipError_t prepare(const void* kernel) {
@@ -432,34 +478,27 @@ template <typename P> void launch_grad(GradArgs a, hipStream_t s) {
 }
 
 template <typename T> hipError_t prepare_all() {
-    hipError_t e[9] = {
-        prepare<Large<T, false, false>>((const void*)logit_kernel<Large<T, false, false>>),
-        prepare<Middle<T, false, false>>((const void*)logit_kernel<Middle<T, false, false>>),
-        prepare<Short<T, false, false>>((const void*)logit_kernel<Short<T, false, false>>),
-        prepare<Large<T, false, true>>((const void*)grad_kernel<Large<T, false, true>>),
-        prepare<Middle<T, false, true>>((const void*)grad_kernel<Middle<T, false, true>>),
-        prepare<Short<T, false, true>>((const void*)grad_kernel<Short<T, false, true>>),
-        prepare<Large<T, true, true>>((const void*)grad_kernel<Large<T, true, true>>),
-        prepare<Middle<T, true, true>>((const void*)grad_kernel<Middle<T, true, true>>),
-        hipSuccess,
-    };
-    for (hipError_t x : e)
-        if (x != hipSuccess) return x;
+    for (hipError_t e : {prepare<Large<T, false, false>>((const void*)logit_kernel<Large<T, false, false>>),
+                         prepare<Middle<T, false, false>>((const void*)logit_kernel<Middle<T, false, false>>),
+                         prepare<Short<T, false, false>>((const void*)logit_kernel<Short<T, false, false>>),
+                         prepare<Narrow<T, false, false>>((const void*)logit_kernel<Narrow<T, false, false>>),
+                         prepare<Large<T, false, true>>((const void*)grad_kernel<Large<T, false, true>>),
+                         prepare<Middle<T, false, true>>((const void*)grad_kernel<Middle<T, false, true>>),
+                         prepare<Short<T, false, true>>((const void*)grad_kernel<Short<T, false, true>>),
+                         prepare<Narrow<T, false, true>>((const void*)grad_kernel<Narrow<T, false, true>>),
+                         prepare<Large<T, true, true>>((const void*)grad_kernel<Large<T, true, true>>),
+                         prepare<Middle<T, true, true>>((const void*)grad_kernel<Middle<T, true, true>>)})
+        if (e != hipSuccess) return e;
     return hipSuccess;
 }
 
 // Columns of the first product's tiles, a piece of the vocabulary.
-int piece_width(TileKind k) { return k == LARGE ? 256 : 128; }
+int piece_width(TileKind k) { return COST[k].bn; }
 
-// Splits of dx's product over the vocabulary: until the tiles fill the chip,
-// with at least 16 steps of k each.
-int splits_for(int64_t m, int64_t n, int64_t k) {
-    const TileKind t = tile_for(m, n);
-    const int64_t tiles = t == LARGE ? fc::ceil_div(m, 256) * fc::ceil_div(n, 256)
-                                     : fc::ceil_div(m, t == MIDDLE ? 128 : 64) * fc::ceil_div(n, 128);
-    if (tiles >= CUS) return 1;
-    return (int)std::max<int64_t>(1, std::min<int64_t>(2 * CUS / tiles, k / (16 * fc::GEMM_BK)));
-}
+// The choices of the three products for m tokens.
+Choice logit_choice(int64_t m, int64_t rows, int64_t dim) { return choose(m, rows, dim, m <= 64, false); }
+Choice dx_choice(int64_t m, int64_t rows, int64_t dim) { return choose(m, dim, rows, m <= 64, true); }
+Choice dw_choice(int64_t m, int64_t rows, int64_t dim, bool one_chunk) { return choose(rows, dim, m, false, one_chunk); }
 
 constexpr int64_t ROWS_LIMIT = 1 << 21, LD_LIMIT = 1 << 21, TOKENS_LIMIT = (int64_t)1 << 31;
 constexpr int64_t NUMER_BYTES = (int64_t)4 << 30;
@@ -493,6 +532,10 @@ template <typename T>
 int run(fc_xent* p, const void* x, int64_t ldx, const void* w, int64_t ldw, const void* targets, int target_bytes, int64_t n,
         float scale, float* loss, void* dx, int xdt, int64_t lddx, void* dw, int wdt, int64_t lddw, hipStream_t s) {
     const bool grads = dx || dw;
+    auto join_splits = [&](const GradArgs& g, int splits) {
+        SplitArgs q{g.sum, splits, g.m, g.n, g.scale, g.row, g.out, g.dt, g.ld};
+        split_kernel<<<(unsigned)fc::ceil_div((int64_t)g.m * g.n, 256), 256, 0, s>>>(q);
+    };
     auto pack = [&](const void* in, int64_t ld, void* out, int64_t rows, const void* mask) {
         PackArgs a{in, ld, out, p->ldp, rows, (int)p->dim, mask, target_bytes, (int)p->rows};
         pack_kernel<<<(unsigned)fc::ceil_div(rows * (p->ldp / 8), 256), 256, 0, s>>>(a);
@@ -511,12 +554,13 @@ int run(fc_xent* p, const void* x, int64_t ldx, const void* w, int64_t ldw, cons
         if (p->pack || dw) pack(xt, ldx, p->x, m, yt);
         const Operand ox{p->pack || dw ? p->x : xt, p->pack || dw ? p->ldp : ldx, m, dimk, 0};
         const Operand ow{w, ldw, (int)p->rows, dimk, 0};
-        const TileKind kind = tile_for(m, p->rows);
+        const TileKind kind = logit_choice(m, p->rows, dimk).kind;
         const bool fine = m <= FINE;
         LogitArgs l{ox, ow, m, (int)p->rows, dimk, yt, target_bytes, p->stats, p->target_logit, grads ? fine ? p->fine : p->numer : nullptr, p->ld, fine, 0, 0};
         if (kind == LARGE) launch_logit<Large<T, false, false>>(l, s);
         else if (kind == MIDDLE) launch_logit<Middle<T, false, false>>(l, s);
-        else launch_logit<Short<T, false, false>>(l, s);
+        else if (kind == SHORT) launch_logit<Short<T, false, false>>(l, s);
+        else launch_logit<Narrow<T, false, false>>(l, s);
         const int width = piece_width(kind), pieces = (int)fc::ceil_div(p->rows, width);
         JoinArgs j{p->stats, p->target_logit, yt, target_bytes, m, (int)p->rows, pieces, p->lse, p->row, loss + t0};
         if (m >= 16 * CUS) join_kernel<16><<<(unsigned)fc::ceil_div(m, 16), 256, 0, s>>>(j);
@@ -536,25 +580,21 @@ int run(fc_xent* p, const void* x, int64_t ldx, const void* w, int64_t ldw, cons
             g.m = m;
             g.n = (int)p->dim;
             g.k = (int)p->rows;
-            const int splits = splits_for(m, p->dim, p->rows);
-            g.kper = (int)fc::ceil_div(fc::ceil_div(g.k, splits), fc::GEMM_BK) * fc::GEMM_BK;
+            const Choice c = dx_choice(m, p->rows, p->dim);
+            g.kper = c.steps * fc::GEMM_BK;
             g.scale = back;
             g.row = p->row;
             g.dt = xdt;
             g.out = static_cast<char*>(dx) + t0 * lddx * fc::dtype_bytes(xdt);
             g.ld = lddx;
-            g.wide = fc::vector_width({{dx, n, 4, lddx, fc::dtype_bytes(xdt), true}}, 4) == 4;
-            g.sum = splits > 1 ? p->sum : nullptr;
+            g.sum = c.splits > 1 ? p->sum : nullptr;
             g.first = true;
-            g.last = splits == 1;
-            const TileKind k = tile_for(m, p->dim);
-            if (k == LARGE) launch_grad<Large<T, false, true>>(g, s);
-            else if (k == MIDDLE) launch_grad<Middle<T, false, true>>(g, s);
-            else launch_grad<Short<T, false, true>>(g, s);
-            if (splits > 1) {
-                SplitArgs q{p->sum, (int)fc::ceil_div(g.k, g.kper), m, g.n, back, p->row, g.out, xdt, lddx};
-                split_kernel<<<(unsigned)fc::ceil_div((int64_t)m * g.n, 256), 256, 0, s>>>(q);
-            }
+            g.last = c.splits == 1;
+            if (c.kind == LARGE) launch_grad<Large<T, false, true>>(g, s);
+            else if (c.kind == MIDDLE) launch_grad<Middle<T, false, true>>(g, s);
+            else if (c.kind == SHORT) launch_grad<Short<T, false, true>>(g, s);
+            else launch_grad<Narrow<T, false, true>>(g, s);
+            if (c.splits > 1) join_splits(g, c.splits);
         }
         if (dw) {
             GradArgs g{};
@@ -564,17 +604,18 @@ int run(fc_xent* p, const void* x, int64_t ldx, const void* w, int64_t ldw, cons
             g.m = (int)p->rows;
             g.n = (int)p->dim;
             g.k = m;
-            g.kper = (int)fc::ceil_div(m, fc::GEMM_BK) * fc::GEMM_BK;
+            const Choice c = dw_choice(m, p->rows, p->dim, n <= p->chunk);
+            g.kper = c.steps * fc::GEMM_BK;
             g.scale = back;
             g.out = dw;
             g.dt = wdt;
             g.ld = lddw;
-            g.wide = fc::vector_width({{dw, p->rows, 4, lddw, fc::dtype_bytes(wdt), true}}, 4) == 4;
-            g.sum = n > p->chunk ? p->dw : nullptr;
+            g.sum = n > p->chunk ? p->dw : c.splits > 1 ? p->sum : nullptr;
             g.first = t0 == 0;
-            g.last = t0 + p->chunk >= n;
-            if (tile_for(g.m, g.n) == LARGE) launch_grad<Large<T, true, true>>(g, s);
+            g.last = c.splits == 1 && t0 + p->chunk >= n;
+            if (c.kind == LARGE) launch_grad<Large<T, true, true>>(g, s);
             else launch_grad<Middle<T, true, true>>(g, s);
+            if (c.splits > 1) join_splits(g, c.splits);
         }
     }
     return fc::hip_code(hipGetLastError());
@@ -639,12 +680,12 @@ int fc_xent_create(fc_xent** plan, int64_t rows, int64_t dim, int64_t max_tokens
         if (chunk_tokens) most = std::min(most, chunk_tokens);
         p->chunk = std::max<int64_t>(1, std::min(most, max_tokens));
         const int64_t c = p->chunk;
-        const int64_t stats = c * fc::ceil_div(rows, 128);
-        int64_t sums = 0;  // the most splits of any chunk length up to c
-        for (int64_t m = 1; m <= c; m = m < c && m + 64 > c ? c : m + 64) {
-            const int64_t up = std::min(c, m + 63);
-            const int sp = std::max(splits_for(m, dim, rows), splits_for(up, dim, rows));
-            if (sp > 1) sums = std::max(sums, sp * up * dim);
+        const int64_t stats = std::max(c * fc::ceil_div(rows, 128), std::min(c, (int64_t)64) * fc::ceil_div(rows, 32));
+        int64_t sums = 0;  // of the most splits of any number of tokens up to c
+        for (int64_t m = 64; m < c + 64; m += 64) {
+            const Choice x = dx_choice(m, rows, dim), w = dw_choice(m, rows, dim, true);
+            if (x.splits > 1) sums = std::max(sums, x.splits * std::min(m, c) * dim);
+            if (w.splits > 1) sums = std::max(sums, w.splits * rows * dim);
         }
         fc::Layout at;
         const int64_t few = std::min<int64_t>(c, FINE);
