@@ -574,7 +574,8 @@ int run(fc_xent* p, const void* x, int64_t ldx, const void* w, int64_t ldw, cons
         const float back = scale / D_SCALE<T>;
         if (dx) {
             GradArgs g{};
-            g.a = Operand{p->numer, p->ld, m, (int)p->ld, low};
+            // past the last row's 8 columns the first product's tiles may end
+            g.a = Operand{p->numer, p->ld, m, (int)fc::ceil_div(p->rows, 8) * 8, low};
             g.parts = fine ? 2 : 1;
             g.b = Operand{w, ldw, (int)p->dim, (int)p->rows, 0};
             g.m = m;

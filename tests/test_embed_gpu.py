@@ -208,3 +208,15 @@ def test_refusals(fc, device):
         with pytest.raises(fc.FcError) as e:
             fc.Embedding(*args)
         assert e.value.code == -1  # FC_EINVAL
+
+
+@pytest.mark.parametrize("n", [1, 300, 9000])
+def test_fresh_workspaces_may_hold_anything(fc, device, n):
+    """Plans made where other memory was: what their workspaces hold before a
+    call does not matter."""
+    junk = [torch.full((1 << 24,), float("nan"), device=device) for _ in range(8)]
+    torch.cuda.synchronize()
+    del junk
+    torch.cuda.empty_cache()
+    run_case(fc, device, 701, 130, n, kind="few")
+    run_case(fc, device, 701, 130, n, kind="same")

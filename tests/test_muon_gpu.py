@@ -303,3 +303,15 @@ def test_refusals(fc, device):
         with pytest.raises(fc.FcError) as e:
             bad()
         assert e.value.code == code
+
+
+@pytest.mark.parametrize("shapes", [[(65, 63), (130, 1000)], [(33, 70), (20, 100)], [(700, 300), (1001, 131), (64, 64)], [(1, 9), (300, 17)]])
+def test_fresh_workspaces_may_hold_anything(fc, device, shapes):
+    """Plans made where other memory was: what their workspaces hold before a
+    call does not matter."""
+    junk = [torch.full((1 << 24,), float("nan"), device=device) for _ in range(8)]
+    torch.cuda.synchronize()
+    del junk
+    torch.cuda.empty_cache()
+    for dtype in DT:
+        run_case(fc, device, shapes, dtype)

@@ -277,3 +277,17 @@ def test_refusals(fc, device):
         with pytest.raises(fc.FcError) as e:
             bad()
         assert e.value.code == code
+
+
+@pytest.mark.parametrize("rows", [1500, 33, 1001, 130, 4000])
+@pytest.mark.parametrize("n", [3, 64, 70, 600])
+def test_fresh_workspaces_may_hold_anything(fc, device, rows, n):
+    """Plans made where other memory was: what their workspaces hold before a
+    call does not matter."""
+    junk = [torch.full((1 << 24,), float("nan"), device=device) for _ in range(8)]
+    torch.cuda.synchronize()
+    del junk
+    torch.cuda.empty_cache()
+    for dtype in ("f16", "bf16"):
+        x, w, y = inputs(device, rows, 264, n, dtype)
+        check(fc, device, x, w, y, dtype, plan=fc.CrossEntropy(rows, 264, n, dtype, chunk=0 if n < 100 else 64))
