@@ -9,33 +9,47 @@ from ._fc import FC_F16, FC_F32, FcError
 from ._fc_lm import FC_BF16, fc_matrix, lib
 
 DTYPES = {"f32": FC_F32, "f16": FC_F16, "bf16": FC_BF16}
-_CODES = None  # torch dtype -> fc_dtype value, made at the first call
+_CODES = {}     # torch dtype -> fc_dtype value
+_INTEGERS = {}  # torch dtype of a token list -> bytes of an entry
 
 
-def _code(t):
-    global _CODES
-    if _CODES is None:
+def _types():
+    """Fills the tables above, at the first plan (importing the package does not
+    import torch)."""
+    if not _CODES:
         import torch
-        _CODES = {torch.float32: FC_F32, torch.float16: FC_F16, torch.bfloat16: FC_BF16}
-    return _CODES.get(t.dtype)
+        _CODES.update({torch.float32: FC_F32, torch.float16: FC_F16, torch.bfloat16: FC_BF16})
+        _INTEGERS.update({torch.int32: 4, torch.int64: 8})
 
+
+def _tensor(t, name):
+    import torch
+    _types()
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{name} must be a torch tensor")
+
+
+# The checks of a call are a few attribute reads each: a small call's kernel is
+# shorter than they are on the host.
 
 def _matrix(t, name, rows, cols, device, code=None):
     """`t` must be a (rows, cols) tensor of a supported type (`code`: of that
     one) on the device, its rows contiguous and any distance apart; returns
     (pointer, type, row stride)."""
-    import torch
-    if not isinstance(t, torch.Tensor):
-        raise ValueError(f"{name} must be a torch tensor")
-    got = _code(t)
+    try:
+        got, shape, (ld, one) = _CODES[t.dtype], t.shape, t.stride()
+    except (AttributeError, KeyError, TypeError, ValueError):  # no tensor, no such type, not two dimensions
+        _tensor(t, name)
+        got, shape, (ld, one) = _CODES.get(t.dtype), t.shape, t.stride() if t.dim() == 2 else (0, 0)
     if got is None or (code is not None and got != code):
         raise ValueError(f"{name} must not be {t.dtype}")
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, the plan on {device}")
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
-        raise ValueError(f"{name} is {tuple(t.shape)}, not {(rows, cols)}")
-    ld = t.stride(0) if rows > 1 else cols
-    if (cols > 1 and t.stride(1) != 1) or ld < cols:
+    if len(shape) != 2 or shape[0] != rows or shape[1] != cols:
+        raise ValueError(f"{name} is {tuple(shape)}, not {(rows, cols)}")
+    if rows <= 1:
+        ld = cols
+    if (one != 1 and cols > 1) or ld < cols:
         raise ValueError(f"{name} must have contiguous rows that do not overlap")
     return t.data_ptr(), got, ld
 
@@ -43,25 +57,25 @@ def _matrix(t, name, rows, cols, device, code=None):
 def _list(t, name, device):
     """`t` must be a contiguous vector of int32 or int64 on the device; returns
     (pointer, bytes of an entry, length)."""
-    import torch
-    if not isinstance(t, torch.Tensor):
-        raise ValueError(f"{name} must be a torch tensor")
-    if t.dtype not in (torch.int32, torch.int64):
+    try:
+        size, shape = _INTEGERS[t.dtype], t.shape
+    except (AttributeError, KeyError):
+        _tensor(t, name)
+        size, shape = _INTEGERS.get(t.dtype), t.shape
+    if size is None:
         raise ValueError(f"{name} must be int32 or int64, not {t.dtype}")
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, the plan on {device}")
-    if t.dim() != 1 or not t.is_contiguous():
+    if len(shape) != 1 or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous vector")
-    return t.data_ptr(), t.element_size(), t.shape[0]
+    return t.data_ptr(), size, shape[0]
 
 
 def _vector(t, name, n, device, code):
     """`t` must be a contiguous vector of n elements of type `code` on the
     device; returns its pointer."""
-    import torch
-    if not isinstance(t, torch.Tensor):
-        raise ValueError(f"{name} must be a torch tensor")
-    if _code(t) != code:
+    _tensor(t, name)
+    if _CODES.get(t.dtype) != code:
         raise ValueError(f"{name} must not be {t.dtype}")
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, the plan on {device}")
@@ -70,9 +84,18 @@ def _vector(t, name, n, device, code):
     return t.data_ptr()
 
 
+_current = None  # the package's _stream, once it is loaded
+
+
 def _stream(stream):
-    from . import _stream as current
-    return current(stream)
+    global _current
+    if _current is None:
+        from . import _stream as _current
+    return _current(stream)
+
+
+_FUNCTIONS = {n: getattr(lib, n) for n in ("fc_embed_lookup", "fc_embed_grad", "fc_xent_loss", "fc_xent_loss_grad",
+                                           "fc_muon_orthogonalize", "fc_muon_step")}
 
 
 class _Handle:
@@ -83,6 +106,7 @@ class _Handle:
 
     def _create(self, make, *args):
         import torch
+        _types()
         h = ctypes.c_void_p()
         rc = getattr(lib, make)(ctypes.byref(h), *args)
         if rc:
@@ -91,7 +115,7 @@ class _Handle:
         self.device = torch.device("cuda", torch.cuda.current_device())
 
     def _call(self, name, *args):
-        rc = getattr(lib, name)(self.handle, *args)
+        rc = _FUNCTIONS[name](self.handle, *args)
         if rc:
             raise FcError(name, rc)
 
@@ -214,10 +238,8 @@ class Muon(_Handle):
         self._create("fc_muon_create", table, len(matrices), self.code, steps, abc, bool(nesterov))
 
     def _flat(self, t, name, code=None):
-        import torch
-        if not isinstance(t, torch.Tensor):
-            raise ValueError(f"{name} must be a torch tensor")
-        got = _code(t)
+        _tensor(t, name)
+        got = _CODES.get(t.dtype)
         if got is None or (code is not None and got != code):
             raise ValueError(f"{name} must not be {t.dtype}")
         if t.device != self.device:
