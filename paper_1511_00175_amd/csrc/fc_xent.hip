@@ -502,6 +502,7 @@ Choice dw_choice(int64_t m, int64_t rows, int64_t dim, bool one_chunk) { return 
 
 constexpr int64_t ROWS_LIMIT = 1 << 21, LD_LIMIT = 1 << 21, TOKENS_LIMIT = (int64_t)1 << 31;
 constexpr int64_t NUMER_BYTES = (int64_t)4 << 30;
+constexpr int64_t CHUNK_LIMIT = 1 << 18;  // a launch has at most 65535 blocks along y, of 8 tokens each
 
 }  // namespace
 
@@ -677,8 +678,8 @@ int fc_xent_create(fc_xent** plan, int64_t rows, int64_t dim, int64_t max_tokens
         p->ldp = fc::ceil_div(dim, 8) * 8;
         p->pack = dim % 8 != 0;
         int64_t most = NUMER_BYTES / (2 * p->ld);
-        most = std::max<int64_t>(256, most / 256 * 256);
-        if (chunk_tokens) most = std::min(most, chunk_tokens);
+        most = std::min<int64_t>(std::max<int64_t>(256, most / 256 * 256), CHUNK_LIMIT);
+        if (chunk_tokens) most = std::min<int64_t>(most, chunk_tokens);
         p->chunk = std::max<int64_t>(1, std::min(most, max_tokens));
         const int64_t c = p->chunk;
         const int64_t stats = std::max(c * fc::ceil_div(rows, 128), std::min(c, (int64_t)64) * fc::ceil_div(rows, 32));
