@@ -80,10 +80,10 @@ typedef struct fc_xent fc_xent;
 
 /* A plan for a vocabulary of `rows` rows of `dim` elements and up to
  * `max_tokens` tokens a call; x and w are of `dtype`, FC_F16 or FC_BF16.
- * 1 <= rows, dim <= 2^21, 0 <= max_tokens < 2^31.  The workspace holds, for
- * `chunk_tokens` tokens at a time (0: as many as fit in 4 GiB, at least 256),
- * 16 bits per token and row (64 for the first 64), and for plans of more tokens than that 4 bytes per
- * element of dw. */
+ * 1 <= rows, dim <= 2^21, 0 <= max_tokens < 2^31.  The workspace holds 16 bits per
+ * token and row (64 for the first 64) for `chunk_tokens` tokens at a time (0: as
+ * many as fit in 4 GiB, at least 256; at most 2^18 in any case), and for plans of
+ * more tokens than that 4 bytes per element of dw. */
 int fc_xent_create(fc_xent** plan, int64_t rows, int64_t dim, int64_t max_tokens, int dtype, int64_t chunk_tokens);
 void fc_xent_destroy(fc_xent* plan);
 

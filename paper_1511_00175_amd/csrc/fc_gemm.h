@@ -5,7 +5,7 @@
 // either along k ("contiguous") or along the rows ("slow": k is the slow axis):
 // products with a transposed operand need no transposed copy.  A tile goes from
 // memory to LDS without passing through registers (buffer loads with the lds
-// modifier, 16 bytes per lane), one stage ahead of the tile being multiplied.
+// modifier, 16 bytes per lane), STAGES tiles ahead of the one being multiplied.
 // The hardware writes a wave's 64 x 16 bytes to consecutive LDS addresses, so
 // the order that keeps LDS reads free of bank conflicts is made on the side of
 // the memory addresses:
@@ -80,10 +80,15 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
 
 // 16 bytes per lane from memory to LDS at lds + 16 * lane.  In asm, because the
 // compiler would wait for every such load before any LDS read it cannot tell
-// apart; the waits are the caller's.  It has no result in registers.
-__device__ __forceinline__ void load_to_lds(u32x4 desc, uint32_t lds, uint32_t off) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(off), "s"(desc)
-                 : "memory", "m0");
+// apart; the waits are the caller's.  It has no result in registers.  ONCE: of
+// what no other block reads: it displaces nothing in the caches.
+template <bool ONCE> __device__ __forceinline__ void load_to_lds(u32x4 desc, uint32_t lds, uint32_t off) {
+    if constexpr (ONCE)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(lds), "v"(off), "s"(desc)
+                     : "memory", "m0");
+    else
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(off), "s"(desc)
+                     : "memory", "m0");
 }
 
 template <int N> __device__ __forceinline__ void wait_loads() {
@@ -91,7 +96,7 @@ template <int N> __device__ __forceinline__ void wait_loads() {
 }
 
 // One wave's loads of one operand's tiles of R rows; `waves` waves share a tile.
-template <int R, bool SLOW, int WAVES> struct TileLoads {
+template <int R, bool SLOW, int WAVES, bool ONCE = false> struct TileLoads {
     static constexpr int COUNT = R / 8 / WAVES;  // 1 KiB per load
     static_assert(COUNT * 8 * WAVES == R, "a tile is whole loads of every wave");
     uint32_t off[COUNT];
@@ -165,7 +170,7 @@ template <int R, bool SLOW, int WAVES> struct TileLoads {
         return t;
     }
     __device__ __forceinline__ void load(const Tile& t, int i) const {
-        load_to_lds(t.desc, t.to + i * 1024, t.past ? GEMM_OUTSIDE : off[i]);
+        load_to_lds<ONCE>(t.desc, t.to + i * 1024, t.past ? GEMM_OUTSIDE : off[i]);
     }
 };
 
@@ -203,8 +208,9 @@ template <typename T, int R, bool SLOW, int F> struct Fragments {
 
 // The product of one block's BM x BN tile, WM x WN per wave.  RUN > 0: sums are
 // taken over runs of RUN tiles of k and then added, so that a long sum's rounding
-// error grows with the root of RUN + tiles / RUN instead of that of tiles.
-template <typename T_, int BM_, int BN_, int WM_, int WN_, bool AS, bool BS, int STAGES = 2, int RUN = 0> struct Product {
+// error grows with the root of RUN + tiles / RUN instead of that of tiles.  ONCE:
+// every tile of B is read by one block only.
+template <typename T_, int BM_, int BN_, int WM_, int WN_, bool AS, bool BS, int STAGES = 2, int RUN = 0, bool ONCE = false> struct Product {
     typedef T_ T;
     typedef typename Half<T>::v8 v8;
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
@@ -226,7 +232,7 @@ template <typename T_, int BM_, int BN_, int WM_, int WN_, bool AS, bool BS, int
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const uint32_t la = lds_address(lds), lb = la + BM * GEMM_BK * 2;
         TileLoads<BM, AS, WAVES> ta;
-        TileLoads<BN, BS, WAVES> tb;
+        TileLoads<BN, BS, WAVES, ONCE> tb;
         ta.init(A, m0, wave, lane);
         tb.init(B, n0, wave, lane);
         Fragments<T, BM, AS, FM> fa;
@@ -249,7 +255,7 @@ template <typename T_, int BM_, int BN_, int WM_, int WN_, bool AS, bool BS, int
         const int per = (ke - kb + GEMM_BK - 1) / GEMM_BK, total = per * parts;
         int part = 0, k = kb, issued = 0, into = 0;
         typename TileLoads<BM, AS, WAVES>::Tile ia;
-        typename TileLoads<BN, BS, WAVES>::Tile ib;
+        typename TileLoads<BN, BS, WAVES, ONCE>::Tile ib;
         auto prepare = [&]() {
             const bool live = issued < total;
             ia = ta.tile(la + into, k, part == parts - 2, live, wave);

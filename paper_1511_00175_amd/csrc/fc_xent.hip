@@ -33,7 +33,7 @@ typedef __bf16 bf16;
 
 extern __shared__ __align__(1024) char lds[];
 
-constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
+constexpr float LOG2E = 1.44269504088896341f;
 
 // d is stored times this: fp16 then keeps probabilities down to 2^-29 with all
 // their bits, and its largest, 1, is still in range.  bf16 needs no scale.
@@ -413,6 +413,7 @@ template <typename T, bool AS, bool BS> using Large = fc::Product<T, 256, 256, 1
 template <typename T, bool AS, bool BS> using Middle = fc::Product<T, 128, 128, 64, 64, AS, BS>;
 template <typename T, bool AS, bool BS> using Short = fc::Product<T, 64, 128, 64, 32, AS, BS, 3>;
 template <typename T, bool AS, bool BS> using Narrow = fc::Product<T, 64, 32, 16, 32, AS, BS, 6>;
+template <typename T, bool AS, bool BS> using Once = fc::Product<T, 64, 128, 64, 32, AS, BS, 3, 0, true>;
 
 enum TileKind { LARGE, MIDDLE, SHORT, NARROW, KINDS };
 
@@ -482,10 +483,12 @@ template <typename T> hipError_t prepare_all() {
                          prepare<Middle<T, false, false>>((const void*)logit_kernel<Middle<T, false, false>>),
                          prepare<Short<T, false, false>>((const void*)logit_kernel<Short<T, false, false>>),
                          prepare<Narrow<T, false, false>>((const void*)logit_kernel<Narrow<T, false, false>>),
+                         prepare<Once<T, false, false>>((const void*)logit_kernel<Once<T, false, false>>),
                          prepare<Large<T, false, true>>((const void*)grad_kernel<Large<T, false, true>>),
                          prepare<Middle<T, false, true>>((const void*)grad_kernel<Middle<T, false, true>>),
                          prepare<Short<T, false, true>>((const void*)grad_kernel<Short<T, false, true>>),
                          prepare<Narrow<T, false, true>>((const void*)grad_kernel<Narrow<T, false, true>>),
+                         prepare<Once<T, false, true>>((const void*)grad_kernel<Once<T, false, true>>),
                          prepare<Large<T, true, true>>((const void*)grad_kernel<Large<T, true, true>>),
                          prepare<Middle<T, true, true>>((const void*)grad_kernel<Middle<T, true, true>>)})
         if (e != hipSuccess) return e;
@@ -501,6 +504,13 @@ Choice dx_choice(int64_t m, int64_t rows, int64_t dim) { return choose(m, dim, r
 Choice dw_choice(int64_t m, int64_t rows, int64_t dim, bool one_chunk) { return choose(rows, dim, m, false, one_chunk); }
 
 constexpr int64_t ROWS_LIMIT = 1 << 21, LD_LIMIT = 1 << 21, TOKENS_LIMIT = (int64_t)1 << 31;
+// A w that fills the memory-side cache (256 MB) by itself is read past the caches
+// (up to 64 tokens, when every tile of it is read once).  16 tokens, fp16, us,
+// through the caches / past them, first with 300 MB written between the calls,
+// then call after call: w of 268 MB 108 / 64 and 44 / 60, 403 MB 127 / 80 and
+// 84 / 75, 1074 MB 217 / 163 and 177 / 159; with dx 268 MB 197 / 158 and 132 / 156,
+// 1074 MB 635 / 551 and 593 / 543.
+constexpr int64_t CACHE_BYTES = (int64_t)1 << 28;
 constexpr int64_t NUMER_BYTES = (int64_t)4 << 30;
 constexpr int64_t CHUNK_LIMIT = 1 << 18;  // a launch has at most 65535 blocks along y, of 8 tokens each
 
@@ -547,6 +557,7 @@ int run(fc_xent* p, const void* x, int64_t ldx, const void* w, int64_t ldw, cons
         ldw = p->ldp;
     }
     const int dimk = (int)(p->pack ? p->ldp : p->dim);
+    const bool once = p->rows * dimk * 2 >= CACHE_BYTES;
     for (int64_t t0 = 0; t0 < n; t0 += p->chunk) {
         const int m = (int)std::min(p->chunk, n - t0);
         const void* xt = static_cast<const char*>(x) + t0 * ldx * 2;
@@ -560,6 +571,7 @@ int run(fc_xent* p, const void* x, int64_t ldx, const void* w, int64_t ldw, cons
         LogitArgs l{ox, ow, m, (int)p->rows, dimk, yt, target_bytes, p->stats, p->target_logit, grads ? fine ? p->fine : p->numer : nullptr, p->ld, fine, 0, 0};
         if (kind == LARGE) launch_logit<Large<T, false, false>>(l, s);
         else if (kind == MIDDLE) launch_logit<Middle<T, false, false>>(l, s);
+        else if (kind == SHORT && once) launch_logit<Once<T, false, false>>(l, s);
         else if (kind == SHORT) launch_logit<Short<T, false, false>>(l, s);
         else launch_logit<Narrow<T, false, false>>(l, s);
         const int width = piece_width(kind), pieces = (int)fc::ceil_div(p->rows, width);
@@ -594,6 +606,7 @@ int run(fc_xent* p, const void* x, int64_t ldx, const void* w, int64_t ldw, cons
             g.last = c.splits == 1;
             if (c.kind == LARGE) launch_grad<Large<T, false, true>>(g, s);
             else if (c.kind == MIDDLE) launch_grad<Middle<T, false, true>>(g, s);
+            else if (c.kind == SHORT && once) launch_grad<Once<T, false, true>>(g, s);
             else if (c.kind == SHORT) launch_grad<Short<T, false, true>>(g, s);
             else launch_grad<Narrow<T, false, true>>(g, s);
             if (c.splits > 1) join_splits(g, c.splits);

@@ -102,6 +102,12 @@ def test_large_tiles(fc, device, dtype):
     check(fc, device, *inputs(device, 260, 4100, 4200, dtype), dtype)
 
 
+@pytest.mark.parametrize("dtype,n,dim", [("f16", 5, 4104), ("bf16", 64, 4097)])
+def test_weights_larger_than_the_caches(fc, device, dtype, n, dim):
+    """At least 2^28 bytes of w for few tokens."""
+    check(fc, device, *inputs(device, 32801, dim, n, dtype), dtype)
+
+
 @pytest.mark.parametrize("dim", [1, 3, 63, 130, 1001])
 def test_odd_dimensions(fc, device, dim):
     check(fc, device, *inputs(device, 777, dim, 200, "bf16"), "bf16")
