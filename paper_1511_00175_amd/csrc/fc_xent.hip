@@ -104,10 +104,14 @@ template <typename P> __global__ __launch_bounds__(P::THREADS, P::THREADS / 256)
 #pragma unroll
         for (int j = 0; j < P::FN; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                top = fmaxf(top, p.acc[i][j][e]);
-                if (at == 16 * j + e) a.target_logit[m] = p.acc[i][j][e];
-            }
+            for (int e = 0; e < 4; ++e) top = fmaxf(top, p.acc[i][j][e]);
+        if (__any(at >= 0 && at < P::WN)) {  // few tiles hold a target
+#pragma unroll
+            for (int j = 0; j < P::FN; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (at == 16 * j + e) a.target_logit[m] = p.acc[i][j][e];
+        }
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
         tops[i] = top;
