@@ -1,7 +1,9 @@
 // Embedding rows and their gradient (fc_lm.h).
 //
 // lookup: out[t] = scale * table[token[t]].  One pass; bounded by the bytes of
-//   the rows read and written.
+//   the rows read and written: 32768 rows of 2048 fp16 take 48 us (5.6 TB/s), 5001 odd
+//   rows of 1001 from bf16 to fp32 9 us (3.3 TB/s, an element per lane), one row 1.8
+//   (an empty launch's time; 5.6 with the host's part of a call).
 // grad: dtable[r] = scale * sum of dy[t] over token[t] == r.  The tokens are
 //   sorted by a stable radix sort on their (row, t) pairs; then the sorted list
 //   is cut into chunks of CHUNK entries, each summed by its own threads in order.
@@ -10,7 +12,10 @@
 //   kernel.  No atomics on sums: the same inputs give the same bits.  Bounded by
 //   the bytes of dy and of the whole table's gradient, of which the rows without
 //   a token are most: the zeros are stored by blocks that run beside the sort's
-//   few ones, a share in each of its launches.
+//   few ones, a share in each of its launches.  32768 tokens of 2048 fp16 into
+//   65536 rows of fp32 take 171 us: 86 of sort and zeros (537 MB, 6.2 TB/s), 76 of
+//   sums and 8 of joins; in all 671 MB at 3.9 TB/s, where a large copy has 4.8.  256
+//   tokens of 1001 fp32 into 1000 rows: 12 us, three launches one after the other.
 #include <algorithm>
 
 #include "fc_lm_host.h"
@@ -93,7 +98,8 @@ __device__ __forceinline__ uint2 sort_item(const SortPass& a, int i) {
     return a.in ? a.in[i] : make_uint2(a.tokens.key(i), (uint32_t)i);
 }
 
-// Counts of every digit among a block's items.
+// Counts of every digit among a block's items.  21647 tokens: 4.3 us, a launch's
+// latency, as the pass after it, 9.2, is bound by its scan over the bins.
 __global__ __launch_bounds__(SORT_THREADS) void sort_count_kernel(SortPass a) {
     if ((int)blockIdx.x >= a.blocks) return fill_rows(a.fill, blockIdx.x - a.blocks);
     __shared__ uint32_t count[BINS];
@@ -240,7 +246,10 @@ template <typename TO, int V> __device__ __forceinline__ void store_row(const Su
 
 // Sums of one chunk of the sorted list; a thread holds V columns.  The entries
 // are the same for every thread of a block, so keys and branches are uniform;
-// UNROLL rows are loaded before the first is added.
+// UNROLL rows are loaded before the first is added: a row alone would wait for
+// each load.  Bound by reading dy and writing rows (76 us for 32768 tokens of 2048
+// fp16, 402 MB at most: the rows written again after their zeros among them);
+// 4 or 16 rows ahead, narrower vectors and other chunks were no faster.
 template <typename TI, typename TO, int V> __global__ __launch_bounds__(256) void sum_kernel(SumArgs a) {
     constexpr int UNROLL = 8;
     typedef Vec<TI, V> I;
@@ -301,6 +310,7 @@ template <typename TI, typename TO, int V> __global__ __launch_bounds__(256) voi
 
 // The rows that run over chunks: the block of the chunk where a row begins adds
 // its parts, each of 4 waves every fourth one, then the waves' sums in order.
+// Bound by its chain of loads (a search, then parts): 3.3 to 8 us.
 template <typename TO, int V> __global__ __launch_bounds__(256) void join_kernel(SumArgs a) {
     constexpr int UNROLL = 4;
     __shared__ float part[4][64 * V];

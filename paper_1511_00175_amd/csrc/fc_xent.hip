@@ -8,7 +8,7 @@
 // first product holds a piece of the vocabulary for its tokens in fp32: it takes
 // the piece's maximum m and sum of exponentials, keeps both (8 bytes), the
 // target's logit, and, when gradients are wanted, the numerators exp(l - m) in 16
-// bits.  One small kernel joins a token's pieces into lse and the loss; one pass
+// bits (fp32 for up to 64 tokens).  One small kernel joins a token's pieces into lse and the loss; one pass
 // over the numerators then turns them into d (numerator * exp(m - lse), minus one
 // at the target), and two products make the gradients of it.  The alternative
 // that keeps nothing computes the first product twice: 8 instead of 6 units of
@@ -16,6 +16,12 @@
 //
 // Tokens go through in chunks so that the numerators take at most 4 GiB; with
 // more than one chunk, dw is summed in fp32 over them and rounded after the last.
+//
+// Measured, fp16, 8192 tokens, 131072 rows of 2048: 12.2 ms for 13.2 TFLOP (1.08
+// PFLOP/s; a library's three products of these shapes alone 10.9): the first
+// product 4.1 ms, dw 3.9, dx 3.4, the pass from numerators to d 0.82 (4.3 GB), join
+// 0.03, the copy of x 0.02.  bf16, 24 tokens, 65536 rows of 2048, losses only: 61 us,
+// of which the product 56 (268 MB at 4.8 TB/s).
 #include <algorithm>
 
 #include "fc_gemm.h"
@@ -67,6 +73,10 @@ struct LogitArgs {
     int tm, tn;
 };
 
+// Bound by the matrix cores where dim is long (2048: 1.07 PFLOP/s) and by its
+// end, the numerators' stores most, where it is short: 1003 tokens, 50001 rows of 520,
+// bf16: 114 us, 89 without those stores (100 MB), 113 without the exponentials; the
+// blocks of one round end together, so that stores do not run beside products.
 template <typename P> __global__ __launch_bounds__(P::THREADS, P::THREADS / 256) void logit_kernel(LogitArgs a) {
     typedef typename P::T T;
     int ti, tj;
@@ -184,7 +194,8 @@ __device__ __forceinline__ f32x2 join(f32x2 s, f32x2 q) {
 }
 
 // T tokens per block of 256 threads, 256 / T threads each: 16 where there are
-// enough tokens (a piece's stats of 16 tokens are neighbours), else 1.
+// enough tokens (a piece's stats of 16 tokens are neighbours), else 1.  24 tokens of
+// 512 pieces take 4.5 us with 1 per block, 40 more with 16; 8192 tokens 25.
 template <int T> __global__ __launch_bounds__(256) void join_kernel(JoinArgs a) {
     constexpr int Q = 256 / T;
     __shared__ f32x2 part[T][Q + 1];
@@ -230,7 +241,8 @@ struct DiffArgs {
 constexpr int DIFF_ROWS = 8;
 
 // A block's 256 threads hold 8 columns each, of DIFF_ROWS tokens one after the
-// other, whose stats are neighbours in memory.
+// other, whose stats are neighbours in memory.  Bound by HBM: 8192 tokens of 131072
+// rows 0.82 ms, 4.3 GB at 5.2 TB/s.
 template <typename T, typename N> __global__ __launch_bounds__(256) void diff_kernel(DiffArgs a) {
     typedef typename Half<T>::v8 v8;
     typedef N n8 __attribute__((ext_vector_type(8)));
@@ -309,6 +321,9 @@ struct GradArgs {
     int tm, tn;
 };
 
+// Bound by the matrix cores: 8192 tokens, 131072 rows of 2048 take 3.4 ms for dx and
+// 3.9 for dw (1.29 and 1.13 PFLOP/s).  Tiles in groups of 8 rows keep what the blocks
+// of an XCD read in its L2.  Few tokens give few tiles: k is then split.
 template <typename P> __global__ __launch_bounds__(P::THREADS, P::THREADS / 256) void grad_kernel(GradArgs a) {
     int ti, tj;
     fc::tile_place(fc::xcd_order(blockIdx.x, a.tm * a.tn), a.tm, a.tn, 8, ti, tj);
@@ -361,7 +376,8 @@ struct SplitArgs {
     int64_t ld;
 };
 
-// The splits of a product added in order.
+// The splits of a product added in order: 4 to 7 us, a launch's latency and one
+// trip to memory.
 __global__ __launch_bounds__(256) void split_kernel(SplitArgs a) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, total = (int64_t)a.m * a.n;
     if (i >= total) return;
@@ -372,6 +388,8 @@ __global__ __launch_bounds__(256) void split_kernel(SplitArgs a) {
     store_one(a.out, a.dt, (int64_t)m * a.ld + n, a.row && a.row[m] < 0 ? 0.f : v * a.scale);
 }
 
+// Copies with rows of a multiple of 8 elements: bound by HBM (8192 x 2048, 67 MB in
+// all, 16 us).
 struct PackArgs {
     const void* in;
     int64_t ld_in;
