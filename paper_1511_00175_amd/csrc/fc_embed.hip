@@ -2,8 +2,8 @@
 //
 // lookup: out[t] = scale * table[token[t]].  One pass; bounded by the bytes of
 //   the rows read and written: 32768 rows of 2048 fp16 take 48 us (5.6 TB/s), 5001 odd
-//   rows of 1001 from bf16 to fp32 9 us (3.3 TB/s, an element per lane), one row 1.8
-//   (an empty launch's time; 5.6 with the host's part of a call).
+//   rows of 1001 from bf16 to fp32 7 us (4.3 TB/s), one row 1.8 (an empty launch's
+//   time; 5.6 with the host's part of a call).
 // grad: dtable[r] = scale * sum of dy[t] over token[t] == r.  The tokens are
 //   sorted by a stable radix sort on their (row, t) pairs; then the sorted list
 //   is cut into chunks of CHUNK entries, each summed by its own threads in order.
@@ -13,8 +13,8 @@
 //   the bytes of dy and of the whole table's gradient, of which the rows without
 //   a token are most: the zeros are stored by blocks that run beside the sort's
 //   few ones, a share in each of its launches.  32768 tokens of 2048 fp16 into
-//   65536 rows of fp32 take 171 us: 86 of sort and zeros (537 MB, 6.2 TB/s), 76 of
-//   sums and 8 of joins; in all 671 MB at 3.9 TB/s, where a large copy has 4.8.  256
+//   65536 rows of fp32 take 168 us: 86 of sort and zeros (537 MB, 6.2 TB/s), 76 of
+//   sums and 8 of joins; in all 671 MB at 4.0 TB/s, where a large copy has 4.8.  256
 //   tokens of 1001 fp32 into 1000 rows: 12 us, three launches one after the other.
 #include <algorithm>
 
@@ -25,8 +25,15 @@ namespace {
 typedef _Float16 f16;
 typedef __bf16 bf16;
 
-template <typename T, int V> struct alignas(sizeof(T) * V < 16 ? sizeof(T) * V : 16) Vec {
+// V neighbours of a row, which may start at any element: global memory takes any
+// alignment.  A row's last V overlap those before them where its length is no multiple
+// of V.  Measured against vectors as wide as every row's alignment allows, us: 32768
+// rows of 2047 looked up, fp16 41 / 71, fp32 87 / 147; their gradient into 65536 rows,
+// fp16 119 / 195, fp32 241 / 313 (rows of 2048: 38, 81, 121, 214).
+template <typename T, int V> struct Vec {
     T x[V];
+    __device__ __forceinline__ void load(const T* p) { __builtin_memcpy(x, p, sizeof(x)); }
+    __device__ __forceinline__ void store(T* p) const { __builtin_memcpy(p, x, sizeof(x)); }
 };
 
 constexpr int BITS = 9;                  // of a radix digit
@@ -54,34 +61,24 @@ struct Fill {
     int64_t ld_bytes;
     int64_t row_bytes;
     int64_t rows;
-    int unit;       // bytes per store: 16, 8, 4 or 2
     int part, parts;
     int blocks;     // that fill
 };
 
-template <typename U> __device__ __forceinline__ void fill_units(const Fill& f, int64_t block) {
-    const int64_t per_row = f.row_bytes / (int64_t)sizeof(U);
-    const int64_t r0 = f.rows * f.part / f.parts, r1 = f.rows * (f.part + 1) / f.parts;
-    const int64_t lo = r0 + (r1 - r0) * block / f.blocks, hi = r0 + (r1 - r0) * (block + 1) / f.blocks;
-    if (per_row * (int64_t)sizeof(U) == f.ld_bytes) {  // one run of memory
-        U* p = reinterpret_cast<U*>(f.p + lo * f.ld_bytes);
-        const int64_t n = (hi - lo) * per_row;
-        for (int64_t i = threadIdx.x; i < n; i += blockDim.x) p[i] = U{};
-        return;
-    }
-    for (int64_t r = lo; r < hi; ++r) {
-        U* p = reinterpret_cast<U*>(f.p + r * f.ld_bytes);
-        for (int64_t i = threadIdx.x; i < per_row; i += blockDim.x) p[i] = U{};
-    }
+// Zeros, 16 bytes a store but for the ends (any even address and length).
+__device__ __forceinline__ void fill_run(char* p, int64_t bytes) {
+    const int64_t head = min(bytes, (int64_t)(-(uintptr_t)p & 15)), whole = (bytes - head) / 16, tail = bytes - head - 16 * whole;
+    for (int64_t i = threadIdx.x; i < whole; i += blockDim.x) *reinterpret_cast<uint4*>(p + head + 16 * i) = uint4{};
+    const int i = threadIdx.x;
+    if (2 * i < head) reinterpret_cast<uint16_t*>(p)[i] = 0;
+    if (2 * i < tail) reinterpret_cast<uint16_t*>(p + head + 16 * whole)[i] = 0;
 }
 
 __device__ __forceinline__ void fill_rows(const Fill& f, int64_t block) {
-    switch (f.unit) {
-        case 16: return fill_units<uint4>(f, block);
-        case 8: return fill_units<uint2>(f, block);
-        case 4: return fill_units<uint32_t>(f, block);
-        default: return fill_units<uint16_t>(f, block);
-    }
+    const int64_t r0 = f.rows * f.part / f.parts, r1 = f.rows * (f.part + 1) / f.parts;
+    const int64_t lo = r0 + (r1 - r0) * block / f.blocks, hi = r0 + (r1 - r0) * (block + 1) / f.blocks;
+    if (f.row_bytes == f.ld_bytes) return fill_run(f.p + lo * f.ld_bytes, (hi - lo) * f.row_bytes);
+    for (int64_t r = lo; r < hi; ++r) fill_run(f.p + r * f.ld_bytes, f.row_bytes);
 }
 
 struct SortPass {
@@ -229,19 +226,25 @@ struct SumArgs {
     float* parts;            // per chunk: the sum that goes on from the chunk before, and the one that goes on into the next
 };
 
-template <typename TO, int V> __device__ __forceinline__ void store_row(const SumArgs& a, uint32_t row, int col, const float* sum) {
-    typedef Vec<TO, V> O;
-    O* p = reinterpret_cast<O*>(static_cast<TO*>(a.out) + (int64_t)row * a.ld_out + col);
-    O o;
+// The columns before `own` are another thread's as well: it adds to them.
+template <typename TO, int V> __device__ __forceinline__ void store_row(const SumArgs& a, uint32_t row, int col, int own, const float* sum) {
+    TO* const p = static_cast<TO*>(a.out) + (int64_t)row * a.ld_out + col;
+    Vec<TO, V> o;
+    if (a.accumulate && own > col) {
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+            if (col + e >= own) p[e] = (TO)((float)p[e] + a.scale * sum[e]);
+        return;
+    }
     if (a.accumulate) {
-        o = *p;
+        o.load(p);
 #pragma unroll
         for (int e = 0; e < V; ++e) o.x[e] = (TO)((float)o.x[e] + a.scale * sum[e]);
     } else {
 #pragma unroll
         for (int e = 0; e < V; ++e) o.x[e] = (TO)(a.scale * sum[e]);
     }
-    *p = o;
+    o.store(p);
 }
 
 // Sums of one chunk of the sorted list; a thread holds V columns.  The entries
@@ -253,10 +256,10 @@ template <typename TO, int V> __device__ __forceinline__ void store_row(const Su
 template <typename TI, typename TO, int V> __global__ __launch_bounds__(256) void sum_kernel(SumArgs a) {
     constexpr int UNROLL = 8;
     typedef Vec<TI, V> I;
-    const int col = (blockIdx.y * 256 + threadIdx.x) * V;
+    const int own = (blockIdx.y * 256 + threadIdx.x) * V, col = min(own, a.dim - V);
     const int c = blockIdx.x, lo = c * a.chunk, hi = min(lo + a.chunk, a.n);
     uint32_t row = a.sorted[lo].x;
-    if (row >= a.rows || col >= a.dim) return;
+    if (row >= a.rows || own >= a.dim) return;
     bool from_before = c > 0 && a.sorted[lo - 1].x == row;
     float* const head = a.parts + (int64_t)(2 * c) * a.dim + col;
     float* const tail = head + a.dim;
@@ -269,7 +272,7 @@ template <typename TI, typename TO, int V> __global__ __launch_bounds__(256) voi
 #pragma unroll
             for (int e = 0; e < V; ++e) head[e] = sum[e];
         } else {
-            store_row<TO, V>(a, row, col, sum);
+            store_row<TO, V>(a, row, col, own, sum);
         }
     };
     for (int i = lo; i < hi; i += UNROLL) {
@@ -283,7 +286,7 @@ template <typename TI, typename TO, int V> __global__ __launch_bounds__(256) voi
         }
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {  // an entry that names no row has a place in dy as well
-            x[u] = *reinterpret_cast<const I*>(dy + (int64_t)e[u].y * a.ld_dy);
+            x[u].load(dy + (int64_t)e[u].y * a.ld_dy);
         }
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
@@ -315,7 +318,7 @@ template <typename TO, int V> __global__ __launch_bounds__(256) void join_kernel
     constexpr int UNROLL = 4;
     __shared__ float part[4][64 * V];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int col = (blockIdx.y * 64 + lane) * V;
+    const int own = (blockIdx.y * 64 + lane) * V, col = min(own, a.dim - V);
     const int c = blockIdx.x, chunks = (a.n + a.chunk - 1) / a.chunk;
     const int hi = (c + 1) * a.chunk;
     if (hi >= a.n) return;
@@ -333,7 +336,7 @@ template <typename TO, int V> __global__ __launch_bounds__(256) void join_kernel
         }
         end = lo;
     }
-    const bool live = col < a.dim;
+    const bool live = own < a.dim;
     float sum[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) sum[e] = 0.f;
@@ -365,7 +368,7 @@ template <typename TO, int V> __global__ __launch_bounds__(256) void join_kernel
     for (int w = 1; w < 4; ++w)
 #pragma unroll
         for (int e = 0; e < V; ++e) sum[e] += part[w][lane * V + e];
-    store_row<TO, V>(a, row, col, sum);
+    store_row<TO, V>(a, row, col, own, sum);
 }
 
 struct LookupArgs {
@@ -380,25 +383,25 @@ struct LookupArgs {
 };
 
 template <typename TI, typename TO, int V> __global__ __launch_bounds__(256) void lookup_kernel(LookupArgs a) {
-    typedef Vec<TI, V> I;
-    typedef Vec<TO, V> O;
     const int rows_per_block = 256 / a.per_row;
     const int64_t t = (int64_t)blockIdx.x * rows_per_block + threadIdx.x / a.per_row;
     if (t >= a.tokens.n) return;
     const uint32_t row = a.tokens.key((int)t);
     const TI* in = static_cast<const TI*>(a.table) + (int64_t)row * a.ld_table;
     TO* out = static_cast<TO*>(a.out) + t * a.ld_out;
-    for (int col = (threadIdx.x & (a.per_row - 1)) * V; col < a.dim; col += a.per_row * V) {
-        O o;
+    for (int own = (threadIdx.x & (a.per_row - 1)) * V; own < a.dim; own += a.per_row * V) {
+        const int col = min(own, a.dim - V);
+        Vec<TO, V> o;
         if (row < a.tokens.rows) {
-            const I x = *reinterpret_cast<const I*>(in + col);
+            Vec<TI, V> x;
+            x.load(in + col);
 #pragma unroll
             for (int e = 0; e < V; ++e) o.x[e] = (TO)(a.scale * (float)x.x[e]);
         } else {
 #pragma unroll
             for (int e = 0; e < V; ++e) o.x[e] = (TO)0.f;
         }
-        *reinterpret_cast<O*>(out + col) = o;
+        o.store(out + col);
     }
 }
 
@@ -447,6 +450,12 @@ constexpr int64_t DIM_LIMIT = (int64_t)1 << 20;  // column blocks of a launch
 // enough that a row's parts are few.
 int chunk_of(int64_t n) { return n <= 4096 ? 8 : 32; }
 
+// Neighbours per thread: of 16 bytes, or as many as a row has.
+int vector_of(int most, int64_t dim) {
+    while (most > dim) most /= 2;
+    return most;
+}
+
 int64_t most_chunks(int64_t n) { return std::max(fc::ceil_div(std::min<int64_t>(n, 4096), 8), fc::ceil_div(n, 32)); }
 
 int lookup_body(fc_embed* p, const void* table, int tdt, int64_t ld_table, const void* tokens, int token_bytes, int64_t n,
@@ -456,7 +465,7 @@ int lookup_body(fc_embed* p, const void* table, int tdt, int64_t ld_table, const
     const fc::Span so{out, n, p->dim, ld_out, fc::dtype_bytes(odt), true};
     int rc = fc::check_spans({st, so, {tokens, 1, n, n, token_bytes, false}});
     if (rc || n == 0) return rc;
-    const int v = fc::vector_width({st, so}, 16 / std::min(st.bytes, so.bytes));
+    const int v = vector_of(16 / std::min(st.bytes, so.bytes), p->dim);
     LookupArgs a{table, ld_table, {tokens, token_bytes, (int)n, (uint32_t)p->rows}, out, ld_out, (int)p->dim, scale, 0};
     a.per_row = pow2_at_least(fc::ceil_div(p->dim, v), 256);
     const int64_t grid = fc::ceil_div(n, 256 / a.per_row);
@@ -492,11 +501,10 @@ int grad_body(fc_embed* p, const void* dy, int ydt, int64_t ld_dy, const void* t
     const bool few = n <= FEW;
     const int blocks = (int)fc::ceil_div(n, few ? 64 : PER_BLOCK);
     const int launches = few ? 1 : 2 * p->passes;
-    Fill fill{static_cast<char*>(out), ld_out * so.bytes, p->dim * so.bytes, p->rows, 0, 0, launches, 0};
-    fill.unit = so.bytes * fc::vector_width({so}, 16 / so.bytes);
+    Fill fill{static_cast<char*>(out), ld_out * so.bytes, p->dim * so.bytes, p->rows, 0, launches, 0};
     if (!accumulate) {
         // blocks of 1024 threads with about 16 stores each
-        const int64_t units = fill.row_bytes * fill.rows / launches / fill.unit;
+        const int64_t units = fill.row_bytes * fill.rows / launches / 16;
         fill.blocks = (int)std::min<int64_t>(std::max<int64_t>(1, fc::ceil_div(units, 16 * SORT_THREADS)),
                                              std::max<int64_t>(1, p->rows / launches));
     }
@@ -523,8 +531,7 @@ int grad_body(fc_embed* p, const void* dy, int ydt, int64_t ld_dy, const void* t
     if (!rc && n > 0) {
         const int chunk = chunk_of(n);
         SumArgs a{sorted, (int)n, (uint32_t)p->rows, chunk, dy, ld_dy, (int)p->dim, out, ld_out, scale, accumulate, p->parts};
-        const fc::Span sp{p->parts, 2, p->dim, p->dim, 4, true};
-        const int v = fc::vector_width({sy, so, sp}, 16 / sy.bytes);
+        const int v = vector_of(16 / sy.bytes, p->dim);
         const int chunks = (int)fc::ceil_div(n, chunk);
         with_type(odt, [&](auto* to) {
             typedef std::remove_pointer_t<decltype(to)> TO;

@@ -122,14 +122,4 @@ struct Layout {
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// The largest of 8, 4, 2, 1 elements that divides every row length, stride and
-// address of the buffers and is at most 16 bytes of the widest source: lanes
-// then move whole vectors.
-inline int vector_width(std::initializer_list<Span> spans, int most) {
-    int v = most;
-    for (const Span& s : spans)
-        while (v > 1 && (s.len % v || (s.rows > 1 && s.ld % v) || s.lo() % (v * s.bytes < 16 ? v * s.bytes : 16))) v /= 2;
-    return v;
-}
-
 }  // namespace fc

@@ -117,6 +117,13 @@ def test_accumulate(fc, device, to, n):
     run_case(fc, device, 211, 96, n, "f16", to, "few", accumulate=True)
 
 
+@pytest.mark.parametrize("ti,to", [("f16", "f32"), ("bf16", "bf16"), ("f32", "f16")])
+@pytest.mark.parametrize("dim,pad,shift", [(1, 0, 0), (7, 0, 1), (9, 0, 0), (97, 3, 1), (2049, 0, 0)])
+def test_accumulate_rows_of_any_length(fc, device, ti, to, dim, pad, shift):
+    """The last vector of a row overlaps the one before it, whose elements are added to once."""
+    run_case(fc, device, 37, dim, 500, ti, to, "few", pad=pad, shift=shift, accumulate=True)
+
+
 def test_gradient_is_that_of_the_lookup(fc, device):
     """<lookup(table + d) - lookup(table), dy> == <d, grad(dy)>: the lookup is
     linear, so differences are exact but for the roundings (fp32, 1e-4 of the
