@@ -47,6 +47,10 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 b16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 b16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+// Wherever elements may start: global memory takes any alignment.
+typedef f32x4 f32x4_any __attribute__((aligned(4)));
+typedef f16x4 f16x4_any __attribute__((aligned(2)));
+typedef b16x4 b16x4_any __attribute__((aligned(2)));
 
 #define FC_LDS __attribute__((address_space(3)))
 

@@ -42,6 +42,7 @@
 
 using fc::f16x4;
 using fc::f32x4;
+using fc::f32x4_any;
 using fc::Operand;
 using Tile = fc::TileAt;
 
@@ -92,27 +93,27 @@ __device__ __forceinline__ void store_one(const Output& a, const Matrix& m, uint
 }
 
 // Four neighbours of a row of the result, of which those in the matrix are
-// stored, as one vector where rows start on one (offsets are multiples of 4).
+// stored: as one vector, which may start at any element (a row's last few one by one).
 __device__ __forceinline__ void store_out(const Output& a, const Matrix& m, int row, int col, f32x4 u) {
     if (col >= m.cols) return;
     const uint64_t at = m.offset + (uint64_t)row * m.cols + col;
-    if (m.cols % 4) {
+    if (col + 4 > m.cols) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
+        for (int e = 0; e < 3; ++e)
             if (col + e < m.cols) store_one(a, m, at + e, u[e]);
     } else if (!a.out) {
-        f32x4* p = reinterpret_cast<f32x4*>(a.w + at);
+        f32x4_any* p = reinterpret_cast<f32x4_any*>(a.w + at);
         const f32x4 w = *p;
         const float k = a.lr * m.lr_mult, d = a.wd * m.decay_mult;
 #pragma unroll
         for (int e = 0; e < 4; ++e) u[e] = w[e] - k * (m.scale * u[e] + d * w[e]);
         *p = u;
     } else if (a.dt == FC_F32) {
-        *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + at) = u;
+        *reinterpret_cast<f32x4_any*>(static_cast<float*>(a.out) + at) = u;
     } else if (a.dt == FC_F16) {
-        *reinterpret_cast<f16x4*>(static_cast<f16*>(a.out) + at) = __builtin_convertvector(u, f16x4);
+        *reinterpret_cast<fc::f16x4_any*>(static_cast<f16*>(a.out) + at) = __builtin_convertvector(u, f16x4);
     } else {
-        *reinterpret_cast<fc::b16x4*>(static_cast<bf16*>(a.out) + at) = __builtin_convertvector(u, fc::b16x4);
+        *reinterpret_cast<fc::b16x4_any*>(static_cast<bf16*>(a.out) + at) = __builtin_convertvector(u, fc::b16x4);
     }
 }
 
@@ -139,25 +140,22 @@ template <typename T, bool STEP> __device__ __forceinline__ float direction(cons
     return g;
 }
 
-// Four elements from i on, a multiple of 4; UPDATE: the momentum is updated and
-// stored first.
+// Four elements from i on; UPDATE: the momentum is updated and stored first.
 template <typename T, bool STEP, bool UPDATE> __device__ __forceinline__ void direction4(const Source& a, uint64_t i, float* x) {
-    struct alignas(4 * sizeof(T)) G {
-        T x[4];
-    };
-    const G g = *reinterpret_cast<const G*>(static_cast<const T*>(a.g) + i);
+    T g[4];
+    __builtin_memcpy(g, static_cast<const T*>(a.g) + i, sizeof(g));
     f32x4 v;
-    if constexpr (STEP) v = *reinterpret_cast<const f32x4*>(a.v + i);
+    if constexpr (STEP) v = *reinterpret_cast<const f32x4_any*>(a.v + i);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        x[e] = (float)g.x[e];
+        x[e] = (float)g[e];
         if constexpr (STEP) {
             x[e] *= a.c;
             if (UPDATE) v[e] = a.mu * v[e] + x[e];
             x[e] = a.nesterov ? x[e] + a.mu * v[e] : v[e];
         }
     }
-    if constexpr (STEP && UPDATE) *reinterpret_cast<f32x4*>(a.v + i) = v;
+    if constexpr (STEP && UPDATE) *reinterpret_cast<f32x4_any*>(a.v + i) = v;
 }
 
 // Sums of squares of one piece of a matrix, in 64 bits: neither tiny nor huge
@@ -215,11 +213,10 @@ struct ScaleArgs {
     Output to;
 };
 
-// Up to 4 neighbours of the direction, `left` of them in the matrix's row, as one
-// vector where rows start on one.
-template <typename T, bool STEP> __device__ __forceinline__ f32x4 direction_row(const Source& a, uint64_t i, int left, bool wide) {
+// Up to 4 neighbours of the direction, `left` of them in the matrix's row.
+template <typename T, bool STEP> __device__ __forceinline__ f32x4 direction_row(const Source& a, uint64_t i, int left) {
     f32x4 v{0.f, 0.f, 0.f, 0.f};
-    if (wide && left >= 4) {
+    if (left >= 4) {
         float x[4];
         direction4<T, STEP, false>(a, i, x);
 #pragma unroll
@@ -242,12 +239,11 @@ template <typename T, bool STEP> __global__ __launch_bounds__(256) void scale_ke
     const Matrix& m = a.mats[t.mat];
     const int r0 = 64 * (m.turned ? t.j : t.i), c0 = 64 * (m.turned ? t.i : t.j);
     const int y = threadIdx.x / 16, z = threadIdx.x % 16 * 4;
-    const bool wide = m.cols % 4 == 0;
     f32x4 d[4];  // rows y, y + 16, ... of the tile in the vector's order
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         const int r = r0 + y + 16 * q, left = r < m.rows ? m.cols - c0 - z : 0;
-        d[q] = direction_row<T, STEP>(a.d, m.offset + (uint64_t)r * m.cols + c0 + z, left, wide);
+        d[q] = direction_row<T, STEP>(a.d, m.offset + (uint64_t)r * m.cols + c0 + z, left);
     }
     double sum = 0;
 #pragma unroll

@@ -286,11 +286,6 @@ __device__ __forceinline__ void store_one(void* p, int dt, int64_t at, float v) 
     else static_cast<bf16*>(p)[at] = (bf16)v;
 }
 
-// Vectors wherever elements may start: global memory takes any alignment.
-typedef f32x4 f32x4_any __attribute__((aligned(4)));
-typedef fc::f16x4 f16x4_any __attribute__((aligned(2)));
-typedef fc::b16x4 b16x4_any __attribute__((aligned(2)));
-
 // Up to four neighbouring elements of a row, of which `left` are in it.
 __device__ __forceinline__ void store_four(void* p, int dt, int64_t at, f32x4 v, int left) {
     if (left < 4) {
@@ -298,11 +293,11 @@ __device__ __forceinline__ void store_four(void* p, int dt, int64_t at, f32x4 v,
         for (int e = 0; e < 3; ++e)
             if (e < left) store_one(p, dt, at + e, v[e]);
     } else if (dt == FC_F32) {
-        *reinterpret_cast<f32x4_any*>(static_cast<float*>(p) + at) = v;
+        *reinterpret_cast<fc::f32x4_any*>(static_cast<float*>(p) + at) = v;
     } else if (dt == FC_F16) {
-        *reinterpret_cast<f16x4_any*>(static_cast<f16*>(p) + at) = __builtin_convertvector(v, fc::f16x4);
+        *reinterpret_cast<fc::f16x4_any*>(static_cast<f16*>(p) + at) = __builtin_convertvector(v, fc::f16x4);
     } else {
-        *reinterpret_cast<b16x4_any*>(static_cast<bf16*>(p) + at) = __builtin_convertvector(v, fc::b16x4);
+        *reinterpret_cast<fc::b16x4_any*>(static_cast<bf16*>(p) + at) = __builtin_convertvector(v, fc::b16x4);
     }
 }
 
