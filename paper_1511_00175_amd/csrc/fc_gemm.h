@@ -12,9 +12,10 @@
 //   contiguous: row r's 8 chunks of 16 bytes are stored in order c ^ (r & 7);
 //               a fragment is one 16-byte read per lane.
 //   slow:       k's row of R elements is stored in blocks of 16 elements, block
-//               b at b ^ h(k), h(k) = (k & 3) | ((k >> 3) & 3) << 2; a fragment is
-//               two transposing reads (ds_read_b64_tr_b16), which hand each lane
-//               4 values along k from 4 rows of 16 elements.
+//               b at b ^ h(k), h(k) = (k & 3) | ((k >> 3) & 3) << 2 (R not a power of
+//               2: at (b + ((k >> 3) & 3)) mod R / 16); a fragment is two transposing
+//               reads (ds_read_b64_tr_b16), which hand each lane 4 values along k
+//               from 4 rows of 16 elements.
 // Rows and k beyond the operand read as zero (the buffer descriptor's bounds).
 //
 // C is computed transposed (B's fragment is the instruction's first operand),
@@ -110,6 +111,18 @@ template <int N> __device__ __forceinline__ void wait_loads() {
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
+// Where a slow operand's block b of 16 elements of k's row lies (at most 64 of k
+// apart: k, k + 4 and k + 32 agree in what is used of them).
+template <int R> __device__ __forceinline__ int slow_block(int b, int k) {
+    if constexpr ((R & (R - 1)) == 0) return b ^ (((k & 3) | ((k >> 3) & 3) << 2) & (R / 16 - 1));
+    else return (b + ((k >> 3) & 3)) % (R / 16);
+}
+// The block that lies there.
+template <int R> __device__ __forceinline__ int slow_block_at(int at, int k) {
+    if constexpr ((R & (R - 1)) == 0) return slow_block<R>(at, k);
+    else return (at + R / 16 - ((k >> 3) & 3)) % (R / 16);
+}
+
 // One wave's loads of one operand's tiles of R rows; `waves` waves share a tile.
 template <int R, bool SLOW, int WAVES, bool ONCE = false> struct TileLoads {
     static constexpr int COUNT = R / 8 / WAVES;  // 1 KiB per load
@@ -142,16 +155,13 @@ template <int R, bool SLOW, int WAVES, bool ONCE = false> struct TileLoads {
             }
         } else {
             constexpr int SLOTS = R / 8;      // 16-byte slots per k
-            constexpr int PER = 64 / SLOTS;   // k per load
             base = (uint64_t)o.p + 2 * (uint64_t)row0;
             const int cols = (left + 7) & ~7;
             tail = 2u * (cols < R ? cols : R);
 #pragma unroll
             for (int i = 0; i < COUNT; ++i) {
-                const int k = (wave * COUNT + i) * PER + lane / SLOTS;
-                const int slot = lane % SLOTS;
-                const int h = ((k & 3) | ((k >> 3) & 3) << 2) & (R / 16 - 1);
-                const int col = ((slot >> 1) ^ h) * 16 + (slot & 1) * 8;
+                const int at = (wave * COUNT + i) * 64 + lane, k = at / SLOTS, slot = at % SLOTS;
+                const int col = slow_block_at<R>(slot >> 1, k) * 16 + (slot & 1) * 8;
                 off[i] = 2 * col < (int)tail ? (uint32_t)((uint64_t)k * ldb) + 2u * col : GEMM_OUTSIDE;
             }
         }
@@ -200,7 +210,7 @@ template <typename T, int R, bool SLOW, int F> struct Fragments {
         } else {
 #pragma unroll
             for (int f = 0; f < F; ++f)
-                at[f] = (8 * g + (i >> 2)) * (2 * R) + ((((row >> 4) + f) ^ ((lane >> 2) & (R / 16 - 1))) << 5) + (i & 3) * 8;
+                at[f] = (8 * g + (i >> 2)) * (2 * R) + (slow_block<R>((row >> 4) + f, 8 * g + (i >> 2)) << 5) + (i & 3) * 8;
         }
     }
     // Fragment f of the tile at LDS address `tile`, k from 32 kk on.

@@ -423,16 +423,20 @@ __global__ __launch_bounds__(256) void pack_kernel(PackArgs a) {
     *reinterpret_cast<u16x8*>(static_cast<u16*>(a.out) + r * a.ld_out + c) = v;
 }
 
-// Tiles by size; SHORT and NARROW are for up to 64 tokens, which are bound by
+// Tiles by size; BROAD is for the gradients, where dim is often just above a multiple
+// of 256 or fills the chip's rounds better so (the first product's tiles end with more
+// work: 1003 tokens, 50001 rows of 520 took 122 us with it, 119 with LARGE; dw 94, 107
+// with MIDDLE; dx 74, 104; 8192 tokens, 8192 rows of 1280 in all 565, 657).  SHORT and NARROW are for up to 64 tokens, which are bound by
 // reading w: a compute unit reads at most about 50 GB/s, so that few rows of w are
 // read faster by more blocks.
 template <typename T, bool AS, bool BS> using Large = fc::Product<T, 256, 256, 128, 64, AS, BS>;
+template <typename T, bool AS, bool BS> using Broad = fc::Product<T, 256, 192, 128, 48, AS, BS>;
 template <typename T, bool AS, bool BS> using Middle = fc::Product<T, 128, 128, 64, 64, AS, BS>;
 template <typename T, bool AS, bool BS> using Short = fc::Product<T, 64, 128, 64, 32, AS, BS, 3>;
 template <typename T, bool AS, bool BS> using Narrow = fc::Product<T, 64, 32, 16, 32, AS, BS, 6>;
 template <typename T, bool AS, bool BS> using Once = fc::Product<T, 64, 128, 64, 32, AS, BS, 3, 0, true>;
 
-enum TileKind { LARGE, MIDDLE, SHORT, NARROW, KINDS };
+enum TileKind { LARGE, BROAD, MIDDLE, SHORT, NARROW, KINDS };
 
 constexpr int CUS = 256;
 
@@ -443,7 +447,7 @@ struct KindCost {
     double full, alone, once;
     int per;
 };
-constexpr KindCost COST[KINDS] = {{256, 256, 1.7, 1.15, 9.5, 1}, {128, 128, 0.52, 0.6, 5.0, 2}, {64, 128, 0.55, 0.6, 4.0, 2}, {64, 32, 0.2, 0.3, 4.0, 2}};
+constexpr KindCost COST[KINDS] = {{256, 256, 1.7, 1.15, 9.5, 1}, {256, 192, 1.38, 1.0, 8.0, 1}, {128, 128, 0.52, 0.6, 5.0, 2}, {64, 128, 0.55, 0.6, 4.0, 2}, {64, 32, 0.2, 0.3, 4.0, 2}};
 
 struct Choice {
     TileKind kind;
@@ -456,17 +460,20 @@ constexpr int64_t SPLIT_FLOATS = (int64_t)1 << 27;
 // The tiles of an m x n product over k, and the parts k is split into, by the
 // least estimated time; m and k are taken up to multiples of 64, so that the
 // choice is one for every list of as many 64s of tokens.
-Choice choose(int64_t m, int64_t n, int64_t k, bool few, bool may_split) {
+Choice choose(int64_t m, int64_t n, int64_t k, bool few, bool may_split, bool broad) {
     m = fc::ceil_div(m, 64) * 64;
     const int64_t total = fc::ceil_div(k, fc::GEMM_BK);
     Choice best{MIDDLE, 1, (int)total};
     double least = 1e300;
     for (int kind = few ? SHORT : LARGE; kind <= (few ? NARROW : MIDDLE); ++kind) {
+        if (kind == BROAD && !broad) continue;
         const KindCost& c = COST[kind];
         const int64_t tiles = fc::ceil_div(m, c.bm) * fc::ceil_div(n, c.bn);
-        for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+        const int fill = (int)std::min<int64_t>(64, CUS * c.per / tiles);  // as many as the chip takes at once
+        for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, fill}) {
+            if (s < 1) continue;
             const int64_t steps = fc::ceil_div(total, s), parts = fc::ceil_div(total, steps), blocks = tiles * parts;
-            if (s > 1 && (!may_split || steps < 2 || parts * m * n > SPLIT_FLOATS)) break;
+            if (s > 1 && (!may_split || steps < 2 || parts * m * n > SPLIT_FLOATS)) continue;
             const double at_once = (double)std::min<int64_t>(c.per, fc::ceil_div(blocks, CUS));
             double t = fc::ceil_div(blocks, CUS * c.per) * (steps * std::max(c.alone, c.full * at_once) + c.once);
             if (parts > 1) t += 5.0 + 8.0 * parts * m * n / 4.5e6;  // partial sums, written and read
@@ -502,6 +509,8 @@ template <typename T> hipError_t prepare_all() {
                          prepare<Narrow<T, false, false>>((const void*)logit_kernel<Narrow<T, false, false>>),
                          prepare<Once<T, false, false>>((const void*)logit_kernel<Once<T, false, false>>),
                          prepare<Large<T, false, true>>((const void*)grad_kernel<Large<T, false, true>>),
+                         prepare<Broad<T, false, true>>((const void*)grad_kernel<Broad<T, false, true>>),
+                         prepare<Broad<T, true, true>>((const void*)grad_kernel<Broad<T, true, true>>),
                          prepare<Middle<T, false, true>>((const void*)grad_kernel<Middle<T, false, true>>),
                          prepare<Short<T, false, true>>((const void*)grad_kernel<Short<T, false, true>>),
                          prepare<Narrow<T, false, true>>((const void*)grad_kernel<Narrow<T, false, true>>),
@@ -516,9 +525,9 @@ template <typename T> hipError_t prepare_all() {
 int piece_width(TileKind k) { return COST[k].bn; }
 
 // The choices of the three products for m tokens.
-Choice logit_choice(int64_t m, int64_t rows, int64_t dim) { return choose(m, rows, dim, m <= 64, false); }
-Choice dx_choice(int64_t m, int64_t rows, int64_t dim) { return choose(m, dim, rows, m <= 64, true); }
-Choice dw_choice(int64_t m, int64_t rows, int64_t dim, bool one_chunk) { return choose(rows, dim, m, false, one_chunk); }
+Choice logit_choice(int64_t m, int64_t rows, int64_t dim) { return choose(m, rows, dim, m <= 64, false, false); }
+Choice dx_choice(int64_t m, int64_t rows, int64_t dim) { return choose(m, dim, rows, m <= 64, true, true); }
+Choice dw_choice(int64_t m, int64_t rows, int64_t dim, bool one_chunk) { return choose(rows, dim, m, false, one_chunk, true); }
 
 constexpr int64_t ROWS_LIMIT = 1 << 21, LD_LIMIT = 1 << 21, TOKENS_LIMIT = (int64_t)1 << 31;
 // A w that fills the memory-side cache (256 MB) by itself is read past the caches
@@ -622,6 +631,7 @@ int run(fc_xent* p, const void* x, int64_t ldx, const void* w, int64_t ldw, cons
             g.first = true;
             g.last = c.splits == 1;
             if (c.kind == LARGE) launch_grad<Large<T, false, true>>(g, s);
+            else if (c.kind == BROAD) launch_grad<Broad<T, false, true>>(g, s);
             else if (c.kind == MIDDLE) launch_grad<Middle<T, false, true>>(g, s);
             else if (c.kind == SHORT && once) launch_grad<Once<T, false, true>>(g, s);
             else if (c.kind == SHORT) launch_grad<Short<T, false, true>>(g, s);
@@ -646,6 +656,7 @@ int run(fc_xent* p, const void* x, int64_t ldx, const void* w, int64_t ldw, cons
             g.first = t0 == 0;
             g.last = c.splits == 1 && t0 + p->chunk >= n;
             if (c.kind == LARGE) launch_grad<Large<T, true, true>>(g, s);
+            else if (c.kind == BROAD) launch_grad<Broad<T, true, true>>(g, s);
             else launch_grad<Middle<T, true, true>>(g, s);
             if (c.splits > 1) join_splits(g, c.splits);
         }

@@ -100,6 +100,8 @@ def test_large_tiles(fc, device, dtype):
     """Enough tokens, rows and columns for every product's large tiles."""
     check(fc, device, *inputs(device, 17000, 1032, 1100, dtype), dtype)
     check(fc, device, *inputs(device, 260, 4100, 4200, dtype), dtype)
+    check(fc, device, *inputs(device, 20001, 520, 1003, dtype), dtype)
+    check(fc, device, *inputs(device, 4097, 1290, 4100, dtype), dtype)
 
 
 @pytest.mark.parametrize("dtype,n,dim", [("f16", 5, 4104), ("bf16", 64, 4097)])
