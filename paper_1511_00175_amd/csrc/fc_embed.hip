@@ -223,6 +223,7 @@ struct SumArgs {
     int64_t ld_out;
     float scale;
     int accumulate;
+    int first;               // chunk of the launch's first block
     float* parts;            // per chunk: the sum that goes on from the chunk before, and the one that goes on into the next
 };
 
@@ -257,7 +258,7 @@ template <typename TI, typename TO, int V> __global__ __launch_bounds__(256) voi
     constexpr int UNROLL = 8;
     typedef Vec<TI, V> I;
     const int own = (blockIdx.y * 256 + threadIdx.x) * V, col = min(own, a.dim - V);
-    const int c = blockIdx.x, lo = c * a.chunk, hi = min(lo + a.chunk, a.n);
+    const int c = a.first + blockIdx.x, lo = c * a.chunk, hi = min(lo + a.chunk, a.n);
     uint32_t row = a.sorted[lo].x;
     if (row >= a.rows || own >= a.dim) return;
     bool from_before = c > 0 && a.sorted[lo - 1].x == row;
@@ -319,7 +320,7 @@ template <typename TO, int V> __global__ __launch_bounds__(256) void join_kernel
     __shared__ float part[4][64 * V];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int own = (blockIdx.y * 64 + lane) * V, col = min(own, a.dim - V);
-    const int c = blockIdx.x, chunks = (a.n + a.chunk - 1) / a.chunk;
+    const int c = a.first + blockIdx.x, chunks = (a.n + a.chunk - 1) / a.chunk;
     const int hi = (c + 1) * a.chunk;
     if (hi >= a.n) return;
     const uint32_t row = a.sorted[hi].x;
@@ -468,7 +469,6 @@ int lookup_body(fc_embed* p, const void* table, int tdt, int64_t ld_table, const
     const int v = vector_of(16 / std::min(st.bytes, so.bytes), p->dim);
     LookupArgs a{table, ld_table, {tokens, token_bytes, (int)n, (uint32_t)p->rows}, out, ld_out, (int)p->dim, scale, 0};
     a.per_row = pow2_at_least(fc::ceil_div(p->dim, v), 256);
-    const int64_t grid = fc::ceil_div(n, 256 / a.per_row);
     bool note;
     rc = p->order.begin(s, note);
     if (rc) return rc;
@@ -477,7 +477,13 @@ int lookup_body(fc_embed* p, const void* table, int tdt, int64_t ld_table, const
             with_width(v, [&](auto w) {
                 typedef std::remove_pointer_t<decltype(ti)> TI;
                 typedef std::remove_pointer_t<decltype(to)> TO;
-                lookup_kernel<TI, TO, decltype(w)::value><<<dim3(grid), 256, 0, s>>>(a);
+                fc::by_launches(n, a.per_row, [&](int64_t t0, int64_t count) {
+                    LookupArgs b = a;
+                    b.tokens.p = static_cast<const char*>(tokens) + t0 * token_bytes;
+                    b.tokens.n = (int)count;
+                    b.out = static_cast<char*>(out) + t0 * ld_out * so.bytes;
+                    lookup_kernel<TI, TO, decltype(w)::value><<<(unsigned)fc::ceil_div(count, 256 / a.per_row), 256, 0, s>>>(b);
+                });
             });
         });
     });
@@ -530,20 +536,25 @@ int grad_body(fc_embed* p, const void* dy, int ydt, int64_t ld_dy, const void* t
     rc = fc::hip_code(hipGetLastError());
     if (!rc && n > 0) {
         const int chunk = chunk_of(n);
-        SumArgs a{sorted, (int)n, (uint32_t)p->rows, chunk, dy, ld_dy, (int)p->dim, out, ld_out, scale, accumulate, p->parts};
+        SumArgs a{sorted, (int)n, (uint32_t)p->rows, chunk, dy, ld_dy, (int)p->dim, out, ld_out, scale, accumulate, 0, p->parts};
         const int v = vector_of(16 / sy.bytes, p->dim);
         const int chunks = (int)fc::ceil_div(n, chunk);
         with_type(odt, [&](auto* to) {
             typedef std::remove_pointer_t<decltype(to)> TO;
             with_width(v, [&](auto w) {
                 constexpr int V = decltype(w)::value;
-                const dim3 grid(chunks, (unsigned)fc::ceil_div(p->dim, 256 * V));
-                with_type(ydt, [&](auto* ti) {
-                    typedef std::remove_pointer_t<decltype(ti)> TI;
-                    sum_kernel<TI, TO, V><<<grid, 256, 0, s>>>(a);
+                fc::by_launches(chunks, 256, [&](int64_t first, int64_t count) {
+                    a.first = (int)first;
+                    const dim3 grid((unsigned)count, (unsigned)fc::ceil_div(p->dim, 256 * V));
+                    with_type(ydt, [&](auto* ti) {
+                        typedef std::remove_pointer_t<decltype(ti)> TI;
+                        sum_kernel<TI, TO, V><<<grid, 256, 0, s>>>(a);
+                    });
                 });
-                if (chunks > 1)
-                    join_kernel<TO, V><<<dim3(chunks - 1, (unsigned)fc::ceil_div(p->dim, 64 * V)), 256, 0, s>>>(a);
+                fc::by_launches(chunks - 1, 256, [&](int64_t first, int64_t count) {
+                    a.first = (int)first;
+                    join_kernel<TO, V><<<dim3((unsigned)count, (unsigned)fc::ceil_div(p->dim, 64 * V)), 256, 0, s>>>(a);
+                });
             });
         });
         rc = fc::hip_code(hipGetLastError());

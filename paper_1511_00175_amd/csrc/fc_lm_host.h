@@ -8,6 +8,7 @@
 #include <initializer_list>
 #include <new>
 
+#include "fc_launches.h"
 #include "fc_lm.h"
 
 namespace fc {
