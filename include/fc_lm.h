@@ -54,7 +54,7 @@ extern "C" {
 typedef struct fc_embed fc_embed;
 
 /* A plan for tables of `rows` rows of `dim` elements and up to `max_tokens`
- * tokens a gradient (1 <= rows < 2^31, 1 <= dim <= 2^20, 0 <= max_tokens < 2^31).
+ * tokens a gradient (1 <= rows < 2^31, 1 <= dim <= 2^20, 0 <= max_tokens <= 2^30).
  * Its workspace holds the sorted tokens and partial sums: 16 + dim / 4 bytes per
  * token (dim for the first 4096). */
 int fc_embed_create(fc_embed** plan, int64_t rows, int64_t dim, int64_t max_tokens);

@@ -445,6 +445,9 @@ struct fc_embed {
 namespace {
 
 constexpr int64_t LIMIT = (int64_t)1 << 31;
+// Tokens of a gradient: places in the sorted list, and the ends of its chunks, are
+// 32-bit numbers (above 2^31 - 32 tokens the last chunk's end would not be).
+constexpr int64_t TOKENS_LIMIT = (int64_t)1 << 30;
 constexpr int64_t DIM_LIMIT = (int64_t)1 << 20;  // column blocks of a launch
 
 // Entries of the sorted list per chunk: enough chunks to fill the chip, long
@@ -570,7 +573,7 @@ extern "C" {
 int fc_embed_create(fc_embed** plan, int64_t rows, int64_t dim, int64_t max_tokens) {
     if (!plan) return FC_EINVAL;
     *plan = nullptr;
-    if (rows < 1 || dim < 1 || max_tokens < 0 || rows >= LIMIT || dim > DIM_LIMIT || max_tokens >= LIMIT) return FC_EINVAL;
+    if (rows < 1 || dim < 1 || max_tokens < 0 || rows >= LIMIT || dim > DIM_LIMIT || max_tokens > TOKENS_LIMIT) return FC_EINVAL;
     return fc::no_throw([&] {
         fc_embed* p = new fc_embed;
         p->rows = rows;
