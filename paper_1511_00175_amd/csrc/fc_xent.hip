@@ -574,8 +574,11 @@ int run(fc_xent* p, const void* x, int64_t ldx, const void* w, int64_t ldw, cons
         split_kernel<<<(unsigned)fc::ceil_div((int64_t)g.m * g.n, 256), 256, 0, s>>>(q);
     };
     auto pack = [&](const void* in, int64_t ld, void* out, int64_t rows, const void* mask) {
-        PackArgs a{in, ld, out, p->ldp, rows, (int)p->dim, mask, target_bytes, (int)p->rows};
-        pack_kernel<<<(unsigned)fc::ceil_div(rows * (p->ldp / 8), 256), 256, 0, s>>>(a);
+        fc::by_launches(rows, p->ldp / 8, [&](int64_t r0, int64_t count) {
+            PackArgs a{static_cast<const char*>(in) + r0 * ld * 2, ld, static_cast<char*>(out) + r0 * p->ldp * 2, p->ldp, count, (int)p->dim,
+                       mask ? static_cast<const char*>(mask) + r0 * target_bytes : nullptr, target_bytes, (int)p->rows};
+            pack_kernel<<<(unsigned)fc::ceil_div(count * (p->ldp / 8), 256), 256, 0, s>>>(a);
+        });
     };
     if (p->pack) {
         pack(w, ldw, p->w, p->rows, nullptr);
@@ -688,7 +691,11 @@ int call(fc_xent* p, const void* x, int64_t ldx, const void* w, int64_t ldw, con
     rc = p->order.begin(s, note);
     if (rc) return rc;
     if (n == 0) {
-        if (dw) zero_kernel<<<(unsigned)fc::ceil_div(p->rows * p->dim, 256), 256, 0, s>>>(dw, wdt, p->rows, p->dim, lddw);
+        if (dw)
+            fc::by_launches(p->rows, p->dim, [&](int64_t r0, int64_t count) {
+                zero_kernel<<<(unsigned)fc::ceil_div(count * p->dim, 256), 256, 0, s>>>(static_cast<char*>(dw) + r0 * lddw * fc::dtype_bytes(wdt), wdt,
+                                                                                        count, p->dim, lddw);
+            });
         rc = fc::hip_code(hipGetLastError());
     } else if (p->dtype == FC_F16) {
         rc = run<f16>(p, x, ldx, w, ldw, targets, target_bytes, n, scale, loss, dx, xdt, lddx, dw, wdt, lddw, s);
