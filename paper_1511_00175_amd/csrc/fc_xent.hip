@@ -41,8 +41,9 @@ extern __shared__ __align__(1024) char lds[];
 
 constexpr float LOG2E = 1.44269504088896341f;
 
-// d is stored times this: fp16 then keeps probabilities down to 2^-29 with all
-// their bits, and its largest, 1, is still in range.  bf16 needs no scale.
+// Numerators of 16 bits and d are stored times this: fp16 then keeps what is down to
+// 2^-29 of a piece's largest (a numerator) or of 1 (d) with all its bits, and the
+// largest, 1, is still in range.  bf16 needs no scale.
 template <typename T> constexpr float D_SCALE = 1.f;
 template <> constexpr float D_SCALE<f16> = 32768.f;
 
@@ -153,7 +154,7 @@ template <typename P> __global__ __launch_bounds__(P::THREADS, P::THREADS / 256)
                 if (P::BM <= FINE && a.fine)
                     *reinterpret_cast<f32x4*>(static_cast<float*>(a.numer) + to + 16 * j) = q;
                 else
-                    *reinterpret_cast<typename Half<T>::v4*>(static_cast<T*>(a.numer) + to + 16 * j) = __builtin_convertvector(q, typename Half<T>::v4);
+                    *reinterpret_cast<typename Half<T>::v4*>(static_cast<T*>(a.numer) + to + 16 * j) = __builtin_convertvector(q * D_SCALE<T>, typename Half<T>::v4);
             }
         }
         sum += __shfl_xor(sum, 16);
@@ -258,7 +259,7 @@ template <typename T, typename N> __global__ __launch_bounds__(256) void diff_ke
         const int t = min(t0 + i, a.n - 1);
         x[i] = *reinterpret_cast<const n8*>(static_cast<const N*>(a.numer) + t * a.ld + col);
         row[i] = a.row[t];
-        f[i] = exp_(a.stats[(int64_t)piece * a.n + t].x - a.lse[t]) * D_SCALE<T>;
+        f[i] = exp_(a.stats[(int64_t)piece * a.n + t].x - a.lse[t]) * (sizeof(N) == 4 ? D_SCALE<T> : 1.f);  // 16-bit ones have the scale
     }
 #pragma unroll
     for (int i = 0; i < DIFF_ROWS; ++i) {
