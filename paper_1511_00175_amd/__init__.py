@@ -8,6 +8,8 @@ back to every worker (Fig. 3 caption).
 The work is done by HIP kernels behind the C ABI of include/fc.h; this package
 only marshals torch tensors (device memory and the current stream) into it.
 """
+import importlib
+import os
 import weakref
 
 from . import _fc
@@ -20,8 +22,25 @@ from ._fc import (FC_F16, FC_F32, FC_NOALLOC_MAX_ELEMS, FC_ORDER_LINEAR, FC_ORDE
 __all__ = ["Plan", "FcError", "fc_plan_create", "fc_plan_destroy", "fc_plan_query", "fc_plan_set_timing",
            "fc_plan_read_timing", "fc_plan_balance", "fc_tree_reduce", "fc_sgd_step", "fc_broadcast", "fc_step",
            "fc_step_noalloc", "fc_strerror",
-           "fc_lr_at", "fc_train", "lr_policy", "lr_at", "fc_read_probe", "fc_read_probe_blocks", "read_probe",
-           "Embedding", "CrossEntropy", "Muon"]
+           "fc_lr_at", "fc_train", "lr_policy", "lr_at", "fc_read_probe", "fc_read_probe_blocks", "read_probe"]
+
+# Classes of lm.py, whose library (libfc_lm.so) is loaded when one of them is first
+# used: Plan needs libfc.so alone.
+_LM = ("Embedding", "CrossEntropy", "Muon")
+if os.path.exists(os.path.join(_fc.PKG, "libfc_lm.so")):
+    __all__ += _LM
+
+
+def __getattr__(name):
+    if name != "lm" and name not in _LM:
+        raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
+    lm = importlib.import_module(".lm", __name__)
+    globals().update((n, getattr(lm, n)) for n in _LM)
+    return globals()[name]
+
+
+def __dir__():
+    return sorted({*globals(), *_LM})
 
 
 def lr_at(iter, batch, **policy):
@@ -313,6 +332,3 @@ class Plan:
         rc = _lib_step_noalloc(self.handle, g, wp, vp, lr, mu, wd, int(batch), op, bp, _stream(stream))
         if rc:
             raise FcError("fc_step_noalloc", rc)
-
-
-from .lm import CrossEntropy, Embedding, Muon  # noqa: E402,F401
