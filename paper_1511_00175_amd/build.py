@@ -17,7 +17,6 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libfc.so")
-LIB_LM = os.path.join(PKG, "libfc_lm.so")
 SOURCES = ["fc_reduce_f32.hip", "fc_reduce_f16.hip", "fc_update.hip", "fc_api.cpp"]
 SOURCES_LM = ["fc_embed.hip", "fc_xent.hip", "fc_muon.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -62,8 +61,8 @@ def _compile(src, obj, extra):
 
 
 def build(out=LIB, extra=()):
-    """Compile every source and link the shared libraries; returns the first's
-    path."""
+    """Compile every source and link the shared libraries, libfc.so as `out` and
+    libfc_lm.so beside it; returns the first's path."""
     objdir = os.path.join(PKG, "_build")
     os.makedirs(objdir, exist_ok=True)
     sources = SOURCES + SOURCES_LM
@@ -79,7 +78,7 @@ def build(out=LIB, extra=()):
     spill = [n for n, u in usage.items() if u.get("ScratchSize", 0)]
     if spill:
         raise RuntimeError("kernels using scratch memory: " + ", ".join(spill))
-    for lib, part in ((out, objs[:len(SOURCES)]), (LIB_LM, objs[len(SOURCES):])):
+    for lib, part in ((out, objs[:len(SOURCES)]), (os.path.join(os.path.dirname(out), "libfc_lm.so"), objs[len(SOURCES):])):
         tmp = lib + ".tmp"
         subprocess.run([HIPCC, "-shared", "-fPIC", f"--offload-arch={ARCH}", *part, "-o", tmp], check=True)
         os.replace(tmp, lib)
