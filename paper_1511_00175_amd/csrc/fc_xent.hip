@@ -531,13 +531,20 @@ Choice dx_choice(int64_t m, int64_t rows, int64_t dim) { return choose(m, dim, r
 Choice dw_choice(int64_t m, int64_t rows, int64_t dim, bool one_chunk) { return choose(rows, dim, m, false, one_chunk, true); }
 
 constexpr int64_t ROWS_LIMIT = 1 << 21, LD_LIMIT = 1 << 21, TOKENS_LIMIT = (int64_t)1 << 31;
-// A w that fills the memory-side cache (256 MB) by itself is read past the caches
-// (up to 64 tokens, when every tile of it is read once).  16 tokens, fp16, us,
-// through the caches / past them, first with 300 MB written between the calls,
-// then call after call: w of 268 MB 108 / 64 and 44 / 60, 403 MB 127 / 80 and
-// 84 / 75, 1074 MB 217 / 163 and 177 / 159; with dx 268 MB 197 / 158 and 132 / 156,
-// 1074 MB 635 / 551 and 593 / 543.
-constexpr int64_t CACHE_BYTES = (int64_t)1 << 28;
+// A w well beyond the memory-side cache (256 MB) is read past the caches (up to 64
+// tokens, when every tile of it is read once): from the size on at which that is
+// faster or as fast whether the caches hold something else or the end of w.  16
+// tokens, fp16, rows of 2048, us, past the caches / through them, first with 1 GB read
+// between the calls, then call after call:
+//   w of   losses alone     with dx, which reads w again
+//   134 MB 39/42   36/28    92/91   91/77
+//   268 MB 65/70   62/47   162/160 160/136
+//   302 MB 79/83   77/75   185/187 182/163
+//   336 MB 80/86   78/84   198/200 195/182
+//   403 MB 99/104  94/103  248/254 246/234
+//   537 MB 121/129 118/129 319/335 316/321
+// (Where the caches hold 1 GB of results not yet written, 268 MB take 65 / 125.)
+constexpr int64_t CACHE_BYTES = (int64_t)5 << 26, CACHE_BYTES_DX = (int64_t)1 << 29;
 constexpr int64_t NUMER_BYTES = (int64_t)4 << 30;
 constexpr int64_t CHUNK_LIMIT = 1 << 18;  // a launch has at most 65535 blocks along y, of 8 tokens each
 
@@ -587,7 +594,7 @@ int run(fc_xent* p, const void* x, int64_t ldx, const void* w, int64_t ldw, cons
         ldw = p->ldp;
     }
     const int dimk = (int)(p->pack ? p->ldp : p->dim);
-    const bool once = p->rows * dimk * 2 >= CACHE_BYTES;
+    const bool once = p->rows * dimk * 2 >= (dx ? CACHE_BYTES_DX : CACHE_BYTES);
     for (int64_t t0 = 0; t0 < n; t0 += p->chunk) {
         const int m = (int)std::min(p->chunk, n - t0);
         const void* xt = static_cast<const char*>(x) + t0 * ldx * 2;
