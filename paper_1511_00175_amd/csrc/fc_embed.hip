@@ -3,19 +3,22 @@
 // lookup: out[t] = scale * table[token[t]].  One pass; bounded by the bytes of
 //   the rows read and written: 32768 rows of 2048 fp16 take 48 us (5.6 TB/s), 5001 odd
 //   rows of 1001 from bf16 to fp32 7 us (4.3 TB/s), one row 1.8 (an empty launch's
-//   time; 5.6 with the host's part of a call).
+//   time; 6.2 with the host's part of a call).
 // grad: dtable[r] = scale * sum of dy[t] over token[t] == r.  The tokens are
 //   sorted by a stable radix sort on their (row, t) pairs; then the sorted list
-//   is cut into chunks of CHUNK entries, each summed by its own threads in order.
+//   is cut into chunks of 8 or 32 entries, each summed by its own threads in order.
 //   A row whose entries lie in one chunk is written there; the parts of a row
-//   that runs over chunks go to a workspace and are added in order by a second
+//   that runs over chunks go to a workspace and are added in a fixed order by a second
 //   kernel.  No atomics on sums: the same inputs give the same bits.  Bounded by
 //   the bytes of dy and of the whole table's gradient, of which the rows without
 //   a token are most: the zeros are stored by blocks that run beside the sort's
 //   few ones, a share in each of its launches.  32768 tokens of 2048 fp16 into
-//   65536 rows of fp32 take 168 us: 86 of sort and zeros (537 MB, 6.2 TB/s), 76 of
+//   65536 rows of fp32 take 168 us: 87 of sort and zeros (537 MB, 6.2 TB/s), 74 of
 //   sums and 8 of joins; in all 671 MB at 4.0 TB/s, where a large copy has 4.8.  256
 //   tokens of 1001 fp32 into 1000 rows: 12 us, three launches one after the other.
+//   Every block of a sort's second launch adds up all blocks' counts, so that very
+//   long lists are bound by that: rows of 1024 fp16, 2^20 tokens 0.92 ms, 2^22 3.6, 2^24
+//   24.6 (2.6, 2.5 and 1.4 TB/s).
 #include <algorithm>
 
 #include "fc_lm_host.h"
@@ -251,7 +254,7 @@ template <typename TO, int V> __device__ __forceinline__ void store_row(const Su
 // Sums of one chunk of the sorted list; a thread holds V columns.  The entries
 // are the same for every thread of a block, so keys and branches are uniform;
 // UNROLL rows are loaded before the first is added: a row alone would wait for
-// each load.  Bound by reading dy and writing rows (76 us for 32768 tokens of 2048
+// each load.  Bound by reading dy and writing rows (74 us for 32768 tokens of 2048
 // fp16, 402 MB at most: the rows written again after their zeros among them);
 // 4 or 16 rows ahead, narrower vectors and other chunks were no faster.
 template <typename TI, typename TO, int V> __global__ __launch_bounds__(256) void sum_kernel(SumArgs a) {

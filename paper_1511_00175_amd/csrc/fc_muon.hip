@@ -10,11 +10,13 @@
 // operations for s x l (A and B are symmetric: only tiles on and above the
 // diagonal are computed, the others are their mirror image); the bytes are
 // small beside them, so the products are bound by the matrix cores where the
-// matrices fill the chip and by their longest k loop where they do not.
+// matrices fill the chip and by their longest k loop where they do not: 5 matrices of
+// 75 x 8073 with 3 parts take 0.66 ms, A's products most of it, each tile alone with 381
+// steps of 64 of k (plain fp32 products 0.54).
 //
-// Measured, 5 steps: all of AlexNet's layers, fp32 to bf16, 4.1 TFLOP in 4.4 ms (0.94
-// PFLOP/s); 4096 x 4096 with 3 parts, fp32, 4.1 TFLOP in 3.9 ms (1.06); GoogLeNet's 58
-// matrices 0.28 ms in 17 launches, 0.04 TFLOP, bound by each launch's longest tile;
+// Measured, 5 steps: all of AlexNet's layers, fp32 to bf16, 4.1 TFLOP in 4.5 ms (0.91
+// PFLOP/s); 4096 x 4096 with 3 parts, fp32, 4.1 TFLOP in 4.0 ms (1.02); GoogLeNet's 58
+// matrices 0.29 ms in 17 launches, 0.04 TFLOP, bound by each launch's longest tile;
 // 96 x 363 in one block 58 us (93 in 17 launches), bound by latency.
 //
 // Numbers.  Everything is fp16 times a power of two that puts the largest
@@ -25,8 +27,12 @@
 // only along directions X already has -- a X, which carries X's weak directions
 // (a rounding there would be noise of full rank, grown by 3.4 a step), is formed
 // from both halves.  With 3 parts every operand is such a sum and a product is
-// high * high + high * low + low * high: fp32's accuracy for 3 times the work;
-// the sums are then taken in runs of 512 of k.  A matrix of at most 32 rows or
+// high * high + high * low + low * high: fp32's accuracy for 3 times the work.
+// Sums are taken in runs of 512 of k, but for tiles of 256 x 256: X's of 3 parts
+// are one chain of 3 s terms there (fp32 results, error relative to the norm, in
+// 256 x 256 tiles / in 128 x 128 with runs / plain fp32: 4096 x 4096 1.6e-6 / 5.7e-7 /
+// 4.4e-6, 2048 x 8192 1.2e-6 / 5.9e-7 / 3.1e-6; the time 3.91 / 4.35 ms and 2.49 /
+// 2.68).  A matrix of at most 32 rows or
 // columns always has 3 parts: roundings average out over few terms only (with one
 // part the products' error was 1.0 times a bf16 result's own at 16 x 20, 0.7 at
 // 64 x 64, 0.4 at 512 x 512), and its launches are too short for the work to matter.
@@ -303,8 +309,9 @@ struct ProductArgs {
     Output to;
 };
 
-// 4096 x 4096, fp16, a product's launch: with 3 parts A 255 us, B 267, X 379 (0.81, 0.77
-// and 1.09 PFLOP/s: A's and B's 253 tiles of 192 x 192 take one round of the chip); with
+// 4096 x 4096, fp16, a product's launch: with 3 parts A 257 us, B 271, X 390 (0.80, 0.76
+// and 1.06 PFLOP/s, the matrix cores busy 56%, 53% and 68% of a unit's cycles at 1.66 to 1.8
+// GHz: A's and B's 253 tiles of 192 x 192 take one round of the chip); with
 // one part X 141, of which its end 41: it reads and writes X's 8 bytes per element,
 // and no other block's products run beside it.
 template <typename P, int STAGE> __global__ __launch_bounds__(P::THREADS, 2) void product_kernel(ProductArgs a) {
@@ -757,9 +764,9 @@ template <int ST> hipError_t prepare_whole() {
     return hipFuncSetAttribute((const void*)whole_kernel<ST>, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
 }
 
-// By fc::TileKind.  LARGE has no registers left for sums in runs, so symmetric
-// products of fp32's accuracy do without it.  BROAD's 192 is no power of two,
-// which slow operands need: it serves the symmetric products alone.
+// By fc::TileKind.  LARGE has no registers left for sums in runs: symmetric products
+// of fp32's accuracy do without it, X's take it for its speed.  BROAD serves the
+// symmetric products alone; for X it has not been measured.
 template <bool BS> using Large = fc::Product<f16, 256, 256, 128, 64, false, BS>;
 template <bool BS> using Broad = fc::Product<f16, 192, 192, 96, 48, false, BS, 2, 8>;
 template <bool BS> using Middle = fc::Product<f16, 128, 128, 64, 64, false, BS, 2, 8>;

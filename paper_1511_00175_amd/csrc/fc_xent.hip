@@ -4,7 +4,8 @@
 //   d = softmax(l) - onehot(y), dx = scale d w, dw = scale d^T x
 //
 // The products are 2 tokens rows dim operations each and bound everything but
-// short lists, where reading w does.  The logits are never stored.  A block of the
+// short lists, where reading w does.  The logits are never stored, but for gradients
+// 16 bits per token and row are.  A block of the
 // first product holds a piece of the vocabulary for its tokens in fp32: it takes
 // the piece's maximum m and sum of exponentials, keeps both (8 bytes), the
 // target's logit, and, when gradients are wanted, the numerators exp(l - m) in 16
@@ -17,11 +18,11 @@
 // Tokens go through in chunks so that the numerators take at most 4 GiB; with
 // more than one chunk, dw is summed in fp32 over them and rounded after the last.
 //
-// Measured, fp16, 8192 tokens, 131072 rows of 2048: 12.2 ms for 13.2 TFLOP (1.08
-// PFLOP/s; a library's three products of these shapes alone 10.9): the first
-// product 4.1 ms, dw 3.9, dx 3.4, the pass from numerators to d 0.82 (4.3 GB), join
-// 0.03, the copy of x 0.02.  bf16, 24 tokens, 65536 rows of 2048, losses only: 61 us,
-// of which the product 56 (268 MB at 4.8 TB/s).
+// Measured, fp16, 8192 tokens, 131072 rows of 2048: 12.6 ms for 13.2 TFLOP (1.05
+// PFLOP/s; a library's three products of these shapes alone 10.9); in a trace (13.4
+// in all) the first product 4.5 ms, dw 4.3, dx 3.8, the pass from numerators to d 0.81
+// (4.3 GB), join 0.02, the copy of x 0.02.  bf16, 24 tokens, 65536 rows of 2048, losses
+// only: 67 us with other data in the caches (268 MB at 4.0 TB/s), 47 call after call.
 #include <algorithm>
 
 #include "fc_gemm.h"
@@ -47,6 +48,7 @@ constexpr float LOG2E = 1.44269504088896341f;
 template <typename T> constexpr float D_SCALE = 1.f;
 template <> constexpr float D_SCALE<f16> = 32768.f;
 
+// Results below 2^-126 are zero.
 __device__ __forceinline__ float exp_(float x) { return __builtin_amdgcn_exp2f(x * LOG2E); }
 
 __device__ __forceinline__ int64_t target_of(const void* p, int bytes, int64_t t) {
@@ -74,10 +76,13 @@ struct LogitArgs {
     int tm, tn;
 };
 
-// Bound by the matrix cores where dim is long (2048: 1.07 PFLOP/s) and by its
-// end, the numerators' stores most, where it is short: 1003 tokens, 50001 rows of 520,
-// bf16: 114 us, 89 without those stores (100 MB), 113 without the exponentials; the
-// blocks of one round end together, so that stores do not run beside products.
+// Where dim is long (2048: 4.5 ms in a trace, 0.98 PFLOP/s) the matrix cores are busy
+// 57% of a unit's cycles, at the 1.55 GHz that the card then runs at, with no LDS conflicts
+// and 80% of the reads in L2; the rest is tiles' starts and ends and the meetings of
+// a block's waves.  Where dim is short it is bound by its end, the numerators' stores
+// most: 1003 tokens, 50001 rows of 520, bf16: 114 us, 89 without those stores (100 MB),
+// 113 without the exponentials; the blocks of one round end together, so that stores do
+// not run beside products.
 template <typename P> __global__ __launch_bounds__(P::THREADS, P::THREADS / 256) void logit_kernel(LogitArgs a) {
     typedef typename P::T T;
     int ti, tj;
@@ -243,7 +248,7 @@ constexpr int DIFF_ROWS = 8;
 
 // A block's 256 threads hold 8 columns each, of DIFF_ROWS tokens one after the
 // other, whose stats are neighbours in memory.  Bound by HBM: 8192 tokens of 131072
-// rows 0.82 ms, 4.3 GB at 5.2 TB/s.
+// rows 0.81 ms, 4.3 GB at 5.3 TB/s.
 template <typename T, typename N> __global__ __launch_bounds__(256) void diff_kernel(DiffArgs a) {
     typedef typename Half<T>::v8 v8;
     typedef N n8 __attribute__((ext_vector_type(8)));
@@ -317,9 +322,10 @@ struct GradArgs {
     int tm, tn;
 };
 
-// Bound by the matrix cores: 8192 tokens, 131072 rows of 2048 take 3.4 ms for dx and
-// 3.9 for dw (1.29 and 1.13 PFLOP/s).  Tiles in groups of 8 rows keep what the blocks
-// of an XCD read in its L2.  Few tokens give few tiles: k is then split.
+// 8192 tokens, 131072 rows of 2048 take 3.8 ms for dx and 4.3 for dw in a trace (1.17 and
+// 1.02 PFLOP/s): the matrix cores are busy 69% and 60% of a unit's cycles, at 1.54 and 1.66
+// GHz.  Tiles in groups of 8 rows keep what the blocks of an XCD read in its L2 (80% hits).
+// Few tokens give few tiles: k is then split.
 template <typename P> __global__ __launch_bounds__(P::THREADS, P::THREADS / 256) void grad_kernel(GradArgs a) {
     int ti, tj;
     fc::tile_place(fc::xcd_order(blockIdx.x, a.tm * a.tn), a.tm, a.tn, 8, ti, tj);
@@ -426,10 +432,12 @@ __global__ __launch_bounds__(256) void pack_kernel(PackArgs a) {
 
 // Tiles by size; BROAD is for the gradients, where dim is often just above a multiple
 // of 256 or fills the chip's rounds better so (the first product's tiles end with more
-// work: 1003 tokens, 50001 rows of 520 took 122 us with it, 119 with LARGE; dw 94, 107
-// with MIDDLE; dx 74, 104; 8192 tokens, 8192 rows of 1280 in all 565, 657).  SHORT and NARROW are for up to 64 tokens, which are bound by
-// reading w: a compute unit reads at most about 50 GB/s, so that few rows of w are
-// read faster by more blocks.
+// work: 1003 tokens, 50001 rows of 520 took 122 us with it, 119 with LARGE; dx 74, 104
+// with MIDDLE; 8192 tokens, 8192 rows of 1280 in all 565, 657).  The estimate is not always
+// right: for dw of the 1003 tokens it takes MIDDLE (115 us in a trace, the whole call 355
+// to 360), with which BROAD's call takes 341 to 350.  SHORT and NARROW are for up to 64
+// tokens, which are bound by reading w: a compute unit reads at most about 50 GB/s, so
+// that few rows of w are read faster by more blocks.
 template <typename T, bool AS, bool BS> using Large = fc::Product<T, 256, 256, 128, 64, AS, BS>;
 template <typename T, bool AS, bool BS> using Broad = fc::Product<T, 256, 192, 128, 48, AS, BS>;
 template <typename T, bool AS, bool BS> using Middle = fc::Product<T, 128, 128, 64, 64, AS, BS>;

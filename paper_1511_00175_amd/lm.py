@@ -173,7 +173,12 @@ class CrossEntropy(_Handle):
     """Softmax cross entropy over a vocabulary of `rows` rows of `dim` elements
     (fc_xent), from the last layer's outputs x (tokens, dim) and the rows w, both
     of `dtype` ("f16" or "bf16"), for up to `max_tokens` tokens.  The logits are
-    not kept; `chunk` tokens (0: as many as fit) go through together.
+    not stored, but for gradients 16 bits of each are; `chunk` tokens (0: as many as
+    fit) go through together.  Gradients of more than 64 tokens at a time take d in
+    x's type; with `chunk` of at most 64 it keeps twice those bits, for more time.
+
+    x and w lie on 16 bytes with row strides of a multiple of 8, unless dim is no
+    multiple of 8.
 
     Targets outside [0, rows) are padding: loss 0, and no gradient."""
 
