@@ -1,7 +1,7 @@
 /*
- * fc_lm.h -- C ABI of the operators at the ends of a language model and of its
- * matrix update, for MI355X (gfx950): what produces the gradients that fc.h
- * aggregates, and what else may consume their sum.
+ * fc_lm.h -- C ABI of the operators at the ends of a language model, within its
+ * blocks and of its matrix update, for MI355X (gfx950): what produces the gradients
+ * that fc.h aggregates, and what else may consume their sum.
  *   fc_embed : scaled rows of a table for a list of tokens, and the table's
  *              gradient, summed token by token in sorted order
  *   fc_xent  : softmax cross entropy over a vocabulary, computed in pieces of
@@ -9,6 +9,10 @@
  *              (for which 16-bit exponentials are kept, see fc_xent_create)
  *   fc_muon  : momentum updates made orthogonal by Newton-Schulz products,
  *              for every matrix of a flat parameter vector at once
+ *   fc_norm  : the norms before and after a block with its gate and residual
+ *              scale, and their gradients
+ *   fc_ckpt  : activations kept in 8 bits, and a weight's gradient from them
+ *   fc_mxfp  : matrices in microscaled 4-bit floating point, and their products
  *
  * Conventions for every entry point, as in fc.h:
  *   - Buffers are device pointers owned by the caller.  A plan owns its tables
@@ -165,6 +169,74 @@ int fc_muon_orthogonalize(fc_muon* plan, const void* g, int g_dtype, void* out, 
  *   w' = w - lr_j * (sqrt(max(1, rows / cols)) * O + wd_j * w)
  * O at the plan's accuracy (the plan's dtype), all else fp32. */
 int fc_muon_step(fc_muon* plan, float* w, float* v, const float* g, float lr, float mu, float wd, int batch, void* stream);
+
+/* ---- norms around a block ------------------------------------------------ */
+
+/* N(x) of a row x of D = `dim` elements: (x - m) / sqrt(mean((x - m)^2) + eps), m
+ * the row's mean (FC_NORM_LAYER) or 0 (FC_NORM_RMS). */
+#define FC_NORM_RMS 0
+#define FC_NORM_LAYER 1
+
+/* What a gate g multiplies by: a(g) = g, 1 / (1 + exp(-g)) or g / (1 + exp(-g)). */
+#define FC_GATE_NONE 0
+#define FC_GATE_SIGMOID 1
+#define FC_GATE_SILU 2
+
+typedef struct fc_norm fc_norm;
+
+/* A plan for rows of `dim` elements (1 to 16384) and gradients of up to `max_tokens`
+ * of them (0 to 2^31 - 1).
+ *   dtype          : of the block's side: b, y, a gate per token and their gradients
+ *   residual_dtype : of the residual's side: h, x, out and their gradients; `dtype`
+ *                    or FC_F32
+ *   kind, gate     : as above; eps > 0
+ * Per-channel vectors (weights, a gate that is one) are dim contiguous fp32 elements, as
+ * the flat vectors of fc.h hold them; their gradients are of a type that the call names.
+ * A weight may be null: 1.  Everything is computed in fp32 and rounded once, statistics
+ * included: the squares of a row must not run past its range.  Sums over tokens are
+ * fp32, in an order that depends on n and dim alone.  The workspace holds up to 1024
+ * rows of partial sums of two vectors, 8 bytes per element of a row. */
+int fc_norm_create(fc_norm** plan, int64_t dim, int64_t max_tokens, int dtype, int residual_dtype, int kind, float eps,
+                   int gate);
+void fc_norm_destroy(fc_norm* plan);
+
+/* Before a block: y[t, :] = weight * N(x[t, :]), t < n < 2^31. */
+int fc_norm_before(fc_norm* plan, const void* x, int64_t ld_x, int64_t n, const float* weight, void* y,
+                   int64_t ld_y, void* stream);
+
+/* After it: out[t, :] = h[t, :] + scale * a(gate) * weight * N(b[t, :]).  gate is null
+ * (a = 1), a vector (ld_gate 0) or n rows of the plan's dtype, ld_gate apart. */
+int fc_norm_after(fc_norm* plan, const void* h, int64_t ld_h, const void* b, int64_t ld_b, int64_t n, const void* gate,
+                  int64_t ld_gate, const float* weight, float scale, void* out, int64_t ld_out, void* stream);
+
+/* Between two blocks: out as fc_norm_after's, y[t, :] = next_weight * N(out[t, :]) of out as
+ * it is stored, in one pass. */
+int fc_norm_between(fc_norm* plan, const void* h, int64_t ld_h, const void* b, int64_t ld_b, int64_t n, const void* gate,
+                    int64_t ld_gate, const float* weight, const float* next_weight, float scale, void* out,
+                    int64_t ld_out, void* y, int64_t ld_y, void* stream);
+
+/* The gradients of fc_norm_before: dx = dout + N's of weight * dy (dout, the gradient
+ * that comes by the residual, may be null: 0), and dweight = (accumulate ? dweight : 0) +
+ * the sum over t of dy * N(x) (may be null: not wanted).  n <= max_tokens here and below. */
+int fc_norm_before_grad(fc_norm* plan, const void* x, int64_t ld_x, const void* dy, int64_t ld_dy, const void* dout,
+                        int64_t ld_dout, int64_t n, const float* weight, void* dx, int64_t ld_dx, void* dweight,
+                        int dvec_dtype, int accumulate, void* stream);
+
+/* The gradients of fc_norm_after (that of h is dout itself): db; dgate, a vector where the
+ * gate is one (accumulate: added to) and else n rows of the plan's dtype ld_dgate apart
+ * (written), may be null; dweight may be null. */
+int fc_norm_after_grad(fc_norm* plan, const void* b, int64_t ld_b, const void* dout, int64_t ld_dout, int64_t n,
+                       const void* gate, int64_t ld_gate, const float* weight, float scale, void* db,
+                       int64_t ld_db, void* dgate, int64_t ld_dgate, void* dweight, int dvec_dtype, int accumulate,
+                       void* stream);
+
+/* The gradients of fc_norm_between, of both outputs (dout may be null: 0): dh, which is
+ * out's whole gradient, as well; dnext is next_weight's. */
+int fc_norm_between_grad(fc_norm* plan, const void* out, int64_t ld_out, const void* b, int64_t ld_b, const void* dy,
+                         int64_t ld_dy, const void* dout, int64_t ld_dout, int64_t n, const void* gate, int64_t ld_gate,
+                         const float* weight, const float* next_weight, float scale, void* dh, int64_t ld_dh,
+                         void* db, int64_t ld_db, void* dgate, int64_t ld_dgate, void* dweight, void* dnext, int dvec_dtype,
+                         int accumulate, void* stream);
 
 #ifdef __cplusplus
 }

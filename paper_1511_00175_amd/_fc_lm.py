@@ -8,6 +8,8 @@ from ._fc import PKG
 
 LIB_PATH = os.path.join(PKG, "libfc_lm.so")
 FC_BF16 = 2
+FC_NORM_RMS, FC_NORM_LAYER = 0, 1
+FC_GATE_NONE, FC_GATE_SIGMOID, FC_GATE_SILU = 0, 1, 2
 
 
 class fc_matrix(ctypes.Structure):
@@ -39,6 +41,17 @@ lib.fc_muon_destroy.argtypes = [_vp]
 lib.fc_muon_destroy.restype = None
 lib.fc_muon_orthogonalize.argtypes = [_vp, _vp, _i, _vp, _vp]
 lib.fc_muon_step.argtypes = [_vp, _vp, _vp, _vp, _f, _f, _f, _i, _vp]
+lib.fc_norm_create.argtypes = [_pp, _l, _l, _i, _i, _i, _f, _i]
+lib.fc_norm_destroy.argtypes = [_vp]
+lib.fc_norm_destroy.restype = None
+lib.fc_norm_before.argtypes = [_vp, _vp, _l, _l, _vp, _vp, _l, _vp]
+lib.fc_norm_after.argtypes = [_vp, _vp, _l, _vp, _l, _l, _vp, _l, _vp, _f, _vp, _l, _vp]
+lib.fc_norm_between.argtypes = [_vp, _vp, _l, _vp, _l, _l, _vp, _l, _vp, _vp, _f, _vp, _l, _vp, _l, _vp]
+lib.fc_norm_before_grad.argtypes = [_vp, _vp, _l, _vp, _l, _vp, _l, _l, _vp, _vp, _l, _vp, _i, _i, _vp]
+lib.fc_norm_after_grad.argtypes = [_vp, _vp, _l, _vp, _l, _l, _vp, _l, _vp, _f, _vp, _l, _vp, _l, _vp, _i, _i, _vp]
+lib.fc_norm_between_grad.argtypes = [_vp, _vp, _l, _vp, _l, _vp, _l, _vp, _l, _l, _vp, _l, _vp, _vp, _f, _vp, _l, _vp, _l,
+                                     _vp, _l, _vp, _vp, _i, _i, _vp]
 for _n in ("fc_embed_create", "fc_embed_lookup", "fc_embed_grad", "fc_xent_create", "fc_xent_loss", "fc_xent_loss_grad",
-           "fc_muon_create", "fc_muon_orthogonalize", "fc_muon_step"):
+           "fc_muon_create", "fc_muon_orthogonalize", "fc_muon_step", "fc_norm_create", "fc_norm_before", "fc_norm_after",
+           "fc_norm_between", "fc_norm_before_grad", "fc_norm_after_grad", "fc_norm_between_grad"):
     getattr(lib, _n).restype = _i

@@ -1,0 +1,688 @@
+// Norms before and after a block, with its gate and residual scale (fc_lm.h).
+//
+//   N(x) = (x - m) r, m = mean(x) or 0, r = 1 / sqrt(mean((x - m)^2) + eps)
+//   out = h + s a(g) w N(b),  y = w2 N(out)
+// backward, u = w2 dy, xh = N(out), bh = N(b):
+//   do = dout + r (u - mean(u) [where m is a mean] - xh mean(u xh)),  dh = do
+//   e = s do, q = e a(g), v = w q
+//   db = r_b (v - mean(v) [same] - bh mean(v bh)),  dg = e a'(g) w bh
+//   dw = sum over tokens of q bh,  dw2 = sum of dy xh
+//
+// Every matrix is read once and written once: a row's elements stay in registers
+// from its loads to its stores, and the statistics are taken anew from them in the
+// backward pass, so that the forward pass keeps none.  The sums over tokens are kept
+// in registers too, by blocks that go through their share of the rows; their partial
+// sums go through memory, and a second launch adds them in order.  Where the gate is a
+// vector or none, a(g) and w are the same for all tokens, so that one sum, P = sum of e bh,
+// gives both dw = a(g) P and dg = a'(g) w P.
+#include <algorithm>
+
+#include "fc_lm_host.h"
+
+namespace {
+
+typedef _Float16 f16;
+typedef __bf16 bf16;
+
+// 8 neighbours of a row, which may start at any element: global memory takes any
+// alignment.
+template <typename T> struct Eight {
+    typedef T vec __attribute__((ext_vector_type(8)));
+    typedef vec any __attribute__((aligned(alignof(T))));
+};
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+
+// Up to 8 elements from p on, `left` of them in the row; zeros past it.
+template <typename T> __device__ __forceinline__ f32x8 load8(const T* p, int left) {
+    if (left >= 8) return __builtin_convertvector(*reinterpret_cast<const typename Eight<T>::any*>(p), f32x8);
+    f32x8 v{};
+#pragma unroll
+    for (int e = 0; e < 7; ++e)
+        if (e < left) v[e] = (float)p[e];
+    return v;
+}
+
+template <typename T> __device__ __forceinline__ void store8(T* p, int left, f32x8 v) {
+    if (left >= 8) {
+        *reinterpret_cast<typename Eight<T>::any*>(p) = __builtin_convertvector(v, typename Eight<T>::vec);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 7; ++e)
+        if (e < left) p[e] = (T)v[e];
+}
+
+// A channel vector's elements from c on; 1 where there is no vector.
+__device__ __forceinline__ f32x8 channels(const float* p, int c, int left) {
+    if (!p) return f32x8{1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+    return load8(p + c, left);
+}
+
+// To about 2^-22: the exponential's argument is rounded to fp32, for |g| up to 5.
+__device__ __forceinline__ float sigmoid(float g) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(g * -1.44269504088896341f)); }
+
+__device__ __forceinline__ float gate_value(float g, int kind) {
+    return kind == FC_GATE_NONE ? g : kind == FC_GATE_SIGMOID ? sigmoid(g) : g * sigmoid(g);
+}
+
+// a(g) and a'(g).
+__device__ __forceinline__ void gate_both(float g, int kind, float& a, float& slope) {
+    if (kind == FC_GATE_NONE) {
+        a = g;
+        slope = 1.f;
+        return;
+    }
+    const float s = sigmoid(g);
+    a = kind == FC_GATE_SIGMOID ? s : g * s;
+    slope = kind == FC_GATE_SIGMOID ? s * (1.f - s) : s * (1.f + g * (1.f - s));
+}
+
+// ---- how a row lies on threads -------------------------------------------------
+
+// `lanes` threads hold a row, VECTORS times 8 elements each, a vector's neighbours in
+// neighbouring threads: 8 to 64 lanes of a wave, with several rows to a block of 256, or
+// a block of whole waves for one row.
+struct Shape {
+    int lanes, vectors, threads;
+};
+
+constexpr int DIM_LIMIT = 16384;
+
+Shape shape_of(int64_t dim) {
+    if (dim <= 512) {
+        int lanes = 8;
+        while (lanes * 8 < dim) lanes *= 2;
+        return {lanes, 1, 256};
+    }
+    const int vectors = dim <= 8192 ? 1 : 4, threads = (int)fc::ceil_div(dim, 512 * vectors) * 64;
+    return {threads, vectors, threads};
+}
+
+// Sums over a row's lanes, N at once, the same in every lane.  A row's block meets
+// once per call; the parts of one call and the next lie in different places, and a
+// thread that writes a place again has met the others since they read it.
+constexpr int WAVES = 16;
+
+template <int N> struct RowSums {
+    float (*part)[N][WAVES];  // [2]
+    int lanes, turn;
+    __device__ __forceinline__ void init() {
+        if (lanes <= 64) return;
+        if (threadIdx.x < WAVES) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) part[0][k][threadIdx.x] = part[1][k][threadIdx.x] = 0.f;
+        }
+        __syncthreads();
+    }
+    __device__ __forceinline__ void add(float (&v)[N]) {
+#pragma unroll
+        for (int off = 1; off < 64; off *= 2)
+            if (off < lanes) {
+#pragma unroll
+                for (int k = 0; k < N; ++k) v[k] += __shfl_xor(v[k], off);
+            }
+        if (lanes <= 64) return;
+        if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) part[turn][k][threadIdx.x >> 6] = v[k];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            v[k] = 0.f;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) v[k] += part[turn][k][w];
+        }
+        turn ^= 1;
+    }
+};
+
+// ---- forward -------------------------------------------------------------------
+
+struct ForwardArgs {
+    const void *h, *b, *gate;   // b null: y of h alone
+    int64_t ldh, ldb, ldgate;   // ldgate 0: a vector
+    const float *weight, *next;
+    float scale, eps;
+    int kind, act;
+    int64_t n;
+    int dim, lanes;
+    void *out, *y;              // y null: out alone
+    int64_t ldout, ldy;
+};
+
+template <typename T, typename H, int V> __global__ __launch_bounds__(V > 1 ? 512 : 1024) void forward_kernel(ForwardArgs a) {
+    __shared__ __align__(16) float part[2][1][WAVES];
+    RowSums<1> sums{part, a.lanes, 0};
+    sums.init();
+    const bool shared = a.lanes <= 64;  // a block of several rows
+    const int lane = shared ? threadIdx.x & (a.lanes - 1) : threadIdx.x, per = shared ? 256 / a.lanes : 1;
+    const float inv = 1.f / (float)a.dim;
+    int c[V], left[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        c[v] = (v * a.lanes + lane) * 8;
+        left[v] = a.dim - c[v];
+    }
+    // x becomes x - m; returns r
+    auto normalize = [&](f32x8 (&x)[V]) {
+        float s[1] = {0.f};
+        if (a.kind == FC_NORM_LAYER) {
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s[0] += x[v][e];
+            sums.add(s);
+            const float m = s[0] * inv;
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[v][e] = e < left[v] ? x[v][e] - m : 0.f;
+            s[0] = 0.f;
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s[0] += x[v][e] * x[v][e];
+        sums.add(s);
+        return 1.f / sqrtf(s[0] * inv + a.eps);
+    };
+    for (int64_t t = (int64_t)blockIdx.x * per + (shared ? threadIdx.x / a.lanes : 0); t < a.n; t += (int64_t)gridDim.x * per) {
+        f32x8 x[V];
+        const H* const hp = static_cast<const H*>(a.h) + t * a.ldh;
+#pragma unroll
+        for (int v = 0; v < V; ++v) x[v] = load8(hp + c[v], left[v]);
+        if (a.b) {
+            f32x8 b[V], g[V];
+            const T* const bp = static_cast<const T*>(a.b) + t * a.ldb;
+#pragma unroll
+            for (int v = 0; v < V; ++v) b[v] = load8(bp + c[v], left[v]);
+            if (a.gate && a.ldgate) {
+                const T* const gp = static_cast<const T*>(a.gate) + t * a.ldgate;
+#pragma unroll
+                for (int v = 0; v < V; ++v) g[v] = load8(gp + c[v], left[v]);
+            } else {
+#pragma unroll
+                for (int v = 0; v < V; ++v) g[v] = channels(static_cast<const float*>(a.gate), c[v], left[v]);
+            }
+            const float r = normalize(b) * a.scale;
+            H* const op = static_cast<H*>(a.out) + t * a.ldout;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const f32x8 w = channels(a.weight, c[v], left[v]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float f = a.gate ? gate_value(g[v][e], a.act) * w[e] : w[e];
+                    const float o = x[v][e] + f * (b[v][e] * r);
+                    x[v][e] = e < left[v] ? (float)(H)o : 0.f;
+                }
+                store8(op + c[v], left[v], x[v]);
+            }
+        }
+        if (!a.y) continue;
+        const float r = normalize(x);
+        T* const yp = static_cast<T*>(a.y) + t * a.ldy;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const f32x8 w = channels(a.next, c[v], left[v]);
+            store8(yp + c[v], left[v], x[v] * r * w);
+        }
+    }
+}
+
+// ---- backward ------------------------------------------------------------------
+
+struct BackwardArgs {
+    const void *x, *dy, *dout, *b, *gate;     // dy null: no norm before; b null: none after; dout null: 0
+    int64_t ldx, lddy, lddout, ldb, ldgate;
+    const float *weight, *next;
+    float scale, eps;
+    int kind, act;
+    int64_t n;
+    int dim, lanes;
+    void *dh, *db, *dgate;                     // dh null after a block alone; dgate: rows of a gate that is a matrix
+    int64_t lddh, lddb, lddgate;
+    float *sum1, *sum2;                        // [block][ldp]: of the norm after and before, or null
+    int ldp;
+};
+
+// Rows of more than 8192 elements are more than a block's registers hold: they are read
+// again in each pass over them (AGAIN), and the sums over tokens lie in LDS, of which every
+// thread uses its own part.
+extern __shared__ __align__(32) float column_sums[];
+
+template <typename T, typename H, bool AGAIN> __global__ __launch_bounds__(AGAIN ? 512 : 1024) void backward_kernel(BackwardArgs a) {
+    __shared__ __align__(16) float part[2][3][WAVES];
+    RowSums<3> sums{part, a.lanes, 0};
+    sums.init();
+    const bool shared = a.lanes <= 64;  // a block of several rows
+    const int lane = shared ? threadIdx.x & (a.lanes - 1) : threadIdx.x, per = shared ? 256 / a.lanes : 1;
+    const float inv = 1.f / (float)a.dim;
+    const bool layer = a.kind == FC_NORM_LAYER, matrix = a.gate && a.ldgate;
+    auto col = [&](int v) __attribute__((always_inline)) { return (v * a.lanes + lane) * 8; };
+    auto left = [&](int v) __attribute__((always_inline)) { return a.dim - col(v); };
+    const int vectors = AGAIN ? 4 : 1;
+    f32x8 sum1{}, sum2{};
+    auto held = [&](int which, int v) __attribute__((always_inline)) { return reinterpret_cast<f32x8*>(column_sums) + (which * vectors + v) * a.lanes + lane; };
+    if (AGAIN)
+        for (int v = 0; v < 2 * vectors; ++v) *held(0, v) = f32x8{};
+    auto add1 = [&](int v, f32x8 q) __attribute__((always_inline)) {
+        if (AGAIN) *held(0, v) += q;
+        else sum1 += q;
+    };
+    auto add2 = [&](int v, f32x8 q) __attribute__((always_inline)) {
+        if (AGAIN) *held(1, v) += q;
+        else sum2 += q;
+    };
+    for (int64_t t = (int64_t)blockIdx.x * per + (shared ? threadIdx.x / a.lanes : 0); t < a.n; t += (int64_t)gridDim.x * per) {
+        f32x8 x, dy, b, d, g;  // of one vector at a time
+        float s[3], mean_x = 0.f, mean_u = 0.f, mean_b = 0.f, r = 0.f, rb = 0.f, along = 0.f;
+        auto fetch = [&](int v) __attribute__((always_inline)) {
+            const int n = left(v);
+            x = dy = b = d = g = f32x8{};
+            if (a.dy) {
+                x = load8(static_cast<const H*>(a.x) + t * a.ldx + col(v), n);
+                dy = load8(static_cast<const T*>(a.dy) + t * a.lddy + col(v), n);
+            }
+            if (a.b) b = load8(static_cast<const T*>(a.b) + t * a.ldb + col(v), n);
+            if (a.dout) d = load8(static_cast<const H*>(a.dout) + t * a.lddout + col(v), n);
+            if (a.b && matrix) g = load8(static_cast<const T*>(a.gate) + t * a.ldgate + col(v), n);
+        };
+        auto centre = [&](int v) __attribute__((always_inline)) {
+            if (!layer) return;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                x[e] = e < left(v) ? x[e] - mean_x : 0.f;
+                b[e] = e < left(v) ? b[e] - mean_b : 0.f;
+            }
+        };
+        // d becomes the gradient of `out`, dy * N(out) is added to its sum
+        auto before = [&](int v, bool first) __attribute__((always_inline)) {
+            const f32x8 w = channels(a.next, col(v), left(v)), xh = x * r;
+            d += r * (w * dy - mean_u - xh * along);
+            if (first) add2(v, dy * xh);
+        };
+        // d becomes the gradient of N(b), b N(b)
+        auto after = [&](int v, bool first) __attribute__((always_inline)) {
+            const f32x8 w = channels(a.weight, col(v), left(v));
+            const f32x8 gv = matrix ? g : channels(static_cast<const float*>(a.gate), col(v), left(v));
+            f32x8 dg, q;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float bh = b[e] * rb, ee = e < left(v) ? a.scale * d[e] : 0.f;
+                float f = 1.f, slope = 0.f;
+                if (matrix) gate_both(gv[e], a.act, f, slope);
+                else if (a.gate) f = gate_value(gv[e], a.act);
+                dg[e] = ee * slope * w[e] * bh;
+                q[e] = (matrix ? ee * f : ee) * bh;
+                b[e] = bh;
+                d[e] = e < left(v) ? w[e] * (ee * f) : 0.f;
+            }
+            if (first) add1(v, q);
+            if (first && a.dgate && matrix) store8(static_cast<T*>(a.dgate) + t * a.lddgate + col(v), left(v), dg);
+        };
+        s[0] = s[1] = s[2] = 0.f;
+        if (layer || !AGAIN) {
+#pragma unroll 1
+            for (int v = 0; v < vectors; ++v) {
+                fetch(v);
+                if (!layer) continue;
+                const f32x8 w = a.dy ? channels(a.next, col(v), left(v)) : f32x8{};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    s[0] += x[e];
+                    s[1] += w[e] * dy[e];
+                    s[2] += b[e];
+                }
+            }
+        }
+        if (layer) {
+            sums.add(s);
+            mean_x = s[0] * inv;
+            mean_u = s[1] * inv;
+            mean_b = s[2] * inv;
+            s[0] = s[1] = s[2] = 0.f;
+        }
+#pragma unroll 1
+        for (int v = 0; v < vectors; ++v) {
+            if (AGAIN) fetch(v);
+            centre(v);
+            const f32x8 w = a.dy ? channels(a.next, col(v), left(v)) : f32x8{};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                s[0] += x[e] * x[e];
+                s[1] += w[e] * dy[e] * x[e];
+                s[2] += b[e] * b[e];
+            }
+        }
+        sums.add(s);
+        rb = 1.f / sqrtf(s[2] * inv + a.eps);
+        r = 1.f / sqrtf(s[0] * inv + a.eps);
+        along = s[1] * inv * r;
+        s[0] = s[1] = s[2] = 0.f;
+#pragma unroll 1
+        for (int v = 0; v < vectors; ++v) {
+            if (AGAIN) {
+                fetch(v);
+                centre(v);
+            }
+            if (a.dy) {
+                before(v, true);
+                store8(static_cast<H*>(a.dh) + t * a.lddh + col(v), left(v), d);
+            }
+            if (!a.b) continue;
+            after(v, true);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                s[0] += d[e] * b[e];
+                s[1] += d[e];
+            }
+        }
+        if (!a.b) continue;
+        sums.add(s);
+        const float along_b = s[0] * inv, mean = layer ? s[1] * inv : 0.f;
+#pragma unroll 1
+        for (int v = 0; v < vectors; ++v) {
+            if (AGAIN) {
+                fetch(v);
+                centre(v);
+                if (a.dy) before(v, false);
+                after(v, false);
+            }
+            store8(static_cast<T*>(a.db) + t * a.lddb + col(v), left(v), rb * (d - mean - b * along_b));
+        }
+    }
+    // This block's sums: over the rows of a wave, then over its waves.
+    __shared__ __align__(32) float wave_sum[AGAIN ? 1 : 4][64 * 8];
+    auto put = [&](f32x8 sum, float* to, int which) __attribute__((always_inline)) {
+        if (!to) return;
+        to += (int64_t)blockIdx.x * a.ldp;
+        if (!shared) {
+            for (int v = 0; v < vectors; ++v)
+                if (left(v) > 0) *reinterpret_cast<f32x8*>(to + col(v)) = AGAIN ? *held(which, v) : sum;
+            return;
+        }
+        if (AGAIN) return;  // never: those rows have blocks of their own
+#pragma unroll
+        for (int off = 8; off < 64; off *= 2)
+            if (off >= a.lanes) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[e] += __shfl_xor(sum[e], off);
+            }
+        __syncthreads();
+        if ((threadIdx.x & 63) < a.lanes) *reinterpret_cast<f32x8*>(&wave_sum[threadIdx.x >> 6][8 * lane]) = sum;
+        __syncthreads();
+        if (threadIdx.x < a.lanes && left(0) > 0) {
+            f32x8 all{};
+            for (int w = 0; w < 4; ++w) all += *reinterpret_cast<const f32x8*>(&wave_sum[w][8 * lane]);
+            *reinterpret_cast<f32x8*>(to + col(0)) = all;
+        }
+    };
+    put(sum1, a.sum1, 0);
+    put(sum2, a.sum2, 1);
+}
+
+// ---- vectors' gradients -----------------------------------------------------------
+
+struct FinishArgs {
+    const float *sum1, *sum2;   // [blocks][ldp], or null
+    int blocks, ldp, dim;
+    const float *gate, *weight;  // gate: a vector, or null
+    int act;
+    void *dweight, *dgate, *dnext;
+    int dvec, accumulate;
+};
+
+__device__ __forceinline__ void put_channel(void* p, int dt, int c, float v, int accumulate) {
+    if (accumulate) v += dt == FC_F32 ? static_cast<float*>(p)[c] : dt == FC_F16 ? (float)static_cast<f16*>(p)[c] : (float)static_cast<bf16*>(p)[c];
+    if (dt == FC_F32) static_cast<float*>(p)[c] = v;
+    else if (dt == FC_F16) static_cast<f16*>(p)[c] = (f16)v;
+    else static_cast<bf16*>(p)[c] = (bf16)v;
+}
+
+// 32 channels to a block; 32 threads add a channel's partial sums, every 32nd each, and
+// one these.
+__global__ __launch_bounds__(1024) void finish_kernel(FinishArgs a) {
+    const float* const p = blockIdx.y ? a.sum2 : a.sum1;
+    if (!p) return;
+    __shared__ float part[32][33];
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5, c = blockIdx.x * 32 + x;
+    float s = 0.f;
+    if (c < a.dim)
+#pragma unroll 4
+        for (int k = y; k < a.blocks; k += 32) s += p[(int64_t)k * a.ldp + c];
+    part[y][x] = s;
+    __syncthreads();
+    if (y || c >= a.dim) return;
+    s = 0.f;
+    for (int k = 0; k < 32; ++k) s += part[k][x];
+    if (blockIdx.y) {
+        put_channel(a.dnext, a.dvec, c, s, a.accumulate);
+        return;
+    }
+    float f = 1.f, slope = 0.f;
+    if (a.gate) gate_both(a.gate[c], a.act, f, slope);
+    if (a.dgate) put_channel(a.dgate, a.dvec, c, slope * (a.weight ? a.weight[c] : 1.f) * s, a.accumulate);
+    if (a.dweight) put_channel(a.dweight, a.dvec, c, f * s, a.accumulate);
+}
+
+constexpr int64_t TOKENS_LIMIT = (int64_t)1 << 31;
+constexpr int BLOCKS_LIMIT = 1024;       // of a backward pass: rows of partial sums
+constexpr int64_t FORWARD_BLOCKS = 1 << 20;
+
+// Blocks of a backward pass of n rows.
+int64_t backward_blocks(Shape s, int64_t n) { return std::min<int64_t>(fc::ceil_div(n, s.threads / s.lanes), BLOCKS_LIMIT); }
+
+}  // namespace
+
+struct fc_norm {
+    fc::CallOrder order;
+    fc::DeviceBlock block;
+    int64_t dim = 0, max_tokens = 0;
+    int dtype = FC_F16, residual = FC_F32, kind = FC_NORM_RMS, act = FC_GATE_NONE;
+    float eps = 0;
+    Shape shape{};
+    int ldp = 0;
+    float *sum1 = nullptr, *sum2 = nullptr;
+};
+
+namespace {
+
+template <typename T, typename H> void forward(const Shape& s, unsigned grid, const ForwardArgs& a, hipStream_t st) {
+    if (s.vectors > 1) forward_kernel<T, H, 4><<<grid, s.threads, 0, st>>>(a);
+    else forward_kernel<T, H, 1><<<grid, s.threads, 0, st>>>(a);
+}
+
+// The LDS of the longest rows.
+template <typename T, typename H> hipError_t prepare() {
+    return hipFuncSetAttribute((const void*)backward_kernel<T, H, true>, hipFuncAttributeMaxDynamicSharedMemorySize, 8 * DIM_LIMIT);
+}
+
+template <typename T, typename H> void backward(const Shape& s, unsigned grid, const BackwardArgs& a, hipStream_t st) {
+    if (s.vectors > 1) backward_kernel<T, H, true><<<grid, s.threads, 2 * s.vectors * s.lanes * sizeof(f32x8), st>>>(a);
+    else backward_kernel<T, H, false><<<grid, s.threads, 0, st>>>(a);
+}
+
+// f<block side's type, residual side's type>() of a plan.
+template <typename F> void by_types(const fc_norm* p, F&& f) {
+    const bool wide = p->residual == FC_F32;
+    if (p->dtype == FC_F32) f(float{}, float{});
+    else if (p->dtype == FC_F16 && wide) f(f16{}, float{});
+    else if (p->dtype == FC_F16) f(f16{}, f16{});
+    else if (wide) f(bf16{}, float{});
+    else f(bf16{}, bf16{});
+}
+
+// A matrix of a call, or nothing where it is null.
+fc::Span matrix(const void* p, int64_t n, int64_t dim, int64_t ld, int dt, bool written) {
+    return p ? fc::Span{p, n, dim, ld, fc::dtype_bytes(dt), written} : fc::Span{nullptr, 0, 0, 0, 1, false};
+}
+
+// A gate, its gradient: a vector where ld is 0, else n rows.
+fc::Span gate_span(const void* p, int64_t n, int64_t dim, int64_t ld, int dt, int vec, bool vector, bool written) {
+    return vector ? matrix(p, 1, dim, dim, vec, written) : matrix(p, n, dim, ld, dt, written);
+}
+
+int call_forward(fc_norm* p, const void* h, int64_t ldh, const void* b, int64_t ldb, int64_t n, const void* gate, int64_t ldgate,
+                 const float* weight, const float* next, float scale, void* out, int64_t ldout, void* y, int64_t ldy,
+                 bool after, bool before, hipStream_t s) {
+    if (!p || n < 0 || n >= TOKENS_LIMIT) return FC_EINVAL;
+    if (n && (!h || (after && (!b || !out)) || (before && !y))) return FC_EINVAL;
+    const int64_t dim = p->dim;
+    int rc = fc::check_spans({matrix(h, n, dim, ldh, p->residual, false), matrix(b, n, dim, ldb, p->dtype, false),
+                              gate_span(gate, n, dim, ldgate, p->dtype, FC_F32, ldgate == 0, false), matrix(weight, 1, dim, dim, FC_F32, false),
+                              matrix(next, 1, dim, dim, FC_F32, false), matrix(out, n, dim, ldout, p->residual, true),
+                              matrix(y, n, dim, ldy, p->dtype, true)});
+    if (rc) return rc;
+    bool note;
+    rc = p->order.begin(s, note);
+    if (rc) return rc;
+    if (n) {
+        const ForwardArgs a{h, after ? b : nullptr, gate, ldh, ldb, ldgate, weight, next, scale, p->eps, p->kind, p->act, n, (int)dim, p->shape.lanes,
+                            out, before ? y : nullptr, ldout, ldy};
+        const int64_t per = p->shape.threads / p->shape.lanes;
+        const unsigned grid = (unsigned)std::min(fc::ceil_div(n, per), FORWARD_BLOCKS);
+        by_types(p, [&](auto t, auto r) { forward<decltype(t), decltype(r)>(p->shape, grid, a, s); });
+    }
+    rc = fc::hip_code(hipGetLastError());
+    p->order.done(s, note);
+    return rc;
+}
+
+int call_backward(fc_norm* p, const void* x, int64_t ldx, const void* b, int64_t ldb, const void* dy, int64_t lddy, const void* dout,
+                  int64_t lddout, int64_t n, const void* gate, int64_t ldgate, const float* weight, const float* next, float scale,
+                  void* dh, int64_t lddh, void* db, int64_t lddb, void* dgate, int64_t lddgate, void* dweight, void* dnext, int dvec,
+                  int accumulate, bool after, bool before, hipStream_t s) {
+    if (!p || n < 0 || n > p->max_tokens) return FC_EINVAL;
+    if (n && ((before && (!x || !dy || !dh)) || (after && (!b || !db)) || (!before && !dout))) return FC_EINVAL;
+    if (dgate && !gate) return FC_EINVAL;
+    const bool vector = ldgate == 0;
+    if ((dweight || dnext || (dgate && vector)) && !fc::dtype_bytes(dvec)) return FC_EINVAL;
+    const int64_t dim = p->dim;
+    int rc = fc::check_spans({matrix(x, n, dim, ldx, p->residual, false), matrix(b, n, dim, ldb, p->dtype, false),
+                              matrix(dy, n, dim, lddy, p->dtype, false), matrix(dout, n, dim, lddout, p->residual, false),
+                              gate_span(gate, n, dim, ldgate, p->dtype, FC_F32, vector, false), matrix(weight, 1, dim, dim, FC_F32, false),
+                              matrix(next, 1, dim, dim, FC_F32, false), matrix(dh, n, dim, lddh, p->residual, true),
+                              matrix(db, n, dim, lddb, p->dtype, true), gate_span(dgate, n, dim, lddgate, p->dtype, dvec, vector, true),
+                              matrix(dweight, 1, dim, dim, dvec, true), matrix(dnext, 1, dim, dim, dvec, true)});
+    if (rc) return rc;
+    bool note;
+    rc = p->order.begin(s, note);
+    if (rc) return rc;
+    float* const sum1 = dweight || (dgate && vector) ? p->sum1 : nullptr;
+    float* const sum2 = dnext ? p->sum2 : nullptr;
+    const int64_t blocks = backward_blocks(p->shape, n);
+    if (n) {
+        const BackwardArgs a{x, before ? dy : nullptr, dout, after ? b : nullptr, gate, ldx, lddy, lddout, ldb, ldgate, weight, next, scale, p->eps,
+                             p->kind, p->act, n, (int)dim, p->shape.lanes, dh, db, vector ? nullptr : dgate, lddh, lddb, lddgate, sum1, sum2, p->ldp};
+        by_types(p, [&](auto t, auto r) { backward<decltype(t), decltype(r)>(p->shape, (unsigned)blocks, a, s); });
+    }
+    if (sum1 || sum2) {
+        const FinishArgs f{sum1, sum2, (int)blocks, p->ldp, (int)dim, vector ? static_cast<const float*>(gate) : nullptr, weight, p->act, dweight, vector ? dgate : nullptr, dnext,
+                           dvec, accumulate};
+        finish_kernel<<<dim3((unsigned)fc::ceil_div(dim, 32), 2), 1024, 0, s>>>(f);
+    }
+    rc = fc::hip_code(hipGetLastError());
+    p->order.done(s, note);
+    return rc;
+}
+
+}  // namespace
+
+extern "C" {
+
+int fc_norm_create(fc_norm** plan, int64_t dim, int64_t max_tokens, int dtype, int residual_dtype, int kind, float eps, int gate) {
+    if (!plan) return FC_EINVAL;
+    *plan = nullptr;
+    if (dim < 1 || dim > DIM_LIMIT || max_tokens < 0 || max_tokens >= TOKENS_LIMIT || !fc::dtype_bytes(dtype) ||
+        (residual_dtype != dtype && residual_dtype != FC_F32) || (kind != FC_NORM_RMS && kind != FC_NORM_LAYER) || !(eps > 0) ||
+        !(eps < __builtin_inff()) || gate < FC_GATE_NONE || gate > FC_GATE_SILU)
+        return FC_EINVAL;
+    return fc::no_throw([&] {
+        fc_norm* p = new fc_norm;
+        p->dim = dim;
+        p->max_tokens = max_tokens;
+        p->dtype = dtype;
+        p->residual = residual_dtype;
+        p->kind = kind;
+        p->act = gate;
+        p->eps = eps;
+        p->shape = shape_of(dim);
+        p->ldp = (int)fc::ceil_div(dim, 8) * 8;
+        fc::Layout at;
+        const uint64_t each = (uint64_t)backward_blocks(p->shape, max_tokens) * p->ldp * 4;
+        const uint64_t o1 = at.take(each), o2 = at.take(each);
+        int rc = p->order.create();
+        if (!rc && p->shape.vectors > 1) by_types(p, [&](auto t, auto r) { rc = fc::hip_code(prepare<decltype(t), decltype(r)>()); });
+        if (!rc) rc = p->block.create(at.size);
+        if (rc) {
+            fc_norm_destroy(p);
+            return rc;
+        }
+        p->sum1 = reinterpret_cast<float*>(p->block.p + o1);
+        p->sum2 = reinterpret_cast<float*>(p->block.p + o2);
+        *plan = p;
+        return FC_OK;
+    });
+}
+
+void fc_norm_destroy(fc_norm* p) {
+    if (!p) return;
+    p->block.destroy();
+    p->order.destroy();
+    delete p;
+}
+
+int fc_norm_before(fc_norm* p, const void* x, int64_t ld_x, int64_t n, const float* weight, void* y, int64_t ld_y, void* stream) {
+    return fc::no_throw([&] {
+        return call_forward(p, x, ld_x, nullptr, 0, n, nullptr, 0, nullptr, weight, 0.f, nullptr, 0, y, ld_y, false, true,
+                            static_cast<hipStream_t>(stream));
+    });
+}
+
+int fc_norm_after(fc_norm* p, const void* h, int64_t ld_h, const void* b, int64_t ld_b, int64_t n, const void* gate, int64_t ld_gate,
+                  const float* weight, float scale, void* out, int64_t ld_out, void* stream) {
+    return fc::no_throw([&] {
+        return call_forward(p, h, ld_h, b, ld_b, n, gate, ld_gate, weight, nullptr, scale, out, ld_out, nullptr, 0, true, false,
+                            static_cast<hipStream_t>(stream));
+    });
+}
+
+int fc_norm_between(fc_norm* p, const void* h, int64_t ld_h, const void* b, int64_t ld_b, int64_t n, const void* gate, int64_t ld_gate,
+                    const float* weight, const float* next_weight, float scale, void* out, int64_t ld_out, void* y, int64_t ld_y,
+                    void* stream) {
+    return fc::no_throw([&] {
+        return call_forward(p, h, ld_h, b, ld_b, n, gate, ld_gate, weight, next_weight, scale, out, ld_out, y, ld_y, true, true,
+                            static_cast<hipStream_t>(stream));
+    });
+}
+
+int fc_norm_before_grad(fc_norm* p, const void* x, int64_t ld_x, const void* dy, int64_t ld_dy, const void* dout, int64_t ld_dout, int64_t n,
+                        const float* weight, void* dx, int64_t ld_dx, void* dweight, int dvec_dtype, int accumulate,
+                        void* stream) {
+    return fc::no_throw([&] {
+        return call_backward(p, x, ld_x, nullptr, 0, dy, ld_dy, dout, ld_dout, n, nullptr, 0, nullptr, weight, 0.f, dx, ld_dx, nullptr, 0,
+                             nullptr, 0, nullptr, dweight, dvec_dtype, accumulate, false, true, static_cast<hipStream_t>(stream));
+    });
+}
+
+int fc_norm_after_grad(fc_norm* p, const void* b, int64_t ld_b, const void* dout, int64_t ld_dout, int64_t n, const void* gate,
+                       int64_t ld_gate, const float* weight, float scale, void* db, int64_t ld_db, void* dgate,
+                       int64_t ld_dgate, void* dweight, int dvec_dtype, int accumulate, void* stream) {
+    return fc::no_throw([&] {
+        return call_backward(p, nullptr, 0, b, ld_b, nullptr, 0, dout, ld_dout, n, gate, ld_gate, weight, nullptr, scale, nullptr, 0, db,
+                             ld_db, dgate, ld_dgate, dweight, nullptr, dvec_dtype, accumulate, true, false, static_cast<hipStream_t>(stream));
+    });
+}
+
+int fc_norm_between_grad(fc_norm* p, const void* out, int64_t ld_out, const void* b, int64_t ld_b, const void* dy, int64_t ld_dy,
+                         const void* dout, int64_t ld_dout, int64_t n, const void* gate, int64_t ld_gate, const float* weight,
+                         const float* next_weight, float scale, void* dh, int64_t ld_dh, void* db, int64_t ld_db, void* dgate,
+                         int64_t ld_dgate, void* dweight, void* dnext, int dvec_dtype, int accumulate, void* stream) {
+    return fc::no_throw([&] {
+        return call_backward(p, out, ld_out, b, ld_b, dy, ld_dy, dout, ld_dout, n, gate, ld_gate, weight, next_weight, scale, dh, ld_dh, db,
+                             ld_db, dgate, ld_dgate, dweight, dnext, dvec_dtype, accumulate, true, true, static_cast<hipStream_t>(stream));
+    });
+}
+
+}  // extern "C"

@@ -1,12 +1,13 @@
-"""The operators at the ends of a language model and of its matrix update
-(include/fc_lm.h) on torch tensors: they produce the gradients that Plan
+"""The operators at the ends of a language model, within its blocks and of its
+matrix update (include/fc_lm.h) on torch tensors: they produce the gradients that Plan
 aggregates, or consume their sum.  As Plan does, each class checks every buffer
 before it calls the C ABI, which sees only pointers, and enqueues on the given
 stream or torch's current one."""
 import ctypes
 
 from ._fc import FC_F16, FC_F32, FcError
-from ._fc_lm import FC_BF16, fc_matrix, lib
+from ._fc_lm import (FC_BF16, FC_GATE_NONE, FC_GATE_SIGMOID, FC_GATE_SILU, FC_NORM_LAYER, FC_NORM_RMS, fc_matrix,
+                     lib)
 
 DTYPES = {"f32": FC_F32, "f16": FC_F16, "bf16": FC_BF16}
 _CODES = {}     # torch dtype -> fc_dtype value
@@ -84,6 +85,12 @@ def _vector(t, name, n, device, code):
     return t.data_ptr()
 
 
+def _rows(t, name):
+    """The rows of a tensor whose other checks are _matrix's."""
+    _tensor(t, name)
+    return t.shape[0] if t.dim() else -1
+
+
 _current = None  # the package's _stream, once it is loaded
 
 
@@ -95,7 +102,9 @@ def _stream(stream):
 
 
 _FUNCTIONS = {n: getattr(lib, n) for n in ("fc_embed_lookup", "fc_embed_grad", "fc_xent_loss", "fc_xent_loss_grad",
-                                           "fc_muon_orthogonalize", "fc_muon_step")}
+                                           "fc_muon_orthogonalize", "fc_muon_step", "fc_norm_before", "fc_norm_after",
+                                           "fc_norm_between", "fc_norm_before_grad", "fc_norm_after_grad",
+                                           "fc_norm_between_grad")}
 
 
 class _Handle:
@@ -267,3 +276,154 @@ class Muon(_Handle):
         vp, _ = self._flat(v, "v", FC_F32)
         gp, _ = self._flat(g, "g", FC_F32)
         self._call("fc_muon_step", wp, vp, gp, lr, mu, wd, int(batch), _stream(stream))
+
+
+_KINDS = {"rms": FC_NORM_RMS, "layer": FC_NORM_LAYER}
+_GATES = {"none": FC_GATE_NONE, "sigmoid": FC_GATE_SIGMOID, "silu": FC_GATE_SILU}
+
+
+class Norm(_Handle):
+    """The norms before and after a block of a model, with its gate and residual
+    scale (fc_norm), for rows of `dim` elements (at most 16384); gradients of up to
+    `max_tokens` rows.
+
+    dtype   : of the block's side: b, y, dy, db and a gate given per token
+    residual: of the residual's side: h, x, out, dout, dh, dx; `dtype` or "f32"
+    kind    : "rms", x / sqrt(mean(x^2) + eps), or "layer", the same of x - mean(x)
+    gate    : what a gate g multiplies by: "none", g itself, "sigmoid" or "silu"
+
+    Weights are f32 vectors, None is 1; a gate is None (1), an f32 vector or a
+    (tokens, dim) tensor of the block's type.  Vectors' gradients are f32, f16 or
+    bf16, all of a call's of one type; with `accumulate` they are added to.  A
+    gradient given as None is not computed."""
+
+    _destroy = "fc_norm_destroy"
+
+    def __init__(self, dim, max_tokens, dtype="f16", residual="f32", kind="rms", eps=1e-6, gate="none"):
+        for name, value, known in (("dtype", dtype, DTYPES), ("residual", residual, DTYPES), ("kind", kind, _KINDS),
+                                   ("gate", gate, _GATES)):
+            if value not in known:
+                raise ValueError(f"{name} must be one of {', '.join(known)}, not {value}")
+        if residual not in (dtype, "f32"):
+            raise ValueError(f"residual must be {dtype} or f32, not {residual}")
+        self.code, self.residual = DTYPES[dtype], DTYPES[residual]
+        self._create("fc_norm_create", dim, max_tokens, self.code, self.residual, _KINDS[kind], eps, _GATES[gate])
+        self.dim, self.max_tokens = dim, max_tokens
+
+    def _block(self, t, name, n):
+        return _matrix(t, name, n, self.dim, self.device, self.code)[::2]
+
+    def _residual(self, t, name, n):
+        return (None, 0) if t is None else _matrix(t, name, n, self.dim, self.device, self.residual)[::2]
+
+    def _weight(self, t, name):
+        return None if t is None else _vector(t, name, self.dim, self.device, FC_F32)
+
+    def _gate(self, t, n):
+        """(pointer, row stride or 0 for a vector)."""
+        if t is None:
+            return None, 0
+        _tensor(t, "gate")
+        if t.dim() == 1:
+            return _vector(t, "gate", self.dim, self.device, FC_F32), 0
+        return self._block(t, "gate", n)
+
+    def _dgate(self, t, gate, n, code):
+        if t is None:
+            return None, 0
+        _tensor(t, "dgate")
+        if gate is None or t.dim() != gate.dim():
+            raise ValueError("dgate must be a vector or rows as gate is")
+        if t.dim() == 1:
+            return _vector(t, "dgate", self.dim, self.device, code), 0
+        return self._block(t, "dgate", n)
+
+    def _code_of(self, *vectors):
+        """The one type of a call's vector gradients."""
+        for t in vectors:
+            if t is not None and getattr(t, "dim", lambda: 0)() == 1:
+                code = _CODES.get(t.dtype)
+                if code is None:
+                    raise ValueError(f"vectors' gradients must not be {t.dtype}")
+                return code
+        return FC_F32
+
+    def _tokens(self, t, name):
+        n = _rows(t, name)
+        if n > self.max_tokens:
+            raise ValueError(f"{n} tokens for a plan of {self.max_tokens}")
+        return n
+
+    def before(self, x, y, weight=None, stream=None):
+        """y[t] = weight * N(x[t])."""
+        n = _rows(x, "x")
+        xp, xl = self._residual(x, "x", n)
+        yp, yl = self._block(y, "y", n)
+        self._call("fc_norm_before", xp, xl, n, self._weight(weight, "weight"), yp, yl, _stream(stream))
+
+    def after(self, h, b, out, weight=None, gate=None, scale=1.0, stream=None):
+        """out[t] = h[t] + scale * a(gate) * weight * N(b[t])."""
+        n = _rows(h, "h")
+        hp, hl = self._residual(h, "h", n)
+        bp, bl = self._block(b, "b", n)
+        gp, gl = self._gate(gate, n)
+        op, ol = self._residual(out, "out", n)
+        self._call("fc_norm_after", hp, hl, bp, bl, n, gp, gl, self._weight(weight, "weight"), scale, op, ol, _stream(stream))
+
+    def between(self, h, b, out, y, weight=None, gate=None, next_weight=None, scale=1.0, stream=None):
+        """out as after()'s, and y[t] = next_weight * N(out[t]) of out as it is stored."""
+        n = _rows(h, "h")
+        hp, hl = self._residual(h, "h", n)
+        bp, bl = self._block(b, "b", n)
+        gp, gl = self._gate(gate, n)
+        op, ol = self._residual(out, "out", n)
+        yp, yl = self._block(y, "y", n)
+        self._call("fc_norm_between", hp, hl, bp, bl, n, gp, gl, self._weight(weight, "weight"),
+                   self._weight(next_weight, "next_weight"), scale, op, ol, yp, yl, _stream(stream))
+
+    def before_grad(self, x, dy, dx, dout=None, weight=None, dweight=None, accumulate=False, stream=None):
+        """The gradients of before(): dx, to which dout, the gradient that comes by the
+        residual, is added, and dweight."""
+        n = self._tokens(x, "x")
+        xp, xl = self._residual(x, "x", n)
+        yp, yl = self._block(dy, "dy", n)
+        op, ol = self._residual(dout, "dout", n)
+        dp, dl = self._residual(dx, "dx", n)
+        code = self._code_of(dweight)
+        wp = None if dweight is None else _vector(dweight, "dweight", self.dim, self.device, code)
+        self._call("fc_norm_before_grad", xp, xl, yp, yl, op, ol, n, self._weight(weight, "weight"), dp, dl, wp, code,
+                   bool(accumulate), _stream(stream))
+
+    def after_grad(self, b, dout, db, weight=None, dweight=None, gate=None, dgate=None, scale=1.0, accumulate=False,
+                   stream=None):
+        """The gradients of after() by b, gate and weight; that by h is dout itself."""
+        n = self._tokens(b, "b")
+        bp, bl = self._block(b, "b", n)
+        op, ol = self._residual(dout, "dout", n)
+        gp, gl = self._gate(gate, n)
+        dp, dl = self._block(db, "db", n)
+        code = self._code_of(dweight, dgate)
+        dgp, dgl = self._dgate(dgate, gate, n, code)
+        wp = None if dweight is None else _vector(dweight, "dweight", self.dim, self.device, code)
+        self._call("fc_norm_after_grad", bp, bl, op, ol, n, gp, gl, self._weight(weight, "weight"), scale, dp, dl, dgp, dgl, wp,
+                   code, bool(accumulate), _stream(stream))
+
+    def between_grad(self, out, b, dy, dh, db, dout=None, weight=None, dweight=None, gate=None, dgate=None, next_weight=None,
+                     dnext=None, scale=1.0, accumulate=False, stream=None):
+        """The gradients of between(), of both its outputs: dh, db and the vectors' and
+        gate's."""
+        n = self._tokens(out, "out")
+        xp, xl = self._residual(out, "out", n)
+        bp, bl = self._block(b, "b", n)
+        yp, yl = self._block(dy, "dy", n)
+        op, ol = self._residual(dout, "dout", n)
+        gp, gl = self._gate(gate, n)
+        hp, hl = self._residual(dh, "dh", n)
+        dp, dl = self._block(db, "db", n)
+        code = self._code_of(dweight, dnext, dgate)
+        dgp, dgl = self._dgate(dgate, gate, n, code)
+        wp = None if dweight is None else _vector(dweight, "dweight", self.dim, self.device, code)
+        np_ = None if dnext is None else _vector(dnext, "dnext", self.dim, self.device, code)
+        self._call("fc_norm_between_grad", xp, xl, bp, bl, yp, yl, op, ol, n, gp, gl, self._weight(weight, "weight"),
+                   self._weight(next_weight, "next_weight"), scale, hp, hl, dp, dl, dgp, dgl, wp, np_, code, bool(accumulate),
+                   _stream(stream))

@@ -1,0 +1,383 @@
+"""Norms around a block and their gradients on the GPU against the definition in
+64 bits.
+
+Bounds, from the operations, u = 2^-24: a row's sum of D terms is taken by threads
+of 8 to 32 terms each and then by halves, 32 + 16 roundings deep at most, and what
+is formed from sums has some 10 more: C = 64 roundings, relative to the sum of the
+terms' magnitudes.  A centred element x - m carries the mean's error and x's own
+rounding, relative to the row's size, not to the difference: (mean|x| + |x|) r in
+N(x).  Sums over tokens are at most 5 rows (of the sizes here) and 64 partial sums
+deep, with the terms' own errors: 2 C.  A gate's factor: its exponential's
+argument is rounded, |g| u, and some 4 more.  The result is rounded once: U of its
+type.  All is doubled for the terms of second order."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+U = {torch.float32: 2.0 ** -24, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}
+TINY = {torch.float32: 1e-37, torch.float16: 2.0 ** -24, torch.bfloat16: 1e-37}
+C = 64 * 2.0 ** -24
+EPS = 1e-5
+
+
+@pytest.fixture(scope="module")
+def fc(device):
+    import paper_1511_00175_amd as m
+    return m
+
+
+def strided(rows, cols, dtype, dev, pad=0, shift=0):
+    """A (rows, cols) tensor whose rows are cols + pad apart, `shift` elements into its memory."""
+    base = torch.full((shift + max(rows, 1) * (cols + pad),), 7.0, dtype=dtype, device=dev)
+    return base[shift:][:rows * (cols + pad)].view(rows, cols + pad)[:, :cols]
+
+
+def gate_of(g, act):
+    """a(g), its slope and the error of both."""
+    if g is None:
+        return 1.0, 0.0, 0.0
+    if act == "none":
+        return g, torch.ones_like(g), torch.zeros_like(g)
+    s = torch.sigmoid(g)
+    off = (4 + g.abs()) * 2.0 ** -24
+    if act == "sigmoid":
+        return s, s * (1 - s), off
+    return g * s, s * (1 + g * (1 - s)), off * (1 + g.abs())
+
+
+def norm_of(x, kind):
+    """N(x), r, and the error of N(x)."""
+    m = x.mean(1, keepdim=True) if kind == "layer" else 0.0
+    r = ((x - m).square().mean(1, keepdim=True) + EPS).rsqrt()
+    xh = (x - m) * r
+    off = C * xh.abs()
+    if kind == "layer":
+        off = off + C * r * (x.abs().mean(1, keepdim=True) + x.abs()) * (1 + xh.abs())
+    return xh, r, off
+
+
+def back(u, du, xh, r, off, kind):
+    """The gradient of N's input from that of its result, u, which is du off; its error."""
+    mean = lambda q: q.mean(1, keepdim=True)  # noqa: E731
+    m = mean(u) if kind == "layer" else 0.0
+    g = r * (u - m - xh * mean(u * xh))
+    size = u.abs() + mean(u.abs()) + xh.abs() * mean((u * xh).abs())
+    err = r * (du + mean(du) + xh.abs() * mean(du * xh.abs()) + off * mean((u * xh).abs()) + xh.abs() * mean(u.abs() * off))
+    # r's own error, relative as off is to xh
+    slack = C + (off / (xh.abs() + 1e-3)).amax(1, keepdim=True)
+    return g, err + slack * r * size
+
+
+def close(got, want, err):
+    assert got.shape == want.shape
+    bound = 2 * (err + U[got.dtype] * want.abs()) + TINY[got.dtype]
+    bad = (got.double() - want).abs() > bound
+    assert not bool(bad.any()), (int(bad.sum()), float(((got.double() - want).abs() / bound).max()))
+
+
+def inputs(n, dim, dtype, residual, gate, device, seed=0, pad=0, shift=0, offset=0.0):
+    g = torch.Generator(device=device)
+    g.manual_seed(seed + 11 * n + dim)
+
+    def rows(t, size):
+        out = strided(n, dim, t, device, pad, shift)
+        out.copy_(size * torch.randn(n, dim, generator=g, device=device) + offset)
+        return out
+
+    s = {"h": rows(residual, 3.0), "b": rows(dtype, 1.5), "dy": rows(dtype, 0.5), "dout": rows(residual, 0.5),
+         "weight": 1 + 0.3 * torch.randn(dim, generator=g, device=device),
+         "next": 1 + 0.3 * torch.randn(dim, generator=g, device=device), "gate": None}
+    if gate == "vector":
+        s["gate"] = torch.randn(dim, generator=g, device=device)
+    elif gate == "matrix":
+        s["gate"] = rows(dtype, 2.0)
+    return s
+
+
+def run_case(fc, device, n, dim, dtype="f16", residual="f32", kind="rms", gate="vector", act="none", pad=0, shift=0, weights=True,
+             vec=torch.float32, accumulate=False, scale=0.75, offset=0.0):
+    t, h = DT[dtype], DT[residual]
+    s = inputs(n, dim, t, h, gate, device, pad=pad, shift=shift, offset=offset)
+    w, w2 = (s["weight"], s["next"]) if weights else (None, None)
+    plan = fc.Norm(dim, n, dtype, residual, kind=kind, eps=EPS, gate=act)
+    new = lambda like: strided(n, dim, like, device, pad, shift)  # noqa: E731
+    D = lambda x: None if x is None else x.double()  # noqa: E731
+    a, slope, ea = gate_of(D(s["gate"]), act)
+    wd, wn = (D(w), D(w2)) if weights else (1.0, 1.0)
+
+    # forward: y is of what was stored as out
+    out, y, out2, y2 = new(h), new(t), new(h), new(t)
+    plan.between(s["h"], s["b"], out, y, weight=w, gate=s["gate"], next_weight=w2, scale=scale)
+    plan.after(s["h"], s["b"], out2, weight=w, gate=s["gate"], scale=scale)
+    plan.before(out, y2, weight=w2)
+    assert torch.equal(out, out2) and torch.equal(y, y2)
+    bh, rb, eb = norm_of(D(s["b"]), kind)
+    f = scale * a * wd
+    close(out, D(s["h"]) + f * bh, C * (D(s["h"]).abs() + (f * bh).abs()) + (f * torch.ones_like(bh)).abs() * eb + abs(scale) * ea * (wd * bh).abs())
+    xh, r, ex = norm_of(D(out), kind)
+    close(y, wn * xh, (wn * torch.ones_like(xh)).abs() * ex + C * (wn * xh).abs())
+
+    # backward
+    old = {k: torch.randn(dim, device=device).to(vec) for k in ("dweight", "dnext", "dgate")}
+    fresh = lambda k: old[k].clone() if accumulate else torch.full_like(old[k], float("nan"))  # noqa: E731
+
+    def grads(form):
+        got = {"dh": new(h), "db": new(t), "dweight": fresh("dweight"), "dnext": fresh("dnext")}
+        got["dgate"] = None if gate == "none" else fresh("dgate") if gate == "vector" else new(t)
+        if form == "before":
+            plan.before_grad(out, s["dy"], got["dh"], dout=s["dout"], weight=w2, dweight=got["dnext"], accumulate=accumulate)
+        elif form == "after":
+            plan.after_grad(s["b"], s["dout"], got["db"], weight=w, dweight=got["dweight"], gate=s["gate"], dgate=got["dgate"],
+                            scale=scale, accumulate=accumulate)
+        else:
+            plan.between_grad(out, s["b"], s["dy"], got["dh"], got["db"], dout=s["dout"], weight=w, dweight=got["dweight"],
+                              gate=s["gate"], dgate=got["dgate"], next_weight=w2, dnext=got["dnext"], scale=scale,
+                              accumulate=accumulate)
+        return got
+
+    def total(got, name, terms, errs):
+        want, err = terms.sum(0), 2 * C * terms.abs().sum(0) + errs.sum(0)
+        if accumulate:
+            want, err = want + old[name].double(), err + C * old[name].double().abs()
+        close(got[name], want, err)
+
+    for form in ("before", "after", "between"):
+        got, again = grads(form), grads(form)
+        for k, v in got.items():
+            assert v is None or torch.equal(torch.nan_to_num(v, 1.5), torch.nan_to_num(again[k], 1.5)), k  # the same bits again
+        d, ed = D(s["dout"]), torch.zeros_like(D(s["dout"]))
+        if form != "after":
+            dy = D(s["dy"])
+            g, ed = back(dy * wn, C * (dy * wn).abs(), xh, r, ex, kind)
+            ed = ed + C * (d.abs() + g.abs())
+            d = d + g
+            close(got["dh"], d, ed)
+            total(got, "dnext", dy * xh, dy.abs() * ex)
+        if form == "before":
+            continue
+        e, ee = scale * d, abs(scale) * ed + C * (scale * d).abs()
+        v, ev = e * a * wd, (ee * abs(a) + e.abs() * ea) * abs(wd) + C * (e * a * wd).abs()
+        g, eg = back(v, ev, bh, rb, eb, kind)
+        close(got["db"], g, eg)
+        total(got, "dweight", e * a * bh, (ee * abs(a) + e.abs() * ea) * bh.abs() + (e * a).abs() * eb)
+        if gate != "none":
+            terms = e * slope * wd * bh
+            errs = abs(wd) * (ee * (abs(slope) * bh.abs()) + e.abs() * (ea * bh.abs() + abs(slope) * eb)) + C * terms.abs()
+            if gate == "vector":
+                total(got, "dgate", terms, errs)
+            else:
+                close(got["dgate"], terms, errs)
+    if pad and n > 1:  # between the rows nothing is written
+        for m in (out, y, got["dh"], got["db"]):
+            assert bool((torch.as_strided(m, (n - 1, pad), (dim + pad, 1), m.storage_offset() + dim) == 7).all())
+
+
+@pytest.mark.parametrize("n,dim", [(1, 1), (3, 3), (7, 8), (33, 64), (1, 65), (70, 200), (5, 511), (300, 512), (4, 513), (37, 1001),
+                                   (6, 2048), (2, 2303), (3, 4097), (2, 8192), (3, 8193), (2, 9216), (2, 16383), (1, 16384)])
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+def test_sizes(fc, device, n, dim, kind):
+    run_case(fc, device, n, dim, kind=kind)
+
+
+@pytest.mark.parametrize("n,dim", [(40000, 8), (33000, 60), (2500, 600), (1100, 8200)])
+@pytest.mark.parametrize("kind,gate", [("rms", "matrix"), ("layer", "vector")])
+def test_more_rows_than_blocks(fc, device, n, dim, kind, gate):
+    run_case(fc, device, n, dim, kind=kind, gate=gate, act="sigmoid")
+
+
+@pytest.mark.parametrize("dtype,residual", [("f32", "f32"), ("f16", "f16"), ("f16", "f32"), ("bf16", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("dim,pad,shift", [(256, 0, 0), (264, 8, 0), (100, 3, 1), (1027, 5, 3), (8201, 1, 1)])
+def test_types_strides_alignment(fc, device, dtype, residual, dim, pad, shift):
+    run_case(fc, device, 19, dim, dtype, residual, "layer", "matrix", "silu", pad, shift)
+
+
+@pytest.mark.parametrize("gate", ["none", "vector", "matrix"])
+@pytest.mark.parametrize("act", ["none", "sigmoid", "silu"])
+@pytest.mark.parametrize("weights", [True, False])
+@pytest.mark.parametrize("dim", [72, 700])
+def test_gates(fc, device, gate, act, weights, dim):
+    run_case(fc, device, 41, dim, "bf16", "f32", "rms", gate, act, weights=weights)
+
+
+@pytest.mark.parametrize("vec", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("n", [1, 200])
+def test_accumulate(fc, device, vec, n):
+    run_case(fc, device, n, 321, vec=vec, accumulate=True)
+    run_case(fc, device, n, 321, vec=vec, gate="matrix", act="silu")
+
+
+def test_rows_far_from_zero(fc, device):
+    """The mean is taken out before the squares are summed."""
+    run_case(fc, device, 9, 1000, "f32", "f32", "layer", "none", offset=300.0)
+
+
+def test_no_tokens(fc, device):
+    """Gradients of vectors are zeros, or stay as they are."""
+    plan = fc.Norm(40, 0)
+    e = lambda t: torch.empty(0, 40, dtype=t, device=device)  # noqa: E731
+    plan.between(e(torch.float32), e(torch.float16), e(torch.float32), e(torch.float16))
+    dw, dn, dg = (torch.full((40,), 3.0, device=device) for _ in range(3))
+    gate = torch.ones(40, device=device)
+    for accumulate in (True, False):
+        plan.between_grad(e(torch.float32), e(torch.float16), e(torch.float16), e(torch.float32), e(torch.float16), dweight=dw, dnext=dn,
+                          gate=gate, dgate=dg, accumulate=accumulate)
+        assert all(bool((v == (3.0 if accumulate else 0.0)).all()) for v in (dw, dn, dg))
+
+
+def test_rows_do_not_touch_each_other(fc, device):
+    """A row of NaN or infinities makes its own outputs NaN and the vectors' sums, no other row's; a row of zeros
+    is zeros."""
+    n, dim = 13, 130
+    for kind in ("rms", "layer"):
+        plan = fc.Norm(dim, n, "f16", "f32", kind=kind, gate="silu")
+        s = inputs(n, dim, torch.float16, torch.float32, "matrix", device)
+        want = [torch.empty_like(s["h"]), torch.empty_like(s["b"])]
+        plan.between(s["h"], s["b"], *want, gate=s["gate"])
+        for row, value in ((2, float("nan")), (5, float("inf")), (7, 0.0)):
+            s["h"][row] = value
+            s["b"][row] = value
+        got = [torch.empty_like(s["h"]), torch.empty_like(s["b"])]
+        plan.between(s["h"], s["b"], *got, gate=s["gate"])
+        keep = torch.ones(n, dtype=torch.bool, device=device)
+        keep[[2, 5, 7]] = False
+        for a, b in zip(got, want):
+            assert torch.equal(a[keep], b[keep])
+            assert bool(a[2].isnan().all()) and not bool(a[5].isfinite().any()) and bool((a[7] == 0).all())
+        dh, db, dg = torch.empty_like(s["h"]), torch.empty_like(s["b"]), torch.empty_like(s["b"])
+        plan.between_grad(got[0], s["b"], s["dy"], dh, db, dout=s["dout"], gate=s["gate"], dgate=dg)
+        # of the row of zeros r is eps^-1/2 = 1000 in both norms, so that its db is up to 1000 * 1000 * |dy|, past
+        # fp16's 65504: an infinity, and no NaN
+        for v in (dh, db, dg):
+            assert bool(v[keep].isfinite().all()) and not bool(v[7].isnan().any()) and bool(v[2].isnan().all())
+
+
+def test_gradients_against_differences(fc, device):
+    """(L(p + t d) - L(p - t d)) / 2t = <dL/dp, d> for L = <out, dout> + <y, dy> in fp32, along random
+    directions of every input at once: L's rounding, some 1e-6 of its terms' size, over t = 1e-2, and the
+    third-order term, t^2 of the same size, leave 1e-3 of it."""
+    n, dim, t = 23, 96, 1e-2
+    for kind, gate, act in (("rms", "matrix", "silu"), ("layer", "vector", "sigmoid"), ("rms", "none", "none")):
+        plan = fc.Norm(dim, n, "f32", "f32", kind=kind, eps=EPS, gate=act)
+        s = inputs(n, dim, torch.float32, torch.float32, gate, device, seed=5)
+        names = ["h", "b", "weight", "next"] + (["gate"] if gate != "none" else [])
+        g = torch.Generator(device=device)
+        g.manual_seed(9)
+        d = {k: torch.randn(s[k].shape, generator=g, device=device) for k in names}
+
+        def value(step):
+            p = {k: s[k] + step * d[k] for k in names}
+            out, y = torch.empty_like(s["h"]), torch.empty_like(s["b"])
+            plan.between(p["h"], p["b"], out, y, weight=p["weight"], gate=p.get("gate"), next_weight=p["next"], scale=0.6)
+            return (out.double() * s["dout"].double()).sum() + (y.double() * s["dy"].double()).sum(), out
+
+        out = value(0.0)[1]
+        got = {k: torch.empty_like(s[k]) for k in names}
+        plan.between_grad(out, s["b"], s["dy"], got["h"], got["b"], dout=s["dout"], weight=s["weight"], dweight=got["weight"],
+                          gate=s["gate"], dgate=got.get("gate"), next_weight=s["next"], dnext=got["next"], scale=0.6)
+        parts = [(got[k].double() * d[k].double()) for k in names]
+        left = (value(t)[0] - value(-t)[0]) / (2 * t)
+        right, size = sum(p.sum() for p in parts), sum(p.square().sum() for p in parts).sqrt()
+        assert abs(float(left - right)) <= 1e-2 * float(size), (kind, float(left), float(right), float(size))
+
+
+def test_streams_are_ordered(fc, device):
+    """One plan on two streams in turn: the second call waits for the first, which uses the same workspace."""
+    n, dim = 3000, 1500
+    plan = fc.Norm(dim, n, "f16", "f16")
+    sets = [inputs(n, dim, torch.float16, torch.float16, "vector", device, seed=k) for k in range(4)]
+    make = lambda: [[torch.empty(n, dim, dtype=torch.float16, device=device) for _ in range(2)]  # noqa: E731
+                    + [torch.empty(dim, device=device) for _ in range(3)] for _ in sets]
+    call = lambda s, o, **kw: plan.between_grad(s["h"], s["b"], s["dy"], o[0], o[1], gate=s["gate"], dweight=o[2],  # noqa: E731
+                                                dnext=o[3], dgate=o[4], **kw)
+    want, got = make(), make()
+    for s, o in zip(sets, want):
+        call(s, o)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(3):
+        for i, s in enumerate(sets):
+            call(s, got[i], stream=streams[i % 2])
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def test_graph(fc, device):
+    """Captured calls give what eager calls give, replay after replay, with eager calls between."""
+    n, dim = 700, 900
+    plan = fc.Norm(dim, n, "bf16", "f32", gate="sigmoid")
+    s = inputs(n, dim, torch.bfloat16, torch.float32, "vector", device)
+    o = {k: torch.empty_like(s["h"]) for k in ("out", "dh")} | {k: torch.empty_like(s["b"]) for k in ("y", "db")}
+    v = {k: torch.zeros(dim, device=device) for k in ("dweight", "dnext", "dgate")}
+
+    def step(p):
+        p.between(s["h"], s["b"], o["out"], o["y"], weight=s["weight"], gate=s["gate"], next_weight=s["next"])
+        p.between_grad(o["out"], s["b"], s["dy"], o["dh"], o["db"], dout=s["dout"], weight=s["weight"], gate=s["gate"],
+                       next_weight=s["next"], accumulate=True, **v)
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(plan)
+    for k in range(4):
+        fresh = inputs(n, dim, torch.bfloat16, torch.float32, "vector", device, seed=k + 1)
+        for name, x in fresh.items():
+            s[name].copy_(x)
+        for x in v.values():
+            x.fill_(0.5)
+        graph.replay()
+        torch.cuda.synchronize()
+        first = [x.clone() for x in (*o.values(), *v.values())]
+        for x in (*o.values(), *v.values()):
+            x.fill_(0.5)
+        step(fc.Norm(dim, n, "bf16", "f32", gate="sigmoid") if k % 2 else plan)
+        assert all(torch.equal(a, b) for a, b in zip(first, (*o.values(), *v.values()))), k
+
+
+def test_refusals(fc, device):
+    plan = fc.Norm(64, 16)
+    h, b = torch.zeros(16, 64, device=device), torch.zeros(16, 64, dtype=torch.float16, device=device)
+    h2, b2, vec = torch.zeros_like(h), torch.zeros_like(b), torch.zeros(64, device=device)
+    plan.between(h, b, h2, b2, weight=vec, gate=vec)
+    for bad in (lambda: plan.before(b, b2), lambda: plan.before(h, b2[:15]), lambda: plan.before(h, b2.float()),
+                lambda: plan.before(h, b2, weight=vec.half()), lambda: plan.before(h, b2, weight=vec[:63]),
+                lambda: plan.before(h.cpu(), b2), lambda: plan.before(h.tolist(), b2), lambda: plan.before(vec, b2),
+                lambda: plan.after(h, b, h2, gate=b2[:15]), lambda: plan.after(h, b, h2, gate=h),
+                lambda: plan.after(h, b, h2[:, :32].repeat(1, 2).t().contiguous().t()),
+                lambda: plan.after(h, b, h2[:1].expand(16, 64)),
+                lambda: plan.before_grad(h.repeat(2, 1), b.repeat(2, 1), h2.repeat(2, 1)),      # more tokens than the plan's
+                lambda: plan.after_grad(b, h, b2, dgate=vec), lambda: plan.after_grad(b, h, b2, gate=vec, dgate=b.clone()),
+                lambda: plan.after_grad(b, h, b2, gate=vec, dgate=vec.clone(), dweight=vec.half()),
+                lambda: plan.after_grad(b, h, b2, dweight=vec.double())):
+        with pytest.raises(ValueError):
+            bad()
+    for bad in (lambda: plan.after(h, b, h), lambda: plan.between(h, b, h2, b), lambda: plan.before_grad(h, b, h2, dout=h2),
+                lambda: plan.after_grad(b, h, b2, weight=vec, dweight=vec), lambda: plan.after_grad(b, h, b)):
+        with pytest.raises(fc.FcError) as e:
+            bad()
+        assert e.value.code == -3  # FC_EALIAS
+    with pytest.raises(fc.FcError) as e:
+        plan.after_grad(b, None, b2)  # the gradient it starts from is missing
+    assert e.value.code == -1
+    for args in ((0, 1), (16385, 1), (8, -1), (8, 1 << 31)):
+        with pytest.raises(fc.FcError) as e:
+            fc.Norm(*args)
+        assert e.value.code == -1  # FC_EINVAL
+    for kw in ({"eps": 0.0}, {"eps": -1.0}, {"eps": float("nan")}, {"eps": float("inf")}):
+        with pytest.raises(fc.FcError):
+            fc.Norm(8, 1, **kw)
+    for kw in ({"dtype": "f64"}, {"residual": "bf16"}, {"kind": "max"}, {"gate": "relu"}):
+        with pytest.raises(ValueError):
+            fc.Norm(8, 1, **kw)
+
+
+@pytest.mark.parametrize("n", [1, 300])
+def test_fresh_workspaces_may_hold_anything(fc, device, n):
+    junk = [torch.full((1 << 24,), float("nan"), device=device) for _ in range(8)]
+    torch.cuda.synchronize()
+    del junk
+    torch.cuda.empty_cache()
+    run_case(fc, device, n, 130)
+    run_case(fc, device, n, 1300, gate="matrix")
