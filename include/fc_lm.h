@@ -238,6 +238,88 @@ int fc_norm_between_grad(fc_norm* plan, const void* out, int64_t ld_out, const v
                          void* db, int64_t ld_db, void* dgate, int64_t ld_dgate, void* dweight, void* dnext, int dvec_dtype,
                          int accumulate, void* stream);
 
+/* ---- activations in 8 bits ------------------------------------------------- */
+
+/* Rows in blocks of 32 neighbours that share a scale, a power of two 2^(byte - 127) (E8M0;
+ * byte 255 is a NaN): the smallest, from 2^-127 on, with which no element of the block rounds
+ * past the format's largest number.  An element is kept as an integer of 8 bits times it
+ * (FC_BLOCK_I8, 127 the largest: steps of 1/64 to 1/128 of the block's largest magnitude), or
+ * as an e4m3 float times it (FC_BLOCK_E4M3, 448 the largest: 4 bits of every element down to
+ * 2^-14 of the block's largest), rounded to the nearest, ties to even.  A block that holds an
+ * infinity or NaN is kept as NaN.
+ *   codes  : `rows` rows of 32 * ceil(dim / 32) bytes (zeros past dim), ld_codes apart, a
+ *            multiple of 16, on 16 bytes (FC_EALIGN)
+ *   scales : `rows` rows of ceil(dim / 32) bytes, ld_scales apart */
+#define FC_BLOCK_I8 0
+#define FC_BLOCK_E4M3 1
+
+typedef struct fc_ckpt fc_ckpt;
+
+/* A plan for activations of `dim` elements (1 to 2^21) and gradients of weights of up to
+ * max_outs rows (0 to 2^21) from up to max_tokens tokens (0 to 2^31 - 1) and a dy of `dtype`,
+ * FC_F16 or FC_BF16.  The workspace, made here (none where max_outs is 0): 2 bytes per
+ * element of max_tokens activations; 2 per element of dy where max_outs is no multiple of 8;
+ * partial sums of products that are split along the tokens, up to 128 MiB. */
+int fc_ckpt_create(fc_ckpt** plan, int64_t dim, int64_t max_tokens, int64_t max_outs, int dtype, int format);
+void fc_ckpt_destroy(fc_ckpt* plan);
+
+/* n rows x of any type to codes and scales; n < 2^31, here and in fc_ckpt_unpack. */
+int fc_ckpt_pack(fc_ckpt* plan, const void* x, int x_dtype, int64_t ld_x, int64_t n, void* codes, int64_t ld_codes,
+                 void* scales, int64_t ld_scales, void* stream);
+
+/* out[t, :] = the numbers kept, rounded to out's type; one past its largest (a block's
+ * largest element may have been rounded up to a power of two beyond) becomes that. */
+int fc_ckpt_unpack(fc_ckpt* plan, const void* codes, int64_t ld_codes, const void* scales, int64_t ld_scales, int64_t n,
+                   void* out, int out_dtype, int64_t ld_out, void* stream);
+
+/* The gradient of a weight (outs, dim) whose layer's inputs x are kept so and whose outputs'
+ * gradient is dy (n, outs): dw[o, :] = (accumulate ? dw[o, :] : 0) + scale * the sum over t of
+ * dy[t, o] x[t, :], with x as unpacked to dy's type (exact but for what is out of fp16's range),
+ * products and sums fp32, rounded once to dw's type.  n <= max_tokens, outs <= max_outs
+ * (FC_EINVAL).  dy lies on 16 bytes with ld_dy a multiple of 8, or is copied, for which plans
+ * whose max_outs is no multiple of 8 have room (others: FC_EALIGN); ld_dy is at most 2^21. */
+int fc_ckpt_grad(fc_ckpt* plan, const void* dy, int64_t ld_dy, const void* codes, int64_t ld_codes, const void* scales,
+                 int64_t ld_scales, int64_t n, int64_t outs, float scale, void* dw, int dw_dtype, int64_t ld_dw,
+                 int accumulate, void* stream);
+
+/* ---- matrices in 4 bits ------------------------------------------------------ */
+
+/* Rows in blocks of 32 with a scale as above, of e2m1 numbers (0, 0.5, 1, 1.5, 2, 3, 4, 6 and
+ * their negatives; MXFP4), and products along them on the block-scaled matrix cores.
+ *   codes  : rows of 16 * ceil(dim / 32) bytes, the even element in a byte's low half (zeros
+ *            past dim), ld_codes apart, a multiple of 16 and at most 2^21, on 16 bytes
+ *   scales : rows of 8 * ceil(dim / 256) bytes, zeros past the blocks, ld_scales apart, a
+ *            multiple of 8 and at most 2^21, on 8 bytes (FC_EALIGN, both) */
+typedef struct fc_mxfp fc_mxfp;
+
+/* A plan for products with a matrix of `rows` rows of `dim` elements (1 to 2^21 each) and up
+ * to max_tokens rows (0 to 2^31 - 1).  The workspace: fc_mxfp_linear's packed inputs, 0.53
+ * bytes per element of up to 2^18 tokens, and partial sums of products that are split, up to
+ * 128 MiB. */
+int fc_mxfp_create(fc_mxfp** plan, int64_t rows, int64_t dim, int64_t max_tokens);
+void fc_mxfp_destroy(fc_mxfp* plan);
+
+/* `rows` rows (any number below 2^31) of dim elements of any type to codes and scales; with
+ * `transpose` from x's columns: x has dim rows of `rows` elements. */
+int fc_mxfp_pack(fc_mxfp* plan, const void* x, int x_dtype, int64_t ld_x, int64_t rows, int transpose, void* codes,
+                 int64_t ld_codes, void* scales, int64_t ld_scales, void* stream);
+
+/* The numbers kept, as fc_ckpt_unpack's. */
+int fc_mxfp_unpack(fc_mxfp* plan, const void* codes, int64_t ld_codes, const void* scales, int64_t ld_scales, int64_t rows,
+                   void* out, int out_dtype, int64_t ld_out, void* stream);
+
+/* out[t, r] = (accumulate ? out[t, r] : 0) + scale * the sum over k of a[t, k] b[r, k], t < n <=
+ * max_tokens, b of the plan's rows, both packed; the sum is fp32, rounded once to out's type. */
+int fc_mxfp_product(fc_mxfp* plan, const void* a_codes, int64_t ld_a_codes, const void* a_scales, int64_t ld_a_scales,
+                    int64_t n, const void* b_codes, int64_t ld_b_codes, const void* b_scales, int64_t ld_b_scales,
+                    float scale, void* out, int out_dtype, int64_t ld_out, int accumulate, void* stream);
+
+/* The same of n rows x of any type, packed on the way: a layer's outputs from its inputs and
+ * packed weight. */
+int fc_mxfp_linear(fc_mxfp* plan, const void* x, int x_dtype, int64_t ld_x, int64_t n, const void* b_codes,
+                   int64_t ld_b_codes, const void* b_scales, int64_t ld_b_scales, float scale, void* out, int out_dtype,
+                   int64_t ld_out, int accumulate, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

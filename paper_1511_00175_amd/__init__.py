@@ -26,7 +26,7 @@ __all__ = ["Plan", "FcError", "fc_plan_create", "fc_plan_destroy", "fc_plan_quer
 
 # Classes of lm.py, whose library (libfc_lm.so) is loaded when one of them is first
 # used: Plan needs libfc.so alone.
-_LM = ("Embedding", "CrossEntropy", "Muon", "Norm")
+_LM = ("Embedding", "CrossEntropy", "Muon", "Norm", "Checkpoint", "Mxfp4")
 if os.path.exists(os.path.join(_fc.PKG, "libfc_lm.so")):
     __all__ += _LM
 

@@ -9,6 +9,7 @@ from ._fc import PKG
 LIB_PATH = os.path.join(PKG, "libfc_lm.so")
 FC_BF16 = 2
 FC_NORM_RMS, FC_NORM_LAYER = 0, 1
+FC_BLOCK_I8, FC_BLOCK_E4M3 = 0, 1
 FC_GATE_NONE, FC_GATE_SIGMOID, FC_GATE_SILU = 0, 1, 2
 
 
@@ -51,7 +52,22 @@ lib.fc_norm_before_grad.argtypes = [_vp, _vp, _l, _vp, _l, _vp, _l, _l, _vp, _vp
 lib.fc_norm_after_grad.argtypes = [_vp, _vp, _l, _vp, _l, _l, _vp, _l, _vp, _f, _vp, _l, _vp, _l, _vp, _i, _i, _vp]
 lib.fc_norm_between_grad.argtypes = [_vp, _vp, _l, _vp, _l, _vp, _l, _vp, _l, _l, _vp, _l, _vp, _vp, _f, _vp, _l, _vp, _l,
                                      _vp, _l, _vp, _vp, _i, _i, _vp]
+lib.fc_ckpt_create.argtypes = [_pp, _l, _l, _l, _i, _i]
+lib.fc_ckpt_destroy.argtypes = [_vp]
+lib.fc_ckpt_destroy.restype = None
+lib.fc_ckpt_pack.argtypes = [_vp, _vp, _i, _l, _l, _vp, _l, _vp, _l, _vp]
+lib.fc_ckpt_unpack.argtypes = [_vp, _vp, _l, _vp, _l, _l, _vp, _i, _l, _vp]
+lib.fc_ckpt_grad.argtypes = [_vp, _vp, _l, _vp, _l, _vp, _l, _l, _l, _f, _vp, _i, _l, _i, _vp]
+lib.fc_mxfp_create.argtypes = [_pp, _l, _l, _l]
+lib.fc_mxfp_destroy.argtypes = [_vp]
+lib.fc_mxfp_destroy.restype = None
+lib.fc_mxfp_pack.argtypes = [_vp, _vp, _i, _l, _l, _i, _vp, _l, _vp, _l, _vp]
+lib.fc_mxfp_unpack.argtypes = [_vp, _vp, _l, _vp, _l, _l, _vp, _i, _l, _vp]
+lib.fc_mxfp_product.argtypes = [_vp, _vp, _l, _vp, _l, _l, _vp, _l, _vp, _l, _f, _vp, _i, _l, _i, _vp]
+lib.fc_mxfp_linear.argtypes = [_vp, _vp, _i, _l, _l, _vp, _l, _vp, _l, _f, _vp, _i, _l, _i, _vp]
 for _n in ("fc_embed_create", "fc_embed_lookup", "fc_embed_grad", "fc_xent_create", "fc_xent_loss", "fc_xent_loss_grad",
            "fc_muon_create", "fc_muon_orthogonalize", "fc_muon_step", "fc_norm_create", "fc_norm_before", "fc_norm_after",
-           "fc_norm_between", "fc_norm_before_grad", "fc_norm_after_grad", "fc_norm_between_grad"):
+           "fc_norm_between", "fc_norm_before_grad", "fc_norm_after_grad", "fc_norm_between_grad", "fc_ckpt_create",
+           "fc_ckpt_pack", "fc_ckpt_unpack", "fc_ckpt_grad", "fc_mxfp_create", "fc_mxfp_pack", "fc_mxfp_unpack",
+           "fc_mxfp_product", "fc_mxfp_linear"):
     getattr(lib, _n).restype = _i

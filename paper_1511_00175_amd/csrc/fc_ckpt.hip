@@ -1,0 +1,208 @@
+// Activations kept in 8 bits, and a weight's gradient from them (fc_lm.h; the formats are
+// described in fc_blocks.h).
+//
+//   dw[o, i] (+)= scale sum over t of dy[t, o] x[t, i]
+//
+// 2 tokens outs dim operations.  x is first unpacked to dy's type, in which its numbers
+// are exact, and the product then takes both operands across their rows (fc_gemm.h), so that
+// neither is transposed in memory.
+#include "fc_blocks.h"
+#include "fc_products.h"
+
+namespace {
+
+constexpr int64_t ROWS_LIMIT = 1 << 21, LD_LIMIT = 1 << 21, TOKENS_LIMIT = (int64_t)1 << 31;
+
+// Partial sums that a split product may write: two rounds of the chip's largest tiles.
+constexpr int64_t SUMS_LIMIT = (int64_t)1 << 25;
+
+template <typename T, bool ADD> hipError_t prepare_all() {
+    for (hipError_t e : {prepare<Large<T, true, true>>((const void*)grad_kernel<Large<T, true, true>, ADD>),
+                         prepare<Broad<T, true, true>>((const void*)grad_kernel<Broad<T, true, true>, ADD>),
+                         prepare<Middle<T, true, true>>((const void*)grad_kernel<Middle<T, true, true>, ADD>)})
+        if (e != hipSuccess) return e;
+    return hipSuccess;
+}
+
+template <typename T, bool ADD> void launch(TileKind kind, const GradArgs& g, hipStream_t s) {
+    if (kind == LARGE) launch_grad<Large<T, true, true>, ADD>(g, s);
+    else if (kind == BROAD) launch_grad<Broad<T, true, true>, ADD>(g, s);
+    else launch_grad<Middle<T, true, true>, ADD>(g, s);
+}
+
+}  // namespace
+
+struct fc_ckpt {
+    fc::CallOrder order;
+    fc::DeviceBlock block;
+    int64_t dim = 0, max_tokens = 0, max_outs = 0;
+    int dtype = FC_F16, format = FC_BLOCK_I8, blocks = 0;
+    int64_t sums = 0;        // floats of partial sums
+    char* x = nullptr;       // unpacked
+    char* dy = nullptr;      // copied
+    float* sum = nullptr;
+};
+
+namespace {
+
+fc::BlockRows rows_of(const fc_ckpt* p, const void* x, int64_t ldx, const void* codes, int64_t ldc, const void* scales, int64_t lds, int64_t n) {
+    return {x, ldx, static_cast<uint8_t*>(const_cast<void*>(codes)), ldc, static_cast<uint8_t*>(const_cast<void*>(scales)), lds, n, (int)p->dim, p->blocks,
+            p->blocks};
+}
+
+fc::Span codes_span(const fc_ckpt* p, const void* codes, int64_t ldc, int64_t n, bool written) { return {codes, n, 32 * (int64_t)p->blocks, ldc, 1, written}; }
+fc::Span scales_span(const fc_ckpt* p, const void* scales, int64_t lds, int64_t n, bool written) { return {scales, n, p->blocks, lds, 1, written}; }
+
+bool aligned(const void* codes, int64_t ldc) { return ldc % 16 == 0 && reinterpret_cast<uintptr_t>(codes) % 16 == 0; }
+
+template <typename T>
+void grad(fc_ckpt* p, const void* dy, int64_t lddy, const fc::BlockRows& kept, int64_t outs, float scale, void* dw, int dwt, int64_t lddw, bool add,
+          hipStream_t s) {
+    const int64_t n = kept.rows, ldx = fc::ceil_div(p->dim, 8) * 8;
+    if (p->format == FC_BLOCK_I8) fc::unpack_rows<FC_BLOCK_I8>(kept, p->x, p->dtype, ldx, (int)ldx, s);
+    else fc::unpack_rows<FC_BLOCK_E4M3>(kept, p->x, p->dtype, ldx, (int)ldx, s);
+    if (lddy % 8 || reinterpret_cast<uintptr_t>(dy) % 16) {
+        const int64_t ld = fc::ceil_div(outs, 8) * 8;
+        fc::by_launches(n, ld / 8, [&](int64_t r0, int64_t count) {
+            PackArgs a{static_cast<const char*>(dy) + r0 * lddy * 2, lddy, p->dy + r0 * ld * 2, ld, count, (int)outs, nullptr, 0, 0};
+            pack_kernel<<<(unsigned)fc::ceil_div(count * (ld / 8), 256), 256, 0, s>>>(a);
+        });
+        dy = p->dy;
+        lddy = ld;
+    }
+    GradArgs g{};
+    g.a = Operand{dy, lddy, (int)outs, (int)n, 0};
+    g.b = Operand{p->x, ldx, (int)p->dim, (int)n, 0};
+    g.m = (int)outs;
+    g.n = (int)p->dim;
+    g.k = (int)n;
+    g.parts = 1;
+    const Choice c = choose(outs, p->dim, n, false, true, true, p->sums);
+    const bool split = c.splits > 1;
+    g.kper = c.steps * fc::GEMM_BK;
+    g.scale = scale;
+    g.out = dw;
+    g.dt = dwt;
+    g.ld = lddw;
+    g.sum = split ? p->sum : nullptr;
+    g.first = true;
+    g.last = !split;
+    if (add && !split) launch<T, true>(c.kind, g, s);
+    else launch<T, false>(c.kind, g, s);
+    if (split) join_splits(g, c.splits, add, s);
+}
+
+}  // namespace
+
+extern "C" {
+
+int fc_ckpt_create(fc_ckpt** plan, int64_t dim, int64_t max_tokens, int64_t max_outs, int dtype, int format) {
+    if (!plan) return FC_EINVAL;
+    *plan = nullptr;
+    if (dim < 1 || dim > LD_LIMIT || max_tokens < 0 || max_tokens >= TOKENS_LIMIT || max_outs < 0 || max_outs > ROWS_LIMIT ||
+        (dtype != FC_F16 && dtype != FC_BF16) || (format != FC_BLOCK_I8 && format != FC_BLOCK_E4M3))
+        return FC_EINVAL;
+    return fc::no_throw([&] {
+        fc_ckpt* p = new fc_ckpt;
+        p->dim = dim;
+        p->max_tokens = max_tokens;
+        p->max_outs = max_outs;
+        p->dtype = dtype;
+        p->format = format;
+        p->blocks = (int)fc::ceil_div(dim, fc::BLOCK);
+        fc::Layout at;
+        const bool grads = max_outs > 0;
+        p->sums = grads ? std::min<int64_t>(SUMS_LIMIT, 64 * fc::ceil_div(max_outs, 64) * 64 * dim) : 0;
+        const uint64_t o_x = at.take(grads ? max_tokens * fc::ceil_div(dim, 8) * 16 : 0),
+                       o_dy = at.take(max_outs % 8 ? max_tokens * fc::ceil_div(max_outs, 8) * 16 : 0), o_sum = at.take(p->sums * 4);
+        int rc = p->order.create();
+        if (!rc) rc = fc::hip_code(dtype == FC_F16 ? prepare_all<f16, false>() : prepare_all<bf16, false>());
+        if (!rc) rc = fc::hip_code(dtype == FC_F16 ? prepare_all<f16, true>() : prepare_all<bf16, true>());
+        if (!rc) rc = p->block.create(at.size);
+        if (rc) {
+            fc_ckpt_destroy(p);
+            return rc;
+        }
+        p->x = p->block.p + o_x;
+        p->dy = p->block.p + o_dy;
+        p->sum = reinterpret_cast<float*>(p->block.p + o_sum);
+        *plan = p;
+        return FC_OK;
+    });
+}
+
+void fc_ckpt_destroy(fc_ckpt* p) {
+    if (!p) return;
+    p->block.destroy();
+    p->order.destroy();
+    delete p;
+}
+
+int fc_ckpt_pack(fc_ckpt* p, const void* x, int x_dtype, int64_t ld_x, int64_t n, void* codes, int64_t ld_codes, void* scales, int64_t ld_scales,
+                 void* stream) {
+    return fc::no_throw([&]() -> int {
+        if (!p || n < 0 || n >= TOKENS_LIMIT) return FC_EINVAL;
+        int rc = fc::check_spans({{x, n, p->dim, ld_x, fc::dtype_bytes(x_dtype), false}, codes_span(p, codes, ld_codes, n, true), scales_span(p, scales, ld_scales, n, true)});
+        if (rc) return rc;
+        if (!aligned(codes, ld_codes)) return FC_EALIGN;
+        const hipStream_t s = static_cast<hipStream_t>(stream);
+        bool note;
+        rc = p->order.begin(s, note);
+        if (rc) return rc;
+        const fc::BlockRows a = rows_of(p, x, ld_x, codes, ld_codes, scales, ld_scales, n);
+        if (p->format == FC_BLOCK_I8) fc::pack_rows<FC_BLOCK_I8>(a, x_dtype, s);
+        else fc::pack_rows<FC_BLOCK_E4M3>(a, x_dtype, s);
+        rc = fc::hip_code(hipGetLastError());
+        p->order.done(s, note);
+        return rc;
+    });
+}
+
+int fc_ckpt_unpack(fc_ckpt* p, const void* codes, int64_t ld_codes, const void* scales, int64_t ld_scales, int64_t n, void* out, int out_dtype,
+                   int64_t ld_out, void* stream) {
+    return fc::no_throw([&]() -> int {
+        if (!p || n < 0 || n >= TOKENS_LIMIT) return FC_EINVAL;
+        int rc = fc::check_spans({codes_span(p, codes, ld_codes, n, false), scales_span(p, scales, ld_scales, n, false),
+                                  {out, n, p->dim, ld_out, fc::dtype_bytes(out_dtype), true}});
+        if (rc) return rc;
+        if (!aligned(codes, ld_codes)) return FC_EALIGN;
+        const hipStream_t s = static_cast<hipStream_t>(stream);
+        bool note;
+        rc = p->order.begin(s, note);
+        if (rc) return rc;
+        const fc::BlockRows a = rows_of(p, nullptr, 0, codes, ld_codes, scales, ld_scales, n);
+        if (p->format == FC_BLOCK_I8) fc::unpack_rows<FC_BLOCK_I8>(a, out, out_dtype, ld_out, (int)p->dim, s);
+        else fc::unpack_rows<FC_BLOCK_E4M3>(a, out, out_dtype, ld_out, (int)p->dim, s);
+        rc = fc::hip_code(hipGetLastError());
+        p->order.done(s, note);
+        return rc;
+    });
+}
+
+int fc_ckpt_grad(fc_ckpt* p, const void* dy, int64_t ld_dy, const void* codes, int64_t ld_codes, const void* scales, int64_t ld_scales, int64_t n,
+                 int64_t outs, float scale, void* dw, int dw_dtype, int64_t ld_dw, int accumulate, void* stream) {
+    return fc::no_throw([&]() -> int {
+        if (!p || n < 0 || n > p->max_tokens || outs < 0 || outs > p->max_outs || ld_dy > LD_LIMIT) return FC_EINVAL;
+        int rc = fc::check_spans({{dy, n, outs, ld_dy, 2, false}, codes_span(p, codes, ld_codes, n, false), scales_span(p, scales, ld_scales, n, false),
+                                  {dw, outs, p->dim, ld_dw, fc::dtype_bytes(dw_dtype), true}});
+        if (rc) return rc;
+        if (!aligned(codes, ld_codes)) return FC_EALIGN;
+        if (n && outs && p->max_outs % 8 == 0 && (ld_dy % 8 || reinterpret_cast<uintptr_t>(dy) % 16)) return FC_EALIGN;
+        const hipStream_t s = static_cast<hipStream_t>(stream);
+        bool note;
+        rc = p->order.begin(s, note);
+        if (rc) return rc;
+        const fc::BlockRows a = rows_of(p, nullptr, 0, codes, ld_codes, scales, ld_scales, n);
+        if (n == 0) {
+            if (!accumulate && outs) zeros(dw, dw_dtype, outs, p->dim, ld_dw, s);
+        } else if (outs) {
+            if (p->dtype == FC_F16) grad<f16>(p, dy, ld_dy, a, outs, scale, dw, dw_dtype, ld_dw, accumulate != 0, s);
+            else grad<bf16>(p, dy, ld_dy, a, outs, scale, dw, dw_dtype, ld_dw, accumulate != 0, s);
+        }
+        rc = fc::hip_code(hipGetLastError());
+        p->order.done(s, note);
+        return rc;
+    });
+}
+
+}  // extern "C"

@@ -1,0 +1,226 @@
+// The product of fc_gemm.h for operands in 4 bits with a scale for every 32 along k
+// (fc_blocks.h), on the block-scaled matrix cores: C[m, n] = sum over k of A(m, k) B(n, k).
+//
+// A row of codes is read as 16-bit units of 4 elements, along k, so that a tile of 64 units
+// holds 256 of k and goes to LDS and to fragments as fc_gemm.h's contiguous operands do: a
+// lane's 16 bytes are the 32 elements of one scale.  The scales of a tile, 8 bytes for each
+// row, go to LDS beside it, two rows' worth of lanes (4 bytes each) to a row; a lane reads its
+// row's 8 and shifts the byte of its 32 elements down.  An instruction multiplies 16 x 16 by
+// 128 of k in the cycles of a 16-bit one's 32 of k, from as many bytes, so that the same
+// tiles give four times the operations for the same reads.
+#pragma once
+
+#include "fc_gemm.h"
+
+namespace fc {
+
+// p, ld, rows, ks in 16-bit units, as Operand; scales in bytes: 8 for each 64 units, rows
+// `lds` apart, all multiples of 8.
+struct Operand4 {
+    const void* p;
+    int64_t ld;
+    int rows;
+    int ks;
+    const void* scales;
+    int64_t lds;
+};
+
+// 4 bytes per lane from memory to LDS at lds + 4 * lane.
+__device__ __forceinline__ void load_words_to_lds(u32x4 desc, uint32_t lds, uint32_t off) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds), "v"(off), "s"(desc)
+                 : "memory", "m0");
+}
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+// The products of a lane's 32 elements each of a and b, scaled by bytes 0 of sa and sb.
+__device__ __forceinline__ f32x4 mma4(i32x4 a, i32x4 b, f32x4 c, uint32_t sa, uint32_t sb) {
+    const i32x8 x = __builtin_shufflevector(a, a, 0, 1, 2, 3, -1, -1, -1, -1), y = __builtin_shufflevector(b, b, 0, 1, 2, 3, -1, -1, -1, -1);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, 4, 4, 0, (int)sa, 0, (int)sb);
+}
+
+// One wave's loads of one operand's scales for tiles of R rows, of which `waves` waves load
+// 32 rows at a time each.
+template <int R> struct ScaleLoads {
+    uint32_t off;
+    uint64_t base;
+    uint32_t span;
+    // Of the 32 rows from row0 + 32 * part on.
+    __device__ __forceinline__ void init(const Operand4& o, int row0, int part, int lane) {
+        const int left = o.rows - row0 - 32 * part, r = lane >> 1;
+        base = (uint64_t)o.scales + (uint64_t)(row0 + 32 * part) * o.lds;
+        const int valid = left < 32 ? left : 32;
+        span = valid > 0 ? (uint32_t)((uint64_t)(valid - 1) * o.lds) : 0;
+        off = r < valid ? (uint32_t)((uint64_t)r * o.lds) + 4u * (lane & 1) : GEMM_OUTSIDE;
+        if (valid <= 0) base = (uint64_t)o.scales;
+    }
+    // Of the 64 units at step s.
+    __device__ __forceinline__ void load(uint32_t lds, int s, bool live) const {
+        const uint64_t b = base + 8 * (uint64_t)s;
+        u32x4 desc;
+        desc.x = __builtin_amdgcn_readfirstlane((uint32_t)b);
+        desc.y = __builtin_amdgcn_readfirstlane((uint32_t)(b >> 32));
+        desc.z = __builtin_amdgcn_readfirstlane(live ? span + 8 : 0u);
+        desc.w = 0x00020000u;
+        load_words_to_lds(desc, __builtin_amdgcn_readfirstlane(lds), off);
+    }
+};
+
+// The product of one block's BM x BN tile, WM x WN per wave; fc_gemm.h's loop with scales.
+template <int BM_, int BN_, int WM_, int WN_, int STAGES> struct Product4 {
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
+    static constexpr int WAVES = (BM / WM) * (BN / WN), THREADS = 64 * WAVES;
+    static constexpr int FM = WM / 16, FN = WN / 16;
+    static constexpr int CODES = (BM + BN) * GEMM_BK * 2;
+    static constexpr int STAGE = CODES + (BM + BN) * 8;
+    static constexpr int LDS = STAGES * STAGE;
+    static constexpr int SCALES = (BM + BN) / 32 / WAVES;  // loads of 32 rows' scales per wave
+    static constexpr int LOADS = (BM + BN) / 8 / WAVES + SCALES;
+    static_assert(SCALES * 32 * WAVES == BM + BN && BM % 32 == 0, "the scales are whole loads of every wave");
+
+    f32x4 acc[FM][FN];
+
+    // k runs over [kb, ke) in 16-bit units, kb a multiple of 64.
+    __device__ __forceinline__ void run(char* lds, const Operand4& A, const Operand4& B, int m0, int n0, int kb, int ke, int) {
+        const int lane = threadIdx.x & 63;
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const uint32_t la = lds_address(lds), lb = la + BM * GEMM_BK * 2, ls = la + CODES;
+        TileLoads<BM, false, WAVES> ta;
+        TileLoads<BN, false, WAVES> tb;
+        ta.init(Operand{A.p, A.ld, A.rows, A.ks, 0}, m0, wave, lane);
+        tb.init(Operand{B.p, B.ld, B.rows, B.ks, 0}, n0, wave, lane);
+        ScaleLoads<BM> ts[SCALES];
+#pragma unroll
+        for (int i = 0; i < SCALES; ++i) {
+            const int part = wave * SCALES + i;
+            if (part < BM / 32) ts[i].init(A, m0, part, lane);
+            else ts[i].init(B, n0, part - BM / 32, lane);
+        }
+        Fragments<_Float16, BM, false, FM> fa;
+        Fragments<_Float16, BN, false, FN> fb;
+        const int wm = (wave / (BN / WN)) * WM, wn = (wave % (BN / WN)) * WN;
+        fa.init(wm, lane);
+        fb.init(wn, lane);
+        const uint32_t sa_at = ls + 8 * (wm + (lane & 15)), sb_at = ls + 8 * (BM + wn + (lane & 15)), shift = 8 * (lane >> 4);
+        auto frag = [&](auto& f, uint32_t tile, int i, int kk) __attribute__((always_inline)) { return __builtin_bit_cast(i32x4, f.get(tile, i, kk)); };
+        auto scales = [&](uint32_t at, int i) __attribute__((always_inline)) { return *(FC_LDS const u32x2*)(uintptr_t)(at + 128 * i); };
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+        const int total = (ke - kb + GEMM_BK - 1) / GEMM_BK;
+        int k = kb, issued = 0, into = 0;
+        typename TileLoads<BM, false, WAVES>::Tile ia;
+        typename TileLoads<BN, false, WAVES>::Tile ib;
+        uint32_t is = 0;
+        int step = 0;
+        bool live = false;
+        auto prepare = [&]() __attribute__((always_inline)) {
+            live = issued < total;
+            const int from = live ? k : kb;
+            ia = ta.tile(la + into, from, false, live, wave);
+            ib = tb.tile(lb + into, from, false, live, wave);
+            is = ls + into + wave * SCALES * 256;
+            step = from / GEMM_BK;
+            into = into == (STAGES - 1) * STAGE ? 0 : into + STAGE;
+            k += GEMM_BK;
+            ++issued;
+        };
+        auto load = [&](int l) __attribute__((always_inline)) {
+            if (l < ta.COUNT) ta.load(ia, l);
+            else if (l < ta.COUNT + tb.COUNT) tb.load(ib, l - ta.COUNT);
+            else ts[l - ta.COUNT - tb.COUNT].load(is + 256 * (l - ta.COUNT - tb.COUNT), step, live);
+        };
+        for (int s = 0; s < STAGES; ++s) {
+            prepare();
+#pragma unroll
+            for (int l = 0; l < LOADS; ++l) load(l);
+        }
+        wait_loads<(STAGES - 1) * LOADS>();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        i32x4 a[FM], b[FN], next[FN];
+        u32x2 sa[FM], sb[FN], sn[FN];
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+            b[j] = frag(fb, lb, j, 0);
+            sb[j] = scales(sb_at, j);
+        }
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+            a[i] = frag(fa, la, i, 0);
+            sa[i] = scales(sa_at, i);
+        }
+        constexpr int FIRST = FM >= 4 ? 2 : FM >= 2 ? 1 : 0;  // rows that cover the wait for the last reads
+        constexpr int REST = FM - FIRST;
+        constexpr int EACH = (FN + REST - 1) / REST, LEACH = (LOADS + REST - 1) / REST;
+        auto row_of = [&](int i, int kk) __attribute__((always_inline)) {
+            const uint32_t s = sa[i][kk] >> shift;
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int j = 0; j < FN; ++j) acc[i][j] = mma4(b[j], a[i], acc[i][j], sb[j][kk], s);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        uint32_t at = 0;
+        for (int t = 0; t < total; ++t) {
+            const uint32_t then = at == (STAGES - 1) * STAGE ? 0 : at + STAGE;
+            prepare();
+#pragma unroll
+            for (int j = 0; j < FN; ++j) sb[j] >>= shift;
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+                row_of(i, 0);
+#pragma unroll
+                for (int j = 0; j < FN; ++j)
+                    if (j / EACH == i) next[j] = frag(fb, lb + at, j, 1);
+                a[i] = frag(fa, la + at, i, 1);
+            }
+#pragma unroll
+            for (int j = 0; j < FN; ++j) b[j] = next[j];
+#pragma unroll
+            for (int i = 0; i < FIRST; ++i) row_of(i, 1);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            wait_loads<(STAGES - 2) * LOADS>();
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+#pragma unroll
+            for (int i = 0; i < FIRST; ++i) {
+                a[i] = frag(fa, la + then, i, 0);
+                sa[i] = scales(sa_at + then, i);
+            }
+#pragma unroll
+            for (int i = FIRST; i < FM; ++i) {
+#pragma unroll
+                for (int j = 0; j < FN; ++j)
+                    if (j / EACH == i - FIRST) {
+                        next[j] = frag(fb, lb + then, j, 0);
+                        sn[j] = scales(sb_at + then, j);
+                    }
+                row_of(i, 1);
+                a[i] = frag(fa, la + then, i, 0);
+                sa[i] = scales(sa_at + then, i);
+#pragma unroll
+                for (int l = 0; l < LOADS; ++l)
+                    if (l / LEACH == i - FIRST) load(l);
+            }
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                b[j] = next[j];
+                sb[j] = sn[j];
+            }
+            at = then;
+        }
+        wait_loads<0>();  // no store to LDS is left behind
+    }
+    // m and n of acc[i][j][0] within the block's tile.
+    static __device__ __forceinline__ int row(int i) {
+        return ((threadIdx.x >> 6) / (BN / WN)) * WM + 16 * i + (threadIdx.x & 15);
+    }
+    static __device__ __forceinline__ int col(int j) {
+        return ((threadIdx.x >> 6) % (BN / WN)) * WN + 16 * j + 4 * ((threadIdx.x & 63) >> 4);
+    }
+};
+
+}  // namespace fc

@@ -1,0 +1,320 @@
+// Matrices in microscaled 4-bit floating point, and products of them (fc_lm.h; the format
+// is described in fc_blocks.h, the product in fc_gemm4.h).
+//
+//   out[t, r] (+)= scale sum over k of a[t, k] b[r, k]
+#include "fc_blocks.h"
+#include "fc_gemm4.h"
+#include "fc_products.h"
+
+namespace {
+
+using fc::Operand4;
+
+constexpr int64_t LD_LIMIT = 1 << 21, TOKENS_LIMIT = (int64_t)1 << 31;
+constexpr int64_t CHUNK = 1 << 18;  // tokens of one launch, and of linear's packed inputs
+// Partial sums that a split product may write: two rounds of the chip's largest tiles.
+constexpr int64_t SUMS_LIMIT = (int64_t)1 << 25;
+
+// ---- columns to blocks ---------------------------------------------------------------
+
+// A block's tile is 256 of x's rows (a packed row's elements) by 64 of its columns (packed
+// rows): a thread holds two columns of 32 rows, a block of the format each, reads them a row
+// at a time, and the codes go through LDS, so that a packed row's 128 bytes are stored
+// together.
+struct ColumnArgs {
+    const void* x;
+    int64_t ldx;
+    uint8_t* codes;
+    int64_t ldc;
+    uint8_t* scales;
+    int64_t lds;
+    int rows, dim, blocks;   // packed rows
+};
+
+constexpr int COLUMNS = 64;
+
+template <typename T> __global__ __launch_bounds__(256) void pack_columns_kernel(ColumnArgs a) {
+    __shared__ __align__(16) uint32_t tile[COLUMNS][33];  // codes of 256 elements of a packed row
+    __shared__ uint8_t scale[COLUMNS][8];
+    const int kb = threadIdx.x >> 5, c2 = 2 * (threadIdx.x & 31);
+    const int k0 = blockIdx.x * 256 + 32 * kb, r0 = blockIdx.y * COLUMNS;
+    float v[2][32];
+    const T* const p = static_cast<const T*>(a.x) + (int64_t)k0 * a.ldx + r0 + c2;
+    const bool whole = r0 + c2 + 2 <= a.rows;
+    typedef T T2 __attribute__((ext_vector_type(2)));
+    typedef T2 T2_any __attribute__((aligned(alignof(T))));
+#pragma unroll
+    for (int e = 0; e < 32; ++e) {
+        v[0][e] = v[1][e] = 0.f;
+        if (k0 + e >= a.dim) continue;
+        if (whole) {
+            const T2 q = *reinterpret_cast<const T2_any*>(p + e * a.ldx);
+            v[0][e] = (float)q.x;
+            v[1][e] = (float)q.y;
+        } else if (r0 + c2 < a.rows) {
+            v[0][e] = (float)p[e * a.ldx];
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        fc::f32x8 q[4];
+        uint32_t most = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) q[i][e] = v[h][8 * i + e];
+            most = max(most, fc::most_of(q[i]));
+        }
+        const uint32_t byte = fc::scale_byte<fc::E2M1>(most);
+        const float inv = fc::scale_inverse(byte);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) tile[c2 + h][4 * kb + i] = fc::encode8<fc::E2M1>(q[i], inv).lo;
+        scale[c2 + h][kb] = (uint8_t)byte;
+    }
+    __syncthreads();
+    const int first = blockIdx.x * 8;  // block of the format
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int at = threadIdx.x + 256 * i, r = at >> 3, b = at & 7;  // 16 bytes each
+        if (r0 + r >= a.rows) continue;
+        if (first + b < a.blocks)
+            *reinterpret_cast<uint4*>(a.codes + (int64_t)(r0 + r) * a.ldc + 16 * (first + b)) =
+                uint4{tile[r][4 * b], tile[r][4 * b + 1], tile[r][4 * b + 2], tile[r][4 * b + 3]};
+        a.scales[(int64_t)(r0 + r) * a.lds + first + b] = first + b < a.blocks ? scale[r][b] : 0;
+    }
+}
+
+// ---- the product ------------------------------------------------------------------------
+
+using Wide4 = fc::Product4<256, 256, 128, 64, 2>;
+using Half4 = fc::Product4<128, 128, 64, 64, 2>;
+using Small4 = fc::Product4<64, 64, 32, 32, 4>;
+
+enum { WIDE4, HALF4, SMALL4, KINDS4 };
+
+// As COST, for steps of 256 of k.
+constexpr KindCost COST4[KINDS4] = {{256, 256, 1.7, 1.15, 9.5, 1}, {128, 128, 0.52, 0.6, 5.0, 2}, {64, 64, 0.2, 0.3, 4.0, 2}};
+
+template <bool ADD> hipError_t prepare_all() {
+    for (hipError_t e : {prepare<Wide4>((const void*)grad_kernel<Wide4, ADD, Operand4>), prepare<Half4>((const void*)grad_kernel<Half4, ADD, Operand4>),
+                         prepare<Small4>((const void*)grad_kernel<Small4, ADD, Operand4>)})
+        if (e != hipSuccess) return e;
+    return hipSuccess;
+}
+
+template <bool ADD> void launch(int kind, const ResultArgs<Operand4>& g, hipStream_t s) {
+    if (kind == WIDE4) launch_grad<Wide4, ADD, Operand4>(g, s);
+    else if (kind == HALF4) launch_grad<Half4, ADD, Operand4>(g, s);
+    else launch_grad<Small4, ADD, Operand4>(g, s);
+}
+
+}  // namespace
+
+struct fc_mxfp {
+    fc::CallOrder order;
+    fc::DeviceBlock block;
+    int64_t rows = 0, dim = 0, max_tokens = 0;
+    int blocks = 0, width = 0;   // of a row: scales, bytes of scales
+    int64_t sums = 0;            // floats of partial sums
+    uint8_t* codes = nullptr;    // linear's packed inputs
+    uint8_t* scales = nullptr;
+    float* sum = nullptr;
+};
+
+namespace {
+
+// A packed matrix of a call.
+struct Packed {
+    const void* codes;
+    int64_t ldc;
+    const void* scales;
+    int64_t lds;
+    int64_t rows;
+};
+
+fc::Span codes_span(const fc_mxfp* p, const Packed& m, bool written) { return {m.codes, m.rows, 16 * (int64_t)p->blocks, m.ldc, 1, written}; }
+fc::Span scales_span(const fc_mxfp* p, const Packed& m, bool written) { return {m.scales, m.rows, p->width, m.lds, 1, written}; }
+
+// What check_spans does not look at.
+int check_packed(const Packed& m) {
+    if (m.ldc > LD_LIMIT || m.lds > LD_LIMIT) return FC_EINVAL;
+    if (m.ldc % 16 || reinterpret_cast<uintptr_t>(m.codes) % 16 || m.lds % 8 || reinterpret_cast<uintptr_t>(m.scales) % 8) return FC_EALIGN;
+    return FC_OK;
+}
+
+fc::BlockRows rows_of(const fc_mxfp* p, const void* x, int64_t ldx, const Packed& m) {
+    return {x, ldx, static_cast<uint8_t*>(const_cast<void*>(m.codes)), m.ldc, static_cast<uint8_t*>(const_cast<void*>(m.scales)), m.lds, m.rows, (int)p->dim,
+            p->blocks, p->width};
+}
+
+Operand4 operand(const fc_mxfp* p, const Packed& m, int64_t r0, int64_t count) {
+    return {static_cast<const uint8_t*>(m.codes) + r0 * m.ldc, m.ldc / 2, (int)count, 8 * p->blocks, static_cast<const uint8_t*>(m.scales) + r0 * m.lds, m.lds};
+}
+
+// At most CHUNK rows of a.
+void product(fc_mxfp* p, const Operand4& a, const Operand4& b, float scale, void* out, int dt, int64_t ld, bool add, hipStream_t s) {
+    ResultArgs<Operand4> g{};
+    g.a = a;
+    g.b = b;
+    g.m = a.rows;
+    g.n = b.rows;
+    g.k = a.ks;
+    g.parts = 1;
+    const Choice c = choose_tiles(COST4, WIDE4, SMALL4, -1, g.m, g.n, fc::ceil_div(g.k, fc::GEMM_BK), true, p->sums);
+    const bool split = c.splits > 1;
+    g.kper = c.steps * fc::GEMM_BK;
+    g.scale = scale;
+    g.out = out;
+    g.dt = dt;
+    g.ld = ld;
+    g.sum = split ? p->sum : nullptr;
+    g.first = true;
+    g.last = !split;
+    if (add && !split) launch<true>(c.kind, g, s);
+    else launch<false>(c.kind, g, s);
+    if (split) join_splits(g, c.splits, add, s);
+}
+
+}  // namespace
+
+extern "C" {
+
+int fc_mxfp_create(fc_mxfp** plan, int64_t rows, int64_t dim, int64_t max_tokens) {
+    if (!plan) return FC_EINVAL;
+    *plan = nullptr;
+    if (rows < 1 || rows > LD_LIMIT || dim < 1 || dim > LD_LIMIT || max_tokens < 0 || max_tokens >= TOKENS_LIMIT) return FC_EINVAL;
+    return fc::no_throw([&] {
+        fc_mxfp* p = new fc_mxfp;
+        p->rows = rows;
+        p->dim = dim;
+        p->max_tokens = max_tokens;
+        p->blocks = (int)fc::ceil_div(dim, fc::BLOCK);
+        p->width = 8 * (int)fc::ceil_div(dim, 256);
+        const int64_t c = std::min(max_tokens, CHUNK);
+        p->sums = std::min<int64_t>(SUMS_LIMIT, 64 * fc::ceil_div(c, 64) * 64 * rows);
+        fc::Layout at;
+        const uint64_t o_codes = at.take(c * 16 * p->blocks), o_scales = at.take(c * p->width), o_sum = at.take(p->sums * 4);
+        int rc = p->order.create();
+        if (!rc) rc = fc::hip_code(prepare_all<false>());
+        if (!rc) rc = fc::hip_code(prepare_all<true>());
+        if (!rc) rc = p->block.create(at.size);
+        if (rc) {
+            fc_mxfp_destroy(p);
+            return rc;
+        }
+        p->codes = reinterpret_cast<uint8_t*>(p->block.p + o_codes);
+        p->scales = reinterpret_cast<uint8_t*>(p->block.p + o_scales);
+        p->sum = reinterpret_cast<float*>(p->block.p + o_sum);
+        *plan = p;
+        return FC_OK;
+    });
+}
+
+void fc_mxfp_destroy(fc_mxfp* p) {
+    if (!p) return;
+    p->block.destroy();
+    p->order.destroy();
+    delete p;
+}
+
+int fc_mxfp_pack(fc_mxfp* p, const void* x, int x_dtype, int64_t ld_x, int64_t rows, int transpose, void* codes, int64_t ld_codes, void* scales,
+                 int64_t ld_scales, void* stream) {
+    return fc::no_throw([&]() -> int {
+        if (!p || rows < 0 || rows >= TOKENS_LIMIT) return FC_EINVAL;
+        const Packed m{codes, ld_codes, scales, ld_scales, rows};
+        const int bytes = fc::dtype_bytes(x_dtype);
+        int rc = fc::check_spans({transpose ? fc::Span{x, p->dim, rows, ld_x, bytes, false} : fc::Span{x, rows, p->dim, ld_x, bytes, false}, codes_span(p, m, true),
+                                  scales_span(p, m, true)});
+        if (!rc) rc = check_packed(m);
+        if (rc) return rc;
+        const hipStream_t s = static_cast<hipStream_t>(stream);
+        bool note;
+        rc = p->order.begin(s, note);
+        if (rc) return rc;
+        if (!transpose) {
+            fc::pack_rows<fc::E2M1>(rows_of(p, x, ld_x, m), x_dtype, s);
+        } else {
+            const int64_t groups = fc::ceil_div(p->dim, 256), most = (int64_t)COLUMNS * 32768;  // a launch's blocks along y
+            for (int64_t r0 = 0; r0 < rows; r0 += most) {
+                const int64_t count = std::min(most, rows - r0);
+                const ColumnArgs a{static_cast<const char*>(x) + r0 * bytes, ld_x, static_cast<uint8_t*>(codes) + r0 * ld_codes, ld_codes,
+                                   static_cast<uint8_t*>(scales) + r0 * ld_scales, ld_scales, (int)count, (int)p->dim, p->blocks};
+                const dim3 grid((unsigned)groups, (unsigned)fc::ceil_div(count, COLUMNS));
+                fc::by_dtype(x_dtype, [&](auto t) { pack_columns_kernel<decltype(t)><<<grid, 256, 0, s>>>(a); });
+            }
+        }
+        rc = fc::hip_code(hipGetLastError());
+        p->order.done(s, note);
+        return rc;
+    });
+}
+
+int fc_mxfp_unpack(fc_mxfp* p, const void* codes, int64_t ld_codes, const void* scales, int64_t ld_scales, int64_t rows, void* out, int out_dtype,
+                   int64_t ld_out, void* stream) {
+    return fc::no_throw([&]() -> int {
+        if (!p || rows < 0 || rows >= TOKENS_LIMIT) return FC_EINVAL;
+        const Packed m{codes, ld_codes, scales, ld_scales, rows};
+        int rc = fc::check_spans({codes_span(p, m, false), scales_span(p, m, false), {out, rows, p->dim, ld_out, fc::dtype_bytes(out_dtype), true}});
+        if (!rc) rc = check_packed(m);
+        if (rc) return rc;
+        const hipStream_t s = static_cast<hipStream_t>(stream);
+        bool note;
+        rc = p->order.begin(s, note);
+        if (rc) return rc;
+        fc::unpack_rows<fc::E2M1>(rows_of(p, nullptr, 0, m), out, out_dtype, ld_out, (int)p->dim, s);
+        rc = fc::hip_code(hipGetLastError());
+        p->order.done(s, note);
+        return rc;
+    });
+}
+
+int fc_mxfp_product(fc_mxfp* p, const void* a_codes, int64_t ld_a_codes, const void* a_scales, int64_t ld_a_scales, int64_t n, const void* b_codes,
+                    int64_t ld_b_codes, const void* b_scales, int64_t ld_b_scales, float scale, void* out, int out_dtype, int64_t ld_out, int accumulate,
+                    void* stream) {
+    return fc::no_throw([&]() -> int {
+        if (!p || n < 0 || n > p->max_tokens) return FC_EINVAL;
+        const Packed a{a_codes, ld_a_codes, a_scales, ld_a_scales, n}, b{b_codes, ld_b_codes, b_scales, ld_b_scales, p->rows};
+        const int bytes = fc::dtype_bytes(out_dtype);
+        int rc = fc::check_spans({codes_span(p, a, false), scales_span(p, a, false), codes_span(p, b, false), scales_span(p, b, false),
+                                  {out, n, p->rows, ld_out, bytes, true}});
+        if (!rc) rc = check_packed(a);
+        if (!rc) rc = check_packed(b);
+        if (rc) return rc;
+        const hipStream_t s = static_cast<hipStream_t>(stream);
+        bool note;
+        rc = p->order.begin(s, note);
+        if (rc) return rc;
+        for (int64_t t0 = 0; t0 < n; t0 += CHUNK)
+            product(p, operand(p, a, t0, std::min(CHUNK, n - t0)), operand(p, b, 0, p->rows), scale, static_cast<char*>(out) + t0 * ld_out * bytes, out_dtype, ld_out,
+                    accumulate != 0, s);
+        rc = fc::hip_code(hipGetLastError());
+        p->order.done(s, note);
+        return rc;
+    });
+}
+
+int fc_mxfp_linear(fc_mxfp* p, const void* x, int x_dtype, int64_t ld_x, int64_t n, const void* b_codes, int64_t ld_b_codes, const void* b_scales,
+                   int64_t ld_b_scales, float scale, void* out, int out_dtype, int64_t ld_out, int accumulate, void* stream) {
+    return fc::no_throw([&]() -> int {
+        if (!p || n < 0 || n > p->max_tokens) return FC_EINVAL;
+        const Packed b{b_codes, ld_b_codes, b_scales, ld_b_scales, p->rows};
+        const int bytes = fc::dtype_bytes(out_dtype), xbytes = fc::dtype_bytes(x_dtype);
+        int rc = fc::check_spans({{x, n, p->dim, ld_x, xbytes, false}, codes_span(p, b, false), scales_span(p, b, false), {out, n, p->rows, ld_out, bytes, true}});
+        if (!rc) rc = check_packed(b);
+        if (rc) return rc;
+        const hipStream_t s = static_cast<hipStream_t>(stream);
+        bool note;
+        rc = p->order.begin(s, note);
+        if (rc) return rc;
+        for (int64_t t0 = 0; t0 < n; t0 += CHUNK) {
+            const Packed a{p->codes, 16 * (int64_t)p->blocks, p->scales, p->width, std::min(CHUNK, n - t0)};
+            fc::pack_rows<fc::E2M1>(rows_of(p, static_cast<const char*>(x) + t0 * ld_x * xbytes, ld_x, a), x_dtype, s);
+            product(p, operand(p, a, 0, a.rows), operand(p, b, 0, p->rows), scale, static_cast<char*>(out) + t0 * ld_out * bytes, out_dtype, ld_out, accumulate != 0, s);
+        }
+        rc = fc::hip_code(hipGetLastError());
+        p->order.done(s, note);
+        return rc;
+    });
+}
+
+}  // extern "C"

@@ -17,40 +17,16 @@
 // gives both dw = a(g) P and dg = a'(g) w P.
 #include <algorithm>
 
+#include "fc_eight.h"
 #include "fc_lm_host.h"
 
 namespace {
 
 typedef _Float16 f16;
 typedef __bf16 bf16;
-
-// 8 neighbours of a row, which may start at any element: global memory takes any
-// alignment.
-template <typename T> struct Eight {
-    typedef T vec __attribute__((ext_vector_type(8)));
-    typedef vec any __attribute__((aligned(alignof(T))));
-};
-typedef float f32x8 __attribute__((ext_vector_type(8)));
-
-// Up to 8 elements from p on, `left` of them in the row; zeros past it.
-template <typename T> __device__ __forceinline__ f32x8 load8(const T* p, int left) {
-    if (left >= 8) return __builtin_convertvector(*reinterpret_cast<const typename Eight<T>::any*>(p), f32x8);
-    f32x8 v{};
-#pragma unroll
-    for (int e = 0; e < 7; ++e)
-        if (e < left) v[e] = (float)p[e];
-    return v;
-}
-
-template <typename T> __device__ __forceinline__ void store8(T* p, int left, f32x8 v) {
-    if (left >= 8) {
-        *reinterpret_cast<typename Eight<T>::any*>(p) = __builtin_convertvector(v, typename Eight<T>::vec);
-        return;
-    }
-#pragma unroll
-    for (int e = 0; e < 7; ++e)
-        if (e < left) p[e] = (T)v[e];
-}
+using fc::f32x8;
+using fc::load8;
+using fc::store8;
 
 // A channel vector's elements from c on; 1 where there is no vector.
 __device__ __forceinline__ f32x8 channels(const float* p, int c, int left) {

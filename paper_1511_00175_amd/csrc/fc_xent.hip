@@ -23,22 +23,9 @@
 // in all) the first product 4.5 ms, dw 4.3, dx 3.8, the pass from numerators to d 0.81
 // (4.3 GB), join 0.02, the copy of x 0.02.  bf16, 24 tokens, 65536 rows of 2048, losses
 // only: 67 us with other data in the caches (268 MB at 4.0 TB/s), 47 call after call.
-#include <algorithm>
-
-#include "fc_gemm.h"
-#include "fc_lm_host.h"
-
-using fc::Operand;
-using fc::f32x2;
-using fc::f32x4;
-using fc::Half;
+#include "fc_products.h"
 
 namespace {
-
-typedef _Float16 f16;
-typedef __bf16 bf16;
-
-extern __shared__ __align__(1024) char lds[];
 
 constexpr float LOG2E = 1.44269504088896341f;
 
@@ -50,10 +37,6 @@ template <> constexpr float D_SCALE<f16> = 32768.f;
 
 // Results below 2^-126 are zero.
 __device__ __forceinline__ float exp_(float x) { return __builtin_amdgcn_exp2f(x * LOG2E); }
-
-__device__ __forceinline__ int64_t target_of(const void* p, int bytes, int64_t t) {
-    return bytes == 8 ? static_cast<const int64_t*>(p)[t] : static_cast<const int32_t*>(p)[t];
-}
 
 // Up to so many tokens d is kept as a sum of two 16-bit numbers, of numerators in
 // fp32: the rounding of d at the target, up to 2^-9 in bf16, averages out over
@@ -284,231 +267,12 @@ template <typename T, typename N> __global__ __launch_bounds__(256) void diff_ke
     }
 }
 
-// ---- the gradients' products ------------------------------------------------
-
-__device__ __forceinline__ void store_one(void* p, int dt, int64_t at, float v) {
-    if (dt == FC_F32) static_cast<float*>(p)[at] = v;
-    else if (dt == FC_F16) static_cast<f16*>(p)[at] = (f16)v;
-    else static_cast<bf16*>(p)[at] = (bf16)v;
-}
-
-// Up to four neighbouring elements of a row, of which `left` are in it.
-__device__ __forceinline__ void store_four(void* p, int dt, int64_t at, f32x4 v, int left) {
-    if (left < 4) {
-#pragma unroll
-        for (int e = 0; e < 3; ++e)
-            if (e < left) store_one(p, dt, at + e, v[e]);
-    } else if (dt == FC_F32) {
-        *reinterpret_cast<fc::f32x4_any*>(static_cast<float*>(p) + at) = v;
-    } else if (dt == FC_F16) {
-        *reinterpret_cast<fc::f16x4_any*>(static_cast<f16*>(p) + at) = __builtin_convertvector(v, fc::f16x4);
-    } else {
-        *reinterpret_cast<fc::b16x4_any*>(static_cast<bf16*>(p) + at) = __builtin_convertvector(v, fc::b16x4);
-    }
-}
-
-struct GradArgs {
-    Operand a, b;
-    int m, n, k;             // of the product
-    int kper;                // of one split, a multiple of 64
-    int parts;               // 2: a has two halves
-    float scale;
-    const int* row;          // per m: below 0, the result is zero; or null
-    void* out;
-    int dt;
-    int64_t ld;
-    float* sum;              // fp32 sums over calls or splits, [split][m][n], or null
-    bool first, last;        // of the calls that add to `sum`
-    int tm, tn;
-};
-
-// 8192 tokens, 131072 rows of 2048 take 3.8 ms for dx and 4.3 for dw in a trace (1.17 and
-// 1.02 PFLOP/s): the matrix cores are busy 69% and 60% of a unit's cycles, at 1.54 and 1.66
-// GHz.  Tiles in groups of 8 rows keep what the blocks of an XCD read in its L2 (80% hits).
-// Few tokens give few tiles: k is then split.
-template <typename P> __global__ __launch_bounds__(P::THREADS, P::THREADS / 256) void grad_kernel(GradArgs a) {
-    int ti, tj;
-    fc::tile_place(fc::xcd_order(blockIdx.x, a.tm * a.tn), a.tm, a.tn, 8, ti, tj);
-    const int kb = blockIdx.y * a.kper, ke = min(a.k, kb + a.kper);
-    P p;
-    p.run(lds, a.a, a.b, ti * P::BM, tj * P::BN, kb, ke, a.parts);
-    float* const sum = a.sum ? a.sum + (int64_t)blockIdx.y * a.m * a.n : nullptr;
-    // Results go through LDS by strips of 16 rows, so that a row's neighbours are
-    // stored by neighbouring lanes, whatever its start's alignment.
-    float(*const part)[P::WN + 4] = reinterpret_cast<float(*)[P::WN + 4]>(lds + (threadIdx.x >> 6) * 16 * (P::WN + 4) * sizeof(float));
-    static_assert(P::WAVES * 16 * (P::WN + 4) * sizeof(float) <= P::LDS, "the strips of all waves fit");
-    const int lane = threadIdx.x & 63, n0 = tj * P::BN + P::col(0) - 4 * (lane >> 4);
-    __syncthreads();  // the tiles in LDS are done with
-#pragma unroll
-    for (int i = 0; i < P::FM; ++i) {
-        const int m0 = ti * P::BM + P::row(i) - (lane & 15);
-#pragma unroll
-        for (int j = 0; j < P::FN; ++j) *reinterpret_cast<f32x4*>(part[lane & 15] + 16 * j + 4 * (lane >> 4)) = p.acc[i][j];
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll 2
-        for (int k = lane; k < 16 * P::WN / 4; k += 64) {
-            const int y = k / (P::WN / 4), z = k % (P::WN / 4) * 4, m = m0 + y, left = a.n - n0 - z;
-            if (m >= a.m || left <= 0) continue;
-            f32x4 v = *reinterpret_cast<const f32x4*>(part[y] + z);
-            if (sum) {
-                float* const s = sum + (int64_t)m * a.n + n0 + z;
-                if (!a.first) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] += s[min(e, left - 1)];
-                }
-                if (!a.last) {
-                    store_four(s, FC_F32, 0, v, left);
-                    continue;
-                }
-            }
-            store_four(a.out, a.dt, (int64_t)m * a.ld + n0 + z, a.row && a.row[m] < 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : a.scale * v, left);
-        }
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_sched_barrier(0);
-    }
-}
-
-struct SplitArgs {
-    const float* sum;
-    int splits, m, n;
-    float scale;
-    const int* row;
-    void* out;
-    int dt;
-    int64_t ld;
-};
-
-// The splits of a product added in order: 4 to 7 us, a launch's latency and one
-// trip to memory.
-__global__ __launch_bounds__(256) void split_kernel(SplitArgs a) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, total = (int64_t)a.m * a.n;
-    if (i >= total) return;
-    const int m = (int)(i / a.n), n = (int)(i % a.n);
-    float v = 0.f;
-#pragma unroll 8
-    for (int s = 0; s < a.splits; ++s) v += a.sum[s * total + i];
-    store_one(a.out, a.dt, (int64_t)m * a.ld + n, a.row && a.row[m] < 0 ? 0.f : v * a.scale);
-}
-
-// Copies with rows of a multiple of 8 elements: bound by HBM (8192 x 2048, 67 MB in
-// all, 16 us).
-struct PackArgs {
-    const void* in;
-    int64_t ld_in;
-    void* out;
-    int64_t ld_out;          // a multiple of 8; the elements past the row's length are zeros
-    int64_t rows;
-    int len;
-    const void* targets;     // or null: rows without a target become zeros
-    int target_bytes;
-    int targets_below;
-};
-
-__global__ __launch_bounds__(256) void pack_kernel(PackArgs a) {
-    typedef unsigned short u16;
-    const int per_row = (int)(a.ld_out / 8);
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t r = i / per_row;
-    const int c = (int)(i % per_row) * 8;
-    if (r >= a.rows) return;
-    bool keep = true;
-    if (a.targets) {
-        const int64_t y = target_of(a.targets, a.target_bytes, r);
-        keep = y >= 0 && y < a.targets_below;
-    }
-    typedef u16 u16x8 __attribute__((ext_vector_type(8)));
-    typedef u16x8 u16x8_any __attribute__((aligned(2)));
-    const u16* in = static_cast<const u16*>(a.in) + r * a.ld_in + c;
-    u16x8 v{};
-    if (keep && c + 8 <= a.len) {
-        v = *reinterpret_cast<const u16x8_any*>(in);
-    } else if (keep) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (c + e < a.len) v[e] = in[e];
-    }
-    *reinterpret_cast<u16x8*>(static_cast<u16*>(a.out) + r * a.ld_out + c) = v;
-}
-
-// Tiles by size; BROAD is for the gradients, where dim is often just above a multiple
-// of 256 or fills the chip's rounds better so (the first product's tiles end with more
-// work: 1003 tokens, 50001 rows of 520 took 122 us with it, 119 with LARGE; dx 74, 104
-// with MIDDLE; 8192 tokens, 8192 rows of 1280 in all 565, 657).  The estimate is not always
-// right: for dw of the 1003 tokens it takes MIDDLE (115 us in a trace, the whole call 355
-// to 360), with which BROAD's call takes 341 to 350.  SHORT and NARROW are for up to 64
-// tokens, which are bound by reading w: a compute unit reads at most about 50 GB/s, so
-// that few rows of w are read faster by more blocks.
-template <typename T, bool AS, bool BS> using Large = fc::Product<T, 256, 256, 128, 64, AS, BS>;
-template <typename T, bool AS, bool BS> using Broad = fc::Product<T, 256, 192, 128, 48, AS, BS>;
-template <typename T, bool AS, bool BS> using Middle = fc::Product<T, 128, 128, 64, 64, AS, BS>;
-template <typename T, bool AS, bool BS> using Short = fc::Product<T, 64, 128, 64, 32, AS, BS, 3>;
-template <typename T, bool AS, bool BS> using Narrow = fc::Product<T, 64, 32, 16, 32, AS, BS, 6>;
-template <typename T, bool AS, bool BS> using Once = fc::Product<T, 64, 128, 64, 32, AS, BS, 3, 0, true>;
-
-enum TileKind { LARGE, BROAD, MIDDLE, SHORT, NARROW, KINDS };
-
-constexpr int CUS = 256;
-
-// In us, measured with 1 to 512 tiles: a step of 64 of k with the compute unit full
-// of such tiles (`per` at a time) and alone, and a tile's start and end.
-struct KindCost {
-    int bm, bn;
-    double full, alone, once;
-    int per;
-};
-constexpr KindCost COST[KINDS] = {{256, 256, 1.7, 1.15, 9.5, 1}, {256, 192, 1.38, 1.0, 8.0, 1}, {128, 128, 0.52, 0.6, 5.0, 2}, {64, 128, 0.55, 0.6, 4.0, 2}, {64, 32, 0.2, 0.3, 4.0, 2}};
-
-struct Choice {
-    TileKind kind;
-    int splits;      // parts of k, of `steps` of 64 each
-    int steps;
-};
-
-constexpr int64_t SPLIT_FLOATS = (int64_t)1 << 27;
-
-// The tiles of an m x n product over k, and the parts k is split into, by the
-// least estimated time; m and k are taken up to multiples of 64, so that the
-// choice is one for every list of as many 64s of tokens.
-Choice choose(int64_t m, int64_t n, int64_t k, bool few, bool may_split, bool broad) {
-    m = fc::ceil_div(m, 64) * 64;
-    const int64_t total = fc::ceil_div(k, fc::GEMM_BK);
-    Choice best{MIDDLE, 1, (int)total};
-    double least = 1e300;
-    for (int kind = few ? SHORT : LARGE; kind <= (few ? NARROW : MIDDLE); ++kind) {
-        if (kind == BROAD && !broad) continue;
-        const KindCost& c = COST[kind];
-        const int64_t tiles = fc::ceil_div(m, c.bm) * fc::ceil_div(n, c.bn);
-        const int fill = (int)std::min<int64_t>(64, CUS * c.per / tiles);  // as many as the chip takes at once
-        for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, fill}) {
-            if (s < 1) continue;
-            const int64_t steps = fc::ceil_div(total, s), parts = fc::ceil_div(total, steps), blocks = tiles * parts;
-            if (s > 1 && (!may_split || steps < 2 || parts * m * n > SPLIT_FLOATS)) continue;
-            const double at_once = (double)std::min<int64_t>(c.per, fc::ceil_div(blocks, CUS));
-            double t = fc::ceil_div(blocks, CUS * c.per) * (steps * std::max(c.alone, c.full * at_once) + c.once);
-            if (parts > 1) t += 5.0 + 8.0 * parts * m * n / 4.5e6;  // partial sums, written and read
-            if (t < least) {
-                least = t;
-                best = {(TileKind)kind, (int)parts, (int)steps};
-            }
-        }
-    }
-    return best;
-}
-
-template <typename P> hipError_t prepare(const void* kernel) {
-    return P::LDS > 64 * 1024 ? hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, P::LDS) : hipSuccess;
-}
+// ---- the host's side ----------------------------------------------------------
 
 template <typename P> void launch_logit(LogitArgs a, hipStream_t s) {
     a.tm = (int)fc::ceil_div(a.n, P::BM);
     a.tn = (int)fc::ceil_div(a.rows, P::BN);
     logit_kernel<P><<<a.tm * a.tn, P::THREADS, P::LDS, s>>>(a);
-}
-
-template <typename P> void launch_grad(GradArgs a, hipStream_t s) {
-    a.tm = (int)fc::ceil_div(a.m, P::BM);
-    a.tn = (int)fc::ceil_div(a.n, P::BN);
-    grad_kernel<P><<<dim3(a.tm * a.tn, (unsigned)fc::ceil_div(a.k, a.kper)), P::THREADS, P::LDS, s>>>(a);
 }
 
 template <typename T> hipError_t prepare_all() {
@@ -585,10 +349,6 @@ template <typename T>
 int run(fc_xent* p, const void* x, int64_t ldx, const void* w, int64_t ldw, const void* targets, int target_bytes, int64_t n,
         float scale, float* loss, void* dx, int xdt, int64_t lddx, void* dw, int wdt, int64_t lddw, hipStream_t s) {
     const bool grads = dx || dw;
-    auto join_splits = [&](const GradArgs& g, int splits) {
-        SplitArgs q{g.sum, splits, g.m, g.n, g.scale, g.row, g.out, g.dt, g.ld};
-        split_kernel<<<(unsigned)fc::ceil_div((int64_t)g.m * g.n, 256), 256, 0, s>>>(q);
-    };
     auto pack = [&](const void* in, int64_t ld, void* out, int64_t rows, const void* mask) {
         fc::by_launches(rows, p->ldp / 8, [&](int64_t r0, int64_t count) {
             PackArgs a{static_cast<const char*>(in) + r0 * ld * 2, ld, static_cast<char*>(out) + r0 * p->ldp * 2, p->ldp, count, (int)p->dim,
@@ -655,7 +415,7 @@ int run(fc_xent* p, const void* x, int64_t ldx, const void* w, int64_t ldw, cons
             else if (c.kind == SHORT && once) launch_grad<Once<T, false, true>>(g, s);
             else if (c.kind == SHORT) launch_grad<Short<T, false, true>>(g, s);
             else launch_grad<Narrow<T, false, true>>(g, s);
-            if (c.splits > 1) join_splits(g, c.splits);
+            if (c.splits > 1) join_splits(g, c.splits, false, s);
         }
         if (dw) {
             GradArgs g{};
@@ -677,16 +437,10 @@ int run(fc_xent* p, const void* x, int64_t ldx, const void* w, int64_t ldw, cons
             if (c.kind == LARGE) launch_grad<Large<T, true, true>>(g, s);
             else if (c.kind == BROAD) launch_grad<Broad<T, true, true>>(g, s);
             else launch_grad<Middle<T, true, true>>(g, s);
-            if (c.splits > 1) join_splits(g, c.splits);
+            if (c.splits > 1) join_splits(g, c.splits, false, s);
         }
     }
     return fc::hip_code(hipGetLastError());
-}
-
-// Zeros for a gradient without tokens.
-__global__ __launch_bounds__(256) void zero_kernel(void* p, int dt, int64_t rows, int64_t len, int64_t ld) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i < rows * len) store_one(p, dt, i / len * ld + i % len, 0.f);
 }
 
 int call(fc_xent* p, const void* x, int64_t ldx, const void* w, int64_t ldw, const void* targets, int target_bytes, int64_t n,
@@ -707,11 +461,7 @@ int call(fc_xent* p, const void* x, int64_t ldx, const void* w, int64_t ldw, con
     rc = p->order.begin(s, note);
     if (rc) return rc;
     if (n == 0) {
-        if (dw)
-            fc::by_launches(p->rows, p->dim, [&](int64_t r0, int64_t count) {
-                zero_kernel<<<(unsigned)fc::ceil_div(count * p->dim, 256), 256, 0, s>>>(static_cast<char*>(dw) + r0 * lddw * fc::dtype_bytes(wdt), wdt,
-                                                                                        count, p->dim, lddw);
-            });
+        if (dw) zeros(dw, wdt, p->rows, p->dim, lddw, s);
         rc = fc::hip_code(hipGetLastError());
     } else if (p->dtype == FC_F16) {
         rc = run<f16>(p, x, ldx, w, ldw, targets, target_bytes, n, scale, loss, dx, xdt, lddx, dw, wdt, lddw, s);

@@ -6,8 +6,8 @@ stream or torch's current one."""
 import ctypes
 
 from ._fc import FC_F16, FC_F32, FcError
-from ._fc_lm import (FC_BF16, FC_GATE_NONE, FC_GATE_SIGMOID, FC_GATE_SILU, FC_NORM_LAYER, FC_NORM_RMS, fc_matrix,
-                     lib)
+from ._fc_lm import (FC_BF16, FC_BLOCK_E4M3, FC_BLOCK_I8, FC_GATE_NONE, FC_GATE_SIGMOID, FC_GATE_SILU, FC_NORM_LAYER,
+                     FC_NORM_RMS, fc_matrix, lib)
 
 DTYPES = {"f32": FC_F32, "f16": FC_F16, "bf16": FC_BF16}
 _CODES = {}     # torch dtype -> fc_dtype value
@@ -85,6 +85,24 @@ def _vector(t, name, n, device, code):
     return t.data_ptr()
 
 
+def _bytes(t, name, rows, cols, device, dtype):
+    """`t` must be a (rows, cols) tensor of `dtype`, one byte to an element, on the device, its
+    rows contiguous and any distance apart; returns (pointer, row stride)."""
+    _tensor(t, name)
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the plan on {device}")
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+        raise ValueError(f"{name} is {tuple(t.shape)}, not {(rows, cols)}")
+    ld, one = t.stride()
+    if rows <= 1:
+        ld = cols
+    if (one != 1 and cols > 1) or ld < cols:
+        raise ValueError(f"{name} must have contiguous rows that do not overlap")
+    return t.data_ptr(), ld
+
+
 def _rows(t, name):
     """The rows of a tensor whose other checks are _matrix's."""
     _tensor(t, name)
@@ -104,7 +122,8 @@ def _stream(stream):
 _FUNCTIONS = {n: getattr(lib, n) for n in ("fc_embed_lookup", "fc_embed_grad", "fc_xent_loss", "fc_xent_loss_grad",
                                            "fc_muon_orthogonalize", "fc_muon_step", "fc_norm_before", "fc_norm_after",
                                            "fc_norm_between", "fc_norm_before_grad", "fc_norm_after_grad",
-                                           "fc_norm_between_grad")}
+                                           "fc_norm_between_grad", "fc_ckpt_pack", "fc_ckpt_unpack", "fc_ckpt_grad",
+                                           "fc_mxfp_pack", "fc_mxfp_unpack", "fc_mxfp_product", "fc_mxfp_linear")}
 
 
 class _Handle:
@@ -427,3 +446,140 @@ class Norm(_Handle):
         self._call("fc_norm_between_grad", xp, xl, bp, bl, yp, yl, op, ol, n, gp, gl, self._weight(weight, "weight"),
                    self._weight(next_weight, "next_weight"), scale, hp, hl, dp, dl, dgp, dgl, wp, np_, code, bool(accumulate),
                    _stream(stream))
+
+
+_BLOCK = 32  # neighbours of a row that share a scale
+_FORMATS = {"i8": FC_BLOCK_I8, "e4m3": FC_BLOCK_E4M3}
+
+
+class Checkpoint(_Handle):
+    """Activations (tokens, dim) kept in 8 bits, 32 neighbours of a row to a scale
+    (fc_ckpt), and what a backward pass needs of them: the activations themselves,
+    and the gradient of a weight of up to `max_outs` rows from up to `max_tokens`
+    tokens and a dy of `dtype` ("f16" or "bf16").
+
+    format: "i8", steps of 1/64 to 1/128 of the 32's largest magnitude, or "e4m3",
+            4 bits of each element.  A block with an infinity or NaN is kept as NaN.
+
+    They are held by two tensors of the caller's, codes (tokens, 32 ceil(dim / 32))
+    of torch.int8 or torch.float8_e4m3fn on 16 bytes with a row stride of a multiple of 16,
+    and scales (tokens, ceil(dim / 32)) of torch.uint8, the exponents of powers of two plus
+    127, as empty() makes them."""
+
+    _destroy = "fc_ckpt_destroy"
+
+    def __init__(self, dim, max_tokens, max_outs=0, dtype="f16", format="i8"):
+        import torch
+        if dtype not in ("f16", "bf16"):
+            raise ValueError(f"dtype must be f16 or bf16, not {dtype}")
+        if format not in _FORMATS:
+            raise ValueError(f"format must be i8 or e4m3, not {format}")
+        self.code = DTYPES[dtype]
+        self._create("fc_ckpt_create", dim, max_tokens, max_outs, self.code, _FORMATS[format])
+        self.dim, self.max_tokens, self.max_outs = dim, max_tokens, max_outs
+        self.blocks = -(-dim // _BLOCK)
+        self.format = torch.int8 if format == "i8" else torch.float8_e4m3fn
+
+    def empty(self, n):
+        """Codes and scales for n tokens."""
+        import torch
+        return (torch.empty((n, _BLOCK * self.blocks), dtype=self.format, device=self.device),
+                torch.empty((n, self.blocks), dtype=torch.uint8, device=self.device))
+
+    def _kept(self, codes, scales, n):
+        import torch
+        return (*_bytes(codes, "codes", n, _BLOCK * self.blocks, self.device, self.format),
+                *_bytes(scales, "scales", n, self.blocks, self.device, torch.uint8))
+
+    def pack(self, x, codes, scales, stream=None):
+        """Codes and scales of x (tokens, dim), f32, f16 or bf16; any number of tokens."""
+        n = _rows(x, "x")
+        xp, xc, xl = _matrix(x, "x", n, self.dim, self.device)
+        self._call("fc_ckpt_pack", xp, xc, xl, n, *self._kept(codes, scales, n), _stream(stream))
+
+    def unpack(self, codes, scales, out, stream=None):
+        """out = the activations kept, rounded to its type."""
+        n = _rows(out, "out")
+        op, oc, ol = _matrix(out, "out", n, self.dim, self.device)
+        self._call("fc_ckpt_unpack", *self._kept(codes, scales, n), n, op, oc, ol, _stream(stream))
+
+    def grad(self, dy, codes, scales, dw, scale=1.0, accumulate=False, stream=None):
+        """dw[o] = (dw[o] if accumulate else 0) + scale * the sum over t of dy[t, o] x[t],
+        for dy (tokens, outs) and dw (outs, dim) of any type.  dy lies on 16 bytes with a row
+        stride of a multiple of 8, unless max_outs is no multiple of 8."""
+        n, outs = _rows(dy, "dy"), _rows(dw, "dw")
+        if n > self.max_tokens:
+            raise ValueError(f"{n} tokens for a plan of {self.max_tokens}")
+        if outs > self.max_outs:
+            raise ValueError(f"{outs} outputs for a plan of {self.max_outs}")
+        yp, _, yl = _matrix(dy, "dy", n, outs, self.device, self.code)
+        gp, gc, gl = _matrix(dw, "dw", outs, self.dim, self.device)
+        if n <= 1 and not self.max_outs % 8:
+            yl = -(-yl // 8) * 8  # the stride of one row says nothing
+        self._call("fc_ckpt_grad", yp, yl, *self._kept(codes, scales, n), n, outs, scale, gp, gc, gl, bool(accumulate),
+                   _stream(stream))
+
+
+class Mxfp4(_Handle):
+    """Products along `dim` with a matrix of `rows` rows, both operands in 4-bit floating
+    point with a scale for every 32 along the rows (fc_mxfp, MXFP4), for up to `max_tokens`
+    rows a call: a layer's outputs from a weight (rows, dim), or, with a plan of the sizes
+    exchanged and the weight packed with `transpose`, the gradient of its inputs.
+
+    A packed matrix is held by two tensors of the caller's, of torch.uint8: codes (r, 16
+    ceil(dim / 32)), the even element in a byte's low half, on 16 bytes with a row stride of a
+    multiple of 16, and scales (r, 8 ceil(dim / 256)), zeros past the blocks, on 8 bytes with
+    a stride of a multiple of 8, as empty() makes them."""
+
+    _destroy = "fc_mxfp_destroy"
+
+    def __init__(self, rows, dim, max_tokens):
+        self._create("fc_mxfp_create", rows, dim, max_tokens)
+        self.rows, self.dim, self.max_tokens = rows, dim, max_tokens
+        self.widths = 16 * -(-dim // _BLOCK), 8 * -(-dim // (8 * _BLOCK))  # of codes and scales
+
+    def empty(self, n):
+        """Codes and scales for n rows."""
+        import torch
+        return tuple(torch.empty((n, w), dtype=torch.uint8, device=self.device) for w in self.widths)
+
+    def _packed(self, codes, scales, n, name=""):
+        import torch
+        return (*_bytes(codes, name + "codes", n, self.widths[0], self.device, torch.uint8),
+                *_bytes(scales, name + "scales", n, self.widths[1], self.device, torch.uint8))
+
+    def _tokens(self, t, name):
+        n = _rows(t, name)
+        if n > self.max_tokens:
+            raise ValueError(f"{n} tokens for a plan of {self.max_tokens}")
+        return n
+
+    def pack(self, x, codes, scales, transpose=False, stream=None):
+        """Codes and scales of x (n, dim) or, with `transpose`, of the columns of x (dim, n);
+        f32, f16 or bf16, any n."""
+        _tensor(x, "x")
+        n = x.shape[-1] if transpose and x.dim() else _rows(x, "x")
+        xp, xc, xl = _matrix(x, "x", *((self.dim, n) if transpose else (n, self.dim)), self.device)
+        self._call("fc_mxfp_pack", xp, xc, xl, n, bool(transpose), *self._packed(codes, scales, n), _stream(stream))
+
+    def unpack(self, codes, scales, out, stream=None):
+        """out (n, dim) = the numbers kept, rounded to its type."""
+        n = _rows(out, "out")
+        op, oc, ol = _matrix(out, "out", n, self.dim, self.device)
+        self._call("fc_mxfp_unpack", *self._packed(codes, scales, n), n, op, oc, ol, _stream(stream))
+
+    def product(self, a_codes, a_scales, b_codes, b_scales, out, scale=1.0, accumulate=False, stream=None):
+        """out (n, rows) = (out if accumulate else 0) + scale * a b^T, of packed a (n, dim) and
+        b (rows, dim)."""
+        n = self._tokens(out, "out")
+        op, oc, ol = _matrix(out, "out", n, self.rows, self.device)
+        self._call("fc_mxfp_product", *self._packed(a_codes, a_scales, n, "a_"), n,
+                   *self._packed(b_codes, b_scales, self.rows, "b_"), scale, op, oc, ol, bool(accumulate), _stream(stream))
+
+    def linear(self, x, codes, scales, out, scale=1.0, accumulate=False, stream=None):
+        """product() of x (n, dim), f32, f16 or bf16, packed on the way, and a packed weight."""
+        n = self._tokens(x, "x")
+        xp, xc, xl = _matrix(x, "x", n, self.dim, self.device)
+        op, oc, ol = _matrix(out, "out", n, self.rows, self.device)
+        self._call("fc_mxfp_linear", xp, xc, xl, n, *self._packed(codes, scales, self.rows), scale, op, oc, ol,
+                   bool(accumulate), _stream(stream))
