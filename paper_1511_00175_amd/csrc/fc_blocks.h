@@ -157,16 +157,20 @@ template <int F, typename T> __global__ __launch_bounds__(256) void pack_rows_ke
     }
 }
 
-// out is of T, rows of `dim` elements or, padded with zeros, of 8 * per.
-template <int F, typename T> __global__ __launch_bounds__(256) void unpack_rows_kernel(BlockRows a, void* out, int64_t ldout, int len) {
-    const uint32_t per = (len + 7) / 8, i = blockIdx.x * 256 + threadIdx.x;
-    const uint32_t r = i / per, u = i % per;
+// The i-th 8 elements of out, rows of `len` of T: dim or, with zeros past it, up to a
+// multiple of 8.
+template <int F, typename T> __device__ __forceinline__ void unpack_eight(const BlockRows& a, void* out, int64_t ldout, int len, uint32_t i) {
+    const uint32_t per = (len + 7) / 8, r = i / per, u = i % per;
     if (r >= a.rows) return;
     const uint8_t* const from = a.codes + r * a.ldc + u * EIGHT_BYTES<F>;
     Codes c{*reinterpret_cast<const uint32_t*>(from), 0};
     if constexpr (F != E2M1) c.hi = *reinterpret_cast<const uint32_t*>(from + 4);
     const float s = scale_value(a.scales[r * a.lds + u / 4]);
     store8(static_cast<T*>(out) + r * ldout + 8 * u, len - 8 * (int)u, in_range<T>(decode8<F>(c) * s));
+}
+
+template <int F, typename T> __global__ __launch_bounds__(256) void unpack_rows_kernel(BlockRows a, void* out, int64_t ldout, int len) {
+    unpack_eight<F, T>(a, out, ldout, len, blockIdx.x * 256 + threadIdx.x);
 }
 
 // f(element type) of an fc_dtype.

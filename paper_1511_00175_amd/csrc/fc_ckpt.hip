@@ -16,18 +16,66 @@ constexpr int64_t ROWS_LIMIT = 1 << 21, LD_LIMIT = 1 << 21, TOKENS_LIMIT = (int6
 // Partial sums that a split product may write: two rounds of the chip's largest tiles.
 constexpr int64_t SUMS_LIMIT = (int64_t)1 << 25;
 
+// ---- operands --------------------------------------------------------------------
+
+// x unpacked and, where dy lies otherwise than the product reads it, dy copied, in one
+// launch: the first blocks unpack.
+struct OperandArgs {
+    fc::BlockRows kept;
+    void* x;
+    int64_t ldx;
+    unsigned unpacking;      // blocks
+    const void* dy;          // or null
+    int64_t lddy;
+    void* copy;
+    int64_t ldcopy;          // a multiple of 8
+    int outs;
+};
+
+template <int F, typename T> __global__ __launch_bounds__(256) void operands_kernel(OperandArgs a) {
+    if (blockIdx.x < a.unpacking) {
+        fc::unpack_eight<F, T>(a.kept, a.x, a.ldx, (int)a.ldx, blockIdx.x * 256 + threadIdx.x);
+        return;
+    }
+    const uint32_t per = (uint32_t)(a.ldcopy / 8), i = (blockIdx.x - a.unpacking) * 256 + threadIdx.x, r = i / per, u = i % per;
+    if (r >= a.kept.rows) return;
+    typedef typename fc::Eight<T>::vec V;
+    const T* const from = static_cast<const T*>(a.dy) + r * a.lddy + 8 * u;
+    const int left = a.outs - 8 * (int)u;
+    V v{};
+    if (left >= 8) {
+        v = *reinterpret_cast<const typename fc::Eight<T>::any*>(from);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 7; ++e)
+            if (e < left) v[e] = from[e];
+    }
+    *reinterpret_cast<V*>(static_cast<T*>(a.copy) + r * a.ldcopy + 8 * u) = v;
+}
+
+// ---- the product --------------------------------------------------------------------
+
+template <typename T> using Tiny = fc::Product<T, 64, 64, 32, 32, true, true, 4>;
+
+// COST's first three kinds and the one above (0.24 us a step on a full chip).  1003
+// tokens, 1001 x 520: 40 tiles of 128 x 128 take 21 us.
+constexpr int TINY = 3;
+constexpr KindCost COST_DW[] = {COST[LARGE], COST[BROAD], COST[MIDDLE], {64, 64, 0.25, 0.3, 4.0, 2}};
+
 template <typename T, bool ADD> hipError_t prepare_all() {
-    for (hipError_t e : {prepare<Large<T, true, true>>((const void*)grad_kernel<Large<T, true, true>, ADD>),
-                         prepare<Broad<T, true, true>>((const void*)grad_kernel<Broad<T, true, true>, ADD>),
-                         prepare<Middle<T, true, true>>((const void*)grad_kernel<Middle<T, true, true>, ADD>)})
+    for (hipError_t e : {prepare<Large<T, true, true>>((const void*)result_kernel<Large<T, true, true>, ADD, Operand>),
+                         prepare<Broad<T, true, true>>((const void*)result_kernel<Broad<T, true, true>, ADD, Operand>),
+                         prepare<Middle<T, true, true>>((const void*)result_kernel<Middle<T, true, true>, ADD, Operand>),
+                         prepare<Tiny<T>>((const void*)result_kernel<Tiny<T>, ADD, Operand>)})
         if (e != hipSuccess) return e;
     return hipSuccess;
 }
 
-template <typename T, bool ADD> void launch(TileKind kind, const GradArgs& g, hipStream_t s) {
-    if (kind == LARGE) launch_grad<Large<T, true, true>, ADD>(g, s);
-    else if (kind == BROAD) launch_grad<Broad<T, true, true>, ADD>(g, s);
-    else launch_grad<Middle<T, true, true>, ADD>(g, s);
+template <typename T, bool ADD> void launch(int kind, const GradArgs& g, hipStream_t s) {
+    if (kind == LARGE) launch_result<Large<T, true, true>, ADD, Operand>(g, s);
+    else if (kind == BROAD) launch_result<Broad<T, true, true>, ADD, Operand>(g, s);
+    else if (kind == MIDDLE) launch_result<Middle<T, true, true>, ADD, Operand>(g, s);
+    else launch_result<Tiny<T>, ADD, Operand>(g, s);
 }
 
 }  // namespace
@@ -59,14 +107,19 @@ template <typename T>
 void grad(fc_ckpt* p, const void* dy, int64_t lddy, const fc::BlockRows& kept, int64_t outs, float scale, void* dw, int dwt, int64_t lddw, bool add,
           hipStream_t s) {
     const int64_t n = kept.rows, ldx = fc::ceil_div(p->dim, 8) * 8;
-    if (p->format == FC_BLOCK_I8) fc::unpack_rows<FC_BLOCK_I8>(kept, p->x, p->dtype, ldx, (int)ldx, s);
-    else fc::unpack_rows<FC_BLOCK_E4M3>(kept, p->x, p->dtype, ldx, (int)ldx, s);
-    if (lddy % 8 || reinterpret_cast<uintptr_t>(dy) % 16) {
-        const int64_t ld = fc::ceil_div(outs, 8) * 8;
-        fc::by_launches(n, ld / 8, [&](int64_t r0, int64_t count) {
-            PackArgs a{static_cast<const char*>(dy) + r0 * lddy * 2, lddy, p->dy + r0 * ld * 2, ld, count, (int)outs, nullptr, 0, 0};
-            pack_kernel<<<(unsigned)fc::ceil_div(count * (ld / 8), 256), 256, 0, s>>>(a);
-        });
+    const bool copy = lddy % 8 || reinterpret_cast<uintptr_t>(dy) % 16;
+    const int64_t ld = fc::ceil_div(outs, 8) * 8, per = ldx / 8, per_dy = copy ? ld / 8 : 0;
+    fc::by_launches(n, per + per_dy, [&](int64_t r0, int64_t count) {
+        OperandArgs a{kept, p->x + r0 * ldx * 2, ldx, (unsigned)fc::ceil_div(count * per, 256), static_cast<const char*>(dy) + r0 * lddy * 2, lddy,
+                      p->dy + r0 * ld * 2, ld, (int)outs};
+        a.kept.codes += r0 * kept.ldc;
+        a.kept.scales += r0 * kept.lds;
+        a.kept.rows = count;
+        const unsigned grid = a.unpacking + (unsigned)fc::ceil_div(count * per_dy, 256);
+        if (p->format == FC_BLOCK_I8) operands_kernel<FC_BLOCK_I8, T><<<grid, 256, 0, s>>>(a);
+        else operands_kernel<FC_BLOCK_E4M3, T><<<grid, 256, 0, s>>>(a);
+    });
+    if (copy) {
         dy = p->dy;
         lddy = ld;
     }
@@ -77,7 +130,7 @@ void grad(fc_ckpt* p, const void* dy, int64_t lddy, const fc::BlockRows& kept, i
     g.n = (int)p->dim;
     g.k = (int)n;
     g.parts = 1;
-    const Choice c = choose(outs, p->dim, n, false, true, true, p->sums);
+    const Choice c = choose_tiles(COST_DW, LARGE, TINY, -1, outs, p->dim, fc::ceil_div(n, fc::GEMM_BK), true, p->sums);
     const bool split = c.splits > 1;
     g.kper = c.steps * fc::GEMM_BK;
     g.scale = scale;
@@ -85,8 +138,6 @@ void grad(fc_ckpt* p, const void* dy, int64_t lddy, const fc::BlockRows& kept, i
     g.dt = dwt;
     g.ld = lddw;
     g.sum = split ? p->sum : nullptr;
-    g.first = true;
-    g.last = !split;
     if (add && !split) launch<T, true>(c.kind, g, s);
     else launch<T, false>(c.kind, g, s);
     if (split) join_splits(g, c.splits, add, s);

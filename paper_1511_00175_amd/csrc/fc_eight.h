@@ -23,6 +23,13 @@ template <typename T> __device__ __forceinline__ f32x8 load8(const T* p, int lef
     return v;
 }
 
+// 8 elements in the row's type, all of them in the row.
+template <typename T> __device__ __forceinline__ typename Eight<T>::vec raw8(const T* p) { return *reinterpret_cast<const typename Eight<T>::any*>(p); }
+
+template <typename T> __device__ __forceinline__ void put8(T* p, f32x8 v) {
+    *reinterpret_cast<typename Eight<T>::any*>(p) = __builtin_convertvector(v, typename Eight<T>::vec);
+}
+
 template <typename T> __device__ __forceinline__ void store8(T* p, int left, f32x8 v) {
     if (left >= 8) {
         *reinterpret_cast<typename Eight<T>::any*>(p) = __builtin_convertvector(v, typename Eight<T>::vec);

@@ -95,17 +95,140 @@ enum { WIDE4, HALF4, SMALL4, KINDS4 };
 // As COST, for steps of 256 of k.
 constexpr KindCost COST4[KINDS4] = {{256, 256, 1.7, 1.15, 9.5, 1}, {128, 128, 0.52, 0.6, 5.0, 2}, {64, 64, 0.2, 0.3, 4.0, 2}};
 
+// ---- few tokens ---------------------------------------------------------------------------
+
+// Up to 16 NT tokens by 16 rows of b to a block, whose waves share k in steps of 256 and add
+// up through LDS.  Nothing is read twice within a block, so the fragments go from memory to
+// registers: a lane's 16 bytes are its row's 32 elements of one scale.  b's first steps are
+// on their way while X's tokens (X not void: up to 16 of them, not packed) are packed into LDS.
+struct FewArgs {
+    Operand4 a, b;           // a: of packed tokens
+    const void* x;
+    int64_t ldx;
+    int n, dim, blocks, width;
+    float scale;
+    void* out;
+    int dt;
+    int64_t ld;
+    bool add;
+};
+
+constexpr int AHEAD = 3;     // steps of a wave on their way at a time
+
+template <int NT, typename X> __global__ __launch_bounds__(1024) void few_kernel(FewArgs a) {
+    constexpr bool PACK = !__is_same(X, void);
+    typedef fc::i32x4 V;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, r = lane & 15, g = lane >> 4;
+    const int r0 = blockIdx.x * 16, steps = a.width / 8;
+    struct Step {
+        V code[2];
+        uint32_t scale[2];
+    };
+    // A row's codes and scales at step s; zeros past its blocks.
+    auto fetch = [&](const char* codes, const char* scales, int s) __attribute__((always_inline)) {
+        Step q{};
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int block = 8 * s + 4 * h + g;
+            if (block < a.blocks) {
+                q.code[h] = *reinterpret_cast<const V*>(codes + 16 * block);
+                q.scale[h] = *reinterpret_cast<const uint8_t*>(scales + block);
+            }
+        }
+        return q;
+    };
+    const int row = min(r0 + r, a.b.rows - 1);
+    const char* const bc = static_cast<const char*>(a.b.p) + (int64_t)row * 2 * a.b.ld;
+    const char* const bs = static_cast<const char*>(a.b.scales) + (int64_t)row * a.b.lds;
+    Step b[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) b[u] = wave + u * waves < steps ? fetch(bc, bs, wave + u * waves) : Step{};
+    char* const ac = lds;                                   // [token][16 blocks]
+    char* const as = lds + (int64_t)a.n * 16 * a.blocks;    // [token][width]
+    if constexpr (PACK) {
+        const int per = 4 * a.blocks;
+        for (int i = threadIdx.x; i < a.n * per; i += blockDim.x) {
+            const int t = i / per, u = i % per;
+            const fc::f32x8 v = fc::load8(static_cast<const X*>(a.x) + t * a.ldx + 8 * u, a.dim - 8 * u);
+            uint32_t most = fc::most_of(v);
+            most = max(most, (uint32_t)__shfl_xor((int)most, 1));
+            most = max(most, (uint32_t)__shfl_xor((int)most, 2));
+            const uint32_t byte = fc::scale_byte<fc::E2M1>(most);
+            *reinterpret_cast<uint32_t*>(ac + 16 * (int64_t)a.blocks * t + 4 * u) = fc::encode8<fc::E2M1>(v, fc::scale_inverse(byte)).lo;
+            if (u % 4 == 0) as[a.width * t + u / 4] = (char)byte;
+        }
+        __syncthreads();
+    }
+    fc::f32x4 acc[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[j] = fc::f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int s0 = wave; s0 < steps; s0 += AHEAD * waves) {
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int s = s0 + u * waves;
+            if (s >= steps) break;
+            Step x[NT];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                const int t = 16 * j + r;
+                x[j] = Step{};
+                if (t < a.n) {
+                    if constexpr (PACK) x[j] = fetch(ac + 16 * (int64_t)a.blocks * t, as + a.width * t, s);
+                    else x[j] = fetch(static_cast<const char*>(a.a.p) + (int64_t)t * 2 * a.a.ld, static_cast<const char*>(a.a.scales) + (int64_t)t * a.a.lds, s);
+                }
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[j] = fc::mma4(b[u].code[h], x[j].code[h], acc[j], b[u].scale[h], x[j].scale[h]);
+            const int then = s + AHEAD * waves;
+            b[u] = then < steps ? fetch(bc, bs, then) : Step{};
+        }
+    }
+    __syncthreads();  // the packed tokens are done with
+    // acc[j][e]: row 4 g + e of b, token 16 j + r
+    float(*const part)[16 * NT][16 + 1] = reinterpret_cast<float(*)[16 * NT][16 + 1]>(lds);  // [wave][token][row]
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) part[wave][16 * j + r][4 * g + e] = acc[j][e];
+    __syncthreads();
+    for (int i = threadIdx.x; i < 256 * NT; i += blockDim.x) {
+        const int t = i >> 4, c = i & 15;
+        if (t >= a.n || r0 + c >= a.b.rows) continue;
+        float v = 0.f;
+        for (int w = 0; w < waves; ++w) v += part[w][t][c];
+        v *= a.scale;
+        const int64_t at = (int64_t)t * a.ld + r0 + c;
+        if (a.add) v += load_one(a.out, a.dt, at);
+        store_one(a.out, a.dt, at, v);
+    }
+}
+
+constexpr int FEW = 32;            // tokens up to which the kernel above is taken
+constexpr int FEW_PACKED = 32768;  // elements up to which each of its blocks packs them
+
+// Waves of its blocks, and LDS.
+int few_waves(int width) { return width >= 128 ? 16 : width >= 64 ? 8 : 4; }
+int few_lds(int nt, int waves, int64_t packed) { return (int)std::max<int64_t>(waves * 16 * nt * 17 * 4, packed); }
+
+template <int NT, typename X> void launch_few(const FewArgs& a, hipStream_t s) {
+    const int waves = few_waves(a.width);
+    const int64_t packed = __is_same(X, void) ? 0 : (int64_t)a.n * (16 * a.blocks + a.width);
+    few_kernel<NT, X><<<(unsigned)fc::ceil_div(a.b.rows, 16), 64 * waves, few_lds(NT, waves, packed), s>>>(a);
+}
+
 template <bool ADD> hipError_t prepare_all() {
-    for (hipError_t e : {prepare<Wide4>((const void*)grad_kernel<Wide4, ADD, Operand4>), prepare<Half4>((const void*)grad_kernel<Half4, ADD, Operand4>),
-                         prepare<Small4>((const void*)grad_kernel<Small4, ADD, Operand4>)})
+    for (hipError_t e : {prepare<Wide4>((const void*)result_kernel<Wide4, ADD, Operand4>), prepare<Half4>((const void*)result_kernel<Half4, ADD, Operand4>),
+                         prepare<Small4>((const void*)result_kernel<Small4, ADD, Operand4>)})
         if (e != hipSuccess) return e;
     return hipSuccess;
 }
 
 template <bool ADD> void launch(int kind, const ResultArgs<Operand4>& g, hipStream_t s) {
-    if (kind == WIDE4) launch_grad<Wide4, ADD, Operand4>(g, s);
-    else if (kind == HALF4) launch_grad<Half4, ADD, Operand4>(g, s);
-    else launch_grad<Small4, ADD, Operand4>(g, s);
+    if (kind == WIDE4) launch_result<Wide4, ADD, Operand4>(g, s);
+    else if (kind == HALF4) launch_result<Half4, ADD, Operand4>(g, s);
+    else launch_result<Small4, ADD, Operand4>(g, s);
 }
 
 }  // namespace
@@ -151,8 +274,17 @@ Operand4 operand(const fc_mxfp* p, const Packed& m, int64_t r0, int64_t count) {
     return {static_cast<const uint8_t*>(m.codes) + r0 * m.ldc, m.ldc / 2, (int)count, 8 * p->blocks, static_cast<const uint8_t*>(m.scales) + r0 * m.lds, m.lds};
 }
 
+// Whether linear packs its tokens within the product's blocks.
+bool packs_within(const fc_mxfp* p, int64_t n) { return n <= 16 && n * p->dim <= FEW_PACKED; }
+
 // At most CHUNK rows of a.
 void product(fc_mxfp* p, const Operand4& a, const Operand4& b, float scale, void* out, int dt, int64_t ld, bool add, hipStream_t s) {
+    if (a.rows <= FEW) {
+        const FewArgs f{a, b, nullptr, 0, a.rows, (int)p->dim, p->blocks, p->width, scale, out, dt, ld, add};
+        if (a.rows <= 16) launch_few<1, void>(f, s);
+        else launch_few<2, void>(f, s);
+        return;
+    }
     ResultArgs<Operand4> g{};
     g.a = a;
     g.b = b;
@@ -168,8 +300,6 @@ void product(fc_mxfp* p, const Operand4& a, const Operand4& b, float scale, void
     g.dt = dt;
     g.ld = ld;
     g.sum = split ? p->sum : nullptr;
-    g.first = true;
-    g.last = !split;
     if (add && !split) launch<true>(c.kind, g, s);
     else launch<false>(c.kind, g, s);
     if (split) join_splits(g, c.splits, add, s);
@@ -306,6 +436,11 @@ int fc_mxfp_linear(fc_mxfp* p, const void* x, int x_dtype, int64_t ld_x, int64_t
         bool note;
         rc = p->order.begin(s, note);
         if (rc) return rc;
+        if (n && packs_within(p, n)) {
+            const FewArgs f{Operand4{}, operand(p, b, 0, p->rows), x, ld_x, (int)n, (int)p->dim, p->blocks, p->width, scale, out, out_dtype, ld_out, accumulate != 0};
+            fc::by_dtype(x_dtype, [&](auto t) { launch_few<1, decltype(t)>(f, s); });
+            n = 0;
+        }
         for (int64_t t0 = 0; t0 < n; t0 += CHUNK) {
             const Packed a{p->codes, 16 * (int64_t)p->blocks, p->scales, p->width, std::min(CHUNK, n - t0)};
             fc::pack_rows<fc::E2M1>(rows_of(p, static_cast<const char*>(x) + t0 * ld_x * xbytes, ld_x, a), x_dtype, s);

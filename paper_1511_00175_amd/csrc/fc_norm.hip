@@ -26,6 +26,8 @@ typedef _Float16 f16;
 typedef __bf16 bf16;
 using fc::f32x8;
 using fc::load8;
+using fc::put8;
+using fc::raw8;
 using fc::store8;
 
 // A channel vector's elements from c on; 1 where there is no vector.
@@ -57,39 +59,35 @@ __device__ __forceinline__ void gate_both(float g, int kind, float& a, float& sl
 
 // `lanes` threads hold a row, VECTORS times 8 elements each, a vector's neighbours in
 // neighbouring threads: 8 to 64 lanes of a wave, with several rows to a block of 256, or
-// a block of whole waves for one row.
+// a block of whole waves for one row.  Rows of fewer than 8 elements go as the widest do.
 struct Shape {
     int lanes, vectors, threads;
+    int groups;  // rows to a block of the backward pass
 };
 
 constexpr int DIM_LIMIT = 16384;
+constexpr int BLOCK = 256;  // threads of a backward pass's blocks, where a row takes no more
 
 Shape shape_of(int64_t dim) {
+    if (dim < 8) return {64, 4, 64, 1};
     if (dim <= 512) {
         int lanes = 8;
         while (lanes * 8 < dim) lanes *= 2;
-        return {lanes, 1, 256};
+        return {lanes, 1, 256, BLOCK / lanes};
     }
     const int vectors = dim <= 8192 ? 1 : 4, threads = (int)fc::ceil_div(dim, 512 * vectors) * 64;
-    return {threads, vectors, threads};
+    return {threads, vectors, threads, vectors > 1 ? 1 : std::max(1, BLOCK / threads)};
 }
 
-// Sums over a row's lanes, N at once, the same in every lane.  A row's block meets
-// once per call; the parts of one call and the next lie in different places, and a
-// thread that writes a place again has met the others since they read it.
+// Sums over a row's lanes, N at once, the same in every lane.  Rows of several waves go
+// through LDS, where a block meets once per call; the parts of one call and the next lie in
+// different places, and a thread that writes a place again has met the others since they
+// read it.
 constexpr int WAVES = 16;
 
 template <int N> struct RowSums {
     float (*part)[N][WAVES];  // [2]
     int lanes, turn;
-    __device__ __forceinline__ void init() {
-        if (lanes <= 64) return;
-        if (threadIdx.x < WAVES) {
-#pragma unroll
-            for (int k = 0; k < N; ++k) part[0][k][threadIdx.x] = part[1][k][threadIdx.x] = 0.f;
-        }
-        __syncthreads();
-    }
     __device__ __forceinline__ void add(float (&v)[N]) {
 #pragma unroll
         for (int off = 1; off < 64; off *= 2)
@@ -98,18 +96,38 @@ template <int N> struct RowSums {
                 for (int k = 0; k < N; ++k) v[k] += __shfl_xor(v[k], off);
             }
         if (lanes <= 64) return;
+        const int wave = threadIdx.x >> 6, waves = lanes >> 6, first = wave - wave % waves;
         if ((threadIdx.x & 63) == 0) {
 #pragma unroll
-            for (int k = 0; k < N; ++k) part[turn][k][threadIdx.x >> 6] = v[k];
+            for (int k = 0; k < N; ++k) part[turn][k][wave] = v[k];
         }
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < N; ++k) {
-            v[k] = 0.f;
+        for (int k = 0; k < N; ++k) v[k] = 0.f;
+#pragma unroll 4
+        for (int w = 0; w < waves; ++w)
 #pragma unroll
-            for (int w = 0; w < WAVES; ++w) v[k] += part[turn][k][w];
-        }
+            for (int k = 0; k < N; ++k) v[k] += part[turn][k][first + w];
         turn ^= 1;
+    }
+};
+
+// Where in its block's rows a thread is.  Rows of whole waves: the same for a wave, so that
+// a row's address is; a block of several of them has 4 of one wave or 2 of two.
+template <bool SHARED> struct Place {
+    int lane, group, groups;
+    __device__ __forceinline__ explicit Place(int lanes) {
+        if constexpr (SHARED) {
+            const int log = 31 - __builtin_clz(lanes);
+            lane = threadIdx.x & (lanes - 1);
+            group = threadIdx.x >> log;
+            groups = blockDim.x >> log;
+        } else {
+            const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+            groups = (int)blockDim.x == lanes ? 1 : lanes == 64 ? blockDim.x >> 6 : blockDim.x >> 7;
+            group = groups == 1 ? 0 : lanes == 64 ? wave : wave >> 1;
+            lane = threadIdx.x - group * lanes;
+        }
     }
 };
 
@@ -127,12 +145,65 @@ struct ForwardArgs {
     int64_t ldout, ldy;
 };
 
-template <typename T, typename H, int V> __global__ __launch_bounds__(V > 1 ? 512 : 1024) void forward_kernel(ForwardArgs a) {
+// A row's last 8 elements overlap those before them where its length is no multiple of 8:
+// both threads store the same, and only one counts them.
+// SHARED: several rows to a wave.
+template <typename T, typename H, bool SHARED> __global__ __launch_bounds__(1024) void forward_kernel(ForwardArgs a) {
     __shared__ __align__(16) float part[2][1][WAVES];
     RowSums<1> sums{part, a.lanes, 0};
-    sums.init();
-    const bool shared = a.lanes <= 64;  // a block of several rows
-    const int lane = shared ? threadIdx.x & (a.lanes - 1) : threadIdx.x, per = shared ? 256 / a.lanes : 1;
+    const Place<SHARED> at(a.lanes);
+    const int lane = at.lane, per = at.groups;
+    const float inv = 1.f / (float)a.dim;
+    const bool active = lane * 8 < a.dim;
+    const int col = min(lane * 8, a.dim - 8), mine = active ? lane * 8 - col : 8;  // elements below `mine` are another's
+    // x becomes x - m; returns r
+    auto normalize = [&](f32x8& x) __attribute__((always_inline)) {
+        float s[1] = {0.f};
+        if (a.kind == FC_NORM_LAYER) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (e >= mine) s[0] += x[e];
+            sums.add(s);
+            x -= s[0] * inv;
+            s[0] = 0.f;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e >= mine) s[0] += x[e] * x[e];
+        sums.add(s);
+        return 1.f / sqrtf(s[0] * inv + a.eps);
+    };
+    const int64_t step = (int64_t)gridDim.x * per;
+    // every row of a block goes as far, since the block meets; those past the last are the last again
+    for (int64_t first = (int64_t)blockIdx.x * per; first < a.n; first += step) {
+        const int64_t mine_t = first + at.group, t = min(mine_t, a.n - 1);
+        const bool live = active && mine_t < a.n;
+        f32x8 x = load8(static_cast<const H*>(a.h) + t * a.ldh + col, 8), next{};
+        if (a.y) next = channels(a.next, col, 8);
+        if (a.b) {
+            f32x8 b = load8(static_cast<const T*>(a.b) + t * a.ldb + col, 8), f = channels(a.weight, col, 8);
+            if (a.gate) {
+                const f32x8 g = a.ldgate ? load8(static_cast<const T*>(a.gate) + t * a.ldgate + col, 8) : load8(static_cast<const float*>(a.gate) + col, 8);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[e] *= gate_value(g[e], a.act);
+            }
+            const float r = normalize(b) * a.scale;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = (float)(H)(x[e] + f[e] * (b[e] * r));
+            if (live) put8(static_cast<H*>(a.out) + t * a.ldout + col, x);
+        }
+        if (!a.y) continue;
+        const float r = normalize(x);
+        if (live) put8(static_cast<T*>(a.y) + t * a.ldy + col, x * r * next);
+    }
+}
+
+// Rows of more than 8192 elements, and of fewer than 8.
+template <typename T, typename H> __global__ __launch_bounds__(512) void forward_wide_kernel(ForwardArgs a) {
+    constexpr int V = 4;
+    __shared__ __align__(16) float part[2][1][WAVES];
+    RowSums<1> sums{part, a.lanes, 0};
+    const int lane = threadIdx.x;
     const float inv = 1.f / (float)a.dim;
     int c[V], left[V];
 #pragma unroll
@@ -163,7 +234,7 @@ template <typename T, typename H, int V> __global__ __launch_bounds__(V > 1 ? 51
         sums.add(s);
         return 1.f / sqrtf(s[0] * inv + a.eps);
     };
-    for (int64_t t = (int64_t)blockIdx.x * per + (shared ? threadIdx.x / a.lanes : 0); t < a.n; t += (int64_t)gridDim.x * per) {
+    for (int64_t t = blockIdx.x; t < a.n; t += gridDim.x) {
         f32x8 x[V];
         const H* const hp = static_cast<const H*>(a.h) + t * a.ldh;
 #pragma unroll
@@ -222,35 +293,165 @@ struct BackwardArgs {
     int ldp;
 };
 
-// Rows of more than 8192 elements are more than a block's registers hold: they are read
-// again in each pass over them (AGAIN), and the sums over tokens lie in LDS, of which every
-// thread uses its own part.
 extern __shared__ __align__(32) float column_sums[];
 
-template <typename T, typename H, bool AGAIN> __global__ __launch_bounds__(AGAIN ? 512 : 1024) void backward_kernel(BackwardArgs a) {
+// Rows of up to 8192 elements, 8 to a thread, `groups` rows to a block at a time.  The sums
+// over tokens lie in LDS, of which every thread uses its own part.  A row's last 8 elements overlap those
+// before them where its length is no multiple of 8: both threads store the same, and only
+// one counts them.
+template <typename T, typename H, bool SHARED> __global__ __launch_bounds__(1024) void backward_kernel(BackwardArgs a) {
+    typedef typename fc::Eight<T>::vec Tv;
+    typedef typename fc::Eight<H>::vec Hv;
+    __shared__ __align__(16) float part[2][3][WAVES];
+    const Place<SHARED> at(a.lanes);
+    const int lane = at.lane, group = at.group, groups = at.groups;
+    RowSums<3> sums{part, a.lanes, 0};
+    const float inv = 1.f / (float)a.dim;
+    const bool layer = a.kind == FC_NORM_LAYER, matrix = a.gate && a.ldgate;
+    const bool active = lane * 8 < a.dim;
+    const int col = min(lane * 8, a.dim - 8), mine = active ? lane * 8 - col : 8;  // elements below `mine` are another's
+    auto weight_of = [&]() __attribute__((always_inline)) {
+        f32x8 weight = channels(a.weight, col, 8);
+        if (a.gate && !matrix) {
+            const f32x8 g = load8(static_cast<const float*>(a.gate) + col, 8);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) weight[e] *= gate_value(g[e], a.act);
+        }
+        return weight;  // times a(gate) where that is a vector
+    };
+    typedef float f32x4 __attribute__((ext_vector_type(4)));
+    f32x4* const own = reinterpret_cast<f32x4*>(column_sums) + threadIdx.x;  // sum1, sum2, four by four
+    for (int k = 0; k < 4; ++k) own[k * blockDim.x] = f32x4{};
+    auto add = [&](int which, f32x8 q) __attribute__((always_inline)) {
+        own[(2 * which) * blockDim.x] += __builtin_shufflevector(q, q, 0, 1, 2, 3);
+        own[(2 * which + 1) * blockDim.x] += __builtin_shufflevector(q, q, 4, 5, 6, 7);
+    };
+    auto total = [&](int which) __attribute__((always_inline)) {
+        return __builtin_shufflevector(own[(2 * which) * blockDim.x], own[(2 * which + 1) * blockDim.x], 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    const int64_t step = (int64_t)gridDim.x * groups;
+    // every group goes through as many rows, since the block meets; those past the last are the last again
+    for (int64_t first = (int64_t)blockIdx.x * groups; first < a.n; first += step) {
+        const int64_t mine_t = first + group, t = min(mine_t, a.n - 1);
+        Hv x{}, dx{};
+        Tv dy{}, b{}, g{};
+        f32x8 next{};
+        if (a.dy) {
+            next = channels(a.next, col, 8);
+            x = raw8(static_cast<const H*>(a.x) + t * a.ldx + col);
+            dy = raw8(static_cast<const T*>(a.dy) + t * a.lddy + col);
+        }
+        if (a.b) b = raw8(static_cast<const T*>(a.b) + t * a.ldb + col);
+        if (a.dout) dx = raw8(static_cast<const H*>(a.dout) + t * a.lddout + col);
+        if (a.b && matrix) g = raw8(static_cast<const T*>(a.gate) + t * a.ldgate + col);
+        const bool live = mine_t < a.n && active;
+        const int from = live ? mine : 8;  // elements that count
+        float s[3] = {0.f, 0.f, 0.f}, mean_x = 0.f, mean_u = 0.f, mean_b = 0.f;
+        if (layer) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if (e < from) continue;
+                s[0] += (float)x[e];
+                s[1] += next[e] * (float)dy[e];
+                s[2] += (float)b[e];
+            }
+            sums.add(s);
+            mean_x = s[0] * inv;
+            mean_u = s[1] * inv;
+            mean_b = s[2] * inv;
+            s[0] = s[1] = s[2] = 0.f;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if (e < from) continue;
+            const float xm = (float)x[e] - mean_x, bm = (float)b[e] - mean_b;
+            s[0] += xm * xm;
+            s[1] += next[e] * (float)dy[e] * xm;
+            s[2] += bm * bm;
+        }
+        sums.add(s);
+        const float r = 1.f / sqrtf(s[0] * inv + a.eps), rb = 1.f / sqrtf(s[2] * inv + a.eps), along = s[1] * inv * r;
+        f32x8 d = __builtin_convertvector(dx, f32x8);
+        f32x8 q;
+        if (a.dy) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float xh = ((float)x[e] - mean_x) * r, u = (float)dy[e];
+                d[e] += r * (next[e] * u - mean_u - xh * along);
+                q[e] = e >= from ? u * xh : 0.f;
+            }
+            add(1, q);
+            if (live) put8(static_cast<H*>(a.dh) + t * a.lddh + col, d);
+        }
+        if (a.b) {
+            // d becomes the gradient of N(b)
+            f32x8 dg;
+            const f32x8 weight = weight_of();
+            s[0] = s[1] = s[2] = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float bh = ((float)b[e] - mean_b) * rb, ee = a.scale * d[e];
+                float f = 1.f, slope = 0.f;
+                if (matrix) gate_both((float)g[e], a.act, f, slope);
+                dg[e] = ee * slope * weight[e] * bh;
+                d[e] = weight[e] * (ee * f);
+                q[e] = e < from ? 0.f : ee * f * bh;
+                if (e < from) continue;
+                s[0] += d[e] * bh;
+                s[1] += d[e];
+            }
+            add(0, q);
+            if (a.dgate && live) put8(static_cast<T*>(a.dgate) + t * a.lddgate + col, dg);
+            sums.add(s);
+            const float along_b = s[0] * inv, mean = layer ? s[1] * inv : 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) d[e] = rb * (d[e] - mean - ((float)b[e] - mean_b) * rb * along_b);
+            if (live) put8(static_cast<T*>(a.db) + t * a.lddb + col, d);
+        }
+    }
+    // This block's sums, over its rows at a time: within a wave, then through LDS in order.
+    auto put = [&](f32x8 sum, float* to) __attribute__((always_inline)) {
+        if (!to) return;
+#pragma unroll
+        for (int off = 8; off < 64; off *= 2)
+            if (off >= a.lanes) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[e] += __shfl_xor(sum[e], off);
+            }
+        const int parts = a.lanes < 64 ? (int)blockDim.x / 64 : groups, part = a.lanes < 64 ? (int)threadIdx.x / 64 : group;
+        __syncthreads();
+        if (active && (a.lanes >= 64 || (threadIdx.x & 63) < a.lanes)) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (e >= mine) column_sums[part * a.ldp + col + e] = sum[e];
+        }
+        __syncthreads();
+        for (int c = threadIdx.x; c < a.dim; c += blockDim.x) {
+            float all = 0.f;
+            for (int q = 0; q < parts; ++q) all += column_sums[q * a.ldp + c];
+            to[(int64_t)blockIdx.x * a.ldp + c] = all;
+        }
+    };
+    const f32x8 sum1 = total(0), sum2 = total(1);
+    put(sum1, a.sum1);
+    put(sum2, a.sum2);
+}
+
+// Rows of more than 8192 elements are more than a block's registers hold: they are read
+// again in each pass over them (rows of fewer than 8 come here too), and the sums over tokens lie in LDS, of which every
+// thread uses its own part.
+template <typename T, typename H> __global__ __launch_bounds__(512) void backward_wide_kernel(BackwardArgs a) {
     __shared__ __align__(16) float part[2][3][WAVES];
     RowSums<3> sums{part, a.lanes, 0};
-    sums.init();
-    const bool shared = a.lanes <= 64;  // a block of several rows
-    const int lane = shared ? threadIdx.x & (a.lanes - 1) : threadIdx.x, per = shared ? 256 / a.lanes : 1;
+    const int lane = threadIdx.x;
     const float inv = 1.f / (float)a.dim;
     const bool layer = a.kind == FC_NORM_LAYER, matrix = a.gate && a.ldgate;
     auto col = [&](int v) __attribute__((always_inline)) { return (v * a.lanes + lane) * 8; };
     auto left = [&](int v) __attribute__((always_inline)) { return a.dim - col(v); };
-    const int vectors = AGAIN ? 4 : 1;
-    f32x8 sum1{}, sum2{};
+    constexpr int vectors = 4;
     auto held = [&](int which, int v) __attribute__((always_inline)) { return reinterpret_cast<f32x8*>(column_sums) + (which * vectors + v) * a.lanes + lane; };
-    if (AGAIN)
-        for (int v = 0; v < 2 * vectors; ++v) *held(0, v) = f32x8{};
-    auto add1 = [&](int v, f32x8 q) __attribute__((always_inline)) {
-        if (AGAIN) *held(0, v) += q;
-        else sum1 += q;
-    };
-    auto add2 = [&](int v, f32x8 q) __attribute__((always_inline)) {
-        if (AGAIN) *held(1, v) += q;
-        else sum2 += q;
-    };
-    for (int64_t t = (int64_t)blockIdx.x * per + (shared ? threadIdx.x / a.lanes : 0); t < a.n; t += (int64_t)gridDim.x * per) {
+    for (int v = 0; v < 2 * vectors; ++v) *held(0, v) = f32x8{};
+    for (int64_t t = blockIdx.x; t < a.n; t += gridDim.x) {
         f32x8 x, dy, b, d, g;  // of one vector at a time
         float s[3], mean_x = 0.f, mean_u = 0.f, mean_b = 0.f, r = 0.f, rb = 0.f, along = 0.f;
         auto fetch = [&](int v) __attribute__((always_inline)) {
@@ -276,7 +477,7 @@ template <typename T, typename H, bool AGAIN> __global__ __launch_bounds__(AGAIN
         auto before = [&](int v, bool first) __attribute__((always_inline)) {
             const f32x8 w = channels(a.next, col(v), left(v)), xh = x * r;
             d += r * (w * dy - mean_u - xh * along);
-            if (first) add2(v, dy * xh);
+            if (first) *held(1, v) += dy * xh;
         };
         // d becomes the gradient of N(b), b N(b)
         auto after = [&](int v, bool first) __attribute__((always_inline)) {
@@ -294,15 +495,14 @@ template <typename T, typename H, bool AGAIN> __global__ __launch_bounds__(AGAIN
                 b[e] = bh;
                 d[e] = e < left(v) ? w[e] * (ee * f) : 0.f;
             }
-            if (first) add1(v, q);
+            if (first) *held(0, v) += q;
             if (first && a.dgate && matrix) store8(static_cast<T*>(a.dgate) + t * a.lddgate + col(v), left(v), dg);
         };
         s[0] = s[1] = s[2] = 0.f;
-        if (layer || !AGAIN) {
+        if (layer) {
 #pragma unroll 1
             for (int v = 0; v < vectors; ++v) {
                 fetch(v);
-                if (!layer) continue;
                 const f32x8 w = a.dy ? channels(a.next, col(v), left(v)) : f32x8{};
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
@@ -321,7 +521,7 @@ template <typename T, typename H, bool AGAIN> __global__ __launch_bounds__(AGAIN
         }
 #pragma unroll 1
         for (int v = 0; v < vectors; ++v) {
-            if (AGAIN) fetch(v);
+            fetch(v);
             centre(v);
             const f32x8 w = a.dy ? channels(a.next, col(v), left(v)) : f32x8{};
 #pragma unroll
@@ -338,10 +538,8 @@ template <typename T, typename H, bool AGAIN> __global__ __launch_bounds__(AGAIN
         s[0] = s[1] = s[2] = 0.f;
 #pragma unroll 1
         for (int v = 0; v < vectors; ++v) {
-            if (AGAIN) {
-                fetch(v);
-                centre(v);
-            }
+            fetch(v);
+            centre(v);
             if (a.dy) {
                 before(v, true);
                 store8(static_cast<H*>(a.dh) + t * a.lddh + col(v), left(v), d);
@@ -359,43 +557,20 @@ template <typename T, typename H, bool AGAIN> __global__ __launch_bounds__(AGAIN
         const float along_b = s[0] * inv, mean = layer ? s[1] * inv : 0.f;
 #pragma unroll 1
         for (int v = 0; v < vectors; ++v) {
-            if (AGAIN) {
-                fetch(v);
-                centre(v);
-                if (a.dy) before(v, false);
-                after(v, false);
-            }
+            fetch(v);
+            centre(v);
+            if (a.dy) before(v, false);
+            after(v, false);
             store8(static_cast<T*>(a.db) + t * a.lddb + col(v), left(v), rb * (d - mean - b * along_b));
         }
     }
-    // This block's sums: over the rows of a wave, then over its waves.
-    __shared__ __align__(32) float wave_sum[AGAIN ? 1 : 4][64 * 8];
-    auto put = [&](f32x8 sum, float* to, int which) __attribute__((always_inline)) {
-        if (!to) return;
-        to += (int64_t)blockIdx.x * a.ldp;
-        if (!shared) {
-            for (int v = 0; v < vectors; ++v)
-                if (left(v) > 0) *reinterpret_cast<f32x8*>(to + col(v)) = AGAIN ? *held(which, v) : sum;
-            return;
-        }
-        if (AGAIN) return;  // never: those rows have blocks of their own
 #pragma unroll
-        for (int off = 8; off < 64; off *= 2)
-            if (off >= a.lanes) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) sum[e] += __shfl_xor(sum[e], off);
-            }
-        __syncthreads();
-        if ((threadIdx.x & 63) < a.lanes) *reinterpret_cast<f32x8*>(&wave_sum[threadIdx.x >> 6][8 * lane]) = sum;
-        __syncthreads();
-        if (threadIdx.x < a.lanes && left(0) > 0) {
-            f32x8 all{};
-            for (int w = 0; w < 4; ++w) all += *reinterpret_cast<const f32x8*>(&wave_sum[w][8 * lane]);
-            *reinterpret_cast<f32x8*>(to + col(0)) = all;
-        }
-    };
-    put(sum1, a.sum1, 0);
-    put(sum2, a.sum2, 1);
+    for (int which = 0; which < 2; ++which) {
+        float* const to = which ? a.sum2 : a.sum1;
+        if (!to) continue;
+        for (int v = 0; v < vectors; ++v)
+            if (left(v) > 0) *reinterpret_cast<f32x8*>(to + (int64_t)blockIdx.x * a.ldp + col(v)) = *held(which, v);
+    }
 }
 
 // ---- vectors' gradients -----------------------------------------------------------
@@ -443,11 +618,14 @@ __global__ __launch_bounds__(1024) void finish_kernel(FinishArgs a) {
 }
 
 constexpr int64_t TOKENS_LIMIT = (int64_t)1 << 31;
-constexpr int BLOCKS_LIMIT = 1024;       // of a backward pass: rows of partial sums
 constexpr int64_t FORWARD_BLOCKS = 1 << 20;
 
+// Blocks of a backward pass that the chip holds at once: 16 waves to a compute unit, and one
+// block of the widest rows, whose sums fill its LDS.
+int64_t blocks_limit(Shape s) { return 256 * (s.lanes >= 64 && s.vectors > 1 ? 1 : 1024 / (s.groups * s.lanes)); }
+
 // Blocks of a backward pass of n rows.
-int64_t backward_blocks(Shape s, int64_t n) { return std::min<int64_t>(fc::ceil_div(n, s.threads / s.lanes), BLOCKS_LIMIT); }
+int64_t backward_blocks(Shape s, int64_t n) { return std::min<int64_t>(fc::ceil_div(n, s.groups), blocks_limit(s)); }
 
 }  // namespace
 
@@ -465,18 +643,23 @@ struct fc_norm {
 namespace {
 
 template <typename T, typename H> void forward(const Shape& s, unsigned grid, const ForwardArgs& a, hipStream_t st) {
-    if (s.vectors > 1) forward_kernel<T, H, 4><<<grid, s.threads, 0, st>>>(a);
-    else forward_kernel<T, H, 1><<<grid, s.threads, 0, st>>>(a);
+    if (s.vectors > 1) forward_wide_kernel<T, H><<<grid, s.threads, 0, st>>>(a);
+    else if (s.lanes < 64) forward_kernel<T, H, true><<<grid, s.threads, 0, st>>>(a);
+    else forward_kernel<T, H, false><<<grid, s.threads, 0, st>>>(a);
 }
 
 // The LDS of the longest rows.
 template <typename T, typename H> hipError_t prepare() {
-    return hipFuncSetAttribute((const void*)backward_kernel<T, H, true>, hipFuncAttributeMaxDynamicSharedMemorySize, 8 * DIM_LIMIT);
+    return hipFuncSetAttribute((const void*)backward_wide_kernel<T, H>, hipFuncAttributeMaxDynamicSharedMemorySize, 8 * DIM_LIMIT);
 }
 
 template <typename T, typename H> void backward(const Shape& s, unsigned grid, const BackwardArgs& a, hipStream_t st) {
-    if (s.vectors > 1) backward_kernel<T, H, true><<<grid, s.threads, 2 * s.vectors * s.lanes * sizeof(f32x8), st>>>(a);
-    else backward_kernel<T, H, false><<<grid, s.threads, 0, st>>>(a);
+    if (s.vectors > 1) backward_wide_kernel<T, H><<<grid, s.threads, 2 * s.vectors * s.lanes * sizeof(f32x8), st>>>(a);
+    else {
+        const int threads = s.groups * s.lanes;
+        if (s.lanes < 64) backward_kernel<T, H, true><<<grid, threads, threads * 2 * sizeof(f32x8), st>>>(a);
+        else backward_kernel<T, H, false><<<grid, threads, threads * 2 * sizeof(f32x8), st>>>(a);
+    }
 }
 
 // f<block side's type, residual side's type>() of a plan.

@@ -5,6 +5,7 @@
 
 #include <algorithm>
 
+#include "fc_eight.h"
 #include "fc_gemm.h"
 #include "fc_lm_host.h"
 
@@ -71,8 +72,7 @@ typedef ResultArgs<Operand> GradArgs;
 // 1.02 PFLOP/s): the matrix cores are busy 69% and 60% of a unit's cycles, at 1.54 and 1.66
 // GHz.  Tiles in groups of 8 rows keep what the blocks of an XCD read in its L2 (80% hits).
 // Few tokens give few tiles: k is then split.
-// ADD: to what `out` holds.
-template <typename P, bool ADD = false, typename O = Operand> __global__ __launch_bounds__(P::THREADS, P::THREADS / 256) void grad_kernel(ResultArgs<O> a) {
+template <typename P> __global__ __launch_bounds__(P::THREADS, P::THREADS / 256) void grad_kernel(GradArgs a) {
     int ti, tj;
     fc::tile_place(fc::xcd_order(blockIdx.x, a.tm * a.tn), a.tm, a.tn, 8, ti, tj);
     const int kb = blockIdx.y * a.kper, ke = min(a.k, kb + a.kper);
@@ -107,17 +107,63 @@ template <typename P, bool ADD = false, typename O = Operand> __global__ __launc
                     continue;
                 }
             }
-            v = a.row && a.row[m] < 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : a.scale * v;
-            const int64_t at = (int64_t)m * a.ld + n0 + z;
-            if constexpr (ADD) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] += load_one(a.out, a.dt, at + min(e, left - 1));
-            }
-            store_four(a.out, a.dt, at, v, left);
+            store_four(a.out, a.dt, (int64_t)m * a.ld + n0 + z, a.row && a.row[m] < 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : a.scale * v, left);
         }
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_sched_barrier(0);
     }
+}
+
+// Results of one call, or one part of k, straight from registers: two neighbouring fragments'
+// 4 neighbours of a lane become 8 neighbours of one fragment by an exchange with the lane 16
+// away, so that 16 rows get 32 or 64 bytes each in one store.  Against the strips above,
+// which also hold sums over calls and padding: 256 x 256 tiles of 16-bit results that all
+// end at once took 11 us for them, 4 so.
+template <typename P, bool ADD, typename T, typename O>
+__device__ __forceinline__ void store_tile_as(const ResultArgs<O>& a, const P& p, T* out, int64_t ld, float scale, int m0, int n0) {
+    const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int i = 0; i < P::FM; ++i) {
+        const int m = m0 + P::row(i);
+        const bool live = m < a.m;
+        T* const row = out + (int64_t)m * ld;
+#pragma unroll
+        for (int j = 0; j + 1 < P::FN; j += 2) {
+            fc::f32x8 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float x = p.acc[i][j][e], y = p.acc[i][j + 1][e];
+                const auto both = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, y), false, false);
+                const uint32_t lo = both[0], hi = both[1];
+                v[e] = __builtin_bit_cast(float, lo);
+                v[e + 4] = __builtin_bit_cast(float, hi);
+            }
+            const int n = n0 + P::col(0) - 4 * g + 16 * (j + (g & 1)) + 8 * (g >> 1), left = a.n - n;
+            v = v * scale;
+            if (!live || left <= 0) continue;
+            if constexpr (ADD) v += fc::load8(row + n, left);
+            fc::store8(row + n, left, v);
+        }
+        if constexpr (P::FN % 2) {
+            const int n = n0 + P::col(P::FN - 1), left = a.n - n;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (live && e < left) row[n + e] = (T)(p.acc[i][P::FN - 1][e] * scale + (ADD ? (float)row[n + e] : 0.f));
+        }
+    }
+}
+
+// ADD: to what `out` holds.
+template <typename P, bool ADD, typename O> __global__ __launch_bounds__(P::THREADS, P::THREADS / 256) void result_kernel(ResultArgs<O> a) {
+    int ti, tj;
+    fc::tile_place(fc::xcd_order(blockIdx.x, a.tm * a.tn), a.tm, a.tn, 8, ti, tj);
+    const int kb = blockIdx.y * a.kper, ke = min(a.k, kb + a.kper);
+    P p;
+    p.run(lds, a.a, a.b, ti * P::BM, tj * P::BN, kb, ke, a.parts);
+    if (a.sum) store_tile_as<P, false, float>(a, p, a.sum + (int64_t)blockIdx.y * a.m * a.n, a.n, 1.f, ti * P::BM, tj * P::BN);
+    else if (a.dt == FC_F32) store_tile_as<P, ADD, float>(a, p, static_cast<float*>(a.out), a.ld, a.scale, ti * P::BM, tj * P::BN);
+    else if (a.dt == FC_F16) store_tile_as<P, ADD, f16>(a, p, static_cast<f16*>(a.out), a.ld, a.scale, ti * P::BM, tj * P::BN);
+    else store_tile_as<P, ADD, bf16>(a, p, static_cast<bf16*>(a.out), a.ld, a.scale, ti * P::BM, tj * P::BN);
 }
 
 struct SplitArgs {
@@ -267,10 +313,16 @@ template <typename P> hipError_t prepare(const void* kernel) {
     return P::LDS > 64 * 1024 ? hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, P::LDS) : hipSuccess;
 }
 
-template <typename P, bool ADD = false, typename O = Operand> void launch_grad(ResultArgs<O> a, hipStream_t s) {
+template <typename P> void launch_grad(GradArgs a, hipStream_t s) {
     a.tm = (int)fc::ceil_div(a.m, P::BM);
     a.tn = (int)fc::ceil_div(a.n, P::BN);
-    grad_kernel<P, ADD, O><<<dim3(a.tm * a.tn, (unsigned)fc::ceil_div(a.k, a.kper)), P::THREADS, P::LDS, s>>>(a);
+    grad_kernel<P><<<dim3(a.tm * a.tn, (unsigned)fc::ceil_div(a.k, a.kper)), P::THREADS, P::LDS, s>>>(a);
+}
+
+template <typename P, bool ADD, typename O> void launch_result(ResultArgs<O> a, hipStream_t s) {
+    a.tm = (int)fc::ceil_div(a.m, P::BM);
+    a.tn = (int)fc::ceil_div(a.n, P::BN);
+    result_kernel<P, ADD, O><<<dim3(a.tm * a.tn, (unsigned)fc::ceil_div(a.k, a.kper)), P::THREADS, P::LDS, s>>>(a);
 }
 
 __global__ __launch_bounds__(256) void zero_kernel(void* p, int dt, int64_t rows, int64_t len, int64_t ld) {
