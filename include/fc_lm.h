@@ -243,7 +243,7 @@ int fc_norm_between_grad(fc_norm* plan, const void* out, int64_t ld_out, const v
 /* Rows in blocks of 32 neighbours that share a scale, a power of two 2^(byte - 127) (E8M0;
  * byte 255 is a NaN): the smallest, from 2^-127 on, with which no element of the block rounds
  * past the format's largest number.  An element is kept as an integer of 8 bits times it
- * (FC_BLOCK_I8, 127 the largest: steps of 1/64 to 1/128 of the block's largest magnitude), or
+ * (FC_BLOCK_I8, 127 the largest: steps of 1/63 to 1/128 of the block's largest magnitude), or
  * as an e4m3 float times it (FC_BLOCK_E4M3, 448 the largest: 4 bits of every element down to
  * 2^-14 of the block's largest), rounded to the nearest, ties to even.  A block that holds an
  * infinity or NaN is kept as NaN.
@@ -294,7 +294,7 @@ typedef struct fc_mxfp fc_mxfp;
 
 /* A plan for products with a matrix of `rows` rows of `dim` elements (1 to 2^21 each) and up
  * to max_tokens rows (0 to 2^31 - 1).  The workspace: fc_mxfp_linear's packed inputs, 0.53
- * bytes per element of up to 2^18 tokens, and partial sums of products that are split, up to
+ * bytes per element of up to 2^18 tokens, the matrix's scales in another order, and partial sums of products that are split, up to
  * 128 MiB. */
 int fc_mxfp_create(fc_mxfp** plan, int64_t rows, int64_t dim, int64_t max_tokens);
 void fc_mxfp_destroy(fc_mxfp* plan);

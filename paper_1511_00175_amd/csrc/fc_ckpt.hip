@@ -95,7 +95,7 @@ namespace {
 
 fc::BlockRows rows_of(const fc_ckpt* p, const void* x, int64_t ldx, const void* codes, int64_t ldc, const void* scales, int64_t lds, int64_t n) {
     return {x, ldx, static_cast<uint8_t*>(const_cast<void*>(codes)), ldc, static_cast<uint8_t*>(const_cast<void*>(scales)), lds, n, (int)p->dim, p->blocks,
-            p->blocks};
+            p->blocks, 8};
 }
 
 fc::Span codes_span(const fc_ckpt* p, const void* codes, int64_t ldc, int64_t n, bool written) { return {codes, n, 32 * (int64_t)p->blocks, ldc, 1, written}; }

@@ -166,6 +166,15 @@ template <int R, bool SLOW, int WAVES, bool ONCE = false> struct TileLoads {
             }
         }
     }
+    // Contiguous: from now on tiles of the rows from row0 on, after an init of rows 0 to R as
+    // if all were the operand's.  The rows past its last are past the descriptor's bound by
+    // themselves: row r is at r ldb, and the bound at most ldb beyond the last row's start.
+    __device__ __forceinline__ void move(const Operand& o, int row0) {
+        static_assert(!SLOW);
+        const int left = o.rows - row0, valid = left < R ? left : R;
+        base = (uint64_t)o.p + (uint64_t)row0 * ldb;
+        span = (uint32_t)((uint64_t)(valid - 1) * ldb);
+    }
     // The loads of one tile: where from, where to.
     struct Tile {
         u32x4 desc;

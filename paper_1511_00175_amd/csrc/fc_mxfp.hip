@@ -17,10 +17,9 @@ constexpr int64_t SUMS_LIMIT = (int64_t)1 << 25;
 
 // ---- columns to blocks ---------------------------------------------------------------
 
-// A block's tile is 256 of x's rows (a packed row's elements) by 64 of its columns (packed
-// rows): a thread holds two columns of 32 rows, a block of the format each, reads them a row
-// at a time, and the codes go through LDS, so that a packed row's 128 bytes are stored
-// together.
+// A block's tile is 256 of x's rows (a packed row's elements) by 128 of its columns (packed
+// rows).  A thread holds 8 columns of 8 rows, four threads a block of the format for each of
+// the columns; the codes go through LDS, so that a packed row's 128 bytes are stored together.
 struct ColumnArgs {
     const void* x;
     int64_t ldx;
@@ -31,57 +30,74 @@ struct ColumnArgs {
     int rows, dim, blocks;   // packed rows
 };
 
-constexpr int COLUMNS = 64;
+constexpr int COLUMNS = 128;
 
-template <typename T> __global__ __launch_bounds__(256) void pack_columns_kernel(ColumnArgs a) {
+template <typename T> __global__ __launch_bounds__(512) void pack_columns_kernel(ColumnArgs a) {
     __shared__ __align__(16) uint32_t tile[COLUMNS][33];  // codes of 256 elements of a packed row
     __shared__ uint8_t scale[COLUMNS][8];
-    const int kb = threadIdx.x >> 5, c2 = 2 * (threadIdx.x & 31);
-    const int k0 = blockIdx.x * 256 + 32 * kb, r0 = blockIdx.y * COLUMNS;
-    float v[2][32];
-    const T* const p = static_cast<const T*>(a.x) + (int64_t)k0 * a.ldx + r0 + c2;
-    const bool whole = r0 + c2 + 2 <= a.rows;
-    typedef T T2 __attribute__((ext_vector_type(2)));
-    typedef T2 T2_any __attribute__((aligned(alignof(T))));
+    const int lane = threadIdx.x & 63, kb = threadIdx.x >> 6, sub = lane >> 4, c = 8 * (lane & 15);
+    const int k0 = blockIdx.x * 256 + 32 * kb + 8 * sub, r0 = blockIdx.y * COLUMNS, left = a.rows - r0 - c;
+    const T* const p = static_cast<const T*>(a.x) + (int64_t)k0 * a.ldx + r0 + c;
+    typename fc::Eight<T>::vec v[8];
 #pragma unroll
-    for (int e = 0; e < 32; ++e) {
-        v[0][e] = v[1][e] = 0.f;
+    for (int e = 0; e < 8; ++e) {
+        v[e] = typename fc::Eight<T>::vec{};
         if (k0 + e >= a.dim) continue;
-        if (whole) {
-            const T2 q = *reinterpret_cast<const T2_any*>(p + e * a.ldx);
-            v[0][e] = (float)q.x;
-            v[1][e] = (float)q.y;
-        } else if (r0 + c2 < a.rows) {
-            v[0][e] = (float)p[e * a.ldx];
+        if (left >= 8) {
+            v[e] = fc::raw8(p + e * a.ldx);
+        } else {
+#pragma unroll
+            for (int q = 0; q < 7; ++q)
+                if (q < left) v[e][q] = p[e * a.ldx + q];
         }
     }
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        fc::f32x8 q[4];
-        uint32_t most = 0;
+    for (int q = 0; q < 8; ++q) {
+        fc::f32x8 x;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) q[i][e] = v[h][8 * i + e];
-            most = max(most, fc::most_of(q[i]));
-        }
+        for (int e = 0; e < 8; ++e) x[e] = (float)v[e][q];
+        uint32_t most = fc::most_of(x);
+        most = max(most, (uint32_t)__shfl_xor((int)most, 16));
+        most = max(most, (uint32_t)__shfl_xor((int)most, 32));
         const uint32_t byte = fc::scale_byte<fc::E2M1>(most);
-        const float inv = fc::scale_inverse(byte);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) tile[c2 + h][4 * kb + i] = fc::encode8<fc::E2M1>(q[i], inv).lo;
-        scale[c2 + h][kb] = (uint8_t)byte;
+        tile[c + q][4 * kb + sub] = fc::encode8<fc::E2M1>(x, fc::scale_inverse(byte)).lo;
+        if (sub == 0) scale[c + q][kb] = (uint8_t)byte;
     }
     __syncthreads();
     const int first = blockIdx.x * 8;  // block of the format
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const int at = threadIdx.x + 256 * i, r = at >> 3, b = at & 7;  // 16 bytes each
+        const int at = threadIdx.x + 512 * i, r = at >> 3, b = at & 7;  // 16 bytes each
         if (r0 + r >= a.rows) continue;
         if (first + b < a.blocks)
             *reinterpret_cast<uint4*>(a.codes + (int64_t)(r0 + r) * a.ldc + 16 * (first + b)) =
                 uint4{tile[r][4 * b], tile[r][4 * b + 1], tile[r][4 * b + 2], tile[r][4 * b + 3]};
         a.scales[(int64_t)(r0 + r) * a.lds + first + b] = first + b < a.blocks ? scale[r][b] : 0;
     }
+}
+
+// Scales of a packed matrix in the order in which 256 x 256 tiles read them: all rows' first 8,
+// all rows' next 8.
+struct ScaleArgs {
+    const uint8_t* from;
+    int64_t lds;
+    uint64_t* to;
+    int64_t rows;
+    int groups;
+};
+
+__device__ __forceinline__ void reorder_scales(const ScaleArgs& a, int64_t i) {
+    const int64_t r = i % a.rows, g = i / a.rows;
+    if (g < a.groups) a.to[i] = *reinterpret_cast<const uint64_t*>(a.from + r * a.lds + 8 * g);
+}
+
+__global__ __launch_bounds__(256) void scales_kernel(ScaleArgs a) { reorder_scales(a, (int64_t)blockIdx.x * 256 + threadIdx.x); }
+
+// A product's inputs packed and its weight's scales reordered, in one launch: the first
+// blocks pack.
+template <typename T> __global__ __launch_bounds__(256) void inputs_kernel(fc::BlockRows a, unsigned packing, ScaleArgs b) {
+    if (blockIdx.x < packing) fc::pack_eight<fc::E2M1, T>(a, blockIdx.x * 256 + threadIdx.x);
+    else reorder_scales(b, (int64_t)(blockIdx.x - packing) * 256 + threadIdx.x);
 }
 
 // ---- the product ------------------------------------------------------------------------
@@ -91,6 +107,37 @@ using Half4 = fc::Product4<128, 128, 64, 64, 2>;
 using Small4 = fc::Product4<64, 64, 32, 32, 4>;
 
 enum { WIDE4, HALF4, SMALL4, KINDS4 };
+
+// A block goes through every gridDim.x-th tile, in the order of result_kernel's.
+template <typename P, typename T> __global__ __launch_bounds__(P::THREADS, P::THREADS / 256) void tiles_kernel(ResultArgs<Operand4> a) {
+    const int count = a.tm * a.tn;
+    P p;
+    p.run_tiles(
+        lds, a.a, a.b,
+        [&](int i, int& m0, int& n0) __attribute__((always_inline)) {
+            const int at = blockIdx.x + i * gridDim.x;
+            if (at >= count) return false;
+            fc::tile_place(fc::xcd_order(at, count), a.tm, a.tn, 8, m0, n0);
+            m0 *= P::BM;
+            n0 *= P::BN;
+            return true;
+        },
+        [&](int m0, int n0) __attribute__((always_inline)) { store_tile_as<P, false, T>(a, p, static_cast<T*>(a.out), a.ld, a.scale, m0, n0); });
+}
+
+template <typename P> void launch_tiles(ResultArgs<Operand4> a, hipStream_t s) {
+    a.tm = (int)fc::ceil_div(a.m, P::BM);
+    a.tn = (int)fc::ceil_div(a.n, P::BN);
+    const unsigned grid = (unsigned)std::min<int64_t>(CUS, (int64_t)a.tm * a.tn);
+    fc::by_dtype(a.dt, [&](auto t) { tiles_kernel<P, decltype(t)><<<grid, P::THREADS, P::LDS, s>>>(a); });
+}
+
+template <typename P> hipError_t prepare_tiles() {
+    for (hipError_t e : {prepare<P>((const void*)tiles_kernel<P, float>), prepare<P>((const void*)tiles_kernel<P, f16>),
+                         prepare<P>((const void*)tiles_kernel<P, bf16>)})
+        if (e != hipSuccess) return e;
+    return hipSuccess;
+}
 
 // As COST, for steps of 256 of k.
 constexpr KindCost COST4[KINDS4] = {{256, 256, 1.7, 1.15, 9.5, 1}, {128, 128, 0.52, 0.6, 5.0, 2}, {64, 64, 0.2, 0.3, 4.0, 2}};
@@ -220,12 +267,15 @@ template <int NT, typename X> void launch_few(const FewArgs& a, hipStream_t s) {
 
 template <bool ADD> hipError_t prepare_all() {
     for (hipError_t e : {prepare<Wide4>((const void*)result_kernel<Wide4, ADD, Operand4>), prepare<Half4>((const void*)result_kernel<Half4, ADD, Operand4>),
-                         prepare<Small4>((const void*)result_kernel<Small4, ADD, Operand4>)})
+                         prepare<Small4>((const void*)result_kernel<Small4, ADD, Operand4>), prepare_tiles<Wide4>()})
         if (e != hipSuccess) return e;
     return hipSuccess;
 }
 
 template <bool ADD> void launch(int kind, const ResultArgs<Operand4>& g, hipStream_t s) {
+    if constexpr (!ADD) {  // with it the registers do not hold the next tile's first fragments beside the results
+        if (kind == WIDE4 && !g.sum) return launch_tiles<Wide4>(g, s);
+    }
     if (kind == WIDE4) launch_result<Wide4, ADD, Operand4>(g, s);
     else if (kind == HALF4) launch_result<Half4, ADD, Operand4>(g, s);
     else launch_result<Small4, ADD, Operand4>(g, s);
@@ -240,7 +290,8 @@ struct fc_mxfp {
     int blocks = 0, width = 0;   // of a row: scales, bytes of scales
     int64_t sums = 0;            // floats of partial sums
     uint8_t* codes = nullptr;    // linear's packed inputs
-    uint8_t* scales = nullptr;
+    uint8_t* scales = nullptr;   // theirs, or those of a product's, reordered
+    uint8_t* b_scales = nullptr; // the weight's, reordered
     float* sum = nullptr;
 };
 
@@ -253,6 +304,7 @@ struct Packed {
     const void* scales;
     int64_t lds;
     int64_t rows;
+    int64_t group = 8;  // from 8 scales of a row to its next
 };
 
 fc::Span codes_span(const fc_mxfp* p, const Packed& m, bool written) { return {m.codes, m.rows, 16 * (int64_t)p->blocks, m.ldc, 1, written}; }
@@ -267,33 +319,49 @@ int check_packed(const Packed& m) {
 
 fc::BlockRows rows_of(const fc_mxfp* p, const void* x, int64_t ldx, const Packed& m) {
     return {x, ldx, static_cast<uint8_t*>(const_cast<void*>(m.codes)), m.ldc, static_cast<uint8_t*>(const_cast<void*>(m.scales)), m.lds, m.rows, (int)p->dim,
-            p->blocks, p->width};
+            p->blocks, p->width, m.group};
 }
 
 Operand4 operand(const fc_mxfp* p, const Packed& m, int64_t r0, int64_t count) {
-    return {static_cast<const uint8_t*>(m.codes) + r0 * m.ldc, m.ldc / 2, (int)count, 8 * p->blocks, static_cast<const uint8_t*>(m.scales) + r0 * m.lds, m.lds};
+    return {static_cast<const uint8_t*>(m.codes) + r0 * m.ldc, m.ldc / 2, (int)count, 8 * p->blocks, static_cast<const uint8_t*>(m.scales) + r0 * m.lds, m.lds, m.group};
 }
 
 // Whether linear packs its tokens within the product's blocks.
 bool packs_within(const fc_mxfp* p, int64_t n) { return n <= 16 && n * p->dim <= FEW_PACKED; }
 
+Choice choice(const fc_mxfp* p, int64_t n) { return choose_tiles(COST4, WIDE4, SMALL4, -1, n, p->rows, p->width / 8, true, p->sums); }
+
+// Whether scales go to the product in the order of its tiles.
+bool reorders(const fc_mxfp* p, int64_t n) { return n > FEW && choice(p, n).kind == WIDE4; }
+
+ScaleArgs reordered(const fc_mxfp* p, Packed& m, uint8_t* to) {
+    const ScaleArgs a{static_cast<const uint8_t*>(m.scales), m.lds, reinterpret_cast<uint64_t*>(to), m.rows, p->width / 8};
+    m.scales = to;
+    m.lds = 8;
+    m.group = 8 * m.rows;
+    return a;
+}
+
+unsigned blocks_of(const ScaleArgs& a) { return (unsigned)fc::ceil_div(a.rows * a.groups, 256); }
+
 // At most CHUNK rows of a.
-void product(fc_mxfp* p, const Operand4& a, const Operand4& b, float scale, void* out, int dt, int64_t ld, bool add, hipStream_t s) {
+void product(fc_mxfp* p, const Packed& a, const Packed& b, float scale, void* out, int dt, int64_t ld, bool add, hipStream_t s) {
+    const Operand4 oa = operand(p, a, 0, a.rows), ob = operand(p, b, 0, b.rows);
     if (a.rows <= FEW) {
-        const FewArgs f{a, b, nullptr, 0, a.rows, (int)p->dim, p->blocks, p->width, scale, out, dt, ld, add};
+        const FewArgs f{oa, ob, nullptr, 0, (int)a.rows, (int)p->dim, p->blocks, p->width, scale, out, dt, ld, add};
         if (a.rows <= 16) launch_few<1, void>(f, s);
         else launch_few<2, void>(f, s);
         return;
     }
-    ResultArgs<Operand4> g{};
-    g.a = a;
-    g.b = b;
-    g.m = a.rows;
-    g.n = b.rows;
-    g.k = a.ks;
-    g.parts = 1;
-    const Choice c = choose_tiles(COST4, WIDE4, SMALL4, -1, g.m, g.n, fc::ceil_div(g.k, fc::GEMM_BK), true, p->sums);
+    const Choice c = choice(p, a.rows);
     const bool split = c.splits > 1;
+    ResultArgs<Operand4> g{};
+    g.a = oa;
+    g.b = ob;
+    g.m = (int)a.rows;
+    g.n = (int)b.rows;
+    g.k = oa.ks;
+    g.parts = 1;
     g.kper = c.steps * fc::GEMM_BK;
     g.scale = scale;
     g.out = out;
@@ -323,7 +391,7 @@ int fc_mxfp_create(fc_mxfp** plan, int64_t rows, int64_t dim, int64_t max_tokens
         const int64_t c = std::min(max_tokens, CHUNK);
         p->sums = std::min<int64_t>(SUMS_LIMIT, 64 * fc::ceil_div(c, 64) * 64 * rows);
         fc::Layout at;
-        const uint64_t o_codes = at.take(c * 16 * p->blocks), o_scales = at.take(c * p->width), o_sum = at.take(p->sums * 4);
+        const uint64_t o_codes = at.take(c * 16 * p->blocks), o_scales = at.take(c * p->width), o_b = at.take(rows * p->width), o_sum = at.take(p->sums * 4);
         int rc = p->order.create();
         if (!rc) rc = fc::hip_code(prepare_all<false>());
         if (!rc) rc = fc::hip_code(prepare_all<true>());
@@ -334,6 +402,7 @@ int fc_mxfp_create(fc_mxfp** plan, int64_t rows, int64_t dim, int64_t max_tokens
         }
         p->codes = reinterpret_cast<uint8_t*>(p->block.p + o_codes);
         p->scales = reinterpret_cast<uint8_t*>(p->block.p + o_scales);
+        p->b_scales = reinterpret_cast<uint8_t*>(p->block.p + o_b);
         p->sum = reinterpret_cast<float*>(p->block.p + o_sum);
         *plan = p;
         return FC_OK;
@@ -370,7 +439,7 @@ int fc_mxfp_pack(fc_mxfp* p, const void* x, int x_dtype, int64_t ld_x, int64_t r
                 const ColumnArgs a{static_cast<const char*>(x) + r0 * bytes, ld_x, static_cast<uint8_t*>(codes) + r0 * ld_codes, ld_codes,
                                    static_cast<uint8_t*>(scales) + r0 * ld_scales, ld_scales, (int)count, (int)p->dim, p->blocks};
                 const dim3 grid((unsigned)groups, (unsigned)fc::ceil_div(count, COLUMNS));
-                fc::by_dtype(x_dtype, [&](auto t) { pack_columns_kernel<decltype(t)><<<grid, 256, 0, s>>>(a); });
+                fc::by_dtype(x_dtype, [&](auto t) { pack_columns_kernel<decltype(t)><<<grid, 512, 0, s>>>(a); });
             }
         }
         rc = fc::hip_code(hipGetLastError());
@@ -414,9 +483,16 @@ int fc_mxfp_product(fc_mxfp* p, const void* a_codes, int64_t ld_a_codes, const v
         bool note;
         rc = p->order.begin(s, note);
         if (rc) return rc;
-        for (int64_t t0 = 0; t0 < n; t0 += CHUNK)
-            product(p, operand(p, a, t0, std::min(CHUNK, n - t0)), operand(p, b, 0, p->rows), scale, static_cast<char*>(out) + t0 * ld_out * bytes, out_dtype, ld_out,
-                    accumulate != 0, s);
+        for (int64_t t0 = 0; t0 < n; t0 += CHUNK) {
+            Packed at{static_cast<const char*>(a_codes) + t0 * ld_a_codes, ld_a_codes, static_cast<const char*>(a_scales) + t0 * ld_a_scales, ld_a_scales, std::min(CHUNK, n - t0)};
+            Packed bt = b;
+            if (reorders(p, at.rows)) {
+                const ScaleArgs sa = reordered(p, at, p->scales), sb = reordered(p, bt, p->b_scales);
+                scales_kernel<<<blocks_of(sa), 256, 0, s>>>(sa);
+                scales_kernel<<<blocks_of(sb), 256, 0, s>>>(sb);
+            }
+            product(p, at, bt, scale, static_cast<char*>(out) + t0 * ld_out * bytes, out_dtype, ld_out, accumulate != 0, s);
+        }
         rc = fc::hip_code(hipGetLastError());
         p->order.done(s, note);
         return rc;
@@ -442,9 +518,24 @@ int fc_mxfp_linear(fc_mxfp* p, const void* x, int x_dtype, int64_t ld_x, int64_t
             n = 0;
         }
         for (int64_t t0 = 0; t0 < n; t0 += CHUNK) {
-            const Packed a{p->codes, 16 * (int64_t)p->blocks, p->scales, p->width, std::min(CHUNK, n - t0)};
-            fc::pack_rows<fc::E2M1>(rows_of(p, static_cast<const char*>(x) + t0 * ld_x * xbytes, ld_x, a), x_dtype, s);
-            product(p, operand(p, a, 0, a.rows), operand(p, b, 0, p->rows), scale, static_cast<char*>(out) + t0 * ld_out * bytes, out_dtype, ld_out, accumulate != 0, s);
+            Packed a{p->codes, 16 * (int64_t)p->blocks, p->scales, p->width, std::min(CHUNK, n - t0)}, bt = b;
+            const void* const xt = static_cast<const char*>(x) + t0 * ld_x * xbytes;
+            const int64_t eights = a.rows * 4 * p->blocks;
+            if (reorders(p, a.rows)) {
+                a.lds = 8;
+                a.group = 8 * a.rows;
+                const ScaleArgs sb = reordered(p, bt, p->b_scales);
+                if (eights < fc::LAUNCH_THREADS) {
+                    const unsigned packing = (unsigned)fc::ceil_div(eights, 256);
+                    fc::by_dtype(x_dtype, [&](auto t) { inputs_kernel<decltype(t)><<<packing + blocks_of(sb), 256, 0, s>>>(rows_of(p, xt, ld_x, a), packing, sb); });
+                } else {
+                    fc::pack_rows<fc::E2M1>(rows_of(p, xt, ld_x, a), x_dtype, s);
+                    scales_kernel<<<blocks_of(sb), 256, 0, s>>>(sb);
+                }
+            } else {
+                fc::pack_rows<fc::E2M1>(rows_of(p, xt, ld_x, a), x_dtype, s);
+            }
+            product(p, a, bt, scale, static_cast<char*>(out) + t0 * ld_out * bytes, out_dtype, ld_out, accumulate != 0, s);
         }
         rc = fc::hip_code(hipGetLastError());
         p->order.done(s, note);

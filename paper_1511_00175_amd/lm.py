@@ -85,11 +85,18 @@ def _vector(t, name, n, device, code):
     return t.data_ptr()
 
 
-def _bytes(t, name, rows, cols, device, dtype):
-    """`t` must be a (rows, cols) tensor of `dtype`, one byte to an element, on the device, its
-    rows contiguous and any distance apart; returns (pointer, row stride)."""
-    _tensor(t, name)
-    if t.dtype != dtype:
+def _typed(t, name, rows, cols, dtype, device):
+    """`t` must be a (rows, cols) tensor of torch's `dtype` on the device, its rows
+    contiguous and any distance apart; returns (pointer, row stride)."""
+    try:
+        if t.dtype is dtype and t.device == device and t.shape == (rows, cols):
+            ld, one = t.stride()
+            if one == 1 and (ld >= cols or rows <= 1):
+                return t.data_ptr(), ld if rows > 1 else cols
+    except (AttributeError, TypeError):
+        pass
+    _tensor(t, name)  # what is wrong, or a single column
+    if t.dtype is not dtype:
         raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, the plan on {device}")
@@ -103,10 +110,29 @@ def _bytes(t, name, rows, cols, device, dtype):
     return t.data_ptr(), ld
 
 
-def _rows(t, name):
-    """The rows of a tensor whose other checks are _matrix's."""
+def _typed_vector(t, name, n, dtype, device):
+    """`t` must be a contiguous vector of n elements of torch's `dtype` on the device;
+    returns its pointer."""
+    try:
+        if t.dtype is dtype and t.device == device and t.shape == (n,) and t.is_contiguous():
+            return t.data_ptr()
+    except (AttributeError, TypeError):
+        pass
     _tensor(t, name)
-    return t.shape[0] if t.dim() else -1
+    if t.dtype is not dtype:
+        raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the plan on {device}")
+    raise ValueError(f"{name} must be a contiguous vector of {n} elements")
+
+
+def _rows(t, name):
+    """The rows of a tensor whose other checks follow."""
+    try:
+        return t.shape[0]
+    except (AttributeError, TypeError, IndexError):
+        _tensor(t, name)
+        raise ValueError(f"{name} must have two dimensions") from None
 
 
 _current = None  # the package's _stream, once it is loaded
@@ -325,47 +351,39 @@ class Norm(_Handle):
                 raise ValueError(f"{name} must be one of {', '.join(known)}, not {value}")
         if residual not in (dtype, "f32"):
             raise ValueError(f"residual must be {dtype} or f32, not {residual}")
-        self.code, self.residual = DTYPES[dtype], DTYPES[residual]
-        self._create("fc_norm_create", dim, max_tokens, self.code, self.residual, _KINDS[kind], eps, _GATES[gate])
+        import torch
+        self._create("fc_norm_create", dim, max_tokens, DTYPES[dtype], DTYPES[residual], _KINDS[kind], eps, _GATES[gate])
         self.dim, self.max_tokens = dim, max_tokens
+        types = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+        self.block, self.residual, self.vector = types[dtype], types[residual], torch.float32
 
-    def _block(self, t, name, n):
-        return _matrix(t, name, n, self.dim, self.device, self.code)[::2]
-
-    def _residual(self, t, name, n):
-        return (None, 0) if t is None else _matrix(t, name, n, self.dim, self.device, self.residual)[::2]
-
-    def _weight(self, t, name):
-        return None if t is None else _vector(t, name, self.dim, self.device, FC_F32)
+    def _weights(self, **vectors):
+        return [None if t is None else _typed_vector(t, name, self.dim, self.vector, self.device) for name, t in vectors.items()]
 
     def _gate(self, t, n):
         """(pointer, row stride or 0 for a vector)."""
         if t is None:
             return None, 0
-        _tensor(t, "gate")
-        if t.dim() == 1:
-            return _vector(t, "gate", self.dim, self.device, FC_F32), 0
-        return self._block(t, "gate", n)
+        if getattr(t, "ndim", 2) == 1:
+            return _typed_vector(t, "gate", self.dim, self.vector, self.device), 0
+        return _typed(t, "gate", n, self.dim, self.block, self.device)
 
-    def _dgate(self, t, gate, n, code):
-        if t is None:
-            return None, 0
-        _tensor(t, "dgate")
-        if gate is None or t.dim() != gate.dim():
+    def _sums(self, gate, n, dgate, *vectors):
+        """Gradients of vectors, all of one type, and of the gate: (the type, [the vectors' pointers], dgate's pointer and
+        row stride)."""
+        if dgate is not None and (gate is None or getattr(dgate, "ndim", -1) != gate.ndim):
             raise ValueError("dgate must be a vector or rows as gate is")
-        if t.dim() == 1:
-            return _vector(t, "dgate", self.dim, self.device, code), 0
-        return self._block(t, "dgate", n)
-
-    def _code_of(self, *vectors):
-        """The one type of a call's vector gradients."""
-        for t in vectors:
-            if t is not None and getattr(t, "dim", lambda: 0)() == 1:
-                code = _CODES.get(t.dtype)
-                if code is None:
-                    raise ValueError(f"vectors' gradients must not be {t.dtype}")
-                return code
-        return FC_F32
+        of_vector = dgate is not None and gate.ndim == 1
+        dtype = next((t.dtype for _, t in (*vectors, ("dgate", dgate if of_vector else None)) if hasattr(t, "dtype")), self.vector)
+        if dtype not in _CODES:
+            raise ValueError(f"vectors' gradients must not be {dtype}")
+        got = [None if t is None else _typed_vector(t, name, self.dim, dtype, self.device) for name, t in vectors]
+        place = (None, 0)
+        if of_vector:
+            place = _typed_vector(dgate, "dgate", self.dim, dtype, self.device), 0
+        elif dgate is not None:
+            place = _typed(dgate, "dgate", n, self.dim, self.block, self.device)
+        return _CODES[dtype], got, place
 
     def _tokens(self, t, name):
         n = _rows(t, name)
@@ -375,77 +393,75 @@ class Norm(_Handle):
 
     def before(self, x, y, weight=None, stream=None):
         """y[t] = weight * N(x[t])."""
-        n = _rows(x, "x")
-        xp, xl = self._residual(x, "x", n)
-        yp, yl = self._block(y, "y", n)
-        self._call("fc_norm_before", xp, xl, n, self._weight(weight, "weight"), yp, yl, _stream(stream))
+        n, dim, dev = _rows(x, "x"), self.dim, self.device
+        xp, xl = _typed(x, "x", n, dim, self.residual, dev)
+        yp, yl = _typed(y, "y", n, dim, self.block, dev)
+        wp = None if weight is None else _typed_vector(weight, "weight", dim, self.vector, dev)
+        self._call("fc_norm_before", xp, xl, n, wp, yp, yl, _stream(stream))
 
     def after(self, h, b, out, weight=None, gate=None, scale=1.0, stream=None):
         """out[t] = h[t] + scale * a(gate) * weight * N(b[t])."""
-        n = _rows(h, "h")
-        hp, hl = self._residual(h, "h", n)
-        bp, bl = self._block(b, "b", n)
+        n, dim, dev = _rows(h, "h"), self.dim, self.device
+        hp, hl = _typed(h, "h", n, dim, self.residual, dev)
+        bp, bl = _typed(b, "b", n, dim, self.block, dev)
+        op, ol = _typed(out, "out", n, dim, self.residual, dev)
         gp, gl = self._gate(gate, n)
-        op, ol = self._residual(out, "out", n)
-        self._call("fc_norm_after", hp, hl, bp, bl, n, gp, gl, self._weight(weight, "weight"), scale, op, ol, _stream(stream))
+        wp = None if weight is None else _typed_vector(weight, "weight", dim, self.vector, dev)
+        self._call("fc_norm_after", hp, hl, bp, bl, n, gp, gl, wp, scale, op, ol, _stream(stream))
 
     def between(self, h, b, out, y, weight=None, gate=None, next_weight=None, scale=1.0, stream=None):
         """out as after()'s, and y[t] = next_weight * N(out[t]) of out as it is stored."""
-        n = _rows(h, "h")
-        hp, hl = self._residual(h, "h", n)
-        bp, bl = self._block(b, "b", n)
+        n, dim, dev = _rows(h, "h"), self.dim, self.device
+        hp, hl = _typed(h, "h", n, dim, self.residual, dev)
+        bp, bl = _typed(b, "b", n, dim, self.block, dev)
+        op, ol = _typed(out, "out", n, dim, self.residual, dev)
+        yp, yl = _typed(y, "y", n, dim, self.block, dev)
         gp, gl = self._gate(gate, n)
-        op, ol = self._residual(out, "out", n)
-        yp, yl = self._block(y, "y", n)
-        self._call("fc_norm_between", hp, hl, bp, bl, n, gp, gl, self._weight(weight, "weight"),
-                   self._weight(next_weight, "next_weight"), scale, op, ol, yp, yl, _stream(stream))
+        wp = None if weight is None else _typed_vector(weight, "weight", dim, self.vector, dev)
+        np_ = None if next_weight is None else _typed_vector(next_weight, "next_weight", dim, self.vector, dev)
+        self._call("fc_norm_between", hp, hl, bp, bl, n, gp, gl, wp, np_, scale, op, ol, yp, yl, _stream(stream))
 
     def before_grad(self, x, dy, dx, dout=None, weight=None, dweight=None, accumulate=False, stream=None):
         """The gradients of before(): dx, to which dout, the gradient that comes by the
         residual, is added, and dweight."""
-        n = self._tokens(x, "x")
-        xp, xl = self._residual(x, "x", n)
-        yp, yl = self._block(dy, "dy", n)
-        op, ol = self._residual(dout, "dout", n)
-        dp, dl = self._residual(dx, "dx", n)
-        code = self._code_of(dweight)
-        wp = None if dweight is None else _vector(dweight, "dweight", self.dim, self.device, code)
-        self._call("fc_norm_before_grad", xp, xl, yp, yl, op, ol, n, self._weight(weight, "weight"), dp, dl, wp, code,
-                   bool(accumulate), _stream(stream))
+        n, dim, dev = self._tokens(x, "x"), self.dim, self.device
+        xp, xl = _typed(x, "x", n, dim, self.residual, dev)
+        yp, yl = _typed(dy, "dy", n, dim, self.block, dev)
+        op, ol = (None, 0) if dout is None else _typed(dout, "dout", n, dim, self.residual, dev)
+        dp, dl = _typed(dx, "dx", n, dim, self.residual, dev)
+        wp, = self._weights(weight=weight)
+        code, (dwp,), _ = self._sums(None, n, None, ("dweight", dweight))
+        self._call("fc_norm_before_grad", xp, xl, yp, yl, op, ol, n, wp, dp, dl, dwp, code, bool(accumulate), _stream(stream))
 
     def after_grad(self, b, dout, db, weight=None, dweight=None, gate=None, dgate=None, scale=1.0, accumulate=False,
                    stream=None):
         """The gradients of after() by b, gate and weight; that by h is dout itself."""
-        n = self._tokens(b, "b")
-        bp, bl = self._block(b, "b", n)
-        op, ol = self._residual(dout, "dout", n)
+        n, dim, dev = self._tokens(b, "b"), self.dim, self.device
+        bp, bl = _typed(b, "b", n, dim, self.block, dev)
+        op, ol = (None, 0) if dout is None else _typed(dout, "dout", n, dim, self.residual, dev)
         gp, gl = self._gate(gate, n)
-        dp, dl = self._block(db, "db", n)
-        code = self._code_of(dweight, dgate)
-        dgp, dgl = self._dgate(dgate, gate, n, code)
-        wp = None if dweight is None else _vector(dweight, "dweight", self.dim, self.device, code)
-        self._call("fc_norm_after_grad", bp, bl, op, ol, n, gp, gl, self._weight(weight, "weight"), scale, dp, dl, dgp, dgl, wp,
-                   code, bool(accumulate), _stream(stream))
+        dp, dl = _typed(db, "db", n, dim, self.block, dev)
+        wp, = self._weights(weight=weight)
+        code, (dwp,), (dgp, dgl) = self._sums(gate, n, dgate, ("dweight", dweight))
+        self._call("fc_norm_after_grad", bp, bl, op, ol, n, gp, gl, wp, scale, dp, dl, dgp, dgl, dwp, code, bool(accumulate),
+                   _stream(stream))
 
     def between_grad(self, out, b, dy, dh, db, dout=None, weight=None, dweight=None, gate=None, dgate=None, next_weight=None,
                      dnext=None, scale=1.0, accumulate=False, stream=None):
         """The gradients of between(), of both its outputs: dh, db and the vectors' and
         gate's."""
-        n = self._tokens(out, "out")
-        xp, xl = self._residual(out, "out", n)
-        bp, bl = self._block(b, "b", n)
-        yp, yl = self._block(dy, "dy", n)
-        op, ol = self._residual(dout, "dout", n)
+        n, dim, dev = self._tokens(out, "out"), self.dim, self.device
+        xp, xl = _typed(out, "out", n, dim, self.residual, dev)
+        bp, bl = _typed(b, "b", n, dim, self.block, dev)
+        yp, yl = _typed(dy, "dy", n, dim, self.block, dev)
+        op, ol = (None, 0) if dout is None else _typed(dout, "dout", n, dim, self.residual, dev)
         gp, gl = self._gate(gate, n)
-        hp, hl = self._residual(dh, "dh", n)
-        dp, dl = self._block(db, "db", n)
-        code = self._code_of(dweight, dnext, dgate)
-        dgp, dgl = self._dgate(dgate, gate, n, code)
-        wp = None if dweight is None else _vector(dweight, "dweight", self.dim, self.device, code)
-        np_ = None if dnext is None else _vector(dnext, "dnext", self.dim, self.device, code)
-        self._call("fc_norm_between_grad", xp, xl, bp, bl, yp, yl, op, ol, n, gp, gl, self._weight(weight, "weight"),
-                   self._weight(next_weight, "next_weight"), scale, hp, hl, dp, dl, dgp, dgl, wp, np_, code, bool(accumulate),
-                   _stream(stream))
+        hp, hl = _typed(dh, "dh", n, dim, self.residual, dev)
+        dp, dl = _typed(db, "db", n, dim, self.block, dev)
+        wp, np_ = self._weights(weight=weight, next_weight=next_weight)
+        code, (dwp, dnp), (dgp, dgl) = self._sums(gate, n, dgate, ("dweight", dweight), ("dnext", dnext))
+        self._call("fc_norm_between_grad", xp, xl, bp, bl, yp, yl, op, ol, n, gp, gl, wp, np_, scale, hp, hl, dp, dl, dgp, dgl,
+                   dwp, dnp, code, bool(accumulate), _stream(stream))
 
 
 _BLOCK = 32  # neighbours of a row that share a scale
@@ -458,7 +474,7 @@ class Checkpoint(_Handle):
     and the gradient of a weight of up to `max_outs` rows from up to `max_tokens`
     tokens and a dy of `dtype` ("f16" or "bf16").
 
-    format: "i8", steps of 1/64 to 1/128 of the 32's largest magnitude, or "e4m3",
+    format: "i8", steps of 1/63 to 1/128 of the 32's largest magnitude, or "e4m3",
             4 bits of each element.  A block with an infinity or NaN is kept as NaN.
 
     They are held by two tensors of the caller's, codes (tokens, 32 ceil(dim / 32))
@@ -474,50 +490,49 @@ class Checkpoint(_Handle):
             raise ValueError(f"dtype must be f16 or bf16, not {dtype}")
         if format not in _FORMATS:
             raise ValueError(f"format must be i8 or e4m3, not {format}")
-        self.code = DTYPES[dtype]
-        self._create("fc_ckpt_create", dim, max_tokens, max_outs, self.code, _FORMATS[format])
+        self._create("fc_ckpt_create", dim, max_tokens, max_outs, DTYPES[dtype], _FORMATS[format])
         self.dim, self.max_tokens, self.max_outs = dim, max_tokens, max_outs
         self.blocks = -(-dim // _BLOCK)
-        self.format = torch.int8 if format == "i8" else torch.float8_e4m3fn
+        self.dtype = torch.float16 if dtype == "f16" else torch.bfloat16
+        self.types = torch.int8 if format == "i8" else torch.float8_e4m3fn, torch.uint8  # of codes and scales
 
     def empty(self, n):
         """Codes and scales for n tokens."""
         import torch
-        return (torch.empty((n, _BLOCK * self.blocks), dtype=self.format, device=self.device),
-                torch.empty((n, self.blocks), dtype=torch.uint8, device=self.device))
-
-    def _kept(self, codes, scales, n):
-        import torch
-        return (*_bytes(codes, "codes", n, _BLOCK * self.blocks, self.device, self.format),
-                *_bytes(scales, "scales", n, self.blocks, self.device, torch.uint8))
+        return tuple(torch.empty((n, w), dtype=t, device=self.device) for w, t in zip((_BLOCK * self.blocks, self.blocks), self.types))
 
     def pack(self, x, codes, scales, stream=None):
         """Codes and scales of x (tokens, dim), f32, f16 or bf16; any number of tokens."""
-        n = _rows(x, "x")
-        xp, xc, xl = _matrix(x, "x", n, self.dim, self.device)
-        self._call("fc_ckpt_pack", xp, xc, xl, n, *self._kept(codes, scales, n), _stream(stream))
+        n, dev = _rows(x, "x"), self.device
+        xp, xc, xl = _matrix(x, "x", n, self.dim, dev)
+        cp, cl = _typed(codes, "codes", n, _BLOCK * self.blocks, self.types[0], dev)
+        sp, sl = _typed(scales, "scales", n, self.blocks, self.types[1], dev)
+        self._call("fc_ckpt_pack", xp, xc, xl, n, cp, cl, sp, sl, _stream(stream))
 
     def unpack(self, codes, scales, out, stream=None):
         """out = the activations kept, rounded to its type."""
-        n = _rows(out, "out")
-        op, oc, ol = _matrix(out, "out", n, self.dim, self.device)
-        self._call("fc_ckpt_unpack", *self._kept(codes, scales, n), n, op, oc, ol, _stream(stream))
+        n, dev = _rows(out, "out"), self.device
+        op, oc, ol = _matrix(out, "out", n, self.dim, dev)
+        cp, cl = _typed(codes, "codes", n, _BLOCK * self.blocks, self.types[0], dev)
+        sp, sl = _typed(scales, "scales", n, self.blocks, self.types[1], dev)
+        self._call("fc_ckpt_unpack", cp, cl, sp, sl, n, op, oc, ol, _stream(stream))
 
     def grad(self, dy, codes, scales, dw, scale=1.0, accumulate=False, stream=None):
         """dw[o] = (dw[o] if accumulate else 0) + scale * the sum over t of dy[t, o] x[t],
         for dy (tokens, outs) and dw (outs, dim) of any type.  dy lies on 16 bytes with a row
         stride of a multiple of 8, unless max_outs is no multiple of 8."""
-        n, outs = _rows(dy, "dy"), _rows(dw, "dw")
+        n, outs, dev = _rows(dy, "dy"), _rows(dw, "dw"), self.device
         if n > self.max_tokens:
             raise ValueError(f"{n} tokens for a plan of {self.max_tokens}")
         if outs > self.max_outs:
             raise ValueError(f"{outs} outputs for a plan of {self.max_outs}")
-        yp, _, yl = _matrix(dy, "dy", n, outs, self.device, self.code)
-        gp, gc, gl = _matrix(dw, "dw", outs, self.dim, self.device)
-        if n <= 1 and not self.max_outs % 8:
+        yp, yl = _typed(dy, "dy", n, outs, self.dtype, dev)
+        gp, gc, gl = _matrix(dw, "dw", outs, self.dim, dev)
+        cp, cl = _typed(codes, "codes", n, _BLOCK * self.blocks, self.types[0], dev)
+        sp, sl = _typed(scales, "scales", n, self.blocks, self.types[1], dev)
+        if n <= 1:
             yl = -(-yl // 8) * 8  # the stride of one row says nothing
-        self._call("fc_ckpt_grad", yp, yl, *self._kept(codes, scales, n), n, outs, scale, gp, gc, gl, bool(accumulate),
-                   _stream(stream))
+        self._call("fc_ckpt_grad", yp, yl, cp, cl, sp, sl, n, outs, scale, gp, gc, gl, bool(accumulate), _stream(stream))
 
 
 class Mxfp4(_Handle):
@@ -534,19 +549,20 @@ class Mxfp4(_Handle):
     _destroy = "fc_mxfp_destroy"
 
     def __init__(self, rows, dim, max_tokens):
+        import torch
         self._create("fc_mxfp_create", rows, dim, max_tokens)
         self.rows, self.dim, self.max_tokens = rows, dim, max_tokens
         self.widths = 16 * -(-dim // _BLOCK), 8 * -(-dim // (8 * _BLOCK))  # of codes and scales
+        self.type = torch.uint8
 
     def empty(self, n):
         """Codes and scales for n rows."""
         import torch
-        return tuple(torch.empty((n, w), dtype=torch.uint8, device=self.device) for w in self.widths)
+        return tuple(torch.empty((n, w), dtype=self.type, device=self.device) for w in self.widths)
 
     def _packed(self, codes, scales, n, name=""):
-        import torch
-        return (*_bytes(codes, name + "codes", n, self.widths[0], self.device, torch.uint8),
-                *_bytes(scales, name + "scales", n, self.widths[1], self.device, torch.uint8))
+        return (*_typed(codes, name + "codes", n, self.widths[0], self.type, self.device),
+                *_typed(scales, name + "scales", n, self.widths[1], self.type, self.device))
 
     def _tokens(self, t, name):
         n = _rows(t, name)
@@ -557,8 +573,7 @@ class Mxfp4(_Handle):
     def pack(self, x, codes, scales, transpose=False, stream=None):
         """Codes and scales of x (n, dim) or, with `transpose`, of the columns of x (dim, n);
         f32, f16 or bf16, any n."""
-        _tensor(x, "x")
-        n = x.shape[-1] if transpose and x.dim() else _rows(x, "x")
+        n = _rows(codes, "codes")
         xp, xc, xl = _matrix(x, "x", *((self.dim, n) if transpose else (n, self.dim)), self.device)
         self._call("fc_mxfp_pack", xp, xc, xl, n, bool(transpose), *self._packed(codes, scales, n), _stream(stream))
 
@@ -578,8 +593,9 @@ class Mxfp4(_Handle):
 
     def linear(self, x, codes, scales, out, scale=1.0, accumulate=False, stream=None):
         """product() of x (n, dim), f32, f16 or bf16, packed on the way, and a packed weight."""
-        n = self._tokens(x, "x")
-        xp, xc, xl = _matrix(x, "x", n, self.dim, self.device)
-        op, oc, ol = _matrix(out, "out", n, self.rows, self.device)
-        self._call("fc_mxfp_linear", xp, xc, xl, n, *self._packed(codes, scales, self.rows), scale, op, oc, ol,
-                   bool(accumulate), _stream(stream))
+        n, rows, dev = self._tokens(x, "x"), self.rows, self.device
+        xp, xc, xl = _matrix(x, "x", n, self.dim, dev)
+        op, oc, ol = _matrix(out, "out", n, rows, dev)
+        cp, cl = _typed(codes, "codes", rows, self.widths[0], self.type, dev)
+        sp, sl = _typed(scales, "scales", rows, self.widths[1], self.type, dev)
+        self._call("fc_mxfp_linear", xp, xc, xl, n, cp, cl, sp, sl, scale, op, oc, ol, bool(accumulate), _stream(stream))

@@ -131,6 +131,7 @@ def test_no_tokens(fc, device):
 
 def test_nan_stays_in_its_columns(fc, device):
     """A block of NaN spoils the gradient of its 32 inputs, and no other's; activations at fp16's largest stay finite."""
+    torch.manual_seed(7)
     plan = fc.Checkpoint(100, 50, 24)
     x = torch.randn(50, 100, device=device).half()
     x[7, 40] = float("inf")
@@ -148,6 +149,7 @@ def test_nan_stays_in_its_columns(fc, device):
 def test_gradient_is_that_of_the_product(fc, device):
     """<dw, v> = <dy, x v^T> along a random direction v: both sums of the same exact products, fp32 rounding apart."""
     n, d, outs = 200, 96, 56
+    torch.manual_seed(8)
     plan = fc.Checkpoint(d, n, outs)
     x = torch.randn(n, d, device=device)
     codes, scales = plan.empty(n)
@@ -160,9 +162,10 @@ def test_gradient_is_that_of_the_product(fc, device):
     left, right = (dw.double() * v).sum(), (dy.double() * (kept.double() @ v.t())).sum()
     size = (dy.double().abs() * (kept.double().abs() @ v.abs().t())).sum()
     assert abs(float(left - right)) <= (n / 4 + 66) * 2.0 ** -24 * float(size)
-    # i8: half a step of at most 1/64 of the block's largest
+    # i8: half a step.  The largest magnitude is 64 to 127.5 steps, or from 63.75 on where it would round to 128 at
+    # half the step: half a step is at most 1 / 127.5 of it
     most = torch.nn.functional.pad(x, (0, -d % 32)).view(n, -1, 32).abs().amax(2).repeat_interleave(32, 1)[:, :d]
-    assert bool(((kept - x).abs() <= most / 128).all())
+    assert bool(((kept - x).abs() <= most / 127.5).all())
 
 
 def test_streams_and_graph(fc, device):
