@@ -96,142 +96,11 @@ template <int BM_, int BN_, int WM_, int WN_, int STAGES> struct Product4 {
         return {nullptr, 0, a ? A.rows : B.rows, 0, a ? A.scales : B.scales, a ? A.lds : B.lds, a ? A.group : B.group};
     }
 
+    // Tile after tile: place(i, m0, n0) gives the block's i-th or false, done(m0, n0) takes acc.
+    // The loads run ahead from a tile into the next, so that only the first waits for its data.
     // k runs over [kb, ke) in 16-bit units, kb a multiple of 64.
-    __device__ __forceinline__ void run(char* lds, const Operand4& A, const Operand4& B, int m0, int n0, int kb, int ke, int) {
-        const int lane = threadIdx.x & 63;
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        const uint32_t la = lds_address(lds), lb = la + BM * GEMM_BK * 2, ls = la + CODES;
-        TileLoads<BM, false, WAVES> ta;
-        TileLoads<BN, false, WAVES> tb;
-        ta.init(Operand{A.p, A.ld, A.rows, A.ks, 0}, m0, wave, lane);
-        tb.init(Operand{B.p, B.ld, B.rows, B.ks, 0}, n0, wave, lane);
-        ScaleLoads<BM> ts[SCALES];
-#pragma unroll
-        for (int i = 0; i < SCALES; ++i) {
-            const int part = wave * SCALES + i;
-            ts[i].init(side(A, B, part), part < BM / 32 ? m0 + 32 * part : n0 + 32 * part - BM, lane);
-        }
-        Fragments<_Float16, BM, false, FM> fa;
-        Fragments<_Float16, BN, false, FN> fb;
-        const int wm = (wave / (BN / WN)) * WM, wn = (wave % (BN / WN)) * WN;
-        fa.init(wm, lane);
-        fb.init(wn, lane);
-        const uint32_t sa_at = ls + 8 * (wm + (lane & 15)), sb_at = ls + 8 * (BM + wn + (lane & 15)), shift = 8 * (lane >> 4);
-        auto frag = [&](auto& f, uint32_t tile, int i, int kk) __attribute__((always_inline)) { return __builtin_bit_cast(i32x4, f.get(tile, i, kk)); };
-        auto scales = [&](uint32_t at, int i) __attribute__((always_inline)) { return *(FC_LDS const u32x2*)(uintptr_t)(at + 128 * i); };
-#pragma unroll
-        for (int i = 0; i < FM; ++i)
-#pragma unroll
-            for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-
-        const int total = (ke - kb + GEMM_BK - 1) / GEMM_BK;
-        int k = kb, issued = 0, into = 0;
-        typename TileLoads<BM, false, WAVES>::Tile ia;
-        typename TileLoads<BN, false, WAVES>::Tile ib;
-        uint32_t is = 0;
-        int step = 0;
-        bool live = false;
-        auto prepare = [&]() __attribute__((always_inline)) {
-            live = issued < total;
-            const int from = live ? k : kb;
-            ia = ta.tile(la + into, from, false, live, wave);
-            ib = tb.tile(lb + into, from, false, live, wave);
-            is = ls + into + wave * SCALES * 256;
-            step = from / GEMM_BK;
-            into = into == (STAGES - 1) * STAGE ? 0 : into + STAGE;
-            k += GEMM_BK;
-            ++issued;
-        };
-        auto load = [&](int l) __attribute__((always_inline)) {
-            if (l < ta.COUNT) ta.load(ia, l);
-            else if (l < ta.COUNT + tb.COUNT) tb.load(ib, l - ta.COUNT);
-            else ts[l - ta.COUNT - tb.COUNT].load(is + 256 * (l - ta.COUNT - tb.COUNT), step, live);
-        };
-        for (int s = 0; s < STAGES; ++s) {
-            prepare();
-#pragma unroll
-            for (int l = 0; l < LOADS; ++l) load(l);
-        }
-        wait_loads<(STAGES - 1) * LOADS>();
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        i32x4 a[FM], b[FN], next[FN];
-        u32x2 sa[FM], sb[FN], sn[FN];
-#pragma unroll
-        for (int j = 0; j < FN; ++j) {
-            b[j] = frag(fb, lb, j, 0);
-            sb[j] = scales(sb_at, j);
-        }
-#pragma unroll
-        for (int i = 0; i < FM; ++i) {
-            a[i] = frag(fa, la, i, 0);
-            sa[i] = scales(sa_at, i);
-        }
-        constexpr int FIRST = FM >= 4 ? 2 : FM >= 2 ? 1 : 0;  // rows that cover the wait for the last reads
-        constexpr int REST = FM - FIRST;
-        constexpr int EACH = (FN + REST - 1) / REST, LEACH = (LOADS + REST - 1) / REST;
-        auto row_of = [&](int i, int kk) __attribute__((always_inline)) {
-            const uint32_t s = sa[i][kk] >> shift;
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int j = 0; j < FN; ++j) acc[i][j] = mma4(b[j], a[i], acc[i][j], sb[j][kk], s);
-            __builtin_amdgcn_sched_barrier(0);
-        };
-        uint32_t at = 0;
-        for (int t = 0; t < total; ++t) {
-            const uint32_t then = at == (STAGES - 1) * STAGE ? 0 : at + STAGE;
-            prepare();
-#pragma unroll
-            for (int j = 0; j < FN; ++j) sb[j] >>= shift;
-#pragma unroll
-            for (int i = 0; i < FM; ++i) {
-                row_of(i, 0);
-#pragma unroll
-                for (int j = 0; j < FN; ++j)
-                    if (j / EACH == i) next[j] = frag(fb, lb + at, j, 1);
-                a[i] = frag(fa, la + at, i, 1);
-            }
-#pragma unroll
-            for (int j = 0; j < FN; ++j) b[j] = next[j];
-#pragma unroll
-            for (int i = 0; i < FIRST; ++i) row_of(i, 1);
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            wait_loads<(STAGES - 2) * LOADS>();
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-#pragma unroll
-            for (int i = 0; i < FIRST; ++i) {
-                a[i] = frag(fa, la + then, i, 0);
-                sa[i] = scales(sa_at + then, i);
-            }
-#pragma unroll
-            for (int i = FIRST; i < FM; ++i) {
-#pragma unroll
-                for (int j = 0; j < FN; ++j)
-                    if (j / EACH == i - FIRST) {
-                        next[j] = frag(fb, lb + then, j, 0);
-                        sn[j] = scales(sb_at + then, j);
-                    }
-                row_of(i, 1);
-                a[i] = frag(fa, la + then, i, 0);
-                sa[i] = scales(sa_at + then, i);
-#pragma unroll
-                for (int l = 0; l < LOADS; ++l)
-                    if (l / LEACH == i - FIRST) load(l);
-            }
-#pragma unroll
-            for (int j = 0; j < FN; ++j) {
-                b[j] = next[j];
-                sb[j] = sn[j];
-            }
-            at = then;
-        }
-        wait_loads<0>();  // no store to LDS is left behind
-    }
-    // Tile after tile, of all of k: place(i, m0, n0) gives the block's i-th or false, done(m0, n0)
-    // takes acc.  The loads run ahead from a tile into the next, so that only the first waits
-    // for its data.
-    template <typename Place, typename Done> __device__ __forceinline__ void run_tiles(char* lds, const Operand4& A, const Operand4& B, Place&& place, Done&& done) {
+    template <typename Place, typename Done>
+    __device__ __forceinline__ void run_tiles(char* lds, const Operand4& A, const Operand4& B, int kb, int ke, Place&& place, Done&& done) {
         const int lane = threadIdx.x & 63;
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const uint32_t la = lds_address(lds), lb = la + BM * GEMM_BK * 2, ls = la + CODES;
@@ -267,7 +136,7 @@ template <int BM_, int BN_, int WM_, int WN_, int STAGES> struct Product4 {
         const uint32_t sa_at = ls + 8 * (wm + (lane & 15)), sb_at = ls + 8 * (BM + wn + (lane & 15)), shift = 8 * (lane >> 4);
         auto frag = [&](auto& f, uint32_t tile, int i, int kk) __attribute__((always_inline)) { return __builtin_bit_cast(i32x4, f.get(tile, i, kk)); };
         auto scales = [&](uint32_t at, int i) __attribute__((always_inline)) { return *(FC_LDS const u32x2*)(uintptr_t)(at + 128 * i); };
-        const int total = (A.ks + GEMM_BK - 1) / GEMM_BK;
+        const int total = (ke - kb + GEMM_BK - 1) / GEMM_BK;
         int next_step = 0;
         uint32_t into = 0, is = 0;
         typename TileLoads<BM, false, WAVES>::Tile ia;
@@ -281,7 +150,7 @@ template <int BM_, int BN_, int WM_, int WN_, int STAGES> struct Product4 {
                 if (live) move();
             }
             now = live;
-            step = next_step;
+            step = kb / GEMM_BK + next_step;
             ia = ta.tile(la + into, step * GEMM_BK, false, now, wave);
             ib = tb.tile(lb + into, step * GEMM_BK, false, now, wave);
             is = ls + into + wave * SCALES * 256;
@@ -327,60 +196,73 @@ template <int BM_, int BN_, int WM_, int WN_, int STAGES> struct Product4 {
         int m0, n0;
         for (int mine = 0; place(mine, m0, n0); ++mine) {
 #pragma unroll
-        for (int i = 0; i < FM; ++i)
+            for (int i = 0; i < FM; ++i)
 #pragma unroll
-            for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        for (int t = 0; t < total; ++t) {
-            const uint32_t then = at == (STAGES - 1) * STAGE ? 0 : at + STAGE;
-            prepare();
+                for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+            // As fc_gemm.h's loop.  (A read or load after each multiplication instead of a
+            // row's: 124 us for 127, but more registers than there are beside the results.)
+            for (int t = 0; t < total; ++t) {
+                const uint32_t then = at == (STAGES - 1) * STAGE ? 0 : at + STAGE;
+                prepare();
 #pragma unroll
-            for (int j = 0; j < FN; ++j) sb[j] >>= shift;
+                for (int j = 0; j < FN; ++j) sb[j] >>= shift;
 #pragma unroll
-            for (int i = 0; i < FM; ++i) {
-                row_of(i, 0);
+                for (int i = 0; i < FM; ++i) {
+                    row_of(i, 0);
 #pragma unroll
-                for (int j = 0; j < FN; ++j)
-                    if (j / EACH == i) next[j] = frag(fb, lb + at, j, 1);
-                a[i] = frag(fa, la + at, i, 1);
+                    for (int j = 0; j < FN; ++j)
+                        if (j / EACH == i) next[j] = frag(fb, lb + at, j, 1);
+                    a[i] = frag(fa, la + at, i, 1);
+                }
+#pragma unroll
+                for (int j = 0; j < FN; ++j) b[j] = next[j];
+#pragma unroll
+                for (int i = 0; i < FIRST; ++i) row_of(i, 1);
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                wait_loads<(STAGES - 2) * LOADS>();
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" ::: "memory");
+#pragma unroll
+                for (int i = 0; i < FIRST; ++i) {
+                    a[i] = frag(fa, la + then, i, 0);
+                    sa[i] = scales(sa_at + then, i);
+                }
+#pragma unroll
+                for (int i = FIRST; i < FM; ++i) {
+#pragma unroll
+                    for (int j = 0; j < FN; ++j)
+                        if (j / EACH == i - FIRST) {
+                            next[j] = frag(fb, lb + then, j, 0);
+                            sn[j] = scales(sb_at + then, j);
+                        }
+                    row_of(i, 1);
+                    a[i] = frag(fa, la + then, i, 0);
+                    sa[i] = scales(sa_at + then, i);
+#pragma unroll
+                    for (int l = 0; l < LOADS; ++l)
+                        if (l / LEACH == i - FIRST) load(l);
+                }
+#pragma unroll
+                for (int j = 0; j < FN; ++j) {
+                    b[j] = next[j];
+                    sb[j] = sn[j];
+                }
+                at = then;
             }
-#pragma unroll
-            for (int j = 0; j < FN; ++j) b[j] = next[j];
-#pragma unroll
-            for (int i = 0; i < FIRST; ++i) row_of(i, 1);
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            wait_loads<(STAGES - 2) * LOADS>();
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-#pragma unroll
-            for (int i = 0; i < FIRST; ++i) {
-                a[i] = frag(fa, la + then, i, 0);
-                sa[i] = scales(sa_at + then, i);
-            }
-#pragma unroll
-            for (int i = FIRST; i < FM; ++i) {
-#pragma unroll
-                for (int j = 0; j < FN; ++j)
-                    if (j / EACH == i - FIRST) {
-                        next[j] = frag(fb, lb + then, j, 0);
-                        sn[j] = scales(sb_at + then, j);
-                    }
-                row_of(i, 1);
-                a[i] = frag(fa, la + then, i, 0);
-                sa[i] = scales(sa_at + then, i);
-#pragma unroll
-                for (int l = 0; l < LOADS; ++l)
-                    if (l / LEACH == i - FIRST) load(l);
-            }
-#pragma unroll
-            for (int j = 0; j < FN; ++j) {
-                b[j] = next[j];
-                sb[j] = sn[j];
-            }
-            at = then;
-        }
-        done(m0, n0);
+            done(m0, n0);
         }
         wait_loads<0>();  // no store to LDS is left behind
+    }
+    // One tile; acc holds it afterwards.
+    __device__ __forceinline__ void run(char* lds, const Operand4& A, const Operand4& B, int m0, int n0, int kb, int ke, int) {
+        run_tiles(
+            lds, A, B, kb, ke,
+            [&](int i, int& m, int& n) __attribute__((always_inline)) {
+                m = m0;
+                n = n0;
+                return i == 0;
+            },
+            [](int, int) __attribute__((always_inline)) {});
     }
     // m and n of acc[i][j][0] within the block's tile.
     static __device__ __forceinline__ int row(int i) {

@@ -113,7 +113,7 @@ template <typename P, typename T> __global__ __launch_bounds__(P::THREADS, P::TH
     const int count = a.tm * a.tn;
     P p;
     p.run_tiles(
-        lds, a.a, a.b,
+        lds, a.a, a.b, 0, a.k,
         [&](int i, int& m0, int& n0) __attribute__((always_inline)) {
             const int at = blockIdx.x + i * gridDim.x;
             if (at >= count) return false;
@@ -140,7 +140,7 @@ template <typename P> hipError_t prepare_tiles() {
 }
 
 // As COST, for steps of 256 of k.
-constexpr KindCost COST4[KINDS4] = {{256, 256, 1.7, 1.15, 9.5, 1}, {128, 128, 0.52, 0.6, 5.0, 2}, {64, 64, 0.2, 0.3, 4.0, 2}};
+constexpr KindCost COST4[KINDS4] = {{256, 256, 1.78, 1.34, 4.5, 1, 6.0}, {128, 128, 0.56, 0.64, 5.2, 2}, {64, 64, 0.29, 0.38, 4.3, 2}};
 
 // ---- few tokens ---------------------------------------------------------------------------
 

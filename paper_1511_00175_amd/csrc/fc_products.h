@@ -265,6 +265,7 @@ struct KindCost {
     int bm, bn;
     double full, alone, once;
     int per;
+    double before = 0;  // of what the kind needs done first
 };
 constexpr KindCost COST[KINDS] = {{256, 256, 1.7, 1.15, 9.5, 1}, {256, 192, 1.38, 1.0, 8.0, 1}, {128, 128, 0.52, 0.6, 5.0, 2}, {64, 128, 0.55, 0.6, 4.0, 2}, {64, 32, 0.2, 0.3, 4.0, 2}};
 
@@ -294,7 +295,7 @@ inline Choice choose_tiles(const KindCost* cost, int first, int last, int skip, 
             const int64_t steps = fc::ceil_div(total, s), parts = fc::ceil_div(total, steps), blocks = tiles * parts;
             if (s > 1 && (!may_split || steps < 2 || parts * m * n > most)) continue;
             const double at_once = (double)std::min<int64_t>(c.per, fc::ceil_div(blocks, CUS));
-            double t = fc::ceil_div(blocks, CUS * c.per) * (steps * std::max(c.alone, c.full * at_once) + c.once);
+            double t = c.before + fc::ceil_div(blocks, CUS * c.per) * (steps * std::max(c.alone, c.full * at_once) + c.once);
             if (parts > 1) t += 5.0 + 8.0 * parts * m * n / 4.5e6;  // partial sums, written and read
             if (t < least) {
                 least = t;

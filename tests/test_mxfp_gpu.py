@@ -109,6 +109,12 @@ def test_product_accumulates(fc, device, to, n, rows, dim):
     product_case(fc, device, n, rows, dim, to=to, accumulate=True, scale=-1.75)
 
 
+@pytest.mark.parametrize("n,rows,dim", [(5000, 4400, 520), (4700, 4500, 200), (8193, 4300, 256)])
+def test_more_tiles_than_blocks(fc, device, n, rows, dim):
+    """Blocks go through several tiles, of three steps and of one, with the next one's loads under way."""
+    product_case(fc, device, n, rows, dim, to="bf16")
+
+
 def test_fewer_tokens_than_the_plan(fc, device):
     plan = fc.Mxfp4(130, 600, 700)
     for n in (700, 1, 65, 16, 300):
