@@ -256,7 +256,7 @@ int fc_norm_between_grad(fc_norm* plan, const void* out, int64_t ld_out, const v
 typedef struct fc_ckpt fc_ckpt;
 
 /* A plan for activations of `dim` elements (1 to 2^21) and gradients of weights of up to
- * max_outs rows (0 to 2^21) from up to max_tokens tokens (0 to 2^31 - 1) and a dy of `dtype`,
+ * max_outs rows (0 to 2^21) from up to max_tokens tokens (0 to 2^30) and a dy of `dtype`,
  * FC_F16 or FC_BF16.  The workspace, made here (none where max_outs is 0): 2 bytes per
  * element of max_tokens activations; 2 per element of dy where max_outs is no multiple of 8;
  * partial sums of products that are split along the tokens, up to 128 MiB. */

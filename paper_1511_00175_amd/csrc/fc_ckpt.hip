@@ -12,6 +12,7 @@
 namespace {
 
 constexpr int64_t ROWS_LIMIT = 1 << 21, LD_LIMIT = 1 << 21, TOKENS_LIMIT = (int64_t)1 << 31;
+constexpr int64_t GRAD_TOKENS = (int64_t)1 << 30;  // a product's k, up to a multiple of 64, is a 32-bit number
 
 // Partial sums that a split product may write: two rounds of the chip's largest tiles.
 constexpr int64_t SUMS_LIMIT = (int64_t)1 << 25;
@@ -150,7 +151,7 @@ extern "C" {
 int fc_ckpt_create(fc_ckpt** plan, int64_t dim, int64_t max_tokens, int64_t max_outs, int dtype, int format) {
     if (!plan) return FC_EINVAL;
     *plan = nullptr;
-    if (dim < 1 || dim > LD_LIMIT || max_tokens < 0 || max_tokens >= TOKENS_LIMIT || max_outs < 0 || max_outs > ROWS_LIMIT ||
+    if (dim < 1 || dim > LD_LIMIT || max_tokens < 0 || max_tokens > GRAD_TOKENS || max_outs < 0 || max_outs > ROWS_LIMIT ||
         (dtype != FC_F16 && dtype != FC_BF16) || (format != FC_BLOCK_I8 && format != FC_BLOCK_E4M3))
         return FC_EINVAL;
     return fc::no_throw([&] {
