@@ -58,10 +58,10 @@ template <int F, typename T> __global__ __launch_bounds__(256) void operands_ker
 
 template <typename T> using Tiny = fc::Product<T, 64, 64, 32, 32, true, true, 4>;
 
-// COST's first three kinds and the one above (0.24 us a step on a full chip).  1003
-// tokens, 1001 x 520: 40 tiles of 128 x 128 take 21 us.
+// COST's kinds, 128 x 128 slower alone with both operands across their rows, and the one
+// above.  1003 tokens, 1001 x 520: 40 tiles of 128 x 128 take 21 us, 144 of these 9.
 constexpr int TINY = 3;
-constexpr KindCost COST_DW[] = {COST[LARGE], COST[BROAD], COST[MIDDLE], {64, 64, 0.25, 0.3, 4.0, 2}};
+constexpr KindCost COST_DW[] = {COST[LARGE], COST[BROAD], {128, 128, 0.52, 0.7, 5.0, 2}, {64, 64, 0.25, 0.3, 4.0, 2}};
 
 template <typename T, bool ADD> hipError_t prepare_all() {
     for (hipError_t e : {prepare<Large<T, true, true>>((const void*)result_kernel<Large<T, true, true>, ADD, Operand>),
