@@ -144,12 +144,13 @@ constexpr KindCost COST4[KINDS4] = {{256, 256, 1.78, 1.34, 4.5, 1, 6.0}, {128, 1
 
 // ---- few tokens ---------------------------------------------------------------------------
 
-// Up to 16 NT tokens by 16 rows of b to a block, whose waves share k in steps of 256 and add
-// up through LDS.  Nothing is read twice within a block, so the fragments go from memory to
-// registers: a lane's 16 bytes are its row's 32 elements of one scale.  b's first steps are
-// on their way while X's tokens (X not void: up to 16 of them, not packed) are packed into LDS.
+// Up to 16 tokens by 16 rows of b to a block, whose waves share k in steps of 256 and add up
+// through LDS.  b's elements are read once, so they go from memory to registers: a lane's 16
+// bytes are its row's 32 elements of one scale.  The tokens are packed into LDS by every
+// block, while its first steps of b are on their way.  One token, fp16, us, other weights in
+// the caches: 4096 x 9216 (20 MB) 8.5, 8192 x 2048 5.6, 65536 x 2048 (71 MB) 20.
 struct FewArgs {
-    Operand4 a, b;           // a: of packed tokens
+    Operand4 b;
     const void* x;
     int64_t ldx;
     int n, dim, blocks, width;
@@ -162,8 +163,7 @@ struct FewArgs {
 
 constexpr int AHEAD = 3;     // steps of a wave on their way at a time
 
-template <int NT, typename X> __global__ __launch_bounds__(1024) void few_kernel(FewArgs a) {
-    constexpr bool PACK = !__is_same(X, void);
+template <typename X> __global__ __launch_bounds__(1024) void few_kernel(FewArgs a) {
     typedef fc::i32x4 V;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, r = lane & 15, g = lane >> 4;
     const int r0 = blockIdx.x * 16, steps = a.width / 8;
@@ -190,79 +190,61 @@ template <int NT, typename X> __global__ __launch_bounds__(1024) void few_kernel
     Step b[AHEAD];
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) b[u] = wave + u * waves < steps ? fetch(bc, bs, wave + u * waves) : Step{};
-    char* const ac = lds;                                   // [token][16 blocks]
-    char* const as = lds + (int64_t)a.n * 16 * a.blocks;    // [token][width]
-    if constexpr (PACK) {
-        const int per = 4 * a.blocks;
-        for (int i = threadIdx.x; i < a.n * per; i += blockDim.x) {
-            const int t = i / per, u = i % per;
-            const fc::f32x8 v = fc::load8(static_cast<const X*>(a.x) + t * a.ldx + 8 * u, a.dim - 8 * u);
-            uint32_t most = fc::most_of(v);
-            most = max(most, (uint32_t)__shfl_xor((int)most, 1));
-            most = max(most, (uint32_t)__shfl_xor((int)most, 2));
-            const uint32_t byte = fc::scale_byte<fc::E2M1>(most);
-            *reinterpret_cast<uint32_t*>(ac + 16 * (int64_t)a.blocks * t + 4 * u) = fc::encode8<fc::E2M1>(v, fc::scale_inverse(byte)).lo;
-            if (u % 4 == 0) as[a.width * t + u / 4] = (char)byte;
-        }
-        __syncthreads();
+    const int codes = 16 * a.blocks;                        // bytes of a token's
+    char* const xc = lds;                                   // [token][codes]
+    char* const xs = lds + a.n * codes;                     // [token][width]
+    for (int i = threadIdx.x; i < a.n * 4 * a.blocks; i += blockDim.x) {
+        const int t = i / (4 * a.blocks), u = i % (4 * a.blocks);
+        const fc::f32x8 v = fc::load8(static_cast<const X*>(a.x) + t * a.ldx + 8 * u, a.dim - 8 * u);
+        uint32_t most = fc::most_of(v);
+        most = max(most, (uint32_t)__shfl_xor((int)most, 1));
+        most = max(most, (uint32_t)__shfl_xor((int)most, 2));
+        const uint32_t byte = fc::scale_byte<fc::E2M1>(most);
+        *reinterpret_cast<uint32_t*>(xc + t * codes + 4 * u) = fc::encode8<fc::E2M1>(v, fc::scale_inverse(byte)).lo;
+        if (u % 4 == 0) xs[t * a.width + u / 4] = (char)byte;
     }
-    fc::f32x4 acc[NT];
-#pragma unroll
-    for (int j = 0; j < NT; ++j) acc[j] = fc::f32x4{0.f, 0.f, 0.f, 0.f};
+    __syncthreads();
+    fc::f32x4 acc{0.f, 0.f, 0.f, 0.f};
     for (int s0 = wave; s0 < steps; s0 += AHEAD * waves) {
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
             const int s = s0 + u * waves;
             if (s >= steps) break;
-            Step x[NT];
+            const Step x = r < a.n ? fetch(xc + r * codes, xs + r * a.width, s) : Step{};
 #pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                const int t = 16 * j + r;
-                x[j] = Step{};
-                if (t < a.n) {
-                    if constexpr (PACK) x[j] = fetch(ac + 16 * (int64_t)a.blocks * t, as + a.width * t, s);
-                    else x[j] = fetch(static_cast<const char*>(a.a.p) + (int64_t)t * 2 * a.a.ld, static_cast<const char*>(a.a.scales) + (int64_t)t * a.a.lds, s);
-                }
-            }
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int j = 0; j < NT; ++j) acc[j] = fc::mma4(b[u].code[h], x[j].code[h], acc[j], b[u].scale[h], x[j].scale[h]);
+            for (int h = 0; h < 2; ++h) acc = fc::mma4(b[u].code[h], x.code[h], acc, b[u].scale[h], x.scale[h]);
             const int then = s + AHEAD * waves;
             b[u] = then < steps ? fetch(bc, bs, then) : Step{};
         }
     }
     __syncthreads();  // the packed tokens are done with
-    // acc[j][e]: row 4 g + e of b, token 16 j + r
-    float(*const part)[16 * NT][16 + 1] = reinterpret_cast<float(*)[16 * NT][16 + 1]>(lds);  // [wave][token][row]
+    // acc[e]: row 4 g + e of b, token r
+    float(*const part)[16][16 + 1] = reinterpret_cast<float(*)[16][16 + 1]>(lds);  // [wave][token][row]
 #pragma unroll
-    for (int j = 0; j < NT; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) part[wave][16 * j + r][4 * g + e] = acc[j][e];
+    for (int e = 0; e < 4; ++e) part[wave][r][4 * g + e] = acc[e];
     __syncthreads();
-    for (int i = threadIdx.x; i < 256 * NT; i += blockDim.x) {
-        const int t = i >> 4, c = i & 15;
-        if (t >= a.n || r0 + c >= a.b.rows) continue;
-        float v = 0.f;
-        for (int w = 0; w < waves; ++w) v += part[w][t][c];
-        v *= a.scale;
-        const int64_t at = (int64_t)t * a.ld + r0 + c;
-        if (a.add) v += load_one(a.out, a.dt, at);
-        store_one(a.out, a.dt, at, v);
-    }
+    const int t = threadIdx.x >> 4, c = threadIdx.x & 15;
+    if (t >= a.n || r0 + c >= a.b.rows) return;
+    float v = 0.f;
+    for (int w = 0; w < waves; ++w) v += part[w][t][c];
+    v *= a.scale;
+    const int64_t at = (int64_t)t * a.ld + r0 + c;
+    if (a.add) v += load_one(a.out, a.dt, at);
+    store_one(a.out, a.dt, at, v);
 }
 
-constexpr int FEW = 32;            // tokens up to which the kernel above is taken
-constexpr int FEW_PACKED = 32768;  // elements up to which each of its blocks packs them
+// Whether it is taken: n tokens take the time of a block's packing for each round of blocks,
+// against a launch of its own.  us, taken / not: 4096 x 9216, 3 tokens 10.0 / 12.7; 9216 x 9216, 2 tokens
+// 20.0 / 19.5, 4 tokens 22 / 19; 8192 x 2048, 4 tokens 6.4 / 8.5, 8 tokens 8.0 / 8.0; 65536 x 2048, 1
+// token 19.7 / 20, 2 tokens 21.9 / 20; 1001 x 520, 16 tokens 5.6 / 6.8.
+bool is_few(int64_t n, int64_t rows, int64_t dim) { return n <= 16 && n * dim <= 32768 && n * dim * fc::ceil_div(rows, 16) <= 9000000; }
 
-// Waves of its blocks, and LDS.
-int few_waves(int width) { return width >= 128 ? 16 : width >= 64 ? 8 : 4; }
-int few_lds(int nt, int waves, int64_t packed) { return (int)std::max<int64_t>(waves * 16 * nt * 17 * 4, packed); }
-
-template <int NT, typename X> void launch_few(const FewArgs& a, hipStream_t s) {
-    const int waves = few_waves(a.width);
-    const int64_t packed = __is_same(X, void) ? 0 : (int64_t)a.n * (16 * a.blocks + a.width);
-    few_kernel<NT, X><<<(unsigned)fc::ceil_div(a.b.rows, 16), 64 * waves, few_lds(NT, waves, packed), s>>>(a);
+template <typename X> void launch_few(const FewArgs& a, hipStream_t s) {
+    const int blocks = (int)fc::ceil_div(a.b.rows, 16);
+    int waves = 16;  // as many as the chip holds of all blocks at once, 24 to a compute unit, at least 4 and at most a step each
+    while (waves > 4 && (waves * blocks > 24 * CUS || waves > a.width / 8)) waves /= 2;
+    const int bytes = std::max<int>(waves * 16 * 17 * 4, a.n * (16 * a.blocks + a.width));
+    few_kernel<X><<<blocks, 64 * waves, bytes, s>>>(a);
 }
 
 template <bool ADD> hipError_t prepare_all() {
@@ -326,13 +308,10 @@ Operand4 operand(const fc_mxfp* p, const Packed& m, int64_t r0, int64_t count) {
     return {static_cast<const uint8_t*>(m.codes) + r0 * m.ldc, m.ldc / 2, (int)count, 8 * p->blocks, static_cast<const uint8_t*>(m.scales) + r0 * m.lds, m.lds, m.group};
 }
 
-// Whether linear packs its tokens within the product's blocks.
-bool packs_within(const fc_mxfp* p, int64_t n) { return n <= 16 && n * p->dim <= FEW_PACKED; }
-
 Choice choice(const fc_mxfp* p, int64_t n) { return choose_tiles(COST4, WIDE4, SMALL4, -1, n, p->rows, p->width / 8, true, p->sums); }
 
 // Whether scales go to the product in the order of its tiles.
-bool reorders(const fc_mxfp* p, int64_t n) { return n > FEW && choice(p, n).kind == WIDE4; }
+bool reorders(const fc_mxfp* p, int64_t n) { return choice(p, n).kind == WIDE4; }
 
 ScaleArgs reordered(const fc_mxfp* p, Packed& m, uint8_t* to) {
     const ScaleArgs a{static_cast<const uint8_t*>(m.scales), m.lds, reinterpret_cast<uint64_t*>(to), m.rows, p->width / 8};
@@ -347,12 +326,6 @@ unsigned blocks_of(const ScaleArgs& a) { return (unsigned)fc::ceil_div(a.rows * 
 // At most CHUNK rows of a.
 void product(fc_mxfp* p, const Packed& a, const Packed& b, float scale, void* out, int dt, int64_t ld, bool add, hipStream_t s) {
     const Operand4 oa = operand(p, a, 0, a.rows), ob = operand(p, b, 0, b.rows);
-    if (a.rows <= FEW) {
-        const FewArgs f{oa, ob, nullptr, 0, (int)a.rows, (int)p->dim, p->blocks, p->width, scale, out, dt, ld, add};
-        if (a.rows <= 16) launch_few<1, void>(f, s);
-        else launch_few<2, void>(f, s);
-        return;
-    }
     const Choice c = choice(p, a.rows);
     const bool split = c.splits > 1;
     ResultArgs<Operand4> g{};
@@ -512,9 +485,9 @@ int fc_mxfp_linear(fc_mxfp* p, const void* x, int x_dtype, int64_t ld_x, int64_t
         bool note;
         rc = p->order.begin(s, note);
         if (rc) return rc;
-        if (n && packs_within(p, n)) {
-            const FewArgs f{Operand4{}, operand(p, b, 0, p->rows), x, ld_x, (int)n, (int)p->dim, p->blocks, p->width, scale, out, out_dtype, ld_out, accumulate != 0};
-            fc::by_dtype(x_dtype, [&](auto t) { launch_few<1, decltype(t)>(f, s); });
+        if (n && is_few(n, p->rows, p->dim)) {
+            const FewArgs f{operand(p, b, 0, p->rows), x, ld_x, (int)n, (int)p->dim, p->blocks, p->width, scale, out, out_dtype, ld_out, accumulate != 0};
+            fc::by_dtype(x_dtype, [&](auto t) { launch_few<decltype(t)>(f, s); });
             n = 0;
         }
         for (int64_t t0 = 0; t0 < n; t0 += CHUNK) {
