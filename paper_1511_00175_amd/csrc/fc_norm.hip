@@ -16,6 +16,7 @@
 // vector or none, a(g) and w are the same for all tokens, so that one sum, P = sum of e bh,
 // gives both dw = a(g) P and dg = a'(g) w P.
 #include <algorithm>
+#include <type_traits>
 
 #include "fc_eight.h"
 #include "fc_lm_host.h"
@@ -85,16 +86,36 @@ Shape shape_of(int64_t dim) {
 // read it.
 constexpr int WAVES = 16;
 
+// A sum over 8, 16, 32 or 64 neighbouring lanes, without a trip through LDS: within a row of
+// 16 lanes by its permutations, of which the mirrors pair what is already the same in 4 or 8
+// lanes, beyond by exchanges of rows.
+__device__ __forceinline__ float sum_lanes(float v, int lanes) {
+    auto from = [&](auto control) __attribute__((always_inline)) {
+        return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(control)::value, 0xf, 0xf, true));
+    };
+    v += from(std::integral_constant<int, 0xb1>{});    // lanes 1, 0, 3, 2 of 4
+    v += from(std::integral_constant<int, 0x4e>{});    // lanes 2, 3, 0, 1 of 4
+    v += from(std::integral_constant<int, 0x141>{});   // 8 lanes mirrored
+    if (lanes > 8) v += from(std::integral_constant<int, 0x140>{});  // 16 lanes mirrored
+    if (lanes > 16) {
+        const auto both = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+        const uint32_t lo = both[0], hi = both[1];
+        v = __builtin_bit_cast(float, lo) + __builtin_bit_cast(float, hi);
+    }
+    if (lanes > 32) {
+        const auto both = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+        const uint32_t lo = both[0], hi = both[1];
+        v = __builtin_bit_cast(float, lo) + __builtin_bit_cast(float, hi);
+    }
+    return v;
+}
+
 template <int N> struct RowSums {
     float (*part)[N][WAVES];  // [2]
     int lanes, turn;
     __device__ __forceinline__ void add(float (&v)[N]) {
 #pragma unroll
-        for (int off = 1; off < 64; off *= 2)
-            if (off < lanes) {
-#pragma unroll
-                for (int k = 0; k < N; ++k) v[k] += __shfl_xor(v[k], off);
-            }
+        for (int k = 0; k < N; ++k) v[k] = sum_lanes(v[k], lanes);
         if (lanes <= 64) return;
         const int wave = threadIdx.x >> 6, waves = lanes >> 6, first = wave - wave % waves;
         if ((threadIdx.x & 63) == 0) {
@@ -310,15 +331,9 @@ template <typename T, typename H, bool SHARED> __global__ __launch_bounds__(1024
     const bool layer = a.kind == FC_NORM_LAYER, matrix = a.gate && a.ldgate;
     const bool active = lane * 8 < a.dim;
     const int col = min(lane * 8, a.dim - 8), mine = active ? lane * 8 - col : 8;  // elements below `mine` are another's
-    auto weight_of = [&]() __attribute__((always_inline)) {
-        f32x8 weight = channels(a.weight, col, 8);
-        if (a.gate && !matrix) {
-            const f32x8 g = load8(static_cast<const float*>(a.gate) + col, 8);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) weight[e] *= gate_value(g[e], a.act);
-        }
-        return weight;  // times a(gate) where that is a vector
-    };
+    const f32x8 next = channels(a.next, col, 8);
+    f32x8 weight = channels(a.weight, col, 8);  // from the first row on times a(gate) where that is a vector
+    bool gates = a.gate && !matrix;
     typedef float f32x4 __attribute__((ext_vector_type(4)));
     f32x4* const own = reinterpret_cast<f32x4*>(column_sums) + threadIdx.x;  // sum1, sum2, four by four
     for (int k = 0; k < 4; ++k) own[k * blockDim.x] = f32x4{};
@@ -335,9 +350,7 @@ template <typename T, typename H, bool SHARED> __global__ __launch_bounds__(1024
         const int64_t mine_t = first + group, t = min(mine_t, a.n - 1);
         Hv x{}, dx{};
         Tv dy{}, b{}, g{};
-        f32x8 next{};
         if (a.dy) {
-            next = channels(a.next, col, 8);
             x = raw8(static_cast<const H*>(a.x) + t * a.ldx + col);
             dy = raw8(static_cast<const T*>(a.dy) + t * a.lddy + col);
         }
@@ -386,7 +399,12 @@ template <typename T, typename H, bool SHARED> __global__ __launch_bounds__(1024
         if (a.b) {
             // d becomes the gradient of N(b)
             f32x8 dg;
-            const f32x8 weight = weight_of();
+            if (gates) {  // here, so that the first row's loads do not wait for it
+                const f32x8 v = load8(static_cast<const float*>(a.gate) + col, 8);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) weight[e] *= gate_value(v[e], a.act);
+                gates = false;
+            }
             s[0] = s[1] = s[2] = 0.f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -599,9 +617,16 @@ __global__ __launch_bounds__(1024) void finish_kernel(FinishArgs a) {
     __shared__ float part[32][33];
     const int x = threadIdx.x & 31, y = threadIdx.x >> 5, c = blockIdx.x * 32 + x;
     float s = 0.f;
-    if (c < a.dim)
-#pragma unroll 4
-        for (int k = y; k < a.blocks; k += 32) s += p[(int64_t)k * a.ldp + c];
+    for (int k0 = y; k0 < a.blocks; k0 += 32 * 8) {  // 8 on their way at a time
+        float v[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            const int k = k0 + 32 * q;
+            v[q] = k < a.blocks && c < a.dim ? p[(int64_t)k * a.ldp + c] : 0.f;
+        }
+#pragma unroll
+        for (int q = 0; q < 8; ++q) s += v[q];
+    }
     part[y][x] = s;
     __syncthreads();
     if (y || c >= a.dim) return;
