@@ -357,8 +357,8 @@ class Norm(_Handle):
         types = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
         self.block, self.residual, self.vector = types[dtype], types[residual], torch.float32
 
-    def _weights(self, **vectors):
-        return [None if t is None else _typed_vector(t, name, self.dim, self.vector, self.device) for name, t in vectors.items()]
+    def _weight(self, t, name):
+        return None if t is None else _typed_vector(t, name, self.dim, self.vector, self.device)
 
     def _gate(self, t, n):
         """(pointer, row stride or 0 for a vector)."""
@@ -368,22 +368,26 @@ class Norm(_Handle):
             return _typed_vector(t, "gate", self.dim, self.vector, self.device), 0
         return _typed(t, "gate", n, self.dim, self.block, self.device)
 
-    def _sums(self, gate, n, dgate, *vectors):
-        """Gradients of vectors, all of one type, and of the gate: (the type, [the vectors' pointers], dgate's pointer and
+    def _sums(self, gate, n, dgate, weight, next_weight=None):
+        """Gradients of vectors, all of one type, and of the gate: (the type, the weights' pointers, dgate's pointer and
         row stride)."""
-        if dgate is not None and (gate is None or getattr(dgate, "ndim", -1) != gate.ndim):
-            raise ValueError("dgate must be a vector or rows as gate is")
-        of_vector = dgate is not None and gate.ndim == 1
-        dtype = next((t.dtype for _, t in (*vectors, ("dgate", dgate if of_vector else None)) if hasattr(t, "dtype")), self.vector)
+        of_vector = False
+        if dgate is not None:
+            if gate is None or getattr(dgate, "ndim", -1) != gate.ndim:
+                raise ValueError("dgate must be a vector or rows as gate is")
+            of_vector = gate.ndim == 1
+        first = weight if weight is not None else next_weight if next_weight is not None else dgate if of_vector else None
+        dtype = getattr(first, "dtype", self.vector)
         if dtype not in _CODES:
             raise ValueError(f"vectors' gradients must not be {dtype}")
-        got = [None if t is None else _typed_vector(t, name, self.dim, dtype, self.device) for name, t in vectors]
-        place = (None, 0)
+        dim, dev, place = self.dim, self.device, (None, 0)
+        wp = None if weight is None else _typed_vector(weight, "dweight", dim, dtype, dev)
+        np_ = None if next_weight is None else _typed_vector(next_weight, "dnext", dim, dtype, dev)
         if of_vector:
-            place = _typed_vector(dgate, "dgate", self.dim, dtype, self.device), 0
+            place = _typed_vector(dgate, "dgate", dim, dtype, dev), 0
         elif dgate is not None:
-            place = _typed(dgate, "dgate", n, self.dim, self.block, self.device)
-        return _CODES[dtype], got, place
+            place = _typed(dgate, "dgate", n, dim, self.block, dev)
+        return _CODES[dtype], wp, np_, place
 
     def _tokens(self, t, name):
         n = _rows(t, name)
@@ -396,7 +400,7 @@ class Norm(_Handle):
         n, dim, dev = _rows(x, "x"), self.dim, self.device
         xp, xl = _typed(x, "x", n, dim, self.residual, dev)
         yp, yl = _typed(y, "y", n, dim, self.block, dev)
-        wp = None if weight is None else _typed_vector(weight, "weight", dim, self.vector, dev)
+        wp = self._weight(weight, "weight")
         self._call("fc_norm_before", xp, xl, n, wp, yp, yl, _stream(stream))
 
     def after(self, h, b, out, weight=None, gate=None, scale=1.0, stream=None):
@@ -406,7 +410,7 @@ class Norm(_Handle):
         bp, bl = _typed(b, "b", n, dim, self.block, dev)
         op, ol = _typed(out, "out", n, dim, self.residual, dev)
         gp, gl = self._gate(gate, n)
-        wp = None if weight is None else _typed_vector(weight, "weight", dim, self.vector, dev)
+        wp = self._weight(weight, "weight")
         self._call("fc_norm_after", hp, hl, bp, bl, n, gp, gl, wp, scale, op, ol, _stream(stream))
 
     def between(self, h, b, out, y, weight=None, gate=None, next_weight=None, scale=1.0, stream=None):
@@ -417,8 +421,8 @@ class Norm(_Handle):
         op, ol = _typed(out, "out", n, dim, self.residual, dev)
         yp, yl = _typed(y, "y", n, dim, self.block, dev)
         gp, gl = self._gate(gate, n)
-        wp = None if weight is None else _typed_vector(weight, "weight", dim, self.vector, dev)
-        np_ = None if next_weight is None else _typed_vector(next_weight, "next_weight", dim, self.vector, dev)
+        wp = self._weight(weight, "weight")
+        np_ = self._weight(next_weight, "next_weight")
         self._call("fc_norm_between", hp, hl, bp, bl, n, gp, gl, wp, np_, scale, op, ol, yp, yl, _stream(stream))
 
     def before_grad(self, x, dy, dx, dout=None, weight=None, dweight=None, accumulate=False, stream=None):
@@ -429,8 +433,8 @@ class Norm(_Handle):
         yp, yl = _typed(dy, "dy", n, dim, self.block, dev)
         op, ol = (None, 0) if dout is None else _typed(dout, "dout", n, dim, self.residual, dev)
         dp, dl = _typed(dx, "dx", n, dim, self.residual, dev)
-        wp, = self._weights(weight=weight)
-        code, (dwp,), _ = self._sums(None, n, None, ("dweight", dweight))
+        wp = self._weight(weight, "weight")
+        code, dwp, _, _ = self._sums(None, n, None, dweight)
         self._call("fc_norm_before_grad", xp, xl, yp, yl, op, ol, n, wp, dp, dl, dwp, code, bool(accumulate), _stream(stream))
 
     def after_grad(self, b, dout, db, weight=None, dweight=None, gate=None, dgate=None, scale=1.0, accumulate=False,
@@ -441,8 +445,8 @@ class Norm(_Handle):
         op, ol = (None, 0) if dout is None else _typed(dout, "dout", n, dim, self.residual, dev)
         gp, gl = self._gate(gate, n)
         dp, dl = _typed(db, "db", n, dim, self.block, dev)
-        wp, = self._weights(weight=weight)
-        code, (dwp,), (dgp, dgl) = self._sums(gate, n, dgate, ("dweight", dweight))
+        wp = self._weight(weight, "weight")
+        code, dwp, _, (dgp, dgl) = self._sums(gate, n, dgate, dweight)
         self._call("fc_norm_after_grad", bp, bl, op, ol, n, gp, gl, wp, scale, dp, dl, dgp, dgl, dwp, code, bool(accumulate),
                    _stream(stream))
 
@@ -458,8 +462,8 @@ class Norm(_Handle):
         gp, gl = self._gate(gate, n)
         hp, hl = _typed(dh, "dh", n, dim, self.residual, dev)
         dp, dl = _typed(db, "db", n, dim, self.block, dev)
-        wp, np_ = self._weights(weight=weight, next_weight=next_weight)
-        code, (dwp, dnp), (dgp, dgl) = self._sums(gate, n, dgate, ("dweight", dweight), ("dnext", dnext))
+        wp, np_ = self._weight(weight, "weight"), self._weight(next_weight, "next_weight")
+        code, dwp, dnp, (dgp, dgl) = self._sums(gate, n, dgate, dweight, dnext)
         self._call("fc_norm_between_grad", xp, xl, bp, bl, yp, yl, op, ol, n, gp, gl, wp, np_, scale, hp, hl, dp, dl, dgp, dgl,
                    dwp, dnp, code, bool(accumulate), _stream(stream))
 
