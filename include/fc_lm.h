@@ -29,7 +29,8 @@
  *     threads.
  *   - Every call enqueues kernel launches only (no copies, memsets or
  *     allocations), so it may be captured in a HIP graph; a captured call
- *     neither waits for the plan's previous call nor becomes it.
+ *     neither waits for the plan's previous call nor becomes it.  Graphs that
+ *     hold calls of one plan share its workspace: they run one after the other.
  *   - A written buffer may not overlap any other buffer of the call
  *     (FC_EALIAS).
  *   - Results do not depend on timing: sums are taken in a fixed order, so the
@@ -294,8 +295,8 @@ typedef struct fc_mxfp fc_mxfp;
 
 /* A plan for products with a matrix of `rows` rows of `dim` elements (1 to 2^21 each) and up
  * to max_tokens rows (0 to 2^31 - 1).  The workspace: fc_mxfp_linear's packed inputs, 0.53
- * bytes per element of up to 2^18 tokens, the matrix's scales in another order, and partial sums of products that are split, up to
- * 128 MiB. */
+ * bytes per element of up to 2^18 tokens; the matrix's scales in another order; partial sums
+ * of products that are split, up to 128 MiB. */
 int fc_mxfp_create(fc_mxfp** plan, int64_t rows, int64_t dim, int64_t max_tokens);
 void fc_mxfp_destroy(fc_mxfp* plan);
 

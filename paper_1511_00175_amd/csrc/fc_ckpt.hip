@@ -3,9 +3,14 @@
 //
 //   dw[o, i] (+)= scale sum over t of dy[t, o] x[t, i]
 //
-// 2 tokens outs dim operations.  x is first unpacked to dy's type, in which its numbers
-// are exact, and the product then takes both operands across their rows (fc_gemm.h), so that
-// neither is transposed in memory.
+// Packing and unpacking are bound by memory: 32768 rows of 2048, fp16 and int8, 203 MB each way,
+// 45 us (4.5 TB/s) and 31 (the codes, 71 MB, come from the caches after packing).
+//
+// The gradient is 2 tokens outs dim operations.  x is first unpacked to dy's type, in which
+// its numbers are exact (but for what is out of fp16's range), and the product then takes
+// both operands across their rows (fc_gemm.h), so that neither is transposed in memory.
+// Unpacking is 12 us of 240 at 8192 tokens, 8192 x 2048, where 32 tiles read every part of x;
+// the product is 228, 1.2 PFLOP/s, the matrix cores busy 59% of the cycles at 2.06 GHz.  1003 tokens, 1001 x 520: 3.5 + 9.3 us, two launches.
 #include "fc_blocks.h"
 #include "fc_products.h"
 

@@ -8,6 +8,14 @@
 // row's 8 and shifts the byte of its 32 elements down.  An instruction multiplies 16 x 16 by
 // 128 of k in the cycles of a 16-bit one's 32 of k, from as many bytes, so that the same
 // tiles give four times the operations for the same reads.
+//
+// What bounds it, measured on the loop alone, 16384 x 4096 by 4096 of k in 256 x 256 tiles: 127
+// us, 4.3 PFLOP/s, and 109 with zeros for data, at which the clock stays higher; 106 without
+// the loads, 77 the multiplications by themselves (zeros), 69 the loads, 50 the reads of LDS.
+// For a step of 256 of k the multiplications of a unit take about 2060 cycles, what LDS takes
+// in and gives out at 128 bytes a cycle 2048.  No faster were: 32 x 32 instructions of 64 of k
+// (126), 4 waves of 128 x 128 (144), steps of 128 of k in 4 stages (172), padded rows, reads ahead
+// into L2 (149), the results of a tile stored between the next one's products (4% more).
 #pragma once
 
 #include "fc_gemm.h"
