@@ -122,6 +122,9 @@ template <typename T> __device__ __forceinline__ f32x8 in_range(f32x8 v) {
     return v;
 }
 
+// The largest scale's byte with which all of a format's numbers are in a type's range.
+template <int F, typename T> constexpr uint32_t FITS = 127 + (sizeof(T) == 2 && !__is_same(T, __bf16) ? 15 : 127) - (F == FC_BLOCK_I8 ? 7 : F == FC_BLOCK_E4M3 ? 9 : 3);
+
 // ---- rows to blocks and back -----------------------------------------------------
 
 struct BlockRows {

@@ -10,7 +10,7 @@
 // its numbers are exact (but for what is out of fp16's range), and the product then takes
 // both operands across their rows (fc_gemm.h), so that neither is transposed in memory.
 // Unpacking is 12 us of 240 at 8192 tokens, 8192 x 2048, where 32 tiles read every part of x;
-// the product is 228, 1.2 PFLOP/s, the matrix cores busy 59% of the cycles at 2.06 GHz.  1003 tokens, 1001 x 520: 3.5 + 9.3 us, two launches.
+// the product is 228, 1.2 PFLOP/s, the matrix cores busy 59% of the cycles at 2.06 GHz.  Few tiles take one launch (small_kernel).
 #include "fc_blocks.h"
 #include "fc_products.h"
 
@@ -64,7 +64,8 @@ template <int F, typename T> __global__ __launch_bounds__(256) void operands_ker
 template <typename T> using Tiny = fc::Product<T, 64, 64, 32, 32, true, true, 4>;
 
 // COST's kinds, 128 x 128 slower alone with both operands across their rows, and the one
-// above.  1003 tokens, 1001 x 520: 40 tiles of 128 x 128 take 21 us, 144 of these 9.
+// above.  1003 tokens, 1001 x 520: 40 tiles of 128 x 128 take 21 us, 144 of these 9 (the form
+// for few tiles, below, takes that case).
 constexpr int TINY = 3;
 constexpr KindCost COST_DW[] = {COST[LARGE], COST[BROAD], {128, 128, 0.52, 0.7, 5.0, 2}, {64, 64, 0.25, 0.3, 4.0, 2}};
 
@@ -82,6 +83,159 @@ template <typename T, bool ADD> void launch(int kind, const GradArgs& g, hipStre
     else if (kind == BROAD) launch_result<Broad<T, true, true>, ADD, Operand>(g, s);
     else if (kind == MIDDLE) launch_result<Middle<T, true, true>, ADD, Operand>(g, s);
     else launch_result<Tiny<T>, ADD, Operand>(g, s);
+}
+
+// ---- gradients of few tiles -------------------------------------------------------------
+
+// One launch, 64 x 64 of dw to a block: 4 groups of 4 waves go through every 4th step of 64
+// tokens, each with its own buffers, and their sums are added in order at the end.  Both
+// operands pass registers, where x is unpacked and dy may lie on any element.  It is bound by
+// what LDS takes in and gives out for 32 x 32 of a wave and by the unpacking, done again by
+// every block of a column.  In graphs, us, against the operands' launch and the tiles': 1 to 256
+// tokens, 1024 x 1024 5.3 to 5.5, 6.2 to 7.6; 1003 tokens, 1001 x 520 9.8, 11.7; 1003, 2048 x
+// 1024 17.9, 17.2; 4096, 1024 x 1024 27, 30; 4096, 256 x 512, where k is split 22.7, 14.1.
+struct SmallArgs {
+    fc::BlockRows kept;
+    const void* dy;
+    int64_t lddy;
+    int outs;
+    float scale;
+    void* out;
+    int dt;
+    int64_t ld;
+    bool add;
+    int tm, tn;
+};
+
+constexpr int AHEAD = 3;      // steps of a group on their way at a time
+constexpr int SMALL = 64, GROUPS = 4, SMALL_THREADS = GROUPS * 256;
+constexpr int SMALL_TILE = SMALL * SMALL * 2;             // bytes of an operand's
+constexpr int SMALL_LDS = GROUPS * 2 * 2 * SMALL_TILE;    // 2 buffers of both
+
+template <int F, typename T> __global__ __launch_bounds__(SMALL_THREADS) void small_kernel(SmallArgs a) {
+    typedef typename fc::Eight<T>::vec V;
+    int ti, tj;
+    fc::tile_place(fc::xcd_order(blockIdx.x, a.tm * a.tn), a.tm, a.tn, 8, ti, tj);
+    const int m0 = ti * SMALL, n0 = tj * SMALL, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = wave >> 2;
+    const int k = (threadIdx.x & 255) >> 2, c = 16 * (threadIdx.x & 3);  // a thread brings 16 columns of a step's token k
+    const int steps = (int)((a.kept.rows + SMALL - 1) / SMALL);
+    const uint32_t base = fc::lds_address(lds) + g * 4 * SMALL_TILE, to = k * 2 * SMALL + (fc::slow_block<SMALL>(c >> 4, k) << 5);
+    struct Data {
+        V dy[2];
+        fc::Codes x[2];
+        uint32_t scale;
+    };
+    // This thread's next step.
+    int64_t t = (int64_t)g * SMALL + k;
+    const T* dy = static_cast<const T*>(a.dy) + t * a.lddy + m0 + c;
+    const uint8_t *codes = a.kept.codes + t * a.kept.ldc + n0 + c, *scales = a.kept.scales + t * a.kept.lds + (n0 + c) / fc::BLOCK;
+    const int there = a.outs - m0 - c;
+    const bool kept = (n0 + c) / fc::BLOCK < a.kept.blocks;
+    auto fetch = [&]() __attribute__((always_inline)) {
+        Data d{};
+        if (t < a.kept.rows) {
+            // past a row's end anything does: what is made of it is not stored
+            if (there > 0 && (there >= 16 || (a.kept.rows - 1 - t) * a.lddy + there >= 16)) {
+                d.dy[0] = fc::raw8(dy);
+                d.dy[1] = fc::raw8(dy + 8);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 15; ++e)
+                    if (e < there) d.dy[e / 8][e % 8] = dy[e];
+            }
+            if (kept) {
+                const uint4 q = *reinterpret_cast<const uint4*>(codes);
+                d.x[0] = fc::Codes{q.x, q.y};
+                d.x[1] = fc::Codes{q.z, q.w};
+                d.scale = *scales;
+            }
+        }
+        t += GROUPS * SMALL;
+        dy += GROUPS * SMALL * a.lddy;
+        codes += GROUPS * SMALL * a.kept.ldc;
+        scales += GROUPS * SMALL * a.kept.lds;
+        return d;
+    };
+    auto put = [&](const Data& d, uint32_t at) __attribute__((always_inline)) {
+        const float s = fc::scale_value(d.scale);
+        fc::f32x8 x[2] = {fc::decode8<F>(d.x[0]) * s, fc::decode8<F>(d.x[1]) * s};
+        if (d.scale > fc::FITS<F, T>) {  // seldom
+            x[0] = fc::in_range<T>(x[0]);
+            x[1] = fc::in_range<T>(x[1]);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            *(FC_LDS V*)(uintptr_t)(at + to + 16 * h) = d.dy[h];
+            *(FC_LDS V*)(uintptr_t)(at + SMALL_TILE + to + 16 * h) = __builtin_convertvector(x[h], V);
+        }
+    };
+    const int wm = 32 * ((wave >> 1) & 1), wn = 32 * (wave & 1);
+    fc::Fragments<T, SMALL, true, 2> fa, fb;
+    fa.init(wm, lane);
+    fb.init(wn, lane);
+    f32x4 acc[2][2]{};
+    Data d[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) d[u] = fetch();
+    for (int s0 = 0, turn = 0; s0 < steps; s0 += AHEAD * GROUPS) {
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int s = s0 + u * GROUPS;
+            if (s >= steps) break;
+            const uint32_t at = base + turn * 2 * SMALL_TILE;
+            turn ^= 1;
+            put(d[u], at);
+            __syncthreads();
+            d[u] = fetch();
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) acc[i][j] = Half<T>::mma(fb.get(at + SMALL_TILE, j, kk), fa.get(at, i, kk), acc[i][j]);
+        }
+    }
+    __syncthreads();  // the tiles are done with
+    float(*const part)[SMALL][SMALL + 4] = reinterpret_cast<float(*)[SMALL][SMALL + 4]>(lds);
+    static_assert(sizeof(float) * GROUPS * SMALL * (SMALL + 4) <= SMALL_LDS, "the groups' sums fit");
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) *reinterpret_cast<f32x4*>(&part[g][wm + 16 * i + (lane & 15)][wn + 16 * j + 4 * (lane >> 4)]) = acc[i][j];
+    __syncthreads();
+    const int m = threadIdx.x >> 4, n = 4 * (threadIdx.x & 15), left = a.kept.dim - n0 - n;
+    if (m0 + m >= a.outs || left <= 0) return;
+    f32x4 v{};
+#pragma unroll
+    for (int q = 0; q < GROUPS; ++q) v += *reinterpret_cast<const f32x4*>(&part[q][m][n]);
+    v = v * a.scale;
+    const int64_t at = (int64_t)(m0 + m) * a.ld + n0 + n;
+    if (a.add) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < left) v[e] += load_one(a.out, a.dt, at + e);
+    }
+    store_four(a.out, a.dt, at, v, left);
+}
+
+// Estimated, as KindCost's.
+double small_us(int64_t n, int64_t outs, int64_t dim) {
+    const int64_t tiles = fc::ceil_div(outs, SMALL) * fc::ceil_div(dim, SMALL), rounds = fc::ceil_div(n, SMALL * GROUPS);
+    return fc::ceil_div(tiles, CUS) * (3.6 + 1.4 * rounds);
+}
+
+template <int F, typename T> void launch_small(SmallArgs a, hipStream_t s) {
+    a.tm = (int)fc::ceil_div(a.outs, SMALL);
+    a.tn = (int)fc::ceil_div(a.kept.dim, SMALL);
+    small_kernel<F, T><<<a.tm * a.tn, SMALL_THREADS, SMALL_LDS, s>>>(a);
+}
+
+template <typename T> hipError_t prepare_small() {
+    for (const void* k : {(const void*)small_kernel<FC_BLOCK_I8, T>, (const void*)small_kernel<FC_BLOCK_E4M3, T>}) {
+        const hipError_t e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, SMALL_LDS);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace
@@ -113,6 +267,13 @@ template <typename T>
 void grad(fc_ckpt* p, const void* dy, int64_t lddy, const fc::BlockRows& kept, int64_t outs, float scale, void* dw, int dwt, int64_t lddw, bool add,
           hipStream_t s) {
     const int64_t n = kept.rows, ldx = fc::ceil_div(p->dim, 8) * 8;
+    const Choice c = choose_tiles(COST_DW, LARGE, TINY, -1, outs, p->dim, fc::ceil_div(n, fc::GEMM_BK), true, p->sums);
+    if (small_us(n, outs, p->dim) < c.us + 3.0) {  // with the launch that brings the operands
+        const SmallArgs q{kept, dy, lddy, (int)outs, scale, dw, dwt, lddw, add};
+        if (p->format == FC_BLOCK_I8) launch_small<FC_BLOCK_I8, T>(q, s);
+        else launch_small<FC_BLOCK_E4M3, T>(q, s);
+        return;
+    }
     const bool copy = lddy % 8 || reinterpret_cast<uintptr_t>(dy) % 16;
     const int64_t ld = fc::ceil_div(outs, 8) * 8, per = ldx / 8, per_dy = copy ? ld / 8 : 0;
     fc::by_launches(n, per + per_dy, [&](int64_t r0, int64_t count) {
@@ -136,7 +297,6 @@ void grad(fc_ckpt* p, const void* dy, int64_t lddy, const fc::BlockRows& kept, i
     g.n = (int)p->dim;
     g.k = (int)n;
     g.parts = 1;
-    const Choice c = choose_tiles(COST_DW, LARGE, TINY, -1, outs, p->dim, fc::ceil_div(n, fc::GEMM_BK), true, p->sums);
     const bool split = c.splits > 1;
     g.kper = c.steps * fc::GEMM_BK;
     g.scale = scale;
@@ -175,6 +335,7 @@ int fc_ckpt_create(fc_ckpt** plan, int64_t dim, int64_t max_tokens, int64_t max_
         int rc = p->order.create();
         if (!rc) rc = fc::hip_code(dtype == FC_F16 ? prepare_all<f16, false>() : prepare_all<bf16, false>());
         if (!rc) rc = fc::hip_code(dtype == FC_F16 ? prepare_all<f16, true>() : prepare_all<bf16, true>());
+        if (!rc) rc = fc::hip_code(dtype == FC_F16 ? prepare_small<f16>() : prepare_small<bf16>());
         if (!rc) rc = p->block.create(at.size);
         if (rc) {
             fc_ckpt_destroy(p);

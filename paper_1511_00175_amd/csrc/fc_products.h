@@ -273,6 +273,7 @@ struct Choice {
     TileKind kind;
     int splits;      // parts of k, of `steps` of 64 each
     int steps;
+    double us;       // estimated
 };
 
 constexpr int64_t SPLIT_FLOATS = (int64_t)1 << 27;
@@ -283,7 +284,7 @@ constexpr int64_t SPLIT_FLOATS = (int64_t)1 << 27;
 // `most`: floats of partial sums.
 inline Choice choose_tiles(const KindCost* cost, int first, int last, int skip, int64_t m, int64_t n, int64_t total, bool may_split, int64_t most) {
     m = fc::ceil_div(m, 64) * 64;
-    Choice best{(TileKind)last, 1, (int)total};
+    Choice best{(TileKind)last, 1, (int)total, 0};
     double least = 1e300;
     for (int kind = first; kind <= last; ++kind) {
         if (kind == skip) continue;
@@ -299,7 +300,7 @@ inline Choice choose_tiles(const KindCost* cost, int first, int last, int skip, 
             if (parts > 1) t += 5.0 + 8.0 * parts * m * n / 4.5e6;  // partial sums, written and read
             if (t < least) {
                 least = t;
-                best = {(TileKind)kind, (int)parts, (int)steps};
+                best = {(TileKind)kind, (int)parts, (int)steps, t};
             }
         }
     }

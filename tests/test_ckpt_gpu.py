@@ -96,6 +96,31 @@ def test_gradient_sizes(fc, device, kind, n, d, outs):
     grad_case(fc, device, n, d, outs, kind)
 
 
+@pytest.mark.parametrize("kind", ["i8", "e4m3"])
+@pytest.mark.parametrize("n,d,outs,dtype,to,pad,shift,accumulate", [
+    (1, 1100, 1100, "f16", "f32", 0, 0, False), (70, 1300, 1031, "bf16", "f16", 3, 1, True), (300, 2049, 777, "f16", "bf16", 0, 0, False),
+    (77, 1200, 1040, "bf16", "f32", 8, 0, True), (700, 520, 2503, "f16", "f32", 5, 3, False), (4097, 300, 130, "bf16", "f32", 1, 1, True)])
+def test_gradients_of_more_tiles(fc, device, kind, n, d, outs, dtype, to, pad, shift, accumulate):
+    """Past what goes in one launch: more tiles than compute units, or so many tokens that k is split."""
+    grad_case(fc, device, n, d, outs, kind, dtype, to, pad, shift, accumulate=accumulate)
+
+
+def test_largest_activations_stay_in_range(fc, device):
+    """fp16's largest number rounds to 65536 in 8 bits, which is taken as the largest again, by gradients of few tiles and many."""
+    for outs in (64, 4096):
+        plan = fc.Checkpoint(300, 80, outs)
+        x = torch.full((80, 300), 65504.0, dtype=torch.float16, device=device)
+        codes, scales = plan.empty(80)
+        plan.pack(x, codes, scales)
+        dw = torch.empty(outs, 300, device=device)
+        dy = torch.zeros(80, outs, dtype=torch.float16, device=device)
+        dy[33] = 0.5
+        plan.grad(dy, codes, scales, dw)
+        kept = torch.empty_like(x)
+        plan.unpack(codes, scales, kept)
+        assert torch.equal(dw, (kept[33].float() * 0.5).expand(outs, 300))
+
+
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("to", list(DT))
 @pytest.mark.parametrize("pad,shift", [(0, 0), (8, 0), (3, 1)])
