@@ -58,6 +58,12 @@ __device__ __forceinline__ uint32_t most_of(f32x8 v) {
     return m;
 }
 
+// The most of 4 neighbouring lanes', for a block of 32: by a permutation of lanes, not by way of LDS.
+__device__ __forceinline__ uint32_t most_of_four(uint32_t most) {
+    most = max(most, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)most, 0xb1, 0xf, 0xf, true));  // lanes 1, 0, 3, 2
+    return max(most, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)most, 0x4e, 0xf, 0xf, true));  // lanes 2, 3, 0, 1
+}
+
 struct Codes {
     uint32_t lo, hi;  // hi unused by the 4-bit format
 };
@@ -146,10 +152,7 @@ template <int F, typename T> __device__ __forceinline__ void pack_eight(const Bl
     const uint32_t per = 4 * a.blocks, r = i / per, u = i % per;
     if (r >= a.rows) return;
     const f32x8 v = load8(static_cast<const T*>(a.x) + r * a.ldx + 8 * u, a.dim - 8 * (int)u);
-    uint32_t most = most_of(v);
-    most = max(most, (uint32_t)__shfl_xor((int)most, 1));
-    most = max(most, (uint32_t)__shfl_xor((int)most, 2));
-    const uint32_t byte = scale_byte<F>(most);
+    const uint32_t byte = scale_byte<F>(most_of_four(most_of(v)));
     const Codes c = encode8<F>(v, scale_inverse(byte));
     uint8_t* const to = a.codes + r * a.ldc + u * EIGHT_BYTES<F>;
     if constexpr (F == E2M1) *reinterpret_cast<uint32_t*>(to) = c.lo;

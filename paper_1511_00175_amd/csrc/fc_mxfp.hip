@@ -168,6 +168,47 @@ struct FewArgs {
     bool add;
 };
 
+// `tokens` rows of x packed into LDS by all threads of a block, rows of codes and of scales
+// `row` and `scale_row` bytes apart; `after` rows of x follow them.  4 loads of a thread are on
+// their way at a time, whole vectors but at the end of the last row.
+template <typename X>
+__device__ __forceinline__ void pack_tokens(const X* x, int64_t ldx, int tokens, int after, int dim, int blocks, char* codes, int row, char* scales, int scale_row) {
+    typedef typename fc::Eight<X>::vec V;
+    const uint32_t per = 4 * blocks, all = tokens * per;
+    for (uint32_t i0 = threadIdx.x; i0 < all; i0 += 4 * blockDim.x) {
+        V v[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const uint32_t i = i0 + q * blockDim.x, t = i / per, u = i - t * per;
+            const int left = dim - 8 * (int)u;
+            v[q] = V{};
+            if (i >= all || left <= 0) continue;
+            const X* const p = x + t * ldx + 8 * u;
+            if (left >= 8 || (tokens + after - 1 - (int)t) * ldx + left >= 8) {
+                v[q] = fc::raw8(p);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 7; ++e)
+                    if (e < left) v[q][e] = p[e];
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const uint32_t i = i0 + q * blockDim.x, t = i / per, u = i - t * per;
+            if (i >= all) break;  // the same for the 4 threads of a block of the format
+            const int left = dim - 8 * (int)u;
+            fc::f32x8 f = __builtin_convertvector(v[q], fc::f32x8);
+            if (left < 8) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[e] = e < left ? f[e] : 0.f;
+            }
+            const uint32_t byte = fc::scale_byte<fc::E2M1>(fc::most_of_four(fc::most_of(f)));
+            *reinterpret_cast<uint32_t*>(codes + t * row + 4 * u) = fc::encode8<fc::E2M1>(f, fc::scale_inverse(byte)).lo;
+            if (u % 4 == 0) scales[t * scale_row + u / 4] = (char)byte;
+        }
+    }
+}
+
 constexpr int AHEAD = 3;     // steps of a wave on their way at a time
 
 template <typename X> __global__ __launch_bounds__(1024) void few_kernel(FewArgs a) {
@@ -200,16 +241,7 @@ template <typename X> __global__ __launch_bounds__(1024) void few_kernel(FewArgs
     const int codes = 16 * a.blocks;                        // bytes of a token's
     char* const xc = lds;                                   // [token][codes]
     char* const xs = lds + a.n * codes;                     // [token][width]
-    for (int i = threadIdx.x; i < a.n * 4 * a.blocks; i += blockDim.x) {
-        const int t = i / (4 * a.blocks), u = i % (4 * a.blocks);
-        const fc::f32x8 v = fc::load8(static_cast<const X*>(a.x) + t * a.ldx + 8 * u, a.dim - 8 * u);
-        uint32_t most = fc::most_of(v);
-        most = max(most, (uint32_t)__shfl_xor((int)most, 1));
-        most = max(most, (uint32_t)__shfl_xor((int)most, 2));
-        const uint32_t byte = fc::scale_byte<fc::E2M1>(most);
-        *reinterpret_cast<uint32_t*>(xc + t * codes + 4 * u) = fc::encode8<fc::E2M1>(v, fc::scale_inverse(byte)).lo;
-        if (u % 4 == 0) xs[t * a.width + u / 4] = (char)byte;
-    }
+    pack_tokens(static_cast<const X*>(a.x), a.ldx, a.n, 0, a.dim, a.blocks, xc, codes, xs, a.width);
     __syncthreads();
     fc::f32x4 acc{0.f, 0.f, 0.f, 0.f};
     for (int s0 = wave; s0 < steps; s0 += AHEAD * waves) {
@@ -254,9 +286,124 @@ template <typename X> void launch_few(const FewArgs& a, hipStream_t s) {
     few_kernel<X><<<blocks, 64 * waves, bytes, s>>>(a);
 }
 
+// ---- few tiles ----------------------------------------------------------------------------
+
+// 64 tokens by 64 rows of b to a block, in one launch: the block packs its tokens into LDS, and
+// its waves, 32 x 32 of the tile each, share k in steps of 128 by fours and add up through LDS.
+// b's elements go from memory to registers as few_kernel's do.  What bounds it is the packing,
+// done again for every 64 rows of b.
+constexpr int SMALL = 64, PARTS = 4, SMALL_WAVES = 4 * PARTS, SMALL_AHEAD = 2;
+constexpr int SMALL_LDS = PARTS * SMALL * (SMALL + 4) * 4;  // the parts' sums
+
+// Whether it is taken, for up to a block to a compute unit: as long as that takes no more than
+// packing in a launch of its own and the tiles, by when the host has saved a launch (3 us).  In
+// graphs, us, taken / not, fp32: 1003 tokens, 1001 x 520 8.5 / 8.8; 2048, 64 x 64 4.2 / 6.1; 256,
+// 4096 x 512 7.8 / 7.4; 256, 1024 x 1024 11.6 / 7.3; two blocks to a unit: 2048, 1001 x 520 15.1 / 11.0.
+constexpr int SMALL_DIM = 576;
+bool is_small(int64_t n, int64_t rows, int64_t dim) { return dim <= SMALL_DIM && fc::ceil_div(n, SMALL) * fc::ceil_div(rows, SMALL) <= CUS; }
+
+// LDS of a token's codes: an odd number of 16 bytes, so that 16 rows' lie in different banks.
+__host__ __device__ constexpr int small_row(int blocks) { return 16 * (blocks | 1); }
+static_assert(SMALL * (small_row(SMALL_DIM / fc::BLOCK) + SMALL_DIM / fc::BLOCK + 3) <= SMALL_LDS, "the packed tokens fit");
+
+template <typename X> __global__ __launch_bounds__(64 * SMALL_WAVES) void small_kernel(FewArgs a, int tm, int tn) {
+    typedef fc::i32x4 V;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), part = wave >> 2, r = lane & 15, g = lane >> 4;
+    int ti, tj;
+    fc::tile_place(fc::xcd_order(blockIdx.x, tm * tn), tm, tn, 8, ti, tj);
+    const int t0 = ti * SMALL, r0 = tj * SMALL, wm = 32 * ((wave >> 1) & 1), wn = 32 * (wave & 1);
+    const int steps = (a.blocks + 3) / 4, tokens = min(SMALL, a.n - t0);
+    struct Rows {
+        V code[2];
+        uint32_t scale[2];
+    };
+    const char *bc[2], *bs[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int row = min(r0 + wn + 16 * j + r, a.b.rows - 1);
+        bc[j] = static_cast<const char*>(a.b.p) + (int64_t)row * 2 * a.b.ld;
+        bs[j] = static_cast<const char*>(a.b.scales) + (int64_t)row * a.b.lds;
+    }
+    auto fetch = [&](int s) __attribute__((always_inline)) {
+        Rows q{};
+        const int block = 4 * s + g;
+        if (s < steps && block < a.blocks) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                q.code[j] = *reinterpret_cast<const V*>(bc[j] + 16 * block);
+                q.scale[j] = *reinterpret_cast<const uint8_t*>(bs[j] + block);
+            }
+        }
+        return q;
+    };
+    Rows b[SMALL_AHEAD];
+#pragma unroll
+    for (int u = 0; u < SMALL_AHEAD; ++u) b[u] = fetch(part + PARTS * u);
+    const int row = small_row(a.blocks), scales = (a.blocks + 3) / 4 * 4;
+    char* const xc = lds;                                   // [token][row]
+    char* const xs = lds + SMALL * row;                     // [token][scales]
+    pack_tokens(static_cast<const X*>(a.x) + t0 * a.ldx, a.ldx, tokens, a.n - t0 - tokens, a.dim, a.blocks, xc, row, xs, scales);
+    __syncthreads();
+    fc::f32x4 acc[2][2]{};
+    for (int s0 = part; s0 < steps; s0 += PARTS * SMALL_AHEAD) {
+#pragma unroll
+        for (int u = 0; u < SMALL_AHEAD; ++u) {
+            const int s = s0 + PARTS * u;
+            if (s >= steps) break;
+            const int block = 4 * s + g;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int t = wm + 16 * i + r;
+                V code{};
+                uint32_t scale = 0;
+                if (block < a.blocks && t < tokens) {
+                    code = *reinterpret_cast<const V*>(xc + t * row + 16 * block);
+                    scale = *reinterpret_cast<const uint8_t*>(xs + t * scales + block);
+                }
+#pragma unroll
+                for (int j = 0; j < 2; ++j) acc[i][j] = fc::mma4(b[u].code[j], code, acc[i][j], b[u].scale[j], scale);
+            }
+            b[u] = fetch(s + PARTS * SMALL_AHEAD);
+        }
+    }
+    __syncthreads();  // the packed tokens are done with
+    float(*const sums)[SMALL][SMALL + 4] = reinterpret_cast<float(*)[SMALL][SMALL + 4]>(lds);  // [part][token][row]
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) *reinterpret_cast<fc::f32x4*>(&sums[part][wm + 16 * i + r][wn + 16 * j + 4 * g]) = acc[i][j];
+    __syncthreads();
+    const int t = threadIdx.x >> 4, c = 4 * (threadIdx.x & 15), left = a.b.rows - r0 - c;
+    if (t >= tokens || left <= 0) return;
+    fc::f32x4 v{};
+#pragma unroll
+    for (int q = 0; q < PARTS; ++q) v += *reinterpret_cast<const fc::f32x4*>(&sums[q][t][c]);
+    v = v * a.scale;
+    const int64_t to = (int64_t)(t0 + t) * a.ld + r0 + c;
+    if (a.add) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < left) v[e] += load_one(a.out, a.dt, to + e);
+    }
+    store_four(a.out, a.dt, to, v, left);
+}
+
+hipError_t prepare_small() {
+    for (const void* k : {(const void*)small_kernel<float>, (const void*)small_kernel<f16>, (const void*)small_kernel<bf16>}) {
+        const hipError_t e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, SMALL_LDS);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+template <typename X> void launch_small(const FewArgs& a, hipStream_t s) {
+    const int tm = (int)fc::ceil_div(a.n, SMALL), tn = (int)fc::ceil_div(a.b.rows, SMALL);
+    small_kernel<X><<<tm * tn, 64 * SMALL_WAVES, SMALL_LDS, s>>>(a, tm, tn);
+}
+
 template <bool ADD> hipError_t prepare_all() {
     for (hipError_t e : {prepare<Wide4>((const void*)result_kernel<Wide4, ADD, Operand4>), prepare<Half4>((const void*)result_kernel<Half4, ADD, Operand4>),
-                         prepare<Small4>((const void*)result_kernel<Small4, ADD, Operand4>), prepare_tiles<Wide4>()})
+                         prepare<Small4>((const void*)result_kernel<Small4, ADD, Operand4>), prepare_tiles<Wide4>(), prepare_small()})
         if (e != hipSuccess) return e;
     return hipSuccess;
 }
@@ -492,9 +639,10 @@ int fc_mxfp_linear(fc_mxfp* p, const void* x, int x_dtype, int64_t ld_x, int64_t
         bool note;
         rc = p->order.begin(s, note);
         if (rc) return rc;
-        if (n && is_few(n, p->rows, p->dim)) {
+        const bool few = is_few(n, p->rows, p->dim);
+        if (n && (few || is_small(n, p->rows, p->dim))) {
             const FewArgs f{operand(p, b, 0, p->rows), x, ld_x, (int)n, (int)p->dim, p->blocks, p->width, scale, out, out_dtype, ld_out, accumulate != 0};
-            fc::by_dtype(x_dtype, [&](auto t) { launch_few<decltype(t)>(f, s); });
+            fc::by_dtype(x_dtype, [&](auto t) { few ? launch_few<decltype(t)>(f, s) : launch_small<decltype(t)>(f, s); });
             n = 0;
         }
         for (int64_t t0 = 0; t0 < n; t0 += CHUNK) {

@@ -103,6 +103,14 @@ def test_product_types_strides_alignment(fc, device, dtype, to, n, pad, shift):
     product_case(fc, device, n, 77, 300, dtype, to, pad, shift)
 
 
+@pytest.mark.parametrize("dtype,to", [("f32", "f16"), ("f16", "f16"), ("bf16", "f32")])
+@pytest.mark.parametrize("pad,shift", [(0, 0), (3, 1)])
+@pytest.mark.parametrize("n,rows,dim", [(90, 77, 700), (40, 130, 576), (40, 130, 577), (1000, 1024, 552), (1000, 1030, 552), (17, 16300, 40), (17, 16400, 40)])
+def test_inputs_packed_within_the_product_and_before_it(fc, device, dtype, to, pad, shift, n, rows, dim):
+    """Both sides of the widths and tiles up to which one launch packs and multiplies."""
+    product_case(fc, device, n, rows, dim, dtype, to, pad, shift, accumulate=pad > 0)
+
+
 @pytest.mark.parametrize("to", list(DT))
 @pytest.mark.parametrize("n,rows,dim", [(1, 90, 700), (12, 50, 9000), (70, 66, 9000), (300, 200, 96)])
 def test_product_accumulates(fc, device, to, n, rows, dim):
