@@ -69,7 +69,9 @@ __device__ __forceinline__ void gate_both(float g, int kind, float& a, float& sl
 
 // `lanes` threads hold a row, VECTORS times 8 elements each, a vector's neighbours in
 // neighbouring threads: 8 to 64 lanes of a wave, with several rows to a block of 256, or
-// a block of whole waves for one row.  Rows of fewer than 8 elements go as the widest do.
+// a block of whole waves for one row.  Rows of more than 8192 elements take two or four vectors
+// to a thread: at 9216 two, 9 waves, take 113 us forward and 327 backward where four, 5 waves,
+// took 159 and 495 (3640 rows, 16 bits).  Rows of fewer than 8 elements go as they do.
 struct Shape {
     int lanes, vectors, threads;
     int groups;  // rows to a block of the backward pass
@@ -77,15 +79,16 @@ struct Shape {
 
 constexpr int DIM_LIMIT = 16384;
 constexpr int BLOCK = 256;  // threads of a backward pass's blocks, where a row takes no more
+constexpr int MIDDLE = 640;  // threads of rows of two vectors each, at most
 
 Shape shape_of(int64_t dim) {
-    if (dim < 8) return {64, 4, 64, 1};
+    if (dim < 8) return {64, 2, 64, 1};
     if (dim <= 512) {
         int lanes = 8;
         while (lanes * 8 < dim) lanes *= 2;
         return {lanes, 1, 256, BLOCK / lanes};
     }
-    const int vectors = dim <= 8192 ? 1 : 4, threads = (int)fc::ceil_div(dim, 512 * vectors) * 64;
+    const int vectors = dim <= 8192 ? 1 : dim <= 1024 * MIDDLE / 64 ? 2 : 4, threads = (int)fc::ceil_div(dim, 512 * vectors) * 64;
     return {threads, vectors, threads, vectors > 1 ? 1 : std::max(1, BLOCK / threads)};
 }
 
@@ -229,8 +232,7 @@ template <typename T, typename H, bool SHARED> __global__ __launch_bounds__(1024
 }
 
 // Rows of more than 8192 elements, and of fewer than 8.
-template <typename T, typename H> __global__ __launch_bounds__(512) void forward_wide_kernel(ForwardArgs a) {
-    constexpr int V = 4;
+template <typename T, typename H, int V> __global__ __launch_bounds__(V == 2 ? MIDDLE : 512) void forward_wide_kernel(ForwardArgs a) {
     __shared__ __align__(16) float part[2][1][WAVES];
     RowSums<1> sums{part, a.lanes, 0};
     const int lane = threadIdx.x;
@@ -475,9 +477,9 @@ template <typename T, typename H, bool SHARED> __global__ __launch_bounds__(1024
 }
 
 // Rows of more than 8192 elements are more than a block's registers hold: they are read
-// again in each pass over them (rows of fewer than 8 come here too), and the sums over tokens
-// lie in LDS, of which every thread uses its own part.
-template <typename T, typename H> __global__ __launch_bounds__(512) void backward_wide_kernel(BackwardArgs a) {
+// again in each pass over them, from the caches (rows of fewer than 8 come here too), and the sums
+// over tokens lie in LDS, of which every thread uses its own part.  1.6 TB/s, for want of waves.
+template <typename T, typename H, int V> __global__ __launch_bounds__(V == 2 ? MIDDLE : 512) void backward_wide_kernel(BackwardArgs a) {
     __shared__ __align__(16) float part[2][3][WAVES];
     RowSums<3> sums{part, a.lanes, 0};
     const int lane = threadIdx.x;
@@ -485,13 +487,13 @@ template <typename T, typename H> __global__ __launch_bounds__(512) void backwar
     const bool layer = a.kind == FC_NORM_LAYER, matrix = a.gate && a.ldgate;
     auto col = [&](int v) __attribute__((always_inline)) { return (v * a.lanes + lane) * 8; };
     auto left = [&](int v) __attribute__((always_inline)) { return a.dim - col(v); };
-    constexpr int vectors = 4;
+    constexpr int vectors = V;
     auto held = [&](int which, int v) __attribute__((always_inline)) { return reinterpret_cast<f32x8*>(column_sums) + (which * vectors + v) * a.lanes + lane; };
     for (int v = 0; v < 2 * vectors; ++v) *held(0, v) = f32x8{};
     for (int64_t t = blockIdx.x; t < a.n; t += gridDim.x) {
         f32x8 x, dy, b, d, g;  // of one vector at a time
         float s[3], mean_x = 0.f, mean_u = 0.f, mean_b = 0.f, r = 0.f, rb = 0.f, along = 0.f;
-        auto fetch = [&](int v) __attribute__((always_inline)) {
+        auto fetch = [&](int v, bool all) __attribute__((always_inline)) {  // `all`: not for the statistics alone
             const int n = left(v);
             x = dy = b = d = g = f32x8{};
             if (a.dy) {
@@ -499,8 +501,8 @@ template <typename T, typename H> __global__ __launch_bounds__(512) void backwar
                 dy = load8(static_cast<const T*>(a.dy) + t * a.lddy + col(v), n);
             }
             if (a.b) b = load8(static_cast<const T*>(a.b) + t * a.ldb + col(v), n);
-            if (a.dout) d = load8(static_cast<const H*>(a.dout) + t * a.lddout + col(v), n);
-            if (a.b && matrix) g = load8(static_cast<const T*>(a.gate) + t * a.ldgate + col(v), n);
+            if (all && a.dout) d = load8(static_cast<const H*>(a.dout) + t * a.lddout + col(v), n);
+            if (all && a.b && matrix) g = load8(static_cast<const T*>(a.gate) + t * a.ldgate + col(v), n);
         };
         auto centre = [&](int v) __attribute__((always_inline)) {
             if (!layer) return;
@@ -539,7 +541,7 @@ template <typename T, typename H> __global__ __launch_bounds__(512) void backwar
         if (layer) {
 #pragma unroll 1
             for (int v = 0; v < vectors; ++v) {
-                fetch(v);
+                fetch(v, false);
                 const f32x8 w = a.dy ? channels(a.next, col(v), left(v)) : f32x8{};
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
@@ -558,7 +560,7 @@ template <typename T, typename H> __global__ __launch_bounds__(512) void backwar
         }
 #pragma unroll 1
         for (int v = 0; v < vectors; ++v) {
-            fetch(v);
+            fetch(v, false);
             centre(v);
             const f32x8 w = a.dy ? channels(a.next, col(v), left(v)) : f32x8{};
 #pragma unroll
@@ -575,7 +577,7 @@ template <typename T, typename H> __global__ __launch_bounds__(512) void backwar
         s[0] = s[1] = s[2] = 0.f;
 #pragma unroll 1
         for (int v = 0; v < vectors; ++v) {
-            fetch(v);
+            fetch(v, true);
             centre(v);
             if (a.dy) {
                 before(v, true);
@@ -594,7 +596,7 @@ template <typename T, typename H> __global__ __launch_bounds__(512) void backwar
         const float along_b = s[0] * inv, mean = layer ? s[1] * inv : 0.f;
 #pragma unroll 1
         for (int v = 0; v < vectors; ++v) {
-            fetch(v);
+            fetch(v, true);
             centre(v);
             if (a.dy) before(v, false);
             after(v, false);
@@ -670,9 +672,15 @@ __global__ __launch_bounds__(1024) void finish_kernel(FinishArgs a) {
 constexpr int64_t TOKENS_LIMIT = (int64_t)1 << 31;
 constexpr int64_t FORWARD_BLOCKS = 1 << 20;
 
-// Blocks of a backward pass that the chip holds at once: 16 waves to a compute unit, and one
-// block of the widest rows, whose sums fill its LDS.
-int64_t blocks_limit(Shape s) { return 256 * (s.lanes >= 64 && s.vectors > 1 ? 1 : 1024 / (s.groups * s.lanes)); }
+// The sums over tokens of a block of rows of several vectors to a thread.
+int wide_lds(Shape s) { return 2 * s.vectors * s.lanes * (int)sizeof(f32x8); }
+
+// Blocks of a backward pass that the chip holds at once: 16 waves to a compute unit, of rows of
+// several vectors to a thread 12 and as many blocks as its LDS holds.
+int64_t blocks_limit(Shape s) {
+    if (s.vectors == 1) return 256 * (1024 / (s.groups * s.lanes));
+    return 256 * std::max(1, std::min(160 * 1024 / (wide_lds(s) + 1024), 768 / s.lanes));
+}
 
 // Blocks of a backward pass of n rows.
 int64_t backward_blocks(Shape s, int64_t n) { return std::min<int64_t>(fc::ceil_div(n, s.groups), blocks_limit(s)); }
@@ -693,18 +701,21 @@ struct fc_norm {
 namespace {
 
 template <typename T, typename H> void forward(const Shape& s, unsigned grid, const ForwardArgs& a, hipStream_t st) {
-    if (s.vectors > 1) forward_wide_kernel<T, H><<<grid, s.threads, 0, st>>>(a);
+    if (s.vectors == 4) forward_wide_kernel<T, H, 4><<<grid, s.threads, 0, st>>>(a);
+    else if (s.vectors == 2) forward_wide_kernel<T, H, 2><<<grid, s.threads, 0, st>>>(a);
     else if (s.lanes < 64) forward_kernel<T, H, true><<<grid, s.threads, 0, st>>>(a);
     else forward_kernel<T, H, false><<<grid, s.threads, 0, st>>>(a);
 }
 
 // The LDS of the longest rows.
 template <typename T, typename H> hipError_t prepare() {
-    return hipFuncSetAttribute((const void*)backward_wide_kernel<T, H>, hipFuncAttributeMaxDynamicSharedMemorySize, 8 * DIM_LIMIT);
+    const hipError_t e = hipFuncSetAttribute((const void*)backward_wide_kernel<T, H, 2>, hipFuncAttributeMaxDynamicSharedMemorySize, 128 * MIDDLE);
+    return e != hipSuccess ? e : hipFuncSetAttribute((const void*)backward_wide_kernel<T, H, 4>, hipFuncAttributeMaxDynamicSharedMemorySize, 8 * DIM_LIMIT);
 }
 
 template <typename T, typename H> void backward(const Shape& s, unsigned grid, const BackwardArgs& a, hipStream_t st) {
-    if (s.vectors > 1) backward_wide_kernel<T, H><<<grid, s.threads, 2 * s.vectors * s.lanes * sizeof(f32x8), st>>>(a);
+    if (s.vectors == 4) backward_wide_kernel<T, H, 4><<<grid, s.threads, wide_lds(s), st>>>(a);
+    else if (s.vectors == 2) backward_wide_kernel<T, H, 2><<<grid, s.threads, wide_lds(s), st>>>(a);
     else {
         const int threads = s.groups * s.lanes;
         if (s.lanes < 64) backward_kernel<T, H, true><<<grid, threads, threads * 2 * sizeof(f32x8), st>>>(a);

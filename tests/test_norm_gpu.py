@@ -182,6 +182,18 @@ def test_sizes(fc, device, n, dim, kind):
     run_case(fc, device, n, dim, kind=kind)
 
 
+@pytest.mark.parametrize("n,dim", [(2, 9217), (3, 10240), (2, 10241)])
+@pytest.mark.parametrize("kind,gate,dtype,residual", [("rms", "matrix", "bf16", "f32"), ("layer", "vector", "f32", "f32")])
+def test_wide_rows(fc, device, n, dim, kind, gate, dtype, residual):
+    """Two vectors to a thread up to 10240 elements, four beyond."""
+    run_case(fc, device, n, dim, dtype, residual, kind, gate, "silu")
+
+
+@pytest.mark.parametrize("n", [5000, 70000])
+def test_many_short_rows(fc, device, n):
+    run_case(fc, device, n, 5, kind="layer", gate="vector", act="sigmoid")
+
+
 @pytest.mark.parametrize("n,dim", [(40000, 8), (33000, 60), (2500, 600), (1100, 8200)])
 @pytest.mark.parametrize("kind,gate", [("rms", "matrix"), ("layer", "vector")])
 def test_more_rows_than_blocks(fc, device, n, dim, kind, gate):
