@@ -196,7 +196,7 @@ typedef struct fc_norm fc_norm;
  * A weight may be null: 1.  Everything is computed in fp32 and rounded once, statistics
  * included: the squares of a row must not run past its range.  Sums over tokens are
  * fp32, in an order that depends on n and dim alone.  The workspace holds up to 1280
- * rows of partial sums of two vectors, 8 bytes per element of a row (3072 where dim is
+ * rows of partial sums of two vectors, 8 bytes per element of a row (2048 rows where dim is
  * below 8). */
 int fc_norm_create(fc_norm** plan, int64_t dim, int64_t max_tokens, int dtype, int residual_dtype, int kind, float eps,
                    int gate);

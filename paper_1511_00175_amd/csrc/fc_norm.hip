@@ -676,10 +676,10 @@ constexpr int64_t FORWARD_BLOCKS = 1 << 20;
 int wide_lds(Shape s) { return 2 * s.vectors * s.lanes * (int)sizeof(f32x8); }
 
 // Blocks of a backward pass that the chip holds at once: 16 waves to a compute unit, of rows of
-// several vectors to a thread 12 and as many blocks as its LDS holds.
+// several vectors to a thread 12 and as many blocks as its LDS holds, 8 at most.
 int64_t blocks_limit(Shape s) {
     if (s.vectors == 1) return 256 * (1024 / (s.groups * s.lanes));
-    return 256 * std::max(1, std::min(160 * 1024 / (wide_lds(s) + 1024), 768 / s.lanes));
+    return 256 * std::max(1, std::min({160 * 1024 / (wide_lds(s) + 1024), 768 / s.lanes, 8}));
 }
 
 // Blocks of a backward pass of n rows.
