@@ -19,9 +19,6 @@ namespace {
 constexpr int64_t ROWS_LIMIT = 1 << 21, LD_LIMIT = 1 << 21, TOKENS_LIMIT = (int64_t)1 << 31;
 constexpr int64_t GRAD_TOKENS = (int64_t)1 << 30;  // a product's k, up to a multiple of 64, is a 32-bit number
 
-// Partial sums that a split product may write: two rounds of the chip's largest tiles.
-constexpr int64_t SUMS_LIMIT = (int64_t)1 << 25;
-
 // ---- operands --------------------------------------------------------------------
 
 // x unpacked and, where dy lies otherwise than the product reads it, dy copied, in one
@@ -61,13 +58,8 @@ template <int F, typename T> __global__ __launch_bounds__(256) void operands_ker
 
 // ---- the product --------------------------------------------------------------------
 
+// TINY of fc_choice.h.
 template <typename T> using Tiny = fc::Product<T, 64, 64, 32, 32, true, true, 4>;
-
-// COST's kinds, 128 x 128 slower alone with both operands across their rows, and the one
-// above.  1003 tokens, 1001 x 520: 40 tiles of 128 x 128 take 21 us, 144 of these 9 (the form
-// for few tiles, below, takes that case).
-constexpr int TINY = 3;
-constexpr KindCost COST_DW[] = {COST[LARGE], COST[BROAD], {128, 128, 0.52, 0.7, 5.0, 2}, {64, 64, 0.25, 0.3, 4.0, 2}};
 
 template <typename T, bool ADD> hipError_t prepare_all() {
     for (hipError_t e : {prepare<Large<T, true, true>>((const void*)result_kernel<Large<T, true, true>, ADD, Operand>),
@@ -108,7 +100,7 @@ struct SmallArgs {
 };
 
 constexpr int AHEAD = 3;      // steps of a group on their way at a time
-constexpr int SMALL = 64, GROUPS = 4, SMALL_THREADS = GROUPS * 256;
+constexpr int SMALL = CKPT_SMALL, GROUPS = CKPT_GROUPS, SMALL_THREADS = GROUPS * 256;
 constexpr int SMALL_TILE = SMALL * SMALL * 2;             // bytes of an operand's
 constexpr int SMALL_LDS = GROUPS * 2 * 2 * SMALL_TILE;    // 2 buffers of both
 
@@ -218,12 +210,6 @@ template <int F, typename T> __global__ __launch_bounds__(SMALL_THREADS) void sm
     store_four(a.out, a.dt, at, v, left);
 }
 
-// Estimated, as KindCost's.
-double small_us(int64_t n, int64_t outs, int64_t dim) {
-    const int64_t tiles = fc::ceil_div(outs, SMALL) * fc::ceil_div(dim, SMALL), rounds = fc::ceil_div(n, SMALL * GROUPS);
-    return fc::ceil_div(tiles, CUS) * (3.6 + 1.4 * rounds);
-}
-
 template <int F, typename T> void launch_small(SmallArgs a, hipStream_t s) {
     a.tm = (int)fc::ceil_div(a.outs, SMALL);
     a.tn = (int)fc::ceil_div(a.kept.dim, SMALL);
@@ -267,8 +253,8 @@ template <typename T>
 void grad(fc_ckpt* p, const void* dy, int64_t lddy, const fc::BlockRows& kept, int64_t outs, float scale, void* dw, int dwt, int64_t lddw, bool add,
           hipStream_t s) {
     const int64_t n = kept.rows, ldx = fc::ceil_div(p->dim, 8) * 8;
-    const Choice c = choose_tiles(COST_DW, LARGE, TINY, -1, outs, p->dim, fc::ceil_div(n, fc::GEMM_BK), true, p->sums);
-    if (small_us(n, outs, p->dim) < c.us + 3.0) {  // with the launch that brings the operands
+    const Choice c = ckpt_choice(n, outs, p->dim, p->sums);
+    if (ckpt_small(c, n, outs, p->dim)) {
         const SmallArgs q{kept, dy, lddy, (int)outs, scale, dw, dwt, lddw, add};
         if (p->format == FC_BLOCK_I8) launch_small<FC_BLOCK_I8, T>(q, s);
         else launch_small<FC_BLOCK_E4M3, T>(q, s);
@@ -329,7 +315,7 @@ int fc_ckpt_create(fc_ckpt** plan, int64_t dim, int64_t max_tokens, int64_t max_
         p->blocks = (int)fc::ceil_div(dim, fc::BLOCK);
         fc::Layout at;
         const bool grads = max_outs > 0;
-        p->sums = grads ? std::min<int64_t>(SUMS_LIMIT, 64 * fc::ceil_div(max_outs, 64) * 64 * dim) : 0;
+        p->sums = ckpt_sums(max_outs, dim);
         const uint64_t o_x = at.take(grads ? max_tokens * fc::ceil_div(dim, 8) * 16 : 0),
                        o_dy = at.take(max_outs % 8 ? max_tokens * fc::ceil_div(max_outs, 8) * 16 : 0), o_sum = at.take(p->sums * 4);
         int rc = p->order.create();

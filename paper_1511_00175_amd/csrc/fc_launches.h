@@ -11,6 +11,8 @@
 
 namespace fc {
 
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
 // A part's threads: enough that its launch costs nothing beside them.
 constexpr int64_t LAUNCH_THREADS = (int64_t)1 << 28;
 

@@ -121,6 +121,4 @@ struct Layout {
     }
 };
 
-inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
 }  // namespace fc

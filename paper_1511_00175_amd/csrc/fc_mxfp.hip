@@ -18,9 +18,7 @@ namespace {
 using fc::Operand4;
 
 constexpr int64_t LD_LIMIT = 1 << 21, TOKENS_LIMIT = (int64_t)1 << 31;
-constexpr int64_t CHUNK = 1 << 18;  // tokens of one launch, and of linear's packed inputs
-// Partial sums that a split product may write: two rounds of the chip's largest tiles.
-constexpr int64_t SUMS_LIMIT = (int64_t)1 << 25;
+constexpr int64_t CHUNK = MXFP_CHUNK;
 
 // ---- columns to blocks ---------------------------------------------------------------
 
@@ -113,8 +111,6 @@ using Wide4 = fc::Product4<256, 256, 128, 64, 2>;
 using Half4 = fc::Product4<128, 128, 64, 64, 2>;
 using Small4 = fc::Product4<64, 64, 32, 32, 4>;
 
-enum { WIDE4, HALF4, SMALL4, KINDS4 };
-
 // A block goes through every gridDim.x-th tile, in the order of result_kernel's.
 template <typename P, typename T> __global__ __launch_bounds__(P::THREADS, P::THREADS / 256) void tiles_kernel(ResultArgs<Operand4> a) {
     const int count = a.tm * a.tn;
@@ -145,9 +141,6 @@ template <typename P> hipError_t prepare_tiles() {
         if (e != hipSuccess) return e;
     return hipSuccess;
 }
-
-// As COST, for steps of 256 of k.
-constexpr KindCost COST4[KINDS4] = {{256, 256, 1.78, 1.34, 4.5, 1, 6.0}, {128, 128, 0.56, 0.64, 5.2, 2}, {64, 64, 0.29, 0.38, 4.3, 2}};
 
 // ---- few tokens ---------------------------------------------------------------------------
 
@@ -272,12 +265,6 @@ template <typename X> __global__ __launch_bounds__(1024) void few_kernel(FewArgs
     store_one(a.out, a.dt, at, v);
 }
 
-// Whether it is taken: n tokens take the time of a block's packing for each round of blocks,
-// against a launch of its own.  us, taken / not: 4096 x 9216, 3 tokens 10.0 / 12.7; 9216 x 9216, 2 tokens
-// 20.0 / 19.5, 4 tokens 22 / 19; 8192 x 2048, 4 tokens 6.4 / 8.5, 8 tokens 8.0 / 8.0; 65536 x 2048, 1
-// token 19.7 / 20, 2 tokens 21.9 / 20; 1001 x 520, 16 tokens 5.6 / 6.8.
-bool is_few(int64_t n, int64_t rows, int64_t dim) { return n <= 16 && n * dim <= 32768 && n * dim * fc::ceil_div(rows, 16) <= 9000000; }
-
 template <typename X> void launch_few(const FewArgs& a, hipStream_t s) {
     const int blocks = (int)fc::ceil_div(a.b.rows, 16);
     int waves = 16;  // as many as the chip holds of all blocks at once, 24 to a compute unit, at least 4 and at most a step each
@@ -292,19 +279,12 @@ template <typename X> void launch_few(const FewArgs& a, hipStream_t s) {
 // its waves, 32 x 32 of the tile each, share k in steps of 128 by fours and add up through LDS.
 // b's elements go from memory to registers as few_kernel's do.  What bounds it is the packing,
 // done again for every 64 rows of b.
-constexpr int SMALL = 64, PARTS = 4, SMALL_WAVES = 4 * PARTS, SMALL_AHEAD = 2;
+constexpr int SMALL = MXFP_SMALL, PARTS = 4, SMALL_WAVES = 4 * PARTS, SMALL_AHEAD = 2;
 constexpr int SMALL_LDS = PARTS * SMALL * (SMALL + 4) * 4;  // the parts' sums
-
-// Whether it is taken, for up to a block to a compute unit: as long as that takes no more than
-// packing in a launch of its own and the tiles, by when the host has saved a launch (3 us).  In
-// graphs, us, taken / not, fp32: 1003 tokens, 1001 x 520 8.5 / 8.8; 2048, 64 x 64 4.2 / 6.1; 256,
-// 4096 x 512 7.8 / 7.4; 256, 1024 x 1024 11.6 / 7.3; two blocks to a unit: 2048, 1001 x 520 15.1 / 11.0.
-constexpr int SMALL_DIM = 576;
-bool is_small(int64_t n, int64_t rows, int64_t dim) { return dim <= SMALL_DIM && fc::ceil_div(n, SMALL) * fc::ceil_div(rows, SMALL) <= CUS; }
 
 // LDS of a token's codes: an odd number of 16 bytes, so that 16 rows' lie in different banks.
 __host__ __device__ constexpr int small_row(int blocks) { return 16 * (blocks | 1); }
-static_assert(SMALL * (small_row(SMALL_DIM / fc::BLOCK) + SMALL_DIM / fc::BLOCK + 3) <= SMALL_LDS, "the packed tokens fit");
+static_assert(SMALL * (small_row(MXFP_SMALL_DIM / fc::BLOCK) + MXFP_SMALL_DIM / fc::BLOCK + 3) <= SMALL_LDS, "the packed tokens fit");
 
 template <typename X> __global__ __launch_bounds__(64 * SMALL_WAVES) void small_kernel(FewArgs a, int tm, int tn) {
     typedef fc::i32x4 V;
@@ -462,7 +442,7 @@ Operand4 operand(const fc_mxfp* p, const Packed& m, int64_t r0, int64_t count) {
     return {static_cast<const uint8_t*>(m.codes) + r0 * m.ldc, m.ldc / 2, (int)count, 8 * p->blocks, static_cast<const uint8_t*>(m.scales) + r0 * m.lds, m.lds, m.group};
 }
 
-Choice choice(const fc_mxfp* p, int64_t n) { return choose_tiles(COST4, WIDE4, SMALL4, -1, n, p->rows, p->width / 8, true, p->sums); }
+Choice choice(const fc_mxfp* p, int64_t n) { return mxfp_choice(n, p->rows, p->dim, p->sums); }
 
 // Whether scales go to the product in the order of its tiles.
 bool reorders(const fc_mxfp* p, int64_t n) { return choice(p, n).kind == WIDE4; }
@@ -516,7 +496,7 @@ int fc_mxfp_create(fc_mxfp** plan, int64_t rows, int64_t dim, int64_t max_tokens
         p->blocks = (int)fc::ceil_div(dim, fc::BLOCK);
         p->width = 8 * (int)fc::ceil_div(dim, 256);
         const int64_t c = std::min(max_tokens, CHUNK);
-        p->sums = std::min<int64_t>(SUMS_LIMIT, 64 * fc::ceil_div(c, 64) * 64 * rows);
+        p->sums = mxfp_sums(max_tokens, rows);
         fc::Layout at;
         const uint64_t o_codes = at.take(c * 16 * p->blocks), o_scales = at.take(c * p->width), o_b = at.take(rows * p->width), o_sum = at.take(p->sums * 4);
         int rc = p->order.create();
@@ -639,8 +619,8 @@ int fc_mxfp_linear(fc_mxfp* p, const void* x, int x_dtype, int64_t ld_x, int64_t
         bool note;
         rc = p->order.begin(s, note);
         if (rc) return rc;
-        const bool few = is_few(n, p->rows, p->dim);
-        if (n && (few || is_small(n, p->rows, p->dim))) {
+        const bool few = mxfp_few(n, p->rows, p->dim);
+        if (n && (few || mxfp_small(n, p->rows, p->dim))) {
             const FewArgs f{operand(p, b, 0, p->rows), x, ld_x, (int)n, (int)p->dim, p->blocks, p->width, scale, out, out_dtype, ld_out, accumulate != 0};
             fc::by_dtype(x_dtype, [&](auto t) { few ? launch_few<decltype(t)>(f, s) : launch_small<decltype(t)>(f, s); });
             n = 0;

@@ -1,10 +1,9 @@
 // What the operators' products of two 16-bit matrices share beside fc_gemm.h: results
-// with a scale, added up over parts of k or calls, the joins of these parts, copies of
-// operands that lie otherwise than the products need, and the choice of tiles.
+// with a scale, added up over parts of k or calls, the joins of these parts, and copies of
+// operands that lie otherwise than the products need.
 #pragma once
 
-#include <algorithm>
-
+#include "fc_choice.h"
 #include "fc_eight.h"
 #include "fc_gemm.h"
 #include "fc_lm_host.h"
@@ -18,6 +17,8 @@ namespace {
 
 typedef _Float16 f16;
 typedef __bf16 bf16;
+
+static_assert(STEP == fc::GEMM_BK, "the estimates are of the products' steps");
 
 extern __shared__ __align__(1024) char lds[];
 
@@ -254,62 +255,6 @@ template <typename T, bool AS, bool BS> using Middle = fc::Product<T, 128, 128, 
 template <typename T, bool AS, bool BS> using Short = fc::Product<T, 64, 128, 64, 32, AS, BS, 3>;
 template <typename T, bool AS, bool BS> using Narrow = fc::Product<T, 64, 32, 16, 32, AS, BS, 6>;
 template <typename T, bool AS, bool BS> using Once = fc::Product<T, 64, 128, 64, 32, AS, BS, 3, 0, true>;
-
-enum TileKind { LARGE, BROAD, MIDDLE, SHORT, NARROW, KINDS };
-
-constexpr int CUS = 256;
-
-// In us, measured with 1 to 512 tiles: a step of 64 of k with the compute unit full
-// of such tiles (`per` at a time) and alone, and a tile's start and end.
-struct KindCost {
-    int bm, bn;
-    double full, alone, once;
-    int per;
-    double before = 0;  // of what the kind needs done first
-};
-constexpr KindCost COST[KINDS] = {{256, 256, 1.7, 1.15, 9.5, 1}, {256, 192, 1.38, 1.0, 8.0, 1}, {128, 128, 0.52, 0.6, 5.0, 2}, {64, 128, 0.55, 0.6, 4.0, 2}, {64, 32, 0.2, 0.3, 4.0, 2}};
-
-struct Choice {
-    TileKind kind;
-    int splits;      // parts of k, of `steps` of 64 each
-    int steps;
-    double us;       // estimated
-};
-
-constexpr int64_t SPLIT_FLOATS = (int64_t)1 << 27;
-
-// The tiles of an m x n product of `total` steps of k, kinds first to last of `cost` (not
-// `skip`), and the parts k is split into, by the least estimated time; m is taken up to
-// multiples of 64, so that the choice is one for every list of as many 64s of tokens.
-// `most`: floats of partial sums.
-inline Choice choose_tiles(const KindCost* cost, int first, int last, int skip, int64_t m, int64_t n, int64_t total, bool may_split, int64_t most) {
-    m = fc::ceil_div(m, 64) * 64;
-    Choice best{(TileKind)last, 1, (int)total, 0};
-    double least = 1e300;
-    for (int kind = first; kind <= last; ++kind) {
-        if (kind == skip) continue;
-        const KindCost& c = cost[kind];
-        const int64_t tiles = fc::ceil_div(m, c.bm) * fc::ceil_div(n, c.bn);
-        const int fill = (int)std::min<int64_t>(64, CUS * c.per / tiles);  // as many as the chip takes at once
-        for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, fill}) {
-            if (s < 1) continue;
-            const int64_t steps = fc::ceil_div(total, s), parts = fc::ceil_div(total, steps), blocks = tiles * parts;
-            if (s > 1 && (!may_split || steps < 2 || parts * m * n > most)) continue;
-            const double at_once = (double)std::min<int64_t>(c.per, fc::ceil_div(blocks, CUS));
-            double t = c.before + fc::ceil_div(blocks, CUS * c.per) * (steps * std::max(c.alone, c.full * at_once) + c.once);
-            if (parts > 1) t += 5.0 + 8.0 * parts * m * n / 4.5e6;  // partial sums, written and read
-            if (t < least) {
-                least = t;
-                best = {(TileKind)kind, (int)parts, (int)steps, t};
-            }
-        }
-    }
-    return best;
-}
-
-inline Choice choose(int64_t m, int64_t n, int64_t k, bool few, bool may_split, bool broad, int64_t most = SPLIT_FLOATS) {
-    return choose_tiles(COST, few ? SHORT : LARGE, few ? NARROW : MIDDLE, broad ? -1 : BROAD, m, n, fc::ceil_div(k, fc::GEMM_BK), may_split, most);
-}
 
 template <typename P> hipError_t prepare(const void* kernel) {
     return P::LDS > 64 * 1024 ? hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, P::LDS) : hipSuccess;
