@@ -264,7 +264,9 @@ typedef struct fc_ckpt fc_ckpt;
  * max_outs rows (0 to 2^21) from up to max_tokens tokens (0 to 2^30) and a dy of `dtype`,
  * FC_F16 or FC_BF16.  The workspace, made here (none where max_outs is 0): 2 bytes per
  * element of max_tokens activations; 2 per element of dy where max_outs is no multiple of 8;
- * partial sums of products that are split along the tokens, up to 128 MiB. */
+ * partial sums of products that are split along the tokens, up to 128 MiB and at most one part
+ * for every 128 of max_tokens.  Layers of one dim can share a plan (of the largest max_outs), whose
+ * calls run one after the other; a plan for each costs twice their checkpoints' memory. */
 int fc_ckpt_create(fc_ckpt** plan, int64_t dim, int64_t max_tokens, int64_t max_outs, int dtype, int format);
 void fc_ckpt_destroy(fc_ckpt* plan);
 
@@ -300,7 +302,8 @@ typedef struct fc_mxfp fc_mxfp;
 /* A plan for products with a matrix of `rows` rows of `dim` elements (1 to 2^21 each) and up
  * to max_tokens rows (0 to 2^31 - 1).  The workspace: fc_mxfp_linear's packed inputs, 0.53
  * bytes per element of up to 2^18 tokens; the matrix's scales in another order; partial sums
- * of products that are split, up to 128 MiB. */
+ * of products that are split, up to 128 MiB and at most one part for every 512 of dim.  Any
+ * number of matrices of these sizes can share a plan, whose calls run one after the other. */
 int fc_mxfp_create(fc_mxfp** plan, int64_t rows, int64_t dim, int64_t max_tokens);
 void fc_mxfp_destroy(fc_mxfp* plan);
 

@@ -70,6 +70,15 @@ inline Choice choose(int64_t m, int64_t n, int64_t k, bool few, bool may_split, 
 // Partial sums that a split product may write: two rounds of the chip's largest tiles.
 constexpr int64_t SUMS_LIMIT = (int64_t)1 << 25;
 
+// What choose_tiles may count on for products of up to m x n, and the floats of it that any of
+// them writes when k is at most `total` steps: a part has at least two steps, there are at most
+// 64, and m is counted as it is.
+inline int64_t sums_limit(int64_t m, int64_t n) { return std::min<int64_t>(SUMS_LIMIT, 64 * fc::ceil_div(m, 64) * 64 * n); }
+inline int64_t sums_room(int64_t m, int64_t n, int64_t total) {
+    const int64_t parts = std::min<int64_t>(64, fc::ceil_div(total, 2));
+    return parts > 1 ? std::min(sums_limit(m, n), parts * m * n) : 0;
+}
+
 // ---- a weight's gradient from 8-bit activations (fc_ckpt.hip) ----------------------------
 
 // Of a weight's gradient: COST's kinds, 128 x 128 slower alone with both operands across their
@@ -78,8 +87,8 @@ constexpr int64_t SUMS_LIMIT = (int64_t)1 << 25;
 constexpr int TINY = 3;
 constexpr KindCost COST_DW[] = {COST[LARGE], COST[BROAD], {128, 128, 0.52, 0.7, 5.0, 2}, {64, 64, 0.25, 0.3, 4.0, 2}};
 
-// Floats of partial sums of a plan.
-inline int64_t ckpt_sums(int64_t max_outs, int64_t dim) { return std::min<int64_t>(SUMS_LIMIT, 64 * fc::ceil_div(max_outs, 64) * 64 * dim); }
+inline int64_t ckpt_limit(int64_t max_outs, int64_t dim) { return sums_limit(max_outs, dim); }
+inline int64_t ckpt_room(int64_t max_tokens, int64_t max_outs, int64_t dim) { return sums_room(max_outs, dim, fc::ceil_div(max_tokens, STEP)); }
 
 inline Choice ckpt_choice(int64_t n, int64_t outs, int64_t dim, int64_t most) {
     return choose_tiles(COST_DW, LARGE, TINY, -1, outs, dim, fc::ceil_div(n, STEP), true, most);
@@ -102,9 +111,8 @@ enum { WIDE4, HALF4, SMALL4, KINDS4 };
 // As COST, for steps of 256 of k.
 constexpr KindCost COST4[KINDS4] = {{256, 256, 1.78, 1.34, 4.5, 1, 6.0}, {128, 128, 0.56, 0.64, 5.2, 2}, {64, 64, 0.29, 0.38, 4.3, 2}};
 
-inline int64_t mxfp_sums(int64_t max_tokens, int64_t rows) {
-    return std::min<int64_t>(SUMS_LIMIT, 64 * fc::ceil_div(std::min(max_tokens, MXFP_CHUNK), 64) * 64 * rows);
-}
+inline int64_t mxfp_limit(int64_t max_tokens, int64_t rows) { return sums_limit(std::min(max_tokens, MXFP_CHUNK), rows); }
+inline int64_t mxfp_room(int64_t max_tokens, int64_t rows, int64_t dim) { return sums_room(std::min(max_tokens, MXFP_CHUNK), rows, fc::ceil_div(dim, 256)); }
 
 inline Choice mxfp_choice(int64_t n, int64_t rows, int64_t dim, int64_t most) {
     return choose_tiles(COST4, WIDE4, SMALL4, -1, n, rows, fc::ceil_div(dim, 256), true, most);

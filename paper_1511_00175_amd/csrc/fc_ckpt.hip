@@ -231,7 +231,7 @@ struct fc_ckpt {
     fc::DeviceBlock block;
     int64_t dim = 0, max_tokens = 0, max_outs = 0;
     int dtype = FC_F16, format = FC_BLOCK_I8, blocks = 0;
-    int64_t sums = 0;        // floats of partial sums
+    int64_t sums = 0;        // ckpt_limit, of which ckpt_room floats are made
     char* x = nullptr;       // unpacked
     char* dy = nullptr;      // copied
     float* sum = nullptr;
@@ -315,9 +315,9 @@ int fc_ckpt_create(fc_ckpt** plan, int64_t dim, int64_t max_tokens, int64_t max_
         p->blocks = (int)fc::ceil_div(dim, fc::BLOCK);
         fc::Layout at;
         const bool grads = max_outs > 0;
-        p->sums = ckpt_sums(max_outs, dim);
+        p->sums = ckpt_limit(max_outs, dim);
         const uint64_t o_x = at.take(grads ? max_tokens * fc::ceil_div(dim, 8) * 16 : 0),
-                       o_dy = at.take(max_outs % 8 ? max_tokens * fc::ceil_div(max_outs, 8) * 16 : 0), o_sum = at.take(p->sums * 4);
+                       o_dy = at.take(max_outs % 8 ? max_tokens * fc::ceil_div(max_outs, 8) * 16 : 0), o_sum = at.take(ckpt_room(max_tokens, max_outs, dim) * 4);
         int rc = p->order.create();
         if (!rc) rc = fc::hip_code(dtype == FC_F16 ? prepare_all<f16, false>() : prepare_all<bf16, false>());
         if (!rc) rc = fc::hip_code(dtype == FC_F16 ? prepare_all<f16, true>() : prepare_all<bf16, true>());

@@ -404,7 +404,7 @@ struct fc_mxfp {
     fc::DeviceBlock block;
     int64_t rows = 0, dim = 0, max_tokens = 0;
     int blocks = 0, width = 0;   // of a row: scales, bytes of scales
-    int64_t sums = 0;            // floats of partial sums
+    int64_t sums = 0;            // mxfp_limit, of which mxfp_room floats are made
     uint8_t* codes = nullptr;    // linear's packed inputs
     uint8_t* scales = nullptr;   // theirs, or those of a product's, reordered
     uint8_t* b_scales = nullptr; // the weight's, reordered
@@ -496,9 +496,9 @@ int fc_mxfp_create(fc_mxfp** plan, int64_t rows, int64_t dim, int64_t max_tokens
         p->blocks = (int)fc::ceil_div(dim, fc::BLOCK);
         p->width = 8 * (int)fc::ceil_div(dim, 256);
         const int64_t c = std::min(max_tokens, CHUNK);
-        p->sums = mxfp_sums(max_tokens, rows);
+        p->sums = mxfp_limit(max_tokens, rows);
         fc::Layout at;
-        const uint64_t o_codes = at.take(c * 16 * p->blocks), o_scales = at.take(c * p->width), o_b = at.take(rows * p->width), o_sum = at.take(p->sums * 4);
+        const uint64_t o_codes = at.take(c * 16 * p->blocks), o_scales = at.take(c * p->width), o_b = at.take(rows * p->width), o_sum = at.take(mxfp_room(max_tokens, rows, dim) * 4);
         int rc = p->order.create();
         if (!rc) rc = fc::hip_code(prepare_all<false>());
         if (!rc) rc = fc::hip_code(prepare_all<true>());

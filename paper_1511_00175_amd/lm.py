@@ -484,7 +484,8 @@ class Checkpoint(_Handle):
     They are held by two tensors of the caller's, codes (tokens, 32 ceil(dim / 32))
     of torch.int8 or torch.float8_e4m3fn on 16 bytes with a row stride of a multiple of 16,
     and scales (tokens, ceil(dim / 32)) of torch.uint8, the exponents of powers of two plus
-    127, as empty() makes them."""
+    127, as empty() makes them.  Layers of one dim can share a plan, which holds the workspace
+    of a gradient: two bytes for every element of max_tokens activations."""
 
     _destroy = "fc_ckpt_destroy"
 
@@ -548,7 +549,8 @@ class Mxfp4(_Handle):
     A packed matrix is held by two tensors of the caller's, of torch.uint8: codes (r, 16
     ceil(dim / 32)), the even element in a byte's low half, on 16 bytes with a row stride of a
     multiple of 16, and scales (r, 8 ceil(dim / 256)), zeros past the blocks, on 8 bytes with
-    a stride of a multiple of 8, as empty() makes them."""
+    a stride of a multiple of 8, as empty() makes them.  Matrices of the same sizes can share
+    a plan."""
 
     _destroy = "fc_mxfp_destroy"
 
