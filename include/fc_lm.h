@@ -281,10 +281,13 @@ int fc_ckpt_unpack(fc_ckpt* plan, const void* codes, int64_t ld_codes, const voi
 
 /* The gradient of a weight (outs, dim) whose layer's inputs x are kept so and whose outputs'
  * gradient is dy (n, outs): dw[o, :] = (accumulate ? dw[o, :] : 0) + scale * the sum over t of
- * dy[t, o] x[t, :], with x as unpacked to dy's type (exact but for what is out of fp16's range),
- * products and sums fp32, rounded once to dw's type.  n <= max_tokens, outs <= max_outs
- * (FC_EINVAL).  dy lies on 16 bytes with ld_dy a multiple of 8, or is copied, for which plans
- * whose max_outs is no multiple of 8 have room (others: FC_EALIGN); ld_dy is at most 2^21. */
+ * dy[t, o] x[t, :], with x as unpacked to dy's type (exact but for what is out of fp16's range:
+ * past 65504 that, below 2^-14 whole steps of 2^-24, so that less than 2^-25 is lost), products
+ * and sums fp32, in whose roundings a factor of fp16 below 2^-14 counts as 2^-14, rounded once to
+ * dw's type.  n <= max_tokens, outs <= max_outs (FC_EINVAL).  dy lies on 16 bytes with ld_dy a
+ * multiple of 8 and is read by whole 16 bytes (of the last row, too, up to the next 8 elements), or
+ * is copied, for which plans whose max_outs is no multiple of 8 have room (others: FC_EALIGN);
+ * ld_dy is at most 2^21. */
 int fc_ckpt_grad(fc_ckpt* plan, const void* dy, int64_t ld_dy, const void* codes, int64_t ld_codes, const void* scales,
                  int64_t ld_scales, int64_t n, int64_t outs, float scale, void* dw, int dw_dtype, int64_t ld_dw,
                  int accumulate, void* stream);
