@@ -10,7 +10,8 @@
 // its numbers are exact (but for what is out of fp16's range), and the product then takes
 // both operands across their rows (fc_gemm.h), so that neither is transposed in memory.
 // Unpacking is 12 us of 240 at 8192 tokens, 8192 x 2048, where 32 tiles read every part of x;
-// the product is 228, 1.2 PFLOP/s, the matrix cores busy 59% of the cycles at 2.06 GHz.  Few tiles take one launch (small_kernel).
+// the product is 228 to 264 by card and pass, 1.0 to 1.2 PFLOP/s, the matrix cores busy 59% of the
+// cycles at 2.09 GHz.  Few tiles take one launch (small_kernel).
 #include "fc_blocks.h"
 #include "fc_products.h"
 
@@ -81,9 +82,9 @@ template <typename T, bool ADD> void launch(int kind, const GradArgs& g, hipStre
 
 // One launch, 64 x 64 of dw to a block: 4 groups of 4 waves go through every 4th step of 64
 // tokens, each with its own buffers, and their sums are added in order at the end.  Both
-// operands pass registers, where x is unpacked and dy may lie on any element.  It is bound by
-// what LDS takes in and gives out for 32 x 32 of a wave and by the unpacking, done again by
-// every block of a column.  In graphs, us, against the operands' launch and the tiles': 1 to 256
+// operands pass registers, where x is unpacked and dy may lie on any element.  Four
+// steps take 1.4 us, of which 0.64 are what LDS takes in and gives out for 32 x 32 of a wave (192
+// KB): the unpacking, done again by every block of a column, and what it waits for are the rest.  In graphs, us, against the operands' launch and the tiles': 1 to 256
 // tokens, 1024 x 1024 5.3 to 5.5, 6.2 to 7.6; 1003 tokens, 1001 x 520 9.8, 11.7; 1003, 2048 x
 // 1024 17.9, 17.2; 4096, 1024 x 1024 27, 30; 4096, 256 x 512, where k is split 22.7, 14.1.
 struct SmallArgs {

@@ -12,8 +12,11 @@
 // What bounds it, measured on the loop alone, 16384 x 4096 by 4096 of k in 256 x 256 tiles: 127
 // us, 4.3 PFLOP/s, and 109 with zeros for data, at which the clock stays higher; 106 without
 // the loads, 77 the multiplications by themselves (zeros), 69 the loads, 50 the reads of LDS.
-// For a step of 256 of k the multiplications of a unit take about 2060 cycles, what LDS takes
-// in and gives out at 128 bytes a cycle 2048.  No faster were: 32 x 32 instructions of 64 of k
+// A unit does 64 steps of 256 of k there.  A step's multiplications take about 2060 cycles, what
+// LDS takes in and gives out at 128 bytes a cycle 2048: 63 us of the 127 each at 2.1 GHz, so that
+// neither is the bound.  Multiplications and reads of LDS hardly overlap (77 and 50 by
+// themselves, 106 together): it is the order in which they are issued and what they wait for.
+// No faster were: 32 x 32 instructions of 64 of k
 // (126), 4 waves of 128 x 128 (144), steps of 128 of k in 4 stages (172), padded rows, reads ahead
 // into L2 (149), the results of a tile stored between the next one's products (4% more).
 #pragma once

@@ -8,7 +8,7 @@
 // 8192 tokens, 8192 x 2048, bf16: the weight 15.8, the inputs with both operands' scales
 // brought in order 12.5 (44 MB, 3.6 TB/s), the product 81 (3.4 PFLOP/s; its 134 MB of results
 // alone take 19 to 28); 16384 tokens, 4096 x 4096, fp16: the weight by its columns 14, the inputs
-// 42 (177 MB, 4.2 TB/s), the product 137 to 142 (3.9 to 4.0 PFLOP/s).
+// 42 (177 MB, 4.2 TB/s), the product 136 to 156 by card and pass (3.5 to 4.0 PFLOP/s).
 #include "fc_blocks.h"
 #include "fc_gemm4.h"
 #include "fc_products.h"
@@ -147,7 +147,8 @@ template <typename P> hipError_t prepare_tiles() {
 // Up to 16 tokens by 16 rows of b to a block, whose waves share k in steps of 256 and add up
 // through LDS.  b's elements are read once, so they go from memory to registers: a lane's 16
 // bytes are its row's 32 elements of one scale.  The tokens are packed into LDS by every
-// block, while its first steps of b are on their way.  One token, fp16, us, other weights in
+// block, while its first steps of b are on their way; the other steps' loads wait until it is
+// done, so that one token of 9216 takes twice what reading the weight does.  One token, fp16, us, other weights in
 // the caches: 4096 x 9216 (20 MB) 8.5, 8192 x 2048 5.6, 65536 x 2048 (71 MB) 20.
 struct FewArgs {
     Operand4 b;

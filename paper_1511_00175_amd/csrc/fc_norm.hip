@@ -19,10 +19,10 @@
 // dw = a(g) P and dg = a'(g) w P.
 //
 // Measured, forward (out and y) and backward (all gradients): 16384 rows of 4096, bf16 and a
-// residual in fp32, 805 MB, 160 us or 5.0 TB/s; 16384 rows of 2048, all bf16, with the gate a
-// matrix, 537 MB, 125 us or 4.3 TB/s, where a copy of 4 GiB reaches 4.7.  One row of 4096
-// forward 3.9 us and 1003 rows of 1001 backward 13.5 us with the call itself left out: of
-// those 5.6 us are the second launch and what a block does for it, and 4 us is the bytes' time.
+// residual in fp32, 805 MB, 164 to 167 us or 4.9 TB/s; 16384 rows of 2048, all bf16, with the gate
+// a matrix, 537 MB, 125 us or 4.3 TB/s, where a copy of 4 GiB reaches 4.8.  One row of 4096
+// forward 3.9 us, and 1003 rows of 1001 backward 14.3 (14.4 to 15.2 in a graph), of which 11.8 are the
+// first launch and 4.0 the second by themselves and 4 the bytes' time.
 #include <algorithm>
 #include <type_traits>
 
@@ -502,9 +502,10 @@ template <typename T, typename H, bool SHARED> __global__ __launch_bounds__(1024
     put(a.sum2, __builtin_shufflevector(all[2], all[3], 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// Rows of more than 8192 elements are more than a block's registers hold: they are read
-// again in each pass over them, from the caches (rows of fewer than 8 come here too), and the sums
-// over tokens lie in LDS, of which every thread uses its own part.  1.6 TB/s, for want of waves.
+// Rows of more than 8192 elements are read again in each pass over them, from the caches (rows of
+// fewer than 8 come here too), and the sums over tokens lie in LDS, of which every thread uses its
+// own part: 1.6 TB/s, 327 us for 3640 rows of 9216.  9 or 10 waves have 168 registers each, in which
+// the rows as stored would fit, as backward_kernel holds them; such a form has not been built.
 template <typename T, typename H, int V> __global__ __launch_bounds__(V == 2 ? MIDDLE : 512) void backward_wide_kernel(BackwardArgs a) {
     __shared__ __align__(16) float part[2][3][WAVES];
     RowSums<3> sums{part, a.lanes, 0};
